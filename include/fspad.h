@@ -57,7 +57,8 @@ typedef enum {
     FSPAD_ERR_TIMEOUT = -7,        /* a bounded device-side wait ran out               */
     FSPAD_ERR_BAD_TREE = -8,       /* parent[0] != -1 or parent[i] outside [0, i)      */
     FSPAD_ERR_NOMEM = -9,          /* device or host allocation failed at create time  */
-    FSPAD_ERR_TOO_LARGE = -10      /* size beyond the fixed capacity of a no-allocation call */
+    FSPAD_ERR_TOO_LARGE = -10,     /* size beyond the fixed capacity of a no-allocation call */
+    FSPAD_ERR_DEVICE = -11         /* the context belongs to another device than the current one (calls around the 4-bit cache) */
 } fspad_error;
 
 typedef struct {
@@ -412,6 +413,117 @@ int fspad_tree_attn_paged(fspad_ctx *ctx, const fspad_bf16 *q, const fspad_bf16 
 int fspad_kv_compact_paged(fspad_ctx *ctx, fspad_bf16 *pool, const int32_t *block_table, int blocks_per_seq, int n_blocks,
                            const int32_t *accepted_path, const int32_t *n_accepted, const int32_t *prefix_len, int batch,
                            int32_t *new_len, void *stream);
+
+/*
+ * ---- A cache held in 4 bits, and what stands between the QKV product and it ----
+ *
+ * (The paper's cache is what a target keeps between steps; it says nothing of its precision.  Half of a long context's step is reading it.)
+ * A row of 128 elements is kept as eight blocks of 16: one e4m3 scale a block and one e2m1 code an element (sign, and a magnitude of 0, 0.5,
+ * 1, 1.5, 2, 3, 4 or 6), 72 bytes in place of 256.  Element i stands for code_i * scale_(i / 16); bf16 and fp16 hold that value exactly.
+ * The cache is paged as in fspad_tree_attn_paged:
+ *   codes  [n_layers][2][n_blocks][Hkv][128][64] bytes: of a row, byte i holds element 2i in its low and 2i + 1 in its high half
+ *   scales [n_layers][2][n_blocks][Hkv][128][8] bytes (e4m3)
+ * cache row r of sequence b is row r % 128 of block block_table[b][r / 128].  What lies behind a sequence's last row may be anything.
+ *
+ * Writing a row: scale = max |x| / 6 and code = x / scale, each to the nearest value of its type, ties to the even one, beyond the type's
+ * largest value to that (scales: 448, so that magnitudes up to 2688 are kept; where max |x| / 6 is at most 2^-10 the block reads as zeros).  The
+ * sign of an element is kept also where its code is zero.  A block with an infinity or a NaN gets the scale 0x7F (NaN) and codes of zero: it reads as NaN.
+ *
+ * The calls below run on the context's device, which must be the current one (else FSPAD_ERR_DEVICE).
+ */
+
+/* The device a context was created on (-1: NULL). */
+int fspad_device(const fspad_ctx *ctx);
+
+/*
+ * Rotary positions on the rows of the QKV product, several axes ("Preliminaries": the flattened tree is the target's input; a node's
+ * position is its depth behind the prefix, whatever its place in the flattened order).  Pair i of every query and key head turns by
+ *   a_i = p[axis(i)] * theta^(-2i / 128):   y1 = x1 cos a_i - x2 sin a_i,   y2 = x2 cos a_i + x1 sin a_i
+ * axis(i) = 0 (time) for i < sec_t, 1 (height) for the next sec_h pairs, 2 (width) for the last sec_w; plain rotary positions are sec_t = 64.
+ * Pair i is elements (i, 64 + i), or with `adjacent` (2i, 2i + 1).  Angles are reduced in double precision, sines and products are single
+ * precision, the result is rounded once to bf16.  Values pass unchanged.
+ *
+ *   qkv       row r = b * n_nodes + i of [batch][n_nodes] starts at qkv + r * row_stride: Hq query heads, Hkv key heads, Hkv value heads of 128
+ *   row_stride  elements, at least (Hq + 2 Hkv) * 128, a multiple of 8
+ *   positions [batch][n_nodes][3] int32, with start and parent NULL; n_nodes may then be any number of rows (a prompt), batch * n_nodes < 2^31
+ *   start [batch][3] int32 and parent [batch][n_nodes] int32, with positions NULL: node i of tree b stands at start[b][a] + depth(i) on axis a
+ *   q         [batch][n_nodes][Hq][128], k and v [batch][Hkv][n_nodes][128]: what fspad_tree_attn* and the cache calls take
+ * The outputs must not overlap qkv or one another.  Errors: FSPAD_ERR_NULL also where neither or both kinds of positions are given; FSPAD_ERR_SHAPE for sections
+ * that do not sum to 64 and strides outside these rules; FSPAD_ERR_RANGE for a theta that is not finite and positive; FSPAD_ERR_TOO_LARGE
+ * for more than 65535 sequences or 2^31 - 1 rows; a malformed parent[] sets FSPAD_ERR_BAD_TREE in the status word.
+ */
+int fspad_rope_qkv(fspad_ctx *ctx, const fspad_bf16 *qkv, int64_t row_stride, const int32_t *positions, const int32_t *start,
+                   const int32_t *parent, int n_nodes, int batch, double theta, int sec_t, int sec_h, int sec_w, int adjacent,
+                   fspad_bf16 *q, fspad_bf16 *k, fspad_bf16 *v, void *stream);
+
+/*
+ * Block tables of a paged cache and the slots of new rows, from the lengths of the requests (the paper's remark on practical frameworks,
+ * "Performance on Fewer Candidate Tokens", is the only place it touches deployment).  Blocks are of 128 rows.
+ *
+ *   len [batch], add [batch] int32: rows sequence b holds, and rows that it is to hold beyond them after this step
+ *   drop [batch] int32 or NULL: where not 0, the sequence's place goes to a new request: its blocks are given back first (its len is
+ *               the new request's, 0 as a rule)
+ *   block_table [batch][blocks_per_seq], held [batch] int32, updated: the blocks of a sequence, and how many it holds.  Blocks once held stay
+ *               until the sequence is dropped, so room for a path that was not accepted in full serves the next one.
+ *   free_blocks [n_blocks], n_free [1] int32, updated: a stack of the blocks that nobody holds; its top is free_blocks[n_free - 1]
+ * In this order: for b = 0, 1, ... with drop[b], block_table[b][0 .. held[b] - 1] are pushed one by one and held[b] becomes 0; then for b = 0,
+ * 1, ... blocks are popped into block_table[b][held[b]], ... until sequence b holds ceil((len[b] + add[b]) / 128) (or already does).
+ *
+ *   row_start [batch + 1] int32, written: exclusive sums of add
+ *   slots [max_rows] int64, row_seq, row_pos [max_rows] int32 (these two may be NULL), written: for row t of sequence b, at index
+ *               row_start[b] + t: block * 128 + (len[b] + t) % 128, b, and len[b] + t; behind the last row -1
+ * If something does not fit (len or add negative, len + add > 128 * blocks_per_seq, held or n_free outside the arrays, more than max_rows
+ * rows, not enough free blocks, more blocks given back than the stack has room for) FSPAD_ERR_RANGE is set in the status word and nothing of the state is changed;
+ * row_start is then 0 and the others -1 throughout.
+ * Errors: FSPAD_ERR_TOO_LARGE for batch > 1024 or 2^31 rows or more a sequence.
+ */
+int fspad_block_plan(fspad_ctx *ctx, const int32_t *len, const int32_t *add, const int32_t *drop, int batch, int blocks_per_seq,
+                     int n_blocks, int32_t *block_table, int32_t *held, int32_t *free_blocks, int32_t *n_free, int max_rows,
+                     int32_t *row_start, int64_t *slots, int32_t *row_seq, int32_t *row_pos, void *stream);
+
+/*
+ * Rows of one layer into the 4-bit cache by slots: a prompt's rows, of any number of sequences.
+ *
+ *   k, v   [Hkv][rows][128] bf16 (what fspad_rope_qkv writes for batch = 1)
+ *   slots  [rows] int64: block * 128 + row of the block (fspad_block_plan); -1: the row is left out.  No slot may occur twice.
+ *   layer  0 .. n_layers - 1;  codes, scales, n_blocks as above
+ *   k_rounded, v_rounded [Hkv][rows][128] bf16 or both NULL: receive the values that are kept (rows left out: unchanged); may be k and v
+ * A slot outside the cache sets FSPAD_ERR_RANGE in the status word and its row is left out.
+ */
+int fspad_kv_write_packed(fspad_ctx *ctx, const fspad_bf16 *k, const fspad_bf16 *v, const int64_t *slots, int rows, int layer,
+                          uint8_t *codes, uint8_t *scales, int n_blocks, fspad_bf16 *k_rounded, fspad_bf16 *v_rounded, void *stream);
+
+/*
+ * fspad_kv_append for the 4-bit cache: for every layer, K and V, sequence b and kv head, cache row L_b + j receives
+ * tree_kv[..][accepted_path[b][j]], j = 0 .. n_accepted[b] - 1.  new_len[b] = L_b + n_accepted[b] (may be NULL).
+ *
+ *   tree_kv [n_layers][2][batch][Hkv][n_nodes][128] bf16;  accepted_path [batch][max_nodes], n_accepted, prefix_len, new_len [batch] int32
+ *   rounded as tree_kv or NULL: receives the values that are kept, at the nodes' own places (other nodes: unchanged); may be tree_kv
+ * Blocks of the written rows must not be shared.  A path entry outside [0, n_nodes), n_accepted outside [0, n_nodes],
+ * L_b + n_accepted[b] > 128 * blocks_per_seq or a table entry out of range set FSPAD_ERR_RANGE in the status word and the rows
+ * concerned are left out.
+ */
+int fspad_kv_append_packed(fspad_ctx *ctx, uint8_t *codes, uint8_t *scales, const int32_t *block_table, int blocks_per_seq, int n_blocks,
+                           const fspad_bf16 *tree_kv, const int32_t *accepted_path, const int32_t *n_accepted,
+                           const int32_t *prefix_len, int n_nodes, int batch, fspad_bf16 *rounded, int32_t *new_len, void *stream);
+
+/*
+ * fspad_tree_attn_paged over the 4-bit cache: the keys of node i of sequence b are cache rows 0 .. L_b - 1 and, in bf16, the rows of the
+ * node itself and of its ancestors in tree_k / tree_v.  n_nodes = 1 is the single-token step.
+ *
+ *   q, out [batch][n_nodes][Hq][128] bf16;  tree_k, tree_v [batch][Hkv][n_nodes][128] bf16 (required)
+ *   layer  of the cache;  parent [batch][n_nodes], prefix_len [batch] int32, 0 <= L_b <= 128 * blocks_per_seq
+ *   workspace  of at least fspad_tree_attn_packed_workspace_bytes(ctx, n_nodes, batch) bytes, scratch: no other call may use it
+ *              until this one is done
+ * Single-precision accumulation and softmax.  A tree row of V with an infinity or a NaN makes the outputs of the nodes that see it NaN, and of
+ * no others; so does such a row of K.  Errors: FSPAD_ERR_RANGE for a workspace that is too small, and, in the status word, for a
+ * prefix length or a table entry out of range; otherwise as fspad_tree_attn_paged.
+ */
+size_t fspad_tree_attn_packed_workspace_bytes(const fspad_ctx *ctx, int n_nodes, int batch);
+int fspad_tree_attn_packed(fspad_ctx *ctx, const fspad_bf16 *q, const uint8_t *codes, const uint8_t *scales, int layer,
+                           const int32_t *block_table, int blocks_per_seq, int n_blocks, const fspad_bf16 *tree_k,
+                           const fspad_bf16 *tree_v, const int32_t *parent, const int32_t *prefix_len, int n_nodes, int batch,
+                           fspad_bf16 *out, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * One whole verify step on DEVICE buffers ("Preliminaries": the target's single

@@ -23,7 +23,9 @@ _native = None
 
 EXPORTS = ["fspad_create", "fspad_destroy", "fspad_status", "fspad_strerror", "fspad_launch_count",
            "fspad_tree_attn", "fspad_tree_accept", "fspad_accept_stats", "fspad_kv_compact",
-           "fspad_tree_attn_paged", "fspad_kv_compact_paged", "fspad_kv_append", "fspad_lm_head_stats", "fspad_lm_head_accept", "fspad_feature_sampler", "fspad_feature_sampler_workspace_bytes", "fspad_verify_step", "fspad_verify_step_host", "fspad_selftest_wait_timeout", "fspad_accept_stats_noalloc", "fspad_tree_build", "fspad_draft_expand"]
+           "fspad_tree_attn_paged", "fspad_kv_compact_paged", "fspad_kv_append", "fspad_lm_head_stats", "fspad_lm_head_accept", "fspad_feature_sampler", "fspad_feature_sampler_workspace_bytes", "fspad_verify_step", "fspad_verify_step_host", "fspad_selftest_wait_timeout", "fspad_accept_stats_noalloc", "fspad_tree_build", "fspad_draft_expand",
+           "fspad_device", "fspad_rope_qkv", "fspad_block_plan", "fspad_kv_write_packed", "fspad_kv_append_packed", "fspad_tree_attn_packed",
+           "fspad_tree_attn_packed_workspace_bytes"]
 
 
 class FspadConfig(ctypes.Structure):
@@ -74,6 +76,14 @@ def load():
     lib.fspad_verify_step_host.argtypes = [vp] * 12 + [ci, ci] + [vp] * 6
     lib.fspad_tree_build.argtypes = [vp] * 5 + [ci, ci, ci] + [vp] * 6
     lib.fspad_draft_expand.argtypes = [vp] * 4 + [ci] * 6 + [vp] * 6
+    lib.fspad_device.argtypes = [vp]
+    lib.fspad_rope_qkv.argtypes = [vp, vp, ctypes.c_int64, vp, vp, vp, ci, ci, ctypes.c_double, ci, ci, ci, ci, vp, vp, vp, vp]
+    lib.fspad_block_plan.argtypes = [vp] * 4 + [ci] * 3 + [vp] * 4 + [ci] + [vp] * 5
+    lib.fspad_kv_write_packed.argtypes = [vp] * 4 + [ci, ci, vp, vp, ci, vp, vp, vp]
+    lib.fspad_kv_append_packed.argtypes = [vp] * 4 + [ci, ci] + [vp] * 4 + [ci, ci, vp, vp, vp]
+    lib.fspad_tree_attn_packed_workspace_bytes.argtypes = [vp, ci, ci]
+    lib.fspad_tree_attn_packed_workspace_bytes.restype = ctypes.c_size_t
+    lib.fspad_tree_attn_packed.argtypes = [vp] * 4 + [ci, vp, ci, ci] + [vp] * 4 + [ci, ci, vp, vp, ctypes.c_size_t, vp]
     _lib = lib
     return lib
 
@@ -117,6 +127,11 @@ def _stream(stream: Optional[torch.cuda.Stream]):
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
+def _shaped(name: str, t: Optional[torch.Tensor], *shape):
+    if t is not None and t.shape != shape:
+        raise ValueError("%s: expected shape %s, got %s" % (name, shape, tuple(t.shape)))
+
+
 class Context:
     """Owns an `fspad_ctx` on the current CUDA device."""
 
@@ -127,6 +142,8 @@ class Context:
         self.cfg = FspadConfig(n_q_heads, n_kv_heads, head_dim, max_nodes, vocab, n_layers, max_len,
                                max_batch, softmax_scale)
         self._h = ctypes.c_void_p()
+        self._workspaces = []       # of the attention over the 4-bit cache; an outgrown one stays, a captured graph may hold its address
+        self._workspace_sizes = {}
         rc = load().fspad_create(ctypes.byref(self.cfg), ctypes.byref(self._h))
         if rc != 0:
             raise FspadError(rc, "fspad_create")
@@ -359,6 +376,146 @@ class Context:
         if rc != 0:
             raise FspadError(rc, "fspad_verify_step_host")
         return attn_out, accepted_path, n_accepted, bonus_token, new_len
+
+    # -- the cache held in 4 bits: codes [layers][2][n_blocks][Hkv][128][64], scales [layers][2][n_blocks][Hkv][128][8] (uint8, device) ------
+    def new_packed_cache(self, n_blocks: int, device="cuda"):
+        """(codes, scales) of an empty cache of n_blocks blocks of 128 rows, every layer of the context."""
+        shape = (self.cfg.n_layers, 2, n_blocks, self.cfg.n_kv_heads, 128)
+        return (torch.zeros(shape + (64,), dtype=torch.uint8, device=device), torch.zeros(shape + (8,), dtype=torch.uint8, device=device))
+
+    def _packed(self, codes, scales):
+        nb = codes.shape[2] if codes.dim() == 6 else 0
+        shape = (self.cfg.n_layers, 2, nb, self.cfg.n_kv_heads, 128)
+        _shaped("codes", codes, *shape, 64)
+        _shaped("scales", scales, *shape, 8)
+        return nb
+
+    def rope_qkv(self, qkv, theta, sections=(64, 0, 0), parent=None, start=None, positions=None, adjacent=False, q=None, k=None, v=None,
+                 stream=None):
+        """Rows of the QKV product [B][N][(Hq + 2 Hkv) * 128] (bf16, device; rows may stand further apart) -> q [B][N][Hq][128] and k, v
+        [B][Hkv][N][128], queries and keys turned by positions of up to three axes: `positions` [B][N][3], or of tree nodes `start`
+        [B][3] plus the depth in `parent` [B][N].  `sections`: how many of the 64 pairs go by time, height and width."""
+        B, N, width = qkv.shape
+        hq, hkv = self.cfg.n_q_heads, self.cfg.n_kv_heads
+        if width != (hq + 2 * hkv) * 128:
+            raise ValueError("qkv: expected rows of %d elements, got %d" % ((hq + 2 * hkv) * 128, width))
+        rows, row, one = qkv.stride()
+        if N == 1:
+            row = rows if B > 1 else width
+        elif B > 1 and rows != N * row:
+            one = 0
+        if one != 1:
+            raise ValueError("qkv: rows must be contiguous and evenly spaced, got strides %s" % (qkv.stride(),))
+        _shaped("parent", parent, B, N)
+        _shaped("start", start, B, 3)
+        _shaped("positions", positions, B, N, 3)
+        _shaped("q", q, B, N, hq, 128)
+        _shaped("k", k, B, hkv, N, 128)
+        _shaped("v", v, B, hkv, N, 128)
+        bf, dev = torch.bfloat16, qkv.device
+        if q is None:
+            q = torch.empty((B, N, hq, 128), dtype=bf, device=dev)
+        if k is None:
+            k = torch.empty((B, hkv, N, 128), dtype=bf, device=dev)
+        if v is None:
+            v = torch.empty((B, hkv, N, 128), dtype=bf, device=dev)
+        rc = _calls().rope_qkv(self._h.value, qkv, row, positions, start, parent, N, B, theta, sections[0], sections[1], sections[2],
+                               int(adjacent), q, k, v, _stream(stream))
+        if rc != 0:
+            raise FspadError(rc, "fspad_rope_qkv")
+        return q, k, v
+
+    def block_plan(self, length, add, block_table, held, free_blocks, n_free, max_rows, drop=None, out=None, stream=None):
+        """Blocks for add[b] rows behind the length[b] that sequence b holds; block_table [B][blocks], held [B], free_blocks [n_blocks] and
+        n_free [1] (int32, device) are updated.  Returns (row_start [B + 1], slots [max_rows] int64, row_seq, row_pos [max_rows])."""
+        B, bps = block_table.shape
+        _shaped("length", length, B)
+        _shaped("add", add, B)
+        _shaped("drop", drop, B)
+        _shaped("held", held, B)
+        _shaped("n_free", n_free, 1)
+        if out is None:
+            dev, i32 = block_table.device, torch.int32
+            out = (torch.empty((B + 1,), dtype=i32, device=dev), torch.empty((max_rows,), dtype=torch.int64, device=dev),
+                   torch.empty((max_rows,), dtype=i32, device=dev), torch.empty((max_rows,), dtype=i32, device=dev))
+        row_start, slots, row_seq, row_pos = out
+        _shaped("row_start", row_start, B + 1)
+        _shaped("slots", slots, max_rows)
+        _shaped("row_seq", row_seq, max_rows)
+        _shaped("row_pos", row_pos, max_rows)
+        rc = _calls().block_plan(self._h.value, length, add, drop, B, bps, free_blocks.shape[0], block_table, held, free_blocks, n_free,
+                                 max_rows, row_start, slots, row_seq, row_pos, _stream(stream))
+        if rc != 0:
+            raise FspadError(rc, "fspad_block_plan")
+        return out
+
+    def kv_write_packed(self, k, v, slots, codes, scales, layer=0, k_rounded=None, v_rounded=None, stream=None):
+        """Rows k, v [Hkv][rows][128] (bf16, device; a leading axis of one is allowed) into the slots [rows] (int64; -1: left out) of a layer."""
+        hkv, (rows,) = self.cfg.n_kv_heads, slots.shape
+        nb = self._packed(codes, scales)
+        for name, t in (("k", k), ("v", v), ("k_rounded", k_rounded), ("v_rounded", v_rounded)):
+            if t is not None and t.shape != (hkv, rows, 128) and t.shape != (1, hkv, rows, 128):
+                raise ValueError("%s: expected shape %s, got %s" % (name, (hkv, rows, 128), tuple(t.shape)))
+        rc = _calls().kv_write_packed(self._h.value, k, v, slots, rows, layer, codes, scales, nb, k_rounded, v_rounded, _stream(stream))
+        if rc != 0:
+            raise FspadError(rc, "fspad_kv_write_packed")
+
+    def kv_append_packed(self, codes, scales, block_table, tree_kv, accepted_path, n_accepted, prefix_len, rounded=None, new_len=None,
+                         stream=None):
+        """tree_kv [layers][2][B][Hkv][N][128] (bf16): rows of the accepted path written behind the prefix of the 4-bit cache."""
+        (B, bps), N = block_table.shape, tree_kv.shape[4] if tree_kv.dim() == 6 else 0
+        shape = (self.cfg.n_layers, 2, B, self.cfg.n_kv_heads, N, 128)
+        nb = self._packed(codes, scales)
+        _shaped("tree_kv", tree_kv, *shape)
+        _shaped("rounded", rounded, *shape)
+        _shaped("accepted_path", accepted_path, B, self.cfg.max_nodes)
+        _shaped("n_accepted", n_accepted, B)
+        _shaped("prefix_len", prefix_len, B)
+        _shaped("new_len", new_len, B)
+        if new_len is None:
+            new_len = torch.empty((B,), dtype=torch.int32, device=codes.device)
+        rc = _calls().kv_append_packed(self._h.value, codes, scales, block_table, bps, nb, tree_kv, accepted_path, n_accepted, prefix_len,
+                                       N, B, rounded, new_len, _stream(stream))
+        if rc != 0:
+            raise FspadError(rc, "fspad_kv_append_packed")
+        return new_len
+
+    def tree_attn_packed(self, q, codes, scales, block_table, tree_k, tree_v, parent, prefix_len, layer=0, out=None, workspace=None,
+                         stream=None):
+        """Tree-masked attention of q [B][N][Hq][128] over a layer of the 4-bit cache and the tree's bf16 rows [B][Hkv][N][128].  Without
+        `workspace` (uint8) the context's own is used, which calls on one stream at a time may share."""
+        B, N = q.shape[0], q.shape[1]
+        hq, hkv = self.cfg.n_q_heads, self.cfg.n_kv_heads
+        nb = self._packed(codes, scales)
+        _shaped("q", q, B, N, hq, 128)
+        _shaped("tree_k", tree_k, B, hkv, N, 128)
+        _shaped("tree_v", tree_v, B, hkv, N, 128)
+        _shaped("parent", parent, B, N)
+        _shaped("prefix_len", prefix_len, B)
+        _shaped("out", out, B, N, hq, 128)
+        rows, bps = block_table.shape
+        if rows != B:
+            raise ValueError("block_table: expected %d sequences, got %d" % (B, rows))
+        if out is None:
+            out = torch.empty_like(q)
+        if workspace is None:
+            workspace = self._workspace(N, B, q.device)
+        rc = _calls().tree_attn_packed(self._h.value, q, codes, scales, layer, block_table, bps, nb, tree_k, tree_v, parent, prefix_len,
+                                       N, B, out, workspace, workspace.numel(), _stream(stream))
+        if rc != 0:
+            raise FspadError(rc, "fspad_tree_attn_packed")
+        return out
+
+    def tree_attn_packed_workspace_bytes(self, n_nodes: int, batch: int) -> int:
+        return int(load().fspad_tree_attn_packed_workspace_bytes(self._h, n_nodes, batch))
+
+    def _workspace(self, n_nodes, batch, device):
+        need = self._workspace_sizes.get((n_nodes, batch))
+        if need is None:
+            need = self._workspace_sizes[n_nodes, batch] = self.tree_attn_packed_workspace_bytes(n_nodes, batch)
+        if not self._workspaces or self._workspaces[-1].numel() < need:
+            self._workspaces.append(torch.empty((max(need, 16),), dtype=torch.uint8, device=device))
+        return self._workspaces[-1]
 
 
 def accept_stats_noalloc(logits, temperature, rows_per_seq, out, stream=None) -> int:

@@ -182,6 +182,7 @@ const char *fspad_strerror(int err)
     case FSPAD_ERR_BAD_TREE: return "parent[] is not a topologically ordered tree rooted at node 0";
     case FSPAD_ERR_NOMEM: return "allocation failed";
     case FSPAD_ERR_TOO_LARGE: return "size exceeds the fixed capacity of the no-allocation entry point";
+    case FSPAD_ERR_DEVICE: return "the context belongs to another device than the current one";
     default: return "unknown error";
     }
 }

@@ -19,11 +19,14 @@ template <> struct Wanted<fspad_bf16> { static constexpr at::ScalarType type = a
 template <> struct Wanted<float> { static constexpr at::ScalarType type = at::kFloat; static constexpr const char *name = "torch.float32"; };
 template <> struct Wanted<int32_t> { static constexpr at::ScalarType type = at::kInt; static constexpr const char *name = "torch.int32"; };
 template <> struct Wanted<uint64_t> { static constexpr at::ScalarType type = at::kLong; static constexpr const char *name = "torch.int64"; };
+template <> struct Wanted<int64_t> { static constexpr at::ScalarType type = at::kLong; static constexpr const char *name = "torch.int64"; };
+template <> struct Wanted<uint8_t> { static constexpr at::ScalarType type = at::kByte; static constexpr const char *name = "torch.uint8"; };
 template <> struct Wanted<void> { static constexpr at::ScalarType type = at::kByte; static constexpr const char *name = "torch.uint8"; };
 
 // Address of a tensor's data; a Python error is set and false returned where it is not what the call takes.
+// device >= 0: it has to lie on that one of the GPUs.  rows: its rows may stand further apart than they are long.
 template <typename T>
-bool tensor_address(PyObject *o, bool on_gpu, void **out)
+bool tensor_address(PyObject *o, bool on_gpu, int device, bool rows, void **out)
 {
     if (!THPVariable_Check(o)) {
         PyErr_Format(PyExc_TypeError, "expected a tensor of %s, got %R", Wanted<T>::name, (PyObject *)Py_TYPE(o));
@@ -36,7 +39,7 @@ bool tensor_address(PyObject *o, bool on_gpu, void **out)
         Py_XDECREF(is);
         return false;
     }
-    if (!t.is_contiguous()) {
+    if (!rows && !t.is_contiguous()) {
         PyErr_SetString(PyExc_ValueError, "tensor must be contiguous");
         return false;
     }
@@ -44,12 +47,16 @@ bool tensor_address(PyObject *o, bool on_gpu, void **out)
         PyErr_Format(PyExc_ValueError, "tensor must live on %s, not %s", on_gpu ? "cuda" : "cpu", t.device().str().c_str());
         return false;
     }
+    if (device >= 0 && t.get_device() != device) {
+        PyErr_Format(PyExc_ValueError, "tensor must live on cuda:%d, the context's device, not %s", device, t.device().str().c_str());
+        return false;
+    }
     *out = t.data_ptr();
     return true;
 }
 
 template <typename A>
-bool convert(PyObject *o, bool on_gpu, A *out)
+bool convert(PyObject *o, bool on_gpu, int device, bool rows, A *out)
 {
     if constexpr (std::is_pointer_v<A>) {
         using T = std::remove_cv_t<std::remove_pointer_t<A>>;
@@ -60,15 +67,20 @@ bool convert(PyObject *o, bool on_gpu, A *out)
                 p = PyLong_AsVoidPtr(o);
                 if (p == nullptr && PyErr_Occurred()) return false;
             } else if constexpr (std::is_same_v<T, void>) {
-                if (!tensor_address<T>(o, on_gpu, &p)) return false;
+                if (!tensor_address<T>(o, on_gpu, device, rows, &p)) return false;
             } else {
                 PyErr_SetString(PyExc_TypeError, "expected a context's address");
                 return false;
             }
-        } else if (!tensor_address<T>(o, on_gpu, &p)) {
+        } else if (!tensor_address<T>(o, on_gpu, device, rows, &p)) {
             return false;
         }
         *out = static_cast<A>(p);
+        return true;
+    } else if constexpr (std::is_floating_point_v<A>) {
+        const double v = PyFloat_AsDouble(o);
+        if (v == -1.0 && PyErr_Occurred()) return false;
+        *out = static_cast<A>(v);
         return true;
     } else {
         const long long v = PyLong_AsLongLong(o);
@@ -82,10 +94,11 @@ bool convert(PyObject *o, bool on_gpu, A *out)
     }
 }
 
-// host_from: the first argument whose tensors lie in host memory.  A tensor may throw when it is asked for its strides or its address
+// host_from: the first argument whose tensors lie in host memory.  local: every tensor has to lie on the context's device.  rows_at: an argument
+// whose rows may stand further apart (the binding has looked at its strides).  A tensor may throw when it is asked for its strides or its address
 // (one inside vmap or grad, for instance): by torch's own translation that becomes the Python exception.
 template <typename... A, size_t... I>
-PyObject *invoke(int (*fn)(A...), PyObject *const *args, Py_ssize_t n, size_t host_from, std::index_sequence<I...>)
+PyObject *invoke(int (*fn)(A...), PyObject *const *args, Py_ssize_t n, size_t host_from, bool local, size_t rows_at, std::index_sequence<I...>)
 {
     if (n != (Py_ssize_t)sizeof...(A)) {
         PyErr_Format(PyExc_TypeError, "%zd arguments, not %zd", (Py_ssize_t)sizeof...(A), n);
@@ -93,7 +106,13 @@ PyObject *invoke(int (*fn)(A...), PyObject *const *args, Py_ssize_t n, size_t ho
     }
     std::tuple<A...> a{};
     try {
-        if (!(convert(args[I], I < host_from, &std::get<I>(a)) && ...)) return nullptr;
+        int device = -1;
+        if (local) {
+            fspad_ctx *ctx = nullptr;
+            if (!convert(args[0], true, -1, false, &ctx)) return nullptr;
+            device = fspad_device(ctx);
+        }
+        if (!(convert(args[I], I < host_from, device, I == rows_at, &std::get<I>(a)) && ...)) return nullptr;
     } catch (...) {
         torch::translate_exception_to_python(std::current_exception());
         return nullptr;
@@ -105,9 +124,9 @@ PyObject *invoke(int (*fn)(A...), PyObject *const *args, Py_ssize_t n, size_t ho
     return PyLong_FromLong(rc);
 }
 template <typename... A>
-PyObject *invoke(int (*fn)(A...), PyObject *const *args, Py_ssize_t n, size_t host_from = 99)
+PyObject *invoke(int (*fn)(A...), PyObject *const *args, Py_ssize_t n, size_t host_from = 99, bool local = false, size_t rows_at = 99)
 {
-    return invoke(fn, args, n, host_from, std::index_sequence_for<A...>());
+    return invoke(fn, args, n, host_from, local, rows_at, std::index_sequence_for<A...>());
 }
 
 #define FSPAD_CALL(name, ...) \
@@ -124,13 +143,20 @@ FSPAD_CALL(tree_build)
 FSPAD_CALL(draft_expand)
 FSPAD_CALL(verify_step)
 FSPAD_CALL(verify_step_host, 2)
+FSPAD_CALL(rope_qkv, 99, true, 1)
+FSPAD_CALL(block_plan, 99, true)
+FSPAD_CALL(kv_write_packed, 99, true)
+FSPAD_CALL(kv_append_packed, 99, true)
+FSPAD_CALL(tree_attn_packed, 99, true)
 #undef FSPAD_CALL
 
 #define FSPAD_ENTRY(name) {#name, (PyCFunction)(void (*)(void))call_##name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FSPAD_ENTRY(tree_attn), FSPAD_ENTRY(tree_attn_paged), FSPAD_ENTRY(tree_accept), FSPAD_ENTRY(kv_compact),
                          FSPAD_ENTRY(kv_compact_paged), FSPAD_ENTRY(kv_append), FSPAD_ENTRY(lm_head_accept),
                          FSPAD_ENTRY(feature_sampler), FSPAD_ENTRY(tree_build), FSPAD_ENTRY(draft_expand),
-                         FSPAD_ENTRY(verify_step), FSPAD_ENTRY(verify_step_host), {nullptr, nullptr, 0, nullptr}};
+                         FSPAD_ENTRY(verify_step), FSPAD_ENTRY(verify_step_host), FSPAD_ENTRY(rope_qkv),
+                         FSPAD_ENTRY(block_plan), FSPAD_ENTRY(kv_write_packed), FSPAD_ENTRY(kv_append_packed),
+                         FSPAD_ENTRY(tree_attn_packed), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pycall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
