@@ -13,7 +13,7 @@ LIB = os.path.join(PKG, "libfspad.so")
 HEADER = os.path.join(ROOT, "include", "fspad.h")
 CALLS_SRC = os.path.join(CSRC, "pycall.cpp")
 SOURCES = ["api.cu", "accept_stats.cu", "accept_walk.cu", "kv_compact.cu", "tree_attn.cu", "tree_attn_umma.cu", "tree_build.cu", "draft_expand.cu", "lm_head.cu", "feature_sampler.cu",
-           "api_cache.cu", "rope_qkv.cu", "block_plan.cu", "kv_packed.cu", "tree_attn_packed.cu"]
+           "api_cache.cu", "rope_qkv.cu", "block_plan.cu", "kv_packed.cu", "tree_attn_packed.cu", "tree_attn_packed_umma.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-I" + os.path.join(ROOT, "include"), "-I" + CSRC]
 

@@ -1,0 +1,232 @@
+// What the two kernels of the attention over the 4-bit cache share: their arguments, the list of work that its CTAs cut into equal parts, and the merge of
+// the runs that were cut.
+//
+// For every sequence, kv head and tile of BM query rows the list holds a run of units of UNIT keys: the tree's first, then the cache's.  Every CTA takes an
+// equal part of the list wherever the cuts fall, so that ragged lengths and any number of sequences fill the SMs alike, and nothing about the lengths has to be
+// known on the host.  A run that was cut leaves a partial (maximum, sum, unnormalised row) for each piece.
+#pragma once
+#include "packed.cuh"
+#include "umma_common.cuh"
+
+namespace packed {
+
+constexpr int D = FSPAD_HEAD_DIM;
+constexpr float kLazyLog2 = 8.f;         // a row's reference maximum may lag its true maximum by this much (log2)
+// Weights are 2^(score - reference + 7), at most 2^15 with the lag: as fp16 operands they keep their 11 bits down to 2^-21 of the reference's own.
+constexpr float kBiasLog2 = 7.f;
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct Args {
+    const fspad_bf16 *q;
+    const uint8_t *kc, *ks, *vc, *vs;    // codes and scales of one layer's K and V planes
+    const int *table;
+    int table_stride, n_blocks;
+    const fspad_bf16 *tk, *tv;
+    const int *parent, *prefix_len;
+    int N, B, Hq, Hkv, G, M, mtiles;     // M = N * G query rows of a kv head, in mtiles tiles
+    float scale_log2;
+    fspad_bf16 *out;
+    float *part_o;                       // [CTAs][2][BM][D]: of the run that began before the CTA's part, of the one that goes on behind it
+    float2 *part_ml;                     // [CTAs][2][BM]
+    int *cuts;                           // [CTAs][8]: the run that the CTA's part begins inside of, where the part before holds its beginning (see tell_cut)
+    int *status;
+};
+
+// Where a sequence's units lie in the list.
+__device__ __forceinline__ int prefix_of(const Args &a, int b, bool report)
+{
+    const int L = a.prefix_len[b];
+    const long long most = (long long)a.table_stride * 128;
+    if (L >= 0 && L <= most) return L;
+    if (report) fspad_report(a.status, FSPAD_ERR_RANGE);
+    return L < 0 ? 0 : (int)most;
+}
+template <int UNIT> __device__ __forceinline__ int tree_units(const Args &a) { return (a.N + UNIT - 1) / UNIT; }
+template <int UNIT> __device__ __forceinline__ int run_units(const Args &a, int L) { return tree_units<UNIT>(a) + (int)(((long long)L + UNIT - 1) / UNIT); }
+// How many CTAs get a part, and the first unit of the i-th one's (no part is empty).  With chunks of 128 keys for 256 rows a part of a cut run leaves 128 KB,
+// which cost about a thirtieth of what a chunk takes to write and read again: of few chunks, then, fewer parts than SMs (5 sqrt(total)).
+template <int UNIT> __device__ __forceinline__ int parts_of(int total, int ctas)
+{
+    if (UNIT == 128 && total < (ctas * ctas) / 25) ctas = max(1, (int)sqrtf((float)(total * 25)));
+    return min(total, ctas);
+}
+// The list is cut into parts of q or, the first r of them, q + 1 units.  (Units are counted in 32 bits: the host has seen to it that they fit.)
+struct Parts {
+    int n, q, r;                         // parts, units / parts, units % parts
+    __device__ __forceinline__ Parts(int total, int ctas) : n(ctas), q(total / ctas), r(total - q * ctas) {}
+    __device__ __forceinline__ int start(int i) const { return i * q + min(i, r); }
+    __device__ __forceinline__ int owner(int x) const { const int b = r * (q + 1); return x < b ? x / (q + 1) : r + (x - b) / q; }
+};
+
+// The units of all sequences together; `at` and `before`: the sequence that CTA `part`'s part of the list begins in and the units of
+// those before it (of a CTA without a part: nothing).  All T threads of the CTA call it, and there is a CTA barrier in it; scratch holds T / 32 + 2 values.
+template <int T, int UNIT>
+__device__ __forceinline__ int scan_units(const Args &a, int part, int ctas, int &at, int &before, int *scratch, bool report)
+{
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, runs = a.Hkv * a.mtiles;
+    if (a.B <= 32) {                     // every warp for itself
+        int inc = lane < a.B ? runs * run_units<UNIT>(a, prefix_of(a, lane, report)) : 0;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const int o = __shfl_up_sync(0xffffffffu, inc, off);
+            if (lane >= off) inc += o;
+        }
+        const int total = __shfl_sync(0xffffffffu, inc, 31);
+        const Parts p(total, parts_of<UNIT>(total, ctas));
+        const int want = part < p.n ? p.start(part) : total;
+        at = __popc(__ballot_sync(0xffffffffu, inc <= want));
+        before = __shfl_sync(0xffffffffu, inc, max(at - 1, 0));
+        if (at == 0) before = 0;
+        at = min(at, a.B - 1);
+        __syncthreads();
+        return total;
+    }
+    const int per = (a.B + T - 1) / T;
+    const int b0 = min(a.B, tid * per), b1 = min(a.B, b0 + per);
+    int mine = 0;
+#pragma unroll 1
+    for (int b = b0; b < b1; ++b) mine += runs * run_units<UNIT>(a, prefix_of(a, b, report));
+    int inc = mine;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const int o = __shfl_up_sync(0xffffffffu, inc, off);
+        if (lane >= off) inc += o;
+    }
+    if (lane == 31) scratch[warp] = inc;
+    __syncthreads();
+    int total = 0;
+#pragma unroll 4
+    for (int w = 0; w < T / 32; ++w) {
+        if (w < warp) inc += scratch[w];
+        total += scratch[w];
+    }
+    const Parts p(total, parts_of<UNIT>(total, ctas));
+    const int want = part < p.n ? p.start(part) : total;
+    int x = inc - mine;
+    if (x <= want && want < inc) {
+        int b = b0;
+#pragma unroll 1
+        for (; b < b1; ++b) {
+            const int n = runs * run_units<UNIT>(a, prefix_of(a, b, false));
+            if (want < x + n) break;
+            x += n;
+        }
+        scratch[T / 32] = b;
+        scratch[T / 32 + 1] = x;
+    }
+    __syncthreads();
+    at = scratch[T / 32];
+    before = scratch[T / 32 + 1];
+    return total;
+}
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n"
+                 :: "r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
+{
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+// Whether one of the two bf16 of a word is an infinity or a NaN.
+__device__ __forceinline__ bool odd_value(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
+
+// One thread of every CTA: leaves word of the run that its part begins inside of, for the merge, if it holds the run's second piece.
+template <int UNIT>
+__device__ __forceinline__ void tell_cut(const Args &a, const Parts &p, int cta, int b, int before)
+{
+    int4 lo = make_int4(-1, 0, 0, 0);
+    int i1 = 0;
+    if (cta < p.n) {
+        const int pos = p.start(cta), n_run = run_units<UNIT>(a, prefix_of(a, b, false));
+        const int run = (pos - before) / n_run, start = before + run * n_run;
+        if (start < pos) {
+            const int i0 = p.owner(start);
+            if (i0 == cta - 1) {
+                i1 = p.owner(start + n_run - 1);
+                lo = make_int4(b, run / a.mtiles, run % a.mtiles, i0);
+            }
+        }
+    }
+    reinterpret_cast<int4 *>(a.cuts)[2 * cta] = lo;
+    a.cuts[8 * cta + 4] = i1;
+}
+
+// The pieces of the runs that were cut, merged: ROWS rows a CTA, each by WPR warps that take its pieces in turn, four elements a lane.
+template <int BM, int ROWS, int WPR>
+__global__ void __launch_bounds__(ROWS * WPR * 32)
+tree_attn_packed_merge_kernel(const Args a)
+{
+    __shared__ float4 s_acc[ROWS * WPR][32];
+    __shared__ float s_l[ROWS * WPR];
+    fspad_pdl_trigger();
+    fspad_pdl_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp % WPR;
+    const int4 run = __ldcg(reinterpret_cast<const int4 *>(a.cuts) + 2 * blockIdx.x);
+    const int i0 = run.w, i1 = __ldcg(a.cuts + 8 * blockIdx.x + 4);
+    const int row = blockIdx.y * ROWS + warp / WPR, gr = run.z * BM + row;
+    const bool there = run.x >= 0 && gr < a.M;
+    if (WPR == 1 && !there) return;
+    if (run.x < 0 || run.z * BM + (int)blockIdx.y * ROWS >= a.M) return;
+    auto slot_of = [&](int i) { return ((size_t)i * 2 + (i == i0 ? 1 : 0)) * BM + row; };
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float l = 0.f;
+    if (there) {
+        float m = -INFINITY;
+        for (int i = i0 + lane; i <= i1; i += 32) m = fmaxf(m, __ldcg(&a.part_ml[slot_of(i)]).x);
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+#pragma unroll 8
+        for (int i = i0 + part; i <= i1; i += WPR) {
+            const size_t slot = slot_of(i);
+            const float2 ml = __ldcg(&a.part_ml[slot]);
+            const float4 v = __ldcg(reinterpret_cast<const float4 *>(a.part_o + slot * D) + lane);
+            const float w = ml.x == -INFINITY ? 1.f : umma::ex2f(ml.x - m);      // (without a maximum the sum and the row are zero, or NaN)
+            l += w * ml.y;
+            acc.x += w * v.x; acc.y += w * v.y; acc.z += w * v.z; acc.w += w * v.w;
+        }
+    }
+    if (WPR > 1) {
+        s_acc[warp][lane] = acc;
+        if (lane == 0) s_l[warp] = l;
+        __syncthreads();
+        if (part != 0 || !there) return;
+        l = 0.f;
+        acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < WPR; ++w) {
+            const float4 v = s_acc[warp + w][lane];
+            l += s_l[warp + w];
+            acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
+        }
+    }
+    const float inv = 1.f / l;
+    *reinterpret_cast<uint2 *>(a.out + (((size_t)run.x * a.N + gr / a.G) * a.Hq + run.y * a.G + gr % a.G) * D + 4 * lane) =
+        make_uint2(umma::pack_bf16(acc.x * inv, acc.y * inv), umma::pack_bf16(acc.z * inv, acc.w * inv));
+}
+
+// The scratch of a call: partial rows, their maxima and sums, the cuts.
+template <int BM> static inline size_t scratch_bytes(int ctas)
+{
+    return (size_t)ctas * (2 * BM * (D * sizeof(float) + sizeof(float2)) + 8 * sizeof(int));
+}
+template <int BM> static inline void scratch_in(Args &a, int ctas, void *workspace)
+{
+    a.part_o = static_cast<float *>(workspace);
+    a.part_ml = reinterpret_cast<float2 *>(a.part_o + (size_t)ctas * 2 * BM * D);
+    a.cuts = reinterpret_cast<int *>(a.part_ml + (size_t)ctas * 2 * BM);
+}
+
+// Whether the units of a call, at most, can be counted in 32 bits (and 25 times as many as are cut into fewer parts than there are CTAs).
+template <int UNIT> static inline bool units_fit(const Args &a)
+{
+    const long long run = ((long long)a.N + UNIT - 1) / UNIT + ((long long)a.table_stride * 128 + UNIT - 1) / UNIT;
+    return (double)run * a.B * a.Hkv * a.mtiles < 2147483647.0 - 1e6;
+}
+
+}  // namespace packed
+
+size_t fspad_attn_packed_umma_workspace(const fspad_ctx *ctx);
+cudaError_t fspad_launch_attn_packed_umma(fspad_ctx *ctx, packed::Args a, void *workspace, cudaStream_t st);

@@ -14,18 +14,17 @@
 // scales come by bulk copies into a ring of the warp's own; they go from shared memory straight into the registers of the operands (no
 // second trip through shared memory): the order of the elements within a product and of the keys within a unit is chosen so
 // that every lane reads 16 bytes of a row of K, and 8 of a row of V, and finds its operands in them.  The tree's rows are taken as bf16.
-#include "packed.cuh"
-#include "umma_common.cuh"
+#include "packed_list.cuh"
 
 namespace {
 
+using namespace packed;
 using umma::ex2f;
 using umma::mbar_expect_tx;
 using umma::mbar_init;
 using umma::mbar_wait;
 using umma::smem_u32;
 
-constexpr int D = FSPAD_HEAD_DIM;
 constexpr int UNIT = 32;                 // keys of a unit
 constexpr int BM = 16;                   // query rows of a tile
 constexpr int WARPS = 8;
@@ -34,99 +33,7 @@ constexpr int CODES = UNIT * FSPAD_PACKED_CODE_BYTES, SCALES = UNIT * FSPAD_PACK
 constexpr int STAGE = 2 * (CODES + SCALES);          // K codes | V codes | K scales | V scales
 constexpr int OROW = 4 * 36;             // floats of a staged row of 128: runs of 32 with a gap of 4, so that 16-byte stores do not collide
 constexpr int SMEM = WARPS * STAGES * STAGE + WARPS * BM * OROW * 4;
-constexpr float kLazyLog2 = 8.f;         // a row's reference maximum may lag its true maximum by this much (log2)
-// Weights are 2^(score - reference + 7), at most 2^15 with the lag: as fp16 operands they keep their 11 bits down to 2^-21 of the reference's own.
-constexpr float kBiasLog2 = 7.f;
-constexpr float kLog2e = 1.4426950408889634f;
 
-struct Args {
-    const fspad_bf16 *q;
-    const uint8_t *kc, *ks, *vc, *vs;    // codes and scales of one layer's K and V planes
-    const int *table;
-    int table_stride, n_blocks;
-    const fspad_bf16 *tk, *tv;
-    const int *parent, *prefix_len;
-    int N, B, Hq, Hkv, G, M, mtiles;
-    float scale_log2;
-    fspad_bf16 *out;
-    float *part_o;                       // [CTAs][2][BM][D]: of the run that began before the CTA's part, of the one that goes on behind it
-    float2 *part_ml;                     // [CTAs][2][BM]
-    int *status;
-};
-
-// Where a sequence's units lie in the list.
-__device__ __forceinline__ int prefix_of(const Args &a, int b, bool report)
-{
-    const int L = a.prefix_len[b];
-    const long long most = (long long)a.table_stride * 128;
-    if (L >= 0 && L <= most) return L;
-    if (report) fspad_report(a.status, FSPAD_ERR_RANGE);
-    return L < 0 ? 0 : (int)most;
-}
-__device__ __forceinline__ int tree_units(const Args &a) { return (a.N + UNIT - 1) / UNIT; }
-__device__ __forceinline__ int run_units(const Args &a, int L) { return tree_units(a) + (int)(((long long)L + UNIT - 1) / UNIT); }
-// How many CTAs get a part, and the first unit of the i-th one's (no part is empty).
-__device__ __forceinline__ int parts_of(long long total, int ctas) { return total < ctas ? (int)total : ctas; }
-__device__ __forceinline__ long long part_start(long long total, int parts, int i) { return total * i / parts; }
-__device__ __forceinline__ int owner_of(long long total, int parts, long long x)
-{
-    int i = (int)(x * parts / total);
-    while (i + 1 < parts && part_start(total, parts, i + 1) <= x) ++i;
-    while (i > 0 && part_start(total, parts, i) > x) --i;
-    return i;
-}
-
-// The units of all sequences together; `at` and `before`: the sequence that CTA `part`'s part of the list begins in (part < 0: the one that `at` says) and the
-// units of those before it (of a CTA without a part: nothing).  All T threads of the CTA call it; scratch holds T / 32 + 2 values.
-template <int T>
-__device__ long long scan_units(const Args &a, int part, int ctas, int &at, long long &before, long long *scratch, bool report)
-{
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int per = (a.B + T - 1) / T;
-    const int b0 = min(a.B, tid * per), b1 = min(a.B, b0 + per);
-    const long long runs = (long long)a.Hkv * a.mtiles;
-    long long mine = 0;
-    for (int b = b0; b < b1; ++b) mine += runs * run_units(a, prefix_of(a, b, report));
-    long long inc = mine;
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-        const long long o = __shfl_up_sync(0xffffffffu, inc, off);
-        if (lane >= off) inc += o;
-    }
-    if (lane == 31) scratch[warp] = inc;
-    __syncthreads();
-    long long total = 0;
-#pragma unroll
-    for (int w = 0; w < T / 32; ++w) {
-        if (w < warp) inc += scratch[w];
-        total += scratch[w];
-    }
-    const int parts = parts_of(total, ctas);
-    const long long want = part < 0 ? 0 : part < parts ? part_start(total, parts, part) : total;
-    long long x = inc - mine;
-    const bool here = part >= 0 ? x <= want && want < inc : at >= b0 && at < b1;
-    if (here) {
-        int b = b0;
-        for (; b < b1; ++b) {
-            if (part < 0 && b == at) break;
-            const long long n = runs * run_units(a, prefix_of(a, b, false));
-            if (part >= 0 && want < x + n) break;
-            x += n;
-        }
-        scratch[T / 32] = b;
-        scratch[T / 32 + 1] = x;
-    }
-    __syncthreads();
-    at = (int)scratch[T / 32];
-    before = scratch[T / 32 + 1];
-    return total;
-}
-
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
-{
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n"
-                 :: "r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
-}
 __device__ __forceinline__ void mma16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
@@ -136,11 +43,6 @@ __device__ __forceinline__ void mma16_bf(float (&c)[4], const uint32_t (&a)[4], 
 {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
-{
-    const __half2 h = __floats2half2_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t *>(&h);
 }
 __device__ __forceinline__ uint4 ld16(uint32_t at)
 {
@@ -166,9 +68,6 @@ __device__ __forceinline__ uint32_t ld1(uint32_t at)
     asm volatile("ld.shared.u8 %0, [%1];\n" : "=r"(v) : "r"(at));
     return v;
 }
-// Whether one of the two bf16 of a word is an infinity or a NaN.
-__device__ __forceinline__ bool odd_value(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
-
 // Columns 2c and 2c + 1 of a product's tile of eight keys are keys c and 4 + (c ^ 1): rows that the lanes read side by side then begin in
 // different halves of the shared memory's 128-byte line.
 __device__ __forceinline__ int key_of(int column) { return (column & 1) ? 4 + ((column >> 1) ^ 1) : column >> 1; }
@@ -178,7 +77,7 @@ tree_attn_packed_kernel(const Args a)
 {
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ __align__(8) unsigned long long s_bar[WARPS * STAGES];
-    __shared__ long long s_scan[WARPS + 2];
+    __shared__ int s_scan[WARPS + 2];
     __shared__ short s_par[FSPAD_MAX_NODES_WIDE];
     __shared__ float2 s_ml[WARPS][BM];
     __shared__ int s_fail;
@@ -199,21 +98,21 @@ tree_attn_packed_kernel(const Args a)
     fspad_pdl_wait();
 
     const int ctas = gridDim.x, cta = blockIdx.x;
-    int b = 0;
-    long long before = 0;
-    const long long total = scan_units<WARPS * 32>(a, cta, ctas, b, before, s_scan, cta == 0);
-    const int parts = parts_of(total, ctas);
-    long long pos = cta < parts ? part_start(total, parts, cta) : total;
-    const long long end = cta < parts ? part_start(total, parts, cta + 1) : total;
-    const int nt = tree_units(a), runs = a.Hkv * a.mtiles;
+    int b = 0, before = 0;
+    const int total = scan_units<WARPS * 32, UNIT>(a, cta, ctas, b, before, s_scan, cta == 0);
+    const Parts part(total, parts_of<UNIT>(total, ctas));
+    if (tid == 0) tell_cut<UNIT>(a, part, cta, b, before);
+    int pos = cta < part.n ? part.start(cta) : total;
+    const int end = cta < part.n ? part.start(cta + 1) : total;
+    const int nt = tree_units<UNIT>(a), runs = a.Hkv * a.mtiles;
     uint32_t phase = 0;                              // of the ring's barriers, a bit a stage
     bool failed = false;
 
     while (pos < end) {
-        const int L = prefix_of(a, b, false), n_run = run_units(a, L);
-        const int run = (int)((pos - before) / n_run);
-        const int u0 = (int)(pos - before - (long long)run * n_run);
-        const int u1 = (int)min((long long)n_run, (long long)u0 + (end - pos));
+        const int L = prefix_of(a, b, false), n_run = run_units<UNIT>(a, L);
+        const int run = (pos - before) / n_run;
+        const int u0 = pos - before - run * n_run;
+        const int u1 = min(n_run, u0 + (end - pos));
         const int h = run / a.mtiles, row0 = (run % a.mtiles) * BM;
         const int *blocks = a.table + (size_t)b * a.table_stride;
 
@@ -549,67 +448,21 @@ tree_attn_packed_kernel(const Args a)
         if (any_fail) break;
         __syncthreads();                             // the staged rows are read
         pos += u1 - u0;
-        if (pos - before == (long long)n_run * runs) { before = pos; ++b; }
+        if (pos - before == n_run * runs) { before = pos; ++b; }
     }
     if (s_fail != 0 && tid == 0) fspad_report(a.status, FSPAD_ERR_TIMEOUT);
 }
 
-// The pieces of a run that was cut, merged: one CTA a query row, its four warps taking the pieces in turn, four elements a lane.
-__global__ void __launch_bounds__(128)
-tree_attn_packed_merge_kernel(const Args a, int ctas)
-{
-    __shared__ long long s_scan[4 + 2];
-    __shared__ float4 s_acc[4][32];
-    __shared__ float s_l[4];
-    fspad_pdl_trigger();
-    fspad_pdl_wait();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int gr = blockIdx.x % a.M, h = (blockIdx.x / a.M) % a.Hkv;
-    int b = blockIdx.x / a.M / a.Hkv;
-    long long before;
-    const long long total = scan_units<128>(a, -1, ctas, b, before, s_scan, false);
-    const int parts = parts_of(total, ctas);
-    const int n_run = run_units(a, prefix_of(a, b, false));
-    const long long s = before + (long long)(h * a.mtiles + gr / BM) * n_run;
-    const int i0 = owner_of(total, parts, s), i1 = owner_of(total, parts, s + n_run - 1);
-    if (i0 == i1) return;
-    auto slot_of = [&](int i) { return ((size_t)i * 2 + (i == i0 ? 1 : 0)) * BM + gr % BM; };
-    float m = -INFINITY;
-    for (int i = i0 + lane; i <= i1; i += 32) m = fmaxf(m, __ldcg(&a.part_ml[slot_of(i)]).x);
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float l = 0.f;
-#pragma unroll 4
-    for (int i = i0 + warp; i <= i1; i += 4) {
-        const size_t slot = slot_of(i);
-        const float2 ml = __ldcg(&a.part_ml[slot]);
-        const float4 v = __ldcg(reinterpret_cast<const float4 *>(a.part_o + slot * D) + lane);
-        const float w = ml.x == -INFINITY ? 1.f : ex2f(ml.x - m);            // (without a maximum the sum and the row are zero, or NaN)
-        l += w * ml.y;
-        acc.x += w * v.x; acc.y += w * v.y; acc.z += w * v.z; acc.w += w * v.w;
-    }
-    s_acc[warp][lane] = acc;
-    if (lane == 0) s_l[warp] = l;
-    __syncthreads();
-    if (warp != 0) return;
-    l = (s_l[0] + s_l[1]) + (s_l[2] + s_l[3]);
-#pragma unroll
-    for (int w = 1; w < 4; ++w) {
-        const float4 v = s_acc[w][lane];
-        acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
-    }
-    const float inv = 1.f / l;
-    *reinterpret_cast<uint2 *>(a.out + (((size_t)b * a.N + gr / a.G) * a.Hq + h * a.G + gr % a.G) * D + 4 * lane) =
-        make_uint2(umma::pack_bf16(acc.x * inv, acc.y * inv), umma::pack_bf16(acc.z * inv, acc.w * inv));
-}
-
 }  // namespace
+
+// Which of the two kernels takes a call, by the query rows of a kv head.
+static bool many_rows(const fspad_ctx *ctx, int N) { return (long long)N * (ctx->cfg.n_q_heads / ctx->cfg.n_kv_heads) > BM; }
 
 size_t fspad_attn_packed_workspace(const fspad_ctx *ctx, int N, int B)
 {
-    (void)N; (void)B;
-    return (size_t)ctx->sm_count * 2 * BM * (D * sizeof(float) + sizeof(float2));
+    (void)B;
+    if (many_rows(ctx, N)) return fspad_attn_packed_umma_workspace(ctx);
+    return scratch_bytes<BM>(ctx->sm_count);
 }
 
 cudaError_t fspad_launch_tree_attn_packed(fspad_ctx *ctx, const fspad_bf16 *q, const uint8_t *k_codes, const uint8_t *k_scales,
@@ -626,13 +479,13 @@ cudaError_t fspad_launch_tree_attn_packed(fspad_ctx *ctx, const fspad_bf16 *q, c
     a.M = N * a.G; a.mtiles = (a.M + BM - 1) / BM;
     a.scale_log2 = ctx->scale * kLog2e;
     a.out = out; a.status = ctx->d_status;
+    if (many_rows(ctx, N)) return fspad_launch_attn_packed_umma(ctx, a, workspace, st);
     const int ctas = ctx->sm_count;
-    a.part_o = static_cast<float *>(workspace);
-    a.part_ml = reinterpret_cast<float2 *>(a.part_o + (size_t)ctas * 2 * BM * D);
+    scratch_in<BM>(a, ctas, workspace);
     cudaError_t e = cudaFuncSetAttribute(tree_attn_packed_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
     if (e != cudaSuccess) return e;
     ctx->launches += 2;
     e = fspad_launch(tree_attn_packed_kernel, dim3((unsigned)ctas), dim3(WARPS * 32), SMEM, st, 0, a);
     if (e != cudaSuccess) return e;
-    return fspad_launch(tree_attn_packed_merge_kernel, dim3((unsigned)((long long)B * c.n_kv_heads * a.M)), dim3(128), 0, st, 0, a, ctas);
+    return fspad_launch(tree_attn_packed_merge_kernel<BM, 2, 4>, dim3((unsigned)ctas, (unsigned)((a.M < BM ? a.M : BM) + 1) / 2), dim3(256), 0, st, 0, a);
 }
