@@ -21,10 +21,8 @@ constexpr int kInFlight = 4;             // row pairs
 __device__ __forceinline__ uint32_t quantise(uint4 &x, uint32_t &scale, bool rounded)
 {
     uint32_t w[4] = {x.x, x.y, x.z, x.w};
-    uint32_t m = 0;                      // magnitudes of bf16 order like whole numbers, infinities and NaN on top
-#pragma unroll
-    for (int i = 0; i < 4; ++i) m = __vmaxu2(m, w[i] & 0x7fff7fffu);
-    m = max(m & 0xffffu, m >> 16);
+    uint32_t m = fspad_most2(fspad_most2(w[0], w[1]), fspad_most2(w[2], w[3]));
+    m = max(m & 0xffffu, m >> 16);       // (magnitudes of bf16 order like whole numbers, infinities and NaN on top)
     m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
     const bool finite = m < 0x7f80u;
     const float most = __uint_as_float(m << 16) / 6.0f;

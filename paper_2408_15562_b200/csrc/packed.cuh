@@ -55,6 +55,12 @@ __device__ __forceinline__ uint32_t fspad_e4m3_to_f16(uint32_t two_bytes)
     asm("{\n\t.reg .b16 h;\n\tcvt.u16.u32 h, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n\t}\n" : "=r"(r) : "r"(two_bytes));
     return r;
 }
+// Larger magnitudes of two pairs of bf16 (an infinity or a NaN stays one); what comes out has no signs.
+__device__ __forceinline__ uint32_t fspad_most2(uint32_t a, uint32_t b)
+{
+    const __nv_bfloat162 m = __hmax2_nan(__habs2(*reinterpret_cast<const __nv_bfloat162 *>(&a)), __habs2(*reinterpret_cast<const __nv_bfloat162 *>(&b)));
+    return *reinterpret_cast<const uint32_t *>(&m);
+}
 __device__ __forceinline__ uint32_t fspad_hmul2(uint32_t a, uint32_t b)
 {
     const __half2 h = __hmul2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&b));

@@ -16,6 +16,22 @@ constexpr float kLazyLog2 = 8.f;         // a row's reference maximum may lag it
 constexpr float kBiasLog2 = 7.f;
 constexpr float kLog2e = 1.4426950408889634f;
 
+// Division by a number that the host knows: x / d = (x * mul) >> 32 >> shift for 0 <= x < 2^31 (d of s bits: mul = 2^(31 + s) / d rounded up, which is off
+// by less than d / 2^(31 + s) <= 2^-31 of it).
+struct Divisor {
+    unsigned d, mul, shift;
+    void set(unsigned by)
+    {
+        d = by;
+        shift = 0;
+        while (shift < 31 && (1ull << shift) < by) ++shift;
+        mul = by <= 1 ? 0u : (unsigned)(((1ull << (31 + shift)) + by - 1) / by);
+    }
+#ifdef __CUDACC__
+    __device__ __forceinline__ int of(int x) const { return d <= 1u ? x : (int)(__umulhi((unsigned)x, mul) >> (shift - 1)); }
+#endif
+};
+
 struct Args {
     const fspad_bf16 *q;
     const uint8_t *kc, *ks, *vc, *vs;    // codes and scales of one layer's K and V planes
@@ -24,11 +40,13 @@ struct Args {
     const fspad_bf16 *tk, *tv;
     const int *parent, *prefix_len;
     int N, B, Hq, Hkv, G, M, mtiles;     // M = N * G query rows of a kv head, in mtiles tiles
+    Divisor by_G, by_tiles;              // G and mtiles again
     float scale_log2;
     fspad_bf16 *out;
-    float *part_o;                       // [CTAs][2][BM][D]: of the run that began before the CTA's part, of the one that goes on behind it
+    float *part_o;                       // [CTAs][2][BM][D]: of the run that began before the CTA's part, of the one that goes on behind it.  Of 256 rows:
+                                         // [..][2 row tiles][2 halves of the columns][128][64], a row's 16-byte pieces in the order piece ^ (row & 7)
     float2 *part_ml;                     // [CTAs][2][BM]
-    int *cuts;                           // [CTAs][8]: the run that the CTA's part begins inside of, where the part before holds its beginning (see tell_cut)
+    int *cuts;                           // [CTAs][8]: runs that were cut (see tell_cut)
     int *status;
 };
 
@@ -43,43 +61,87 @@ __device__ __forceinline__ int prefix_of(const Args &a, int b, bool report)
 }
 template <int UNIT> __device__ __forceinline__ int tree_units(const Args &a) { return (a.N + UNIT - 1) / UNIT; }
 template <int UNIT> __device__ __forceinline__ int run_units(const Args &a, int L) { return tree_units<UNIT>(a) + (int)(((long long)L + UNIT - 1) / UNIT); }
-// How many CTAs get a part, and the first unit of the i-th one's (no part is empty).  With chunks of 128 keys for 256 rows a part of a cut run leaves 128 KB,
-// which cost about a thirtieth of what a chunk takes to write and read again: of few chunks, then, fewer parts than SMs (5 sqrt(total)).
+// How many parts the list may be cut into.  With chunks of 128 keys for 256 rows a part of a cut run leaves 128 KB, which cost about a thirtieth of what a chunk
+// takes to write and read again: of few chunks, then, fewer parts than SMs (5 sqrt(total)).
 template <int UNIT> __device__ __forceinline__ int parts_of(int total, int ctas)
 {
     if (UNIT == 128 && total < (ctas * ctas) / 25) ctas = max(1, (int)sqrtf((float)(total * 25)));
     return min(total, ctas);
 }
-// The list is cut into parts of q or, the first r of them, q + 1 units.  (Units are counted in 32 bits: the host has seen to it that they fit.)
+
+// The list is cut in one of two ways.  With no more runs than parts (and no more than 32 sequences) every run is cut into pieces of at most `q` units, equal ones,
+// one to a CTA: a stretch of another run in a CTA costs as much as several units.  Otherwise into parts of q units or, the first r of them, q + 1, wherever
+// the cuts fall.  (Units are counted in 32 bits: the host has seen to it that they fit.)
 struct Parts {
     int n, q, r;                         // parts, units / parts, units % parts
-    __device__ __forceinline__ Parts(int total, int ctas) : n(ctas), q(total / ctas), r(total - q * ctas) {}
     __device__ __forceinline__ int start(int i) const { return i * q + min(i, r); }
     __device__ __forceinline__ int owner(int x) const { const int b = r * (q + 1); return x < b ? x / (q + 1) : r + (x - b) / q; }
 };
 
-// The units of all sequences together; `at` and `before`: the sequence that CTA `part`'s part of the list begins in and the units of
-// those before it (of a CTA without a part: nothing).  All T threads of the CTA call it, and there is a CTA barrier in it; scratch holds T / 32 + 2 values.
+// A CTA's part: it begins at unit u of run `run` (kv head and tile) of sequence b and is `left` units long, over further runs and sequences as they come.
+struct Part {
+    int b, run, u, left;
+    int i0, i1;                          // pieces of the run that the part begins in: the CTAs that hold the first and the last of them
+    bool by_run;                         // cut in the first way: i0 and i1 hold
+};
+
+// All T threads of the CTA call it, and there is a CTA barrier in it; scratch holds T / 32 + 2 values.
 template <int T, int UNIT>
-__device__ __forceinline__ int scan_units(const Args &a, int part, int ctas, int &at, int &before, int *scratch, bool report)
+__device__ __forceinline__ Part cut_list(const Args &a, int part, int ctas, Parts &p, int *scratch, bool report)
 {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, runs = a.Hkv * a.mtiles;
+    Part s = {0, 0, 0, 0, 0, 0, false};
     if (a.B <= 32) {                     // every warp for itself
-        int inc = lane < a.B ? runs * run_units<UNIT>(a, prefix_of(a, lane, report)) : 0;
+        const int n = lane < a.B ? run_units<UNIT>(a, prefix_of(a, lane, report)) : 0;
+        int inc = runs * n;
 #pragma unroll
         for (int off = 1; off < 32; off <<= 1) {
             const int o = __shfl_up_sync(0xffffffffu, inc, off);
             if (lane >= off) inc += o;
         }
         const int total = __shfl_sync(0xffffffffu, inc, 31);
-        const Parts p(total, parts_of<UNIT>(total, ctas));
-        const int want = part < p.n ? p.start(part) : total;
-        at = __popc(__ballot_sync(0xffffffffu, inc <= want));
-        before = __shfl_sync(0xffffffffu, inc, max(at - 1, 0));
-        if (at == 0) before = 0;
-        at = min(at, a.B - 1);
+        p.n = parts_of<UNIT>(total, ctas);
+        p.q = total / p.n;
+        p.r = total - p.q * p.n;
+        int want = part < p.n ? p.start(part) : total;
+        if (a.B * runs <= p.n) {
+            // the smallest piece with which there are no more pieces than parts, from below, within a step or two
+            int k, sum, q = max(1, (total + p.n - 1) / p.n);
+            for (;;) {
+                k = lane < a.B ? (n + q - 1) / q : 0;
+                inc = runs * k;
+#pragma unroll
+                for (int off = 1; off < 32; off <<= 1) {
+                    const int o = __shfl_up_sync(0xffffffffu, inc, off);
+                    if (lane >= off) inc += o;
+                }
+                sum = __shfl_sync(0xffffffffu, inc, 31);
+                if (sum <= p.n) break;
+                q += max(1, (int)((float)q * (float)(sum - p.n) / (float)(2 * sum)));        // (ends: at q = n of the longest there is a piece a run)
+            }
+            s.by_run = true;
+            p.n = sum;
+            want = part;
+            if (part < sum) {
+                s.b = __popc(__ballot_sync(0xffffffffu, inc <= part));
+                k = __shfl_sync(0xffffffffu, k, s.b);
+                const int nb = __shfl_sync(0xffffffffu, n, s.b), x = part - (s.b > 0 ? __shfl_sync(0xffffffffu, inc, s.b - 1) : 0);
+                s.run = x / k;
+                const int piece = x - s.run * k, w = nb / k, more = nb - w * k;              // the first `more` pieces are of w + 1 units
+                s.u = piece * w + min(piece, more);
+                s.left = w + (piece < more ? 1 : 0);
+                s.i0 = part - piece;
+                s.i1 = s.i0 + k - 1;
+            }
+        } else if (part < p.n) {
+            s.b = __popc(__ballot_sync(0xffffffffu, inc <= want));
+            const int nb = __shfl_sync(0xffffffffu, n, s.b), x = want - (s.b > 0 ? __shfl_sync(0xffffffffu, inc, s.b - 1) : 0);
+            s.run = x / nb;
+            s.u = x - s.run * nb;
+            s.left = p.start(part + 1) - want;
+        }
         __syncthreads();
-        return total;
+        return s;
     }
     const int per = (a.B + T - 1) / T;
     const int b0 = min(a.B, tid * per), b1 = min(a.B, b0 + per);
@@ -100,7 +162,9 @@ __device__ __forceinline__ int scan_units(const Args &a, int part, int ctas, int
         if (w < warp) inc += scratch[w];
         total += scratch[w];
     }
-    const Parts p(total, parts_of<UNIT>(total, ctas));
+    p.n = parts_of<UNIT>(total, ctas);
+    p.q = total / p.n;
+    p.r = total - p.q * p.n;
     const int want = part < p.n ? p.start(part) : total;
     int x = inc - mine;
     if (x <= want && want < inc) {
@@ -112,12 +176,17 @@ __device__ __forceinline__ int scan_units(const Args &a, int part, int ctas, int
             x += n;
         }
         scratch[T / 32] = b;
-        scratch[T / 32 + 1] = x;
+        scratch[T / 32 + 1] = want - x;
     }
     __syncthreads();
-    at = scratch[T / 32];
-    before = scratch[T / 32 + 1];
-    return total;
+    if (part < p.n) {
+        s.b = scratch[T / 32];
+        const int nb = run_units<UNIT>(a, prefix_of(a, s.b, false));
+        s.run = scratch[T / 32 + 1] / nb;
+        s.u = scratch[T / 32 + 1] - s.run * nb;
+        s.left = p.start(part + 1) - want;
+    }
+    return s;
 }
 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
@@ -125,6 +194,13 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n"
                  :: "r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
+// shared -> global; the thread that issued copies waits until their source may be written again, and until they are done
+__device__ __forceinline__ void bulk_store(void *dst, uint32_t src, uint32_t bytes)
+{
+    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;\n\tcp.async.bulk.commit_group;\n" :: "l"(dst), "r"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bulk_store_read() { asm volatile("cp.async.bulk.wait_group.read 0;\n" ::: "memory"); }
+__device__ __forceinline__ void bulk_store_wait() { asm volatile("cp.async.bulk.wait_group 0;\n" ::: "memory"); }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
 {
     const __half2 h = __floats2half2_rn(lo, hi);
@@ -133,25 +209,28 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
 // Whether one of the two bf16 of a word is an infinity or a NaN.
 __device__ __forceinline__ bool odd_value(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
 
-// One thread of every CTA: leaves word of the run that its part begins inside of, for the merge, if it holds the run's second piece.
+// One thread of every CTA: leaves word of the run that its part begins inside of, for the merge, if it holds the run's second piece: sequence, kv head, tile, and
+// the CTAs that hold the first and the last piece.  A sequence of -1: nothing to merge.
 template <int UNIT>
-__device__ __forceinline__ void tell_cut(const Args &a, const Parts &p, int cta, int b, int before)
+__device__ __forceinline__ void tell_cut(const Args &a, const Parts &p, const Part &s, int cta)
 {
-    int4 lo = make_int4(-1, 0, 0, 0);
-    int i1 = 0;
-    if (cta < p.n) {
-        const int pos = p.start(cta), n_run = run_units<UNIT>(a, prefix_of(a, b, false));
-        const int run = (pos - before) / n_run, start = before + run * n_run;
-        if (start < pos) {
-            const int i0 = p.owner(start);
-            if (i0 == cta - 1) {
-                i1 = p.owner(start + n_run - 1);
-                lo = make_int4(b, run / a.mtiles, run % a.mtiles, i0);
-            }
+    int4 what = make_int4(-1, 0, 0, 0);
+    int last = 0;
+    if (s.left > 0 && s.u > 0) {
+        int i0 = s.i0, i1 = s.i1;
+        if (!s.by_run) {
+            const int start = p.start(cta) - s.u;
+            i0 = p.owner(start);
+            i1 = p.owner(start + run_units<UNIT>(a, prefix_of(a, s.b, false)) - 1);
+        }
+        if (i0 == cta - 1) {
+            const int h = a.by_tiles.of(s.run);
+            what = make_int4(s.b, h, s.run - h * a.mtiles, i0);
+            last = i1;
         }
     }
-    reinterpret_cast<int4 *>(a.cuts)[2 * cta] = lo;
-    a.cuts[8 * cta + 4] = i1;
+    reinterpret_cast<int4 *>(a.cuts)[2 * cta] = what;
+    a.cuts[8 * cta + 4] = last;
 }
 
 // The pieces of the runs that were cut, merged: ROWS rows a CTA, each by WPR warps that take its pieces in turn, four elements a lane.
@@ -182,7 +261,8 @@ tree_attn_packed_merge_kernel(const Args a)
         for (int i = i0 + part; i <= i1; i += WPR) {
             const size_t slot = slot_of(i);
             const float2 ml = __ldcg(&a.part_ml[slot]);
-            const float4 v = __ldcg(reinterpret_cast<const float4 *>(a.part_o + slot * D) + lane);
+            const float4 v = __ldcg(reinterpret_cast<const float4 *>(a.part_o) + (BM == 256 ? (slot >> 7) * 4096 + (lane >> 4) * 2048 + (row & 127) * 16 + ((lane & 15) ^ (row & 7))
+                                                                                              : slot * (D / 4) + lane));
             const float w = ml.x == -INFINITY ? 1.f : umma::ex2f(ml.x - m);      // (without a maximum the sum and the row are zero, or NaN)
             l += w * ml.y;
             acc.x += w * v.x; acc.y += w * v.y; acc.z += w * v.z; acc.w += w * v.w;

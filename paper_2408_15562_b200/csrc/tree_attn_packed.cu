@@ -98,22 +98,17 @@ tree_attn_packed_kernel(const Args a)
     fspad_pdl_wait();
 
     const int ctas = gridDim.x, cta = blockIdx.x;
-    int b = 0, before = 0;
-    const int total = scan_units<WARPS * 32, UNIT>(a, cta, ctas, b, before, s_scan, cta == 0);
-    const Parts part(total, parts_of<UNIT>(total, ctas));
-    if (tid == 0) tell_cut<UNIT>(a, part, cta, b, before);
-    int pos = cta < part.n ? part.start(cta) : total;
-    const int end = cta < part.n ? part.start(cta + 1) : total;
+    Parts parts;
+    Part part = cut_list<WARPS * 32, UNIT>(a, cta, ctas, parts, s_scan, cta == 0);
+    if (tid == 0) tell_cut<UNIT>(a, parts, part, cta);
     const int nt = tree_units<UNIT>(a), runs = a.Hkv * a.mtiles;
     uint32_t phase = 0;                              // of the ring's barriers, a bit a stage
     bool failed = false;
 
-    while (pos < end) {
-        const int L = prefix_of(a, b, false), n_run = run_units<UNIT>(a, L);
-        const int run = (pos - before) / n_run;
-        const int u0 = pos - before - run * n_run;
-        const int u1 = min(n_run, u0 + (end - pos));
-        const int h = run / a.mtiles, row0 = (run % a.mtiles) * BM;
+    while (part.left > 0) {
+        const int b = part.b, L = prefix_of(a, b, false), n_run = run_units<UNIT>(a, L);
+        const int run = part.run, u0 = part.u, u1 = min(n_run, u0 + part.left);
+        const int h = a.by_tiles.of(run), row0 = (run - h * a.mtiles) * BM;
         const int *blocks = a.table + (size_t)b * a.table_stride;
 
         // ---- the warp's first fills: units u0 + warp, u0 + warp + WARPS, ... that lie in the cache ----
@@ -151,8 +146,7 @@ tree_attn_packed_kernel(const Args a)
             uint32_t m = 0;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                m = __vmaxu2(m, w[i].x & 0x7fff7fffu); m = __vmaxu2(m, w[i].y & 0x7fff7fffu);
-                m = __vmaxu2(m, w[i].z & 0x7fff7fffu); m = __vmaxu2(m, w[i].w & 0x7fff7fffu);
+                m = fspad_most2(m, fspad_most2(fspad_most2(w[i].x, w[i].y), fspad_most2(w[i].z, w[i].w)));
             }
             m = max(m & 0xffffu, m >> 16);
             m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
@@ -447,8 +441,9 @@ tree_attn_packed_kernel(const Args a)
         }
         if (any_fail) break;
         __syncthreads();                             // the staged rows are read
-        pos += u1 - u0;
-        if (pos - before == n_run * runs) { before = pos; ++b; }
+        part.left -= u1 - u0;
+        part.u = 0;
+        if (++part.run == runs) { part.run = 0; ++part.b; }
     }
     if (s_fail != 0 && tid == 0) fspad_report(a.status, FSPAD_ERR_TIMEOUT);
 }
@@ -477,6 +472,7 @@ cudaError_t fspad_launch_tree_attn_packed(fspad_ctx *ctx, const fspad_bf16 *q, c
     a.tk = tk; a.tv = tv; a.parent = parent; a.prefix_len = prefix_len;
     a.N = N; a.B = B; a.Hq = c.n_q_heads; a.Hkv = c.n_kv_heads; a.G = c.n_q_heads / c.n_kv_heads;
     a.M = N * a.G; a.mtiles = (a.M + BM - 1) / BM;
+    a.by_G.set((unsigned)a.G); a.by_tiles.set((unsigned)a.mtiles);
     a.scale_log2 = ctx->scale * kLog2e;
     a.out = out; a.status = ctx->d_status;
     if (many_rows(ctx, N)) return fspad_launch_attn_packed_umma(ctx, a, workspace, st);

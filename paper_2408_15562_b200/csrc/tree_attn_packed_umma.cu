@@ -163,36 +163,34 @@ tree_attn_packed_umma_kernel(const Args a)
     fspad_pdl_trigger();
     fspad_pdl_wait();
     tc_fence_before();
-    int b = 0, before = 0;
-    const int cta = blockIdx.x, total = scan_units<NT, UNIT>(a, cta, gridDim.x, b, before, s_scan, cta == 0);       // (with a barrier in it)
+    const int cta = blockIdx.x;
+    Parts parts;
+    Part part = cut_list<NT, UNIT>(a, cta, gridDim.x, parts, s_scan, cta == 0);      // (with a barrier in it)
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
-    const Parts part(total, parts_of<UNIT>(total, gridDim.x));
-    int pos = cta < part.n ? part.start(cta) : total;
-    const int end = cta < part.n ? part.start(cta + 1) : total;
     const int nt = tree_units<UNIT>(a), runs = a.Hkv * a.mtiles;
 
-    if (warp == 11 && lane == 0) tell_cut<UNIT>(a, part, cta, b, before);    // (a warp without another job)
+    if (warp == 11 && lane == 0) tell_cut<UNIT>(a, parts, part, cta);    // (a warp without another job)
 
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t sQ = base, sK = base + 2 * TILE, sV = base + 4 * TILE, sStage = base + 6 * TILE;
 
     // Every warp goes through the CTA's stretches by itself.
     auto next = [&](Segment &s) -> bool {
-        if (pos >= end) return false;
-        s.b = b;
-        s.L = prefix_of(a, b, false);
+        if (part.left <= 0) return false;
+        s.b = part.b;
+        s.L = prefix_of(a, part.b, false);
         s.n_run = run_units<UNIT>(a, s.L);
-        const int run = (pos - before) / s.n_run;
-        s.u0 = pos - before - run * s.n_run;
-        s.n_ch = min(s.n_run - s.u0, end - pos);
+        s.u0 = part.u;
+        s.n_ch = min(s.n_run - s.u0, part.left);
         s.n_tree = max(0, min(nt - s.u0, s.n_ch));
-        s.h = run / a.mtiles;
-        s.row0 = (run % a.mtiles) * BM;
+        s.h = a.by_tiles.of(part.run);
+        s.row0 = (part.run - s.h * a.mtiles) * BM;
         s.rows = min(BM, a.M - s.row0);
         s.two = s.rows > 128;
-        pos += s.n_ch;
-        if (pos - before == s.n_run * runs) { before = pos; ++b; }
+        part.left -= s.n_ch;
+        part.u = 0;
+        if (++part.run == runs) { part.run = 0; ++part.b; }
         return true;
     };
     bool failed = false;
@@ -209,13 +207,13 @@ tree_attn_packed_umma_kernel(const Args a)
             const int gr = s.row0 + (s.two ? grp * 128 : 0) + row;           // row of the kv head
             const bool row_ok = gr < a.M;
             const bool live = s.row0 + (s.two ? grp * 128 : 0) + (warp & 3) * 32 < a.M;
-            const int node = row_ok ? gr / a.G : -1;
+            const int node = row_ok ? a.by_G.of(gr) : -1, head = s.h * a.G + gr - node * a.G;        // (the head of a row that exists)
             float cs = 0.f;
             // The group's rows of queries into tile t, half a warp a row (a thread taking its own row met 32 lines an instruction); code that runs once
             // a stretch is kept short, for it is fetched cold: unrolled it took 12000 cycles.
             auto fetch_q = [&](int t) {
                 const uint32_t to = sQ + (uint32_t)t * TILE;
-                const long long mine = row_ok ? (((long long)s.b * a.N + node) * a.Hq + s.h * a.G + gr % a.G) * D : -1;
+                const long long mine = row_ok ? (((long long)s.b * a.N + node) * a.Hq + head) * D : -1;
                 const int piece = lane & 15, r0 = (warp & 3) * 32;
 #pragma unroll 2
                 for (int k = 0; k < 16; ++k) {
@@ -227,25 +225,35 @@ tree_attn_packed_umma_kernel(const Args a)
                 cp_async_wait<0>();
                 __syncwarp();
             };
-            // the thread's row of tile t as fp16 with its largest magnitude in [2^14, 2^15) (change: false for the factor alone)
+            // The rows of tile t as fp16, each with its largest magnitude in [2^14, 2^15) (change: false for the factors alone, which stay with the rows' threads).
             auto scale_q = [&](int t, bool change) {
                 const uint32_t to = sQ + (uint32_t)t * TILE;
-                uint32_t m = 0;
-#pragma unroll 4
-                for (int i = 0; i < 16; ++i) {
-                    const uint4 w = ld_shared16(to + tile_off(row, i));
-                    m = __vmaxu2(m, __vmaxu2(__vmaxu2(w.x & 0x7fff7fffu, w.y & 0x7fff7fffu), __vmaxu2(w.z & 0x7fff7fffu, w.w & 0x7fff7fffu)));
-                }
-                m = max(m & 0xffffu, m >> 16);
-                const int e = m == 0u || m >= 0x7f80u ? 14 : max((int)(m >> 7) - 127, -100);
-                const float up = __uint_as_float((uint32_t)(127 + 14 - e) << 23);
-                cs = a.scale_log2 * __uint_as_float((uint32_t)(127 - 14 + e) << 23);
-                if (!change) return;
-                auto half2 = [&](uint32_t x) { return pack_f16(__uint_as_float(x << 16) * up, __uint_as_float(x & 0xffff0000u) * up); };
-#pragma unroll 4
-                for (int i = 0; i < 16; ++i) {
-                    const uint4 w = ld_shared16(to + tile_off(row, i));
-                    st_shared16(to + tile_off(row, i), half2(w.x), half2(w.y), half2(w.z), half2(w.w));
+                const int piece = lane & 15, r0 = (warp & 3) * 32;
+#pragma unroll 1
+                for (int k0 = 0; k0 < 16; k0 += 4) {
+                    uint4 w[4];                              // (all of them under way before the first is used)
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) w[y] = ld_shared16(to + tile_off(r0 + 2 * (k0 + y) + (lane >> 4), piece));
+                    uint32_t m[4];
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) m[y] = fspad_most2(fspad_most2(w[y].x, w[y].y), fspad_most2(w[y].z, w[y].w));
+#pragma unroll
+                    for (int off = 8; off > 0; off >>= 1)
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) m[y] = fspad_most2(m[y], __shfl_xor_sync(0xffffffffu, m[y], off));
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {
+                        const uint32_t top = max(m[y] & 0xffffu, m[y] >> 16);
+                        const int e = top == 0u || top >= 0x7f80u ? 14 : max((int)(top >> 7) - 127, -100);
+                        const int mine = __shfl_sync(0xffffffffu, e, (lane & 1) * 16);       // of row 2 (k0 + y) + (lane & 1)
+                        if (lane >> 1 == k0 + y) cs = a.scale_log2 * __uint_as_float((uint32_t)(127 - 14 + mine) << 23);
+                        const float up = __uint_as_float((uint32_t)(127 + 14 - e) << 23);
+                        auto half2 = [&](uint32_t x) { return pack_f16(__uint_as_float(x << 16) * up, __uint_as_float(x & 0xffff0000u) * up); };
+                        w[y] = make_uint4(half2(w[y].x), half2(w[y].y), half2(w[y].z), half2(w[y].w));
+                    }
+                    if (change)
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) st_shared(to + tile_off(r0 + 2 * (k0 + y) + (lane >> 4), piece), w[y]);
                 }
             };
             auto tell_q = [&](int t) {
@@ -318,7 +326,7 @@ tree_attn_packed_umma_kernel(const Args a)
             s_ml[grp][row] = make_float2(m_run, l_run);
             const bool whole = s.n_ch == s.n_run;
             const int slot = cta * 2 + (s.u0 == 0 ? 1 : 0);
-            s_to[grp][row] = !row_ok ? -1 : whole ? (s.b * a.N + node) * a.Hq + s.h * a.G + gr % a.G : slot * BM + (gr - s.row0);
+            s_to[grp][row] = !row_ok ? -1 : whole ? (s.b * a.N + node) * a.Hq + head : slot * BM + (gr - s.row0);
             tc_fence_before();
             asm volatile("bar.sync 1, 256;\n" ::: "memory");
             tc_fence_after();
@@ -376,9 +384,9 @@ tree_attn_packed_umma_kernel(const Args a)
                             st_shared16(stage + (uint32_t)(row * 256 + (((x * 8 + j / 4) ^ (row & 7)) << 4)), r[j], r[j + 1], r[j + 2], r[j + 3]);
                     }
                 }
-                __syncwarp();
-                // a warp writes its own 32 rows: 4 of 128 bytes at a time, or 2 of 256
+                // a warp writes its own 32 rows, 4 of 128 bytes at a time
                 if (whole) {
+                    __syncwarp();
 #pragma unroll 2
                     for (int k = 0; k < 8; ++k) {
                         const int r = (warp & 3) * 32 + 4 * k + (lane >> 3), to = s_to[grp][r];
@@ -386,22 +394,27 @@ tree_attn_packed_umma_kernel(const Args a)
                             reinterpret_cast<uint4 *>(a.out + (size_t)to * D + hf * 64)[lane & 7] =
                                 ld_shared16(stage + (uint32_t)(r * 128 + (((lane & 7) ^ (r & 7)) << 4)));
                     }
+                    __syncwarp();
                 } else {
-#pragma unroll 4
-                    for (int k = 0; k < 16; ++k) {
-                        const int r = (warp & 3) * 32 + 2 * k + (lane >> 4), to = s_to[grp][r];
-                        if (to >= 0)
-                            reinterpret_cast<uint4 *>(a.part_o + (size_t)to * D + hf * 64)[lane & 15] =
-                                ld_shared16(stage + (uint32_t)(r * 256 + (((lane & 15) ^ (r & 7)) << 4)));
+                    // the warp's 32 rows as they lie, 8 KB in one copy (rows that do not exist among them: nobody looks at those)
+                    if (live) {
+                        fence_async_smem();
+                        __syncwarp();
+                        if (lane == 0) {
+                            const int tile = s.two ? grp : 0;
+                            bulk_store(a.part_o + (((size_t)slot * 2 + tile) * 2 + hf) * (128 * 64) + (warp & 3) * (32 * 64), stage + (uint32_t)((warp & 3) * 32 * 256), 32 * 256);
+                            bulk_store_read();
+                        }
+                        __syncwarp();
                     }
                 }
-                __syncwarp();
             }
             // nobody goes on to the next stretch (whose queries, products and exchange use the same places) before all have read
             tc_fence_before();
             asm volatile("bar.sync 1, 256;\n" ::: "memory");
             tc_fence_after();
         }
+        if (lane == 0) bulk_store_wait();                    // (the copies' memory is this CTA's)
     } else if (warp < 12) {
       asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
       if (warp == 8) {
@@ -525,27 +538,41 @@ tree_attn_packed_umma_kernel(const Args a)
                     const int key0 = u * UNIT;
                     uint32_t *odd = s_odd[tree_chunks & 1];
                     ++tree_chunks;
-#pragma unroll 1
-                    for (int plane = 1; plane >= 0; --plane) {
-                        if (cc >= 2 && !mbar_wait(bar((plane ? V_FREE : K_FREE) + slot), ((cc >> 1) - 1u) & 1u)) { failed = true; break; }
-                        if (plane && lane == 0) odd[w4] = 0u;        // (a warp's 32 rows are a word)
-                        __syncwarp();
-                        const fspad_bf16 *src = (plane ? a.tv : a.tk) + ((size_t)s.b * a.Hkv + s.h) * a.N * D;
-                        const uint32_t to = (plane ? sV : sK) + slot * TILE;
-                        const int piece = lane & 15;
+                    const int piece = lane & 15, rows = min(a.N - key0, UNIT);
+                    const size_t first = (((size_t)s.b * a.Hkv + s.h) * a.N + key0) * D + piece * 8;
+                    if (cc >= 2 && !mbar_wait(bar(V_FREE + slot), ((cc >> 1) - 1u) & 1u)) { failed = true; break; }
+                    if (cc >= 2 && !mbar_wait(bar(K_FREE + slot), ((cc >> 1) - 1u) & 1u)) { failed = true; break; }
+                    if (lane == 0) odd[w4] = 0u;             // (a warp's 32 rows are a word)
 #pragma unroll 4
-                        for (int r = w4 * 32 + (lane >> 4); r < w4 * 32 + 32; r += 2) {
-                            uint4 x = make_uint4(0u, 0u, 0u, 0u);
-                            if (key0 + r < a.N) x = __ldg(reinterpret_cast<const uint4 *>(src + (size_t)(key0 + r) * D) + piece);
-                            if (plane && (odd_value(x.x) || odd_value(x.y) || odd_value(x.z) || odd_value(x.w))) {
-                                atomicOr(&odd[w4], 1u << (r & 31));      // out of the product: see softmax
-                                x = make_uint4(0u, 0u, 0u, 0u);
-                            }
-                            st_shared(to + tile_off(r, piece), x);
+                    for (int r = w4 * 32 + (lane >> 4); r < w4 * 32 + 32; r += 2)
+                        cp_async16(sK + slot * TILE + tile_off(r, piece), a.tk + (r < rows ? first + (size_t)r * D : 0), r < rows);
+                    cp_async_commit();
+#pragma unroll 1
+                    for (int r8 = 0; r8 < 32; r8 += 16) {
+                        uint4 x[8];
+#pragma unroll
+                        for (int y = 0; y < 8; ++y) {
+                            const int r = w4 * 32 + r8 + 2 * y + (lane >> 4);
+                            x[y] = make_uint4(0u, 0u, 0u, 0u);
+                            if (r < rows) x[y] = __ldg(reinterpret_cast<const uint4 *>(a.tv + first + (size_t)r * D));
                         }
-                        fence_async_smem();
                         __syncwarp();
-                        if (lane == 0) mbar_arrive(bar((plane ? V_FULL : K_FULL) + slot));
+#pragma unroll
+                        for (int y = 0; y < 8; ++y) {
+                            const int r = r8 + 2 * y + (lane >> 4);
+                            if (odd_value(x[y].x) || odd_value(x[y].y) || odd_value(x[y].z) || odd_value(x[y].w)) {
+                                atomicOr(&odd[w4], 1u << r);         // out of the product: see softmax
+                                x[y] = make_uint4(0u, 0u, 0u, 0u);
+                            }
+                            st_shared(sV + slot * TILE + tile_off(w4 * 32 + r, piece), x[y]);
+                        }
+                    }
+                    cp_async_wait<0>();
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive(bar(V_FULL + slot));
+                        mbar_arrive(bar(K_FULL + slot));
                     }
                 } else {
                     const int left = s.L - (u - nt) * UNIT;  // keys of the chunk that exist
@@ -556,17 +583,21 @@ tree_attn_packed_umma_kernel(const Args a)
                         if (!mbar_wait(bar(ST_FULL + st), (n / STAGES) & 1u)) { failed = true; break; }
                         const uint32_t from = sStage + st * STAGE, to = (plane ? sV : sK) + slot * TILE;
                         // a lane takes a block of 16: blocks 4 x + (lane & 3) of eight rows at a time, so that the stores do not collide
+                        uint32_t w0[8], w1[8], sc[8];        // (all of them under way before the first is used)
 #pragma unroll
                         for (int k = 0; k < 8; ++k) {
-                            const int x = k & 1, r = w4 * 32 + (k >> 1) * 8 + (lane >> 2), blk = 4 * x + (lane & 3);
-                            uint32_t w0, w1, sc;
-                            asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];\n" : "=r"(w0), "=r"(w1) : "r"(from + (uint32_t)(r * 64 + blk * 8)));
-                            asm volatile("ld.shared.u8 %0, [%1];\n" : "=r"(sc) : "r"(from + KCODES + (uint32_t)(r * 8 + blk)));
-                            if (r >= left) sc = 0u;          // what lies behind the end may be anything: zeros
-                            const uint32_t s2 = fspad_e4m3_to_f16(sc * 0x101u);
+                            const int r = w4 * 32 + (k >> 1) * 8 + (lane >> 2), blk = 4 * (k & 1) + (lane & 3);
+                            asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];\n" : "=r"(w0[k]), "=r"(w1[k]) : "r"(from + (uint32_t)(r * 64 + blk * 8)));
+                            asm volatile("ld.shared.u8 %0, [%1];\n" : "=r"(sc[k]) : "r"(from + KCODES + (uint32_t)(r * 8 + blk)));
+                        }
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const int r = w4 * 32 + (k >> 1) * 8 + (lane >> 2), blk = 4 * (k & 1) + (lane & 3);
+                            if (r >= left) sc[k] = 0u;       // what lies behind the end may be anything: zeros
+                            const uint32_t s2 = fspad_e4m3_to_f16(sc[k] * 0x101u);
                             uint32_t f0[4], f1[4];
-                            fspad_e2m1_to_f16(w0, f0);
-                            fspad_e2m1_to_f16(w1, f1);
+                            fspad_e2m1_to_f16(w0[k], f0);
+                            fspad_e2m1_to_f16(w1[k], f1);
 #pragma unroll
                             for (int j = 0; j < 4; ++j) { f0[j] = fspad_hmul2(f0[j], s2); f1[j] = fspad_hmul2(f1[j], s2); }
                             st_shared16(to + tile_off(r, 2 * blk), f0[0], f0[1], f0[2], f0[3]);
@@ -606,6 +637,7 @@ cudaError_t fspad_launch_attn_packed_umma(fspad_ctx *ctx, packed::Args a, void *
 {
     const int ctas = ctx->sm_count;
     a.mtiles = (a.M + BM - 1) / BM;
+    a.by_tiles.set((unsigned)a.mtiles);
     scratch_in<BM>(a, ctas, workspace);
     cudaError_t e = cudaFuncSetAttribute(tree_attn_packed_umma_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
     if (e != cudaSuccess) return e;
