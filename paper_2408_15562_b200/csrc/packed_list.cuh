@@ -1,7 +1,7 @@
 // What the two kernels of the attention over the 4-bit cache share: their arguments, the list of work that its CTAs cut into equal parts, and the merge of
 // the runs that were cut.
 //
-// For every sequence, kv head and tile of BM query rows the list holds a run of units of UNIT keys: the tree's first, then the cache's.  Every CTA takes an
+// For every sequence, kv head and tile of BM query rows the list holds a run of units of UNIT keys: the tree's first, then the cache's.  Every CTA (or warp) takes an
 // equal part of the list wherever the cuts fall, so that ragged lengths and any number of sequences fill the SMs alike, and nothing about the lengths has to be
 // known on the host.  A run that was cut leaves a partial (maximum, sum, unnormalised row) for each piece.
 #pragma once
@@ -43,10 +43,10 @@ struct Args {
     Divisor by_G, by_tiles;              // G and mtiles again
     float scale_log2;
     fspad_bf16 *out;
-    float *part_o;                       // [CTAs][2][BM][D]: of the run that began before the CTA's part, of the one that goes on behind it.  Of 256 rows:
-                                         // [..][2 row tiles][2 halves of the columns][128][64], a row's 16-byte pieces in the order piece ^ (row & 7)
-    float2 *part_ml;                     // [CTAs][2][BM]
-    int *cuts;                           // [CTAs][8]: runs that were cut (see tell_cut)
+    float *part_o;                       // [parts][2][BM][D]: of the run that began before the part, of the one that goes on behind it.  Of 256 rows:
+                                         // [..][2 row tiles][4 quarters of the columns][128][32], a row's 16-byte pieces in the order piece ^ (row & 7)
+    float2 *part_ml;                     // [parts][2][BM]
+    int *cuts;                           // [parts][8]: runs that were cut (see tell_cut)
     int *status;
 };
 
@@ -78,17 +78,19 @@ struct Parts {
     __device__ __forceinline__ int owner(int x) const { const int b = r * (q + 1); return x < b ? x / (q + 1) : r + (x - b) / q; }
 };
 
-// A CTA's part: it begins at unit u of run `run` (kv head and tile) of sequence b and is `left` units long, over further runs and sequences as they come.
+// A part: it begins at unit u of run `run` (kv head and tile) of sequence b and is `left` units long, over further runs and sequences as they come.
 struct Part {
     int b, run, u, left;
-    int i0, i1;                          // pieces of the run that the part begins in: the CTAs that hold the first and the last of them
+    int i0, i1;                          // pieces of the run that the part begins in: the parts that hold the first and the last of them
     bool by_run;                         // cut in the first way: i0 and i1 hold
 };
 
-// All T threads of the CTA call it, and there is a CTA barrier in it; scratch holds T / 32 + 2 values.
-template <int T, int UNIT>
-__device__ __forceinline__ Part cut_list(const Args &a, int part, int ctas, Parts &p, int *scratch, bool report)
+// All T threads of the CTA call it, and there is a CTA barrier in it; scratch holds T / 32 + 2 W values.  W: how many parts a CTA takes: one, which all its
+// threads ask for, or one for each of its W = T / 32 warps (part0: the CTA's first, of `slots` that there may be).
+template <int T, int UNIT, int W>
+__device__ __forceinline__ Part cut_list(const Args &a, int part0, int slots, Parts &p, int *scratch, bool report)
 {
+    const int part = part0 + (W > 1 ? (int)(threadIdx.x >> 5) : 0), ctas = slots;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, runs = a.Hkv * a.mtiles;
     Part s = {0, 0, 0, 0, 0, 0, false};
     if (a.B <= 32) {                     // every warp for itself
@@ -165,26 +167,30 @@ __device__ __forceinline__ Part cut_list(const Args &a, int part, int ctas, Part
     p.n = parts_of<UNIT>(total, ctas);
     p.q = total / p.n;
     p.r = total - p.q * p.n;
-    const int want = part < p.n ? p.start(part) : total;
     int x = inc - mine;
-    if (x <= want && want < inc) {
-        int b = b0;
 #pragma unroll 1
-        for (; b < b1; ++b) {
-            const int n = runs * run_units<UNIT>(a, prefix_of(a, b, false));
-            if (want < x + n) break;
-            x += n;
+    for (int w = 0; w < W; ++w) {
+        const int want = part0 + w < p.n ? p.start(part0 + w) : total;
+        if (x <= want && want < inc) {
+            int b = b0, y = x;
+#pragma unroll 1
+            for (; b < b1; ++b) {
+                const int n = runs * run_units<UNIT>(a, prefix_of(a, b, false));
+                if (want < y + n) break;
+                y += n;
+            }
+            scratch[T / 32 + 2 * w] = b;
+            scratch[T / 32 + 2 * w + 1] = want - y;
         }
-        scratch[T / 32] = b;
-        scratch[T / 32 + 1] = want - x;
     }
     __syncthreads();
     if (part < p.n) {
-        s.b = scratch[T / 32];
+        const int at = T / 32 + 2 * (part - part0);
+        s.b = scratch[at];
         const int nb = run_units<UNIT>(a, prefix_of(a, s.b, false));
-        s.run = scratch[T / 32 + 1] / nb;
-        s.u = scratch[T / 32 + 1] - s.run * nb;
-        s.left = p.start(part + 1) - want;
+        s.run = scratch[at + 1] / nb;
+        s.u = scratch[at + 1] - s.run * nb;
+        s.left = p.start(part + 1) - p.start(part);
     }
     return s;
 }
@@ -200,6 +206,7 @@ __device__ __forceinline__ void bulk_store(void *dst, uint32_t src, uint32_t byt
     asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;\n\tcp.async.bulk.commit_group;\n" :: "l"(dst), "r"(src), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void bulk_store_read() { asm volatile("cp.async.bulk.wait_group.read 0;\n" ::: "memory"); }
+__device__ __forceinline__ void bulk_store_read_but_one() { asm volatile("cp.async.bulk.wait_group.read 1;\n" ::: "memory"); }
 __device__ __forceinline__ void bulk_store_wait() { asm volatile("cp.async.bulk.wait_group 0;\n" ::: "memory"); }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
 {
@@ -209,8 +216,8 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
 // Whether one of the two bf16 of a word is an infinity or a NaN.
 __device__ __forceinline__ bool odd_value(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
 
-// One thread of every CTA: leaves word of the run that its part begins inside of, for the merge, if it holds the run's second piece: sequence, kv head, tile, and
-// the CTAs that hold the first and the last piece.  A sequence of -1: nothing to merge.
+// One thread for every part: leaves word of the run that the part begins inside of, for the merge, if it holds the run's second piece: sequence, kv head, tile, and
+// the parts that hold the first and the last piece.  A sequence of -1: nothing to merge.
 template <int UNIT>
 __device__ __forceinline__ void tell_cut(const Args &a, const Parts &p, const Part &s, int cta)
 {
@@ -233,70 +240,77 @@ __device__ __forceinline__ void tell_cut(const Args &a, const Parts &p, const Pa
     a.cuts[8 * cta + 4] = last;
 }
 
-// The pieces of the runs that were cut, merged: ROWS rows a CTA, each by WPR warps that take its pieces in turn, four elements a lane.
-template <int BM, int ROWS, int WPR>
-__global__ void __launch_bounds__(ROWS * WPR * 32)
-tree_attn_packed_merge_kernel(const Args a)
+// The pieces of the runs that were cut, merged.  A CTA takes `rows` rows (a power of two, at most WARPS) of a run at a time, each by WARPS / rows warps that take its
+// pieces in turn, four elements a lane.
+template <int BM, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32)
+tree_attn_packed_merge_kernel(const Args a, int rows)
 {
-    __shared__ float4 s_acc[ROWS * WPR][32];
-    __shared__ float s_l[ROWS * WPR];
+    __shared__ float4 s_acc[WARPS][32];
+    __shared__ float s_l[WARPS];
     fspad_pdl_trigger();
     fspad_pdl_wait();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp % WPR;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, wpr = WARPS / rows;
     const int4 run = __ldcg(reinterpret_cast<const int4 *>(a.cuts) + 2 * blockIdx.x);
+    if (run.x < 0) return;
     const int i0 = run.w, i1 = __ldcg(a.cuts + 8 * blockIdx.x + 4);
-    const int row = blockIdx.y * ROWS + warp / WPR, gr = run.z * BM + row;
-    const bool there = run.x >= 0 && gr < a.M;
-    if (WPR == 1 && !there) return;
-    if (run.x < 0 || run.z * BM + (int)blockIdx.y * ROWS >= a.M) return;
-    auto slot_of = [&](int i) { return ((size_t)i * 2 + (i == i0 ? 1 : 0)) * BM + row; };
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float l = 0.f;
-    if (there) {
-        float m = -INFINITY;
-        for (int i = i0 + lane; i <= i1; i += 32) m = fmaxf(m, __ldcg(&a.part_ml[slot_of(i)]).x);
+#pragma unroll 1
+    for (int row0 = blockIdx.y * rows; row0 < BM && run.z * BM + row0 < a.M; row0 += gridDim.y * rows) {
+        const int row = row0 + warp % rows, gr = run.z * BM + row;
+        const bool there = gr < a.M;
+        auto slot_of = [&](int i) { return ((size_t)i * 2 + (i == i0 ? 1 : 0)) * BM + row; };
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        float l = 0.f;
+        if (there) {
+            float m = -INFINITY;
+            for (int i = i0 + lane; i <= i1; i += 32) m = fmaxf(m, __ldcg(&a.part_ml[slot_of(i)]).x);
 #pragma unroll
-        for (int off = 16; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+            for (int off = 16; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
 #pragma unroll 8
-        for (int i = i0 + part; i <= i1; i += WPR) {
-            const size_t slot = slot_of(i);
-            const float2 ml = __ldcg(&a.part_ml[slot]);
-            const float4 v = __ldcg(reinterpret_cast<const float4 *>(a.part_o) + (BM == 256 ? (slot >> 7) * 4096 + (lane >> 4) * 2048 + (row & 127) * 16 + ((lane & 15) ^ (row & 7))
-                                                                                              : slot * (D / 4) + lane));
-            const float w = ml.x == -INFINITY ? 1.f : umma::ex2f(ml.x - m);      // (without a maximum the sum and the row are zero, or NaN)
-            l += w * ml.y;
-            acc.x += w * v.x; acc.y += w * v.y; acc.z += w * v.z; acc.w += w * v.w;
+            for (int i = i0 + warp / rows; i <= i1; i += wpr) {
+                const size_t slot = slot_of(i);
+                const float2 ml = __ldcg(&a.part_ml[slot]);
+                const float4 v = __ldcg(reinterpret_cast<const float4 *>(a.part_o) + (BM == 256 ? (slot >> 7) * 4096 + (lane >> 3) * 1024 + (row & 127) * 8 + ((lane & 7) ^ (row & 7))
+                                                                                                  : slot * (D / 4) + lane));
+                const float w = ml.x == -INFINITY ? 1.f : umma::ex2f(ml.x - m);      // (without a maximum the sum and the row are zero, or NaN)
+                l += w * ml.y;
+                acc.x += w * v.x; acc.y += w * v.y; acc.z += w * v.z; acc.w += w * v.w;
+            }
+        }
+        if (wpr > 1) {
+            __syncthreads();
+            s_acc[warp][lane] = acc;
+            if (lane == 0) s_l[warp] = l;
+            __syncthreads();
+            if (warp < rows) {
+                l = 0.f;
+                acc = make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int w = warp; w < WARPS; w += rows) {
+                    const float4 v = s_acc[w][lane];
+                    l += s_l[w];
+                    acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
+                }
+            }
+        }
+        if (warp < rows && there) {
+            const float inv = 1.f / l;
+            const int node = a.by_G.of(gr);
+            *reinterpret_cast<uint2 *>(a.out + (((size_t)run.x * a.N + node) * a.Hq + run.y * a.G + (gr - node * a.G)) * D + 4 * lane) =
+                make_uint2(umma::pack_bf16(acc.x * inv, acc.y * inv), umma::pack_bf16(acc.z * inv, acc.w * inv));
         }
     }
-    if (WPR > 1) {
-        s_acc[warp][lane] = acc;
-        if (lane == 0) s_l[warp] = l;
-        __syncthreads();
-        if (part != 0 || !there) return;
-        l = 0.f;
-        acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int w = 0; w < WPR; ++w) {
-            const float4 v = s_acc[warp + w][lane];
-            l += s_l[warp + w];
-            acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
-        }
-    }
-    const float inv = 1.f / l;
-    *reinterpret_cast<uint2 *>(a.out + (((size_t)run.x * a.N + gr / a.G) * a.Hq + run.y * a.G + gr % a.G) * D + 4 * lane) =
-        make_uint2(umma::pack_bf16(acc.x * inv, acc.y * inv), umma::pack_bf16(acc.z * inv, acc.w * inv));
 }
 
-// The scratch of a call: partial rows, their maxima and sums, the cuts.
-template <int BM> static inline size_t scratch_bytes(int ctas)
+// The scratch of a call of so many parts: partial rows, their maxima and sums, the cuts.
+template <int BM> static inline size_t scratch_bytes(int parts)
 {
-    return (size_t)ctas * (2 * BM * (D * sizeof(float) + sizeof(float2)) + 8 * sizeof(int));
+    return (size_t)parts * (2 * BM * (D * sizeof(float) + sizeof(float2)) + 8 * sizeof(int));
 }
-template <int BM> static inline void scratch_in(Args &a, int ctas, void *workspace)
+template <int BM> static inline void scratch_in(Args &a, int parts, void *workspace)
 {
     a.part_o = static_cast<float *>(workspace);
-    a.part_ml = reinterpret_cast<float2 *>(a.part_o + (size_t)ctas * 2 * BM * D);
-    a.cuts = reinterpret_cast<int *>(a.part_ml + (size_t)ctas * 2 * BM);
+    a.part_ml = reinterpret_cast<float2 *>(a.part_o + (size_t)parts * 2 * BM * D);
+    a.cuts = reinterpret_cast<int *>(a.part_ml + (size_t)parts * 2 * BM);
 }
 
 // Whether the units of a call, at most, can be counted in 32 bits (and 25 times as many as are cut into fewer parts than there are CTAs).

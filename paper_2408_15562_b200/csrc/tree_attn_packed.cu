@@ -5,15 +5,15 @@
 //   s_j = c q_i . k_j,   out_i = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m)
 // over the L_b cached keys, whose rows are code * scale, and over the node itself and its ancestors among the bf16 tree rows.
 //
-// The work is one list: for every sequence, kv head and tile of 16 query rows a run of units of 32 keys, the tree's first.  Every CTA takes an
-// equal part of the list wherever the cuts fall, so that ragged lengths and any number of sequences fill the SMs alike; a run that
-// was cut leaves a partial (maximum, sum, unnormalised row) for each piece, which a second kernel merges.  A CTA's eight warps take the units of a
-// run in turn, each with its own maximum, sum and accumulators, and meet at the run's end.
+// Few query rows a kv head (up to 16; more: tree_attn_packed_umma.cu).  Every warp takes a part of the list of work (packed_list.cuh) by itself, in units of 32 keys,
+// with its own maximum, sum and accumulators; nothing in a CTA waits for anything else of it.
 //
 // A warp keeps its queries in registers as tensor-core operands (fp16, each row scaled by a power of two, which is exact).  A unit's codes and
 // scales come by bulk copies into a ring of the warp's own; they go from shared memory straight into the registers of the operands (no
 // second trip through shared memory): the order of the elements within a product and of the keys within a unit is chosen so
 // that every lane reads 16 bytes of a row of K, and 8 of a row of V, and finds its operands in them.  The tree's rows are taken as bf16.
+#include <type_traits>
+
 #include "packed_list.cuh"
 
 namespace {
@@ -27,12 +27,11 @@ using umma::smem_u32;
 
 constexpr int UNIT = 32;                 // keys of a unit
 constexpr int BM = 16;                   // query rows of a tile
-constexpr int WARPS = 8;
-constexpr int STAGES = 3;
+constexpr int WARPS = 12;
+constexpr int STAGES = 4;
 constexpr int CODES = UNIT * FSPAD_PACKED_CODE_BYTES, SCALES = UNIT * FSPAD_PACKED_SCALE_BYTES;
 constexpr int STAGE = 2 * (CODES + SCALES);          // K codes | V codes | K scales | V scales
-constexpr int OROW = 4 * 36;             // floats of a staged row of 128: runs of 32 with a gap of 4, so that 16-byte stores do not collide
-constexpr int SMEM = WARPS * STAGES * STAGE + WARPS * BM * OROW * 4;
+constexpr int SMEM = WARPS * STAGES * STAGE;
 
 __device__ __forceinline__ void mma16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
@@ -72,97 +71,76 @@ __device__ __forceinline__ uint32_t ld1(uint32_t at)
 // different halves of the shared memory's 128-byte line.
 __device__ __forceinline__ int key_of(int column) { return (column & 1) ? 4 + ((column >> 1) ^ 1) : column >> 1; }
 
+// WIDE: tiles may have more than 8 rows.
+template <bool WIDE>
 __global__ void __launch_bounds__(WARPS * 32, 1)
 tree_attn_packed_kernel(const Args a)
 {
+    constexpr int NX = WIDE ? 2 : 1;
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ __align__(8) unsigned long long s_bar[WARPS * STAGES];
-    __shared__ int s_scan[WARPS + 2];
-    __shared__ short s_par[FSPAD_MAX_NODES_WIDE];
-    __shared__ float2 s_ml[WARPS][BM];
-    __shared__ int s_fail;
+    __shared__ int s_scan[WARPS + 2 * WARPS];
 
     const int tid = threadIdx.x, lane = tid & 31, warp = umma::uniform_warp();
     const int g = lane >> 2, c = lane & 3;           // tensor-core operand rows / columns
     const uint32_t bar0 = smem_u32(&s_bar[warp * STAGES]);
     const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * STAGES * STAGE);
-    float *s_o = reinterpret_cast<float *>(smem + WARPS * STAGES * STAGE);
     if (lane == 0) {
 #pragma unroll
         for (int s = 0; s < STAGES; ++s) mbar_init(bar0 + 8u * s, 1);
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     }
-    if (tid == 0) s_fail = 0;
     __syncwarp();
     fspad_pdl_trigger();
     fspad_pdl_wait();
 
-    const int ctas = gridDim.x, cta = blockIdx.x;
+    const int slot0 = blockIdx.x * WARPS + warp;
     Parts parts;
-    Part part = cut_list<WARPS * 32, UNIT>(a, cta, ctas, parts, s_scan, cta == 0);
-    if (tid == 0) tell_cut<UNIT>(a, parts, part, cta);
+    Part part = cut_list<WARPS * 32, UNIT, WARPS>(a, blockIdx.x * WARPS, gridDim.x * WARPS, parts, s_scan, blockIdx.x == 0);
+    if (lane == 0) tell_cut<UNIT>(a, parts, part, slot0);
     const int nt = tree_units<UNIT>(a), runs = a.Hkv * a.mtiles;
-    uint32_t phase = 0;                              // of the ring's barriers, a bit a stage
-    bool failed = false;
+    uint32_t n_fill = 0, n_use = 0;                  // stages filled and used so far
 
+#pragma unroll 1
     while (part.left > 0) {
         const int b = part.b, L = prefix_of(a, b, false), n_run = run_units<UNIT>(a, L);
-        const int run = part.run, u0 = part.u, u1 = min(n_run, u0 + part.left);
-        const int h = a.by_tiles.of(run), row0 = (run - h * a.mtiles) * BM;
+        const int u0 = part.u, u1 = min(n_run, u0 + part.left);
+        const int h = a.by_tiles.of(part.run), row0 = (part.run - h * a.mtiles) * BM;
         const int *blocks = a.table + (size_t)b * a.table_stride;
 
-        // ---- the warp's first fills: units u0 + warp, u0 + warp + WARPS, ... that lie in the cache ----
-        const int first = u0 + warp;
-        const int first_kv = first >= nt ? first : first + ((nt - first + WARPS - 1) / WARPS) * WARPS;
-        const int n_kv = first_kv < u1 ? (u1 - first_kv + WARPS - 1) / WARPS : 0;
-        auto fill = [&](int i) {                     // lane 0: the warp's i-th unit of the cache
-            const int key0 = (first_kv + i * WARPS - nt) * UNIT, s = i % STAGES;
+        // ---- the first fills ----
+        const int kv0 = max(u0, nt) - nt, n_kv = max(0, u1 - nt - kv0);      // units of the cache
+        auto fill = [&](int i) {                     // lane 0
+            const int key0 = (kv0 + i) * UNIT;
             int blk = __ldg(blocks + (key0 >> 7));
             if (blk < 0 || blk >= a.n_blocks) { fspad_report(a.status, FSPAD_ERR_RANGE); blk = 0; }
             const size_t row = ((size_t)blk * a.Hkv + h) * 128 + (key0 & 127);
-            const uint32_t to = ring + (uint32_t)(s * STAGE), bar = bar0 + 8u * s;
+            const uint32_t st = n_fill % STAGES, to = ring + st * STAGE, bar = bar0 + 8u * st;
             mbar_expect_tx(bar, STAGE);
             bulk_load(to, a.kc + row * FSPAD_PACKED_CODE_BYTES, CODES, bar);
             bulk_load(to + 2 * CODES, a.ks + row * FSPAD_PACKED_SCALE_BYTES, SCALES, bar);
             bulk_load(to + CODES, a.vc + row * FSPAD_PACKED_CODE_BYTES, CODES, bar);
             bulk_load(to + 2 * CODES + SCALES, a.vs + row * FSPAD_PACKED_SCALE_BYTES, SCALES, bar);
         };
-        if (lane == 0)
-            for (int i = 0; i < STAGES && i < n_kv; ++i) fill(i);
+#pragma unroll 1
+        for (int i = 0; i < STAGES && i < n_kv; ++i) {
+            if (lane == 0) fill(i);
+            ++n_fill;
+        }
 
-        // ---- queries: rows g and g + 8 of the tile, elements 32 c .. 32 c + 31, scaled by a power of two so that the row's largest
-        // magnitude lies in [2^14, 2^15): 8 significant bits stay exact down to 2^-31 of the largest ----
-        const fspad_bf16 *qrow[2];
-        float cs[2];                                 // scores -> log2 units
-        uint32_t qf[8][4];
+        // ---- queries: rows g and g + 8 of the tile, elements 32 c .. 32 c + 31, as they are ----
+        uint32_t qf[8][4];                           // [product][a0, a1 (row + 8), a2 (column + 8), a3]
+        int node[2], to_row[2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
             const int gr = row0 + g + 8 * x;
-            const bool there = gr < a.M;
-            qrow[x] = there ? a.q + (((size_t)b * a.N + gr / a.G) * a.Hq + h * a.G + gr % a.G) * D + 32 * c : nullptr;
-            uint4 w[4];
+            const bool there = (WIDE || x == 0) && gr < a.M;
+            node[x] = there ? a.by_G.of(gr) : -1;
+            to_row[x] = there ? (b * a.N + node[x]) * a.Hq + h * a.G + (gr - node[x] * a.G) : -1;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = there ? __ldg(reinterpret_cast<const uint4 *>(qrow[x]) + i) : make_uint4(0u, 0u, 0u, 0u);
-            uint32_t m = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                m = fspad_most2(m, fspad_most2(fspad_most2(w[i].x, w[i].y), fspad_most2(w[i].z, w[i].w)));
-            }
-            m = max(m & 0xffffu, m >> 16);
-            m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-            m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-            // the largest magnitude is in [2^e, 2^(e+1)); of zeros, and of rows that are not finite (whose result is not either), as it is
-            const int e = m == 0u || m >= 0x7f80u ? 14 : max((int)(m >> 7) - 127, -100);
-            const float up = __uint_as_float((uint32_t)(127 + 14 - e) << 23);
-            cs[x] = a.scale_log2 * __uint_as_float((uint32_t)(127 - 14 + e) << 23);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t v[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {        // pair 4 i + j of 16: product 2 i + j / 2, its columns 2c (j even) or 2c + 8
-                    const uint32_t f = pack_f16(__uint_as_float(v[j] << 16) * up, __uint_as_float(v[j] & 0xffff0000u) * up);
-                    qf[2 * i + (j >> 1)][x + 2 * (j & 1)] = f;
-                }
+            for (int i = 0; i < 4; ++i) {            // pair 4 i + j of 16: product 2 i + j / 2, its columns 2c (j even) or 2c + 8
+                const uint4 w = there ? __ldg(reinterpret_cast<const uint4 *>(a.q + (size_t)to_row[x] * D + 32 * c) + i) : make_uint4(0u, 0u, 0u, 0u);
+                qf[2 * i][x] = w.x; qf[2 * i][x + 2] = w.y; qf[2 * i + 1][x] = w.z; qf[2 * i + 1][x + 2] = w.w;
             }
         }
         float o[16][4];
@@ -172,13 +150,14 @@ tree_attn_packed_kernel(const Args a)
             for (int x = 0; x < 4; ++x) o[j][x] = 0.f;
         float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};
 
-        // scores (log2 units, masked) of 32 keys -> weights; the row's reference follows its maximum where that is far ahead of it
-        auto softmax = [&](float (&s)[4][4]) {
+        // scores (log2 units, masked) of 8 T keys -> weights; the row's reference follows its maximum where that is far ahead of it
+        auto softmax = [&](auto &s, auto tiles) {
+            constexpr int T = decltype(tiles)::value;
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
+            for (int x = 0; x < NX; ++x) {
                 float mx = -INFINITY;
 #pragma unroll
-                for (int t = 0; t < 4; ++t) mx = fmaxf(mx, fmaxf(s[t][2 * x], s[t][2 * x + 1]));
+                for (int t = 0; t < T; ++t) mx = fmaxf(fmaxf(mx, s[t][2 * x]), s[t][2 * x + 1]);
                 mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
                 mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
                 const bool move = mx > m_run[x] + kLazyLog2 || (m_run[x] == -INFINITY && mx > -INFINITY);
@@ -192,7 +171,7 @@ tree_attn_packed_kernel(const Args a)
                 }
                 const float ref = m_run[x] == -INFINITY ? 0.f : m_run[x] - kBiasLog2;
 #pragma unroll
-                for (int t = 0; t < 4; ++t)
+                for (int t = 0; t < T; ++t)
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
                         const float p = ex2f(s[t][2 * x + y] - ref);
@@ -202,109 +181,112 @@ tree_attn_packed_kernel(const Args a)
             }
         };
 
-        if (u0 < nt) {
-            __syncthreads();                         // (nobody still walks another sequence's tree)
-            for (int i = tid; i < a.N; i += WARPS * 32) {
-                int p = a.parent[(size_t)b * a.N + i];
-                if (i == 0 ? p != -1 : (p < 0 || p >= i)) { fspad_report(a.status, FSPAD_ERR_BAD_TREE); p = -1; }
-                s_par[i] = (short)p;
-            }
-            __syncthreads();
-        }
-        // ---- units of the tree: bf16 ----
-        for (int u = first; u < min(u1, nt); u += WARPS) {
-            const int t0 = u * UNIT;
-            const fspad_bf16 *tk = a.tk + ((size_t)b * a.Hkv + h) * a.N * D, *tv = a.tv + ((size_t)b * a.Hkv + h) * a.N * D;
-            uint32_t see[2] = {0u, 0u};              // which of the unit's keys a row sees
+        // ---- the tree's keys, 16 at a time: bf16 ----
+        const int t_end = min(a.N, u1 * UNIT);
+#pragma unroll 1
+        for (int t0 = u0 * UNIT; t0 < t_end; t0 += 16) {
+            const size_t first = (((size_t)b * a.Hkv + h) * a.N + t0) * D;
+            uint4 kw[2][4], vw[4][2];
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const int gr = row0 + g + 8 * x;
-                for (int at = gr < a.M ? gr / a.G : -1; at >= t0; at = s_par[at])
-                    if (at < t0 + 32) see[x] |= 1u << (at - t0);
-            }
-            float s[4][4];
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-#pragma unroll
-                for (int x = 0; x < 4; ++x) s[t][x] = 0.f;
-                const int key = t0 + 8 * t + key_of(g);
-                uint4 kw[4];
+            for (int t = 0; t < 2; ++t) {
+                const int key = 8 * t + key_of(g);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    kw[i] = key < a.N ? __ldg(reinterpret_cast<const uint4 *>(tk + (size_t)key * D + 32 * c) + i) : make_uint4(0u, 0u, 0u, 0u);
+                    kw[t][i] = t0 + key < a.N ? __ldg(reinterpret_cast<const uint4 *>(a.tk + first + key * D + 32 * c) + i) : make_uint4(0u, 0u, 0u, 0u);
+            }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint4 q0 = make_uint4(0u, 0u, 0u, 0u), q1 = q0;
-                    if (qrow[0]) q0 = __ldg(reinterpret_cast<const uint4 *>(qrow[0]) + i);
-                    if (qrow[1]) q1 = __ldg(reinterpret_cast<const uint4 *>(qrow[1]) + i);
-                    const uint32_t lo[4] = {q0.x, q1.x, q0.y, q1.y}, hi[4] = {q0.z, q1.z, q0.w, q1.w};
-                    mma16_bf(s[t], lo, kw[i].x, kw[i].y);
-                    mma16_bf(s[t], hi, kw[i].z, kw[i].w);
-                }
+            for (int y = 0; y < 4; ++y) {            // keys of columns 2c, 2c + 1, 2c + 8, 2c + 9: elements 16 g .. 16 g + 15
+                const int key = 8 * (y >> 1) + key_of(2 * c + (y & 1));
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    const int k = 8 * t + key_of(2 * c + (x & 1));
-                    s[t][x] = (see[x >> 1] >> k) & 1u ? s[t][x] * a.scale_log2 : -INFINITY;
+                for (int i = 0; i < 2; ++i)
+                    vw[y][i] = t0 + key < a.N ? __ldg(reinterpret_cast<const uint4 *>(a.tv + first + key * D + 16 * g) + i) : make_uint4(0u, 0u, 0u, 0u);
+            }
+            uint32_t see[2] = {0u, 0u};              // which of the 16 keys a row sees
+#pragma unroll
+            for (int x = 0; x < NX; ++x) {
+                int at = node[x];
+                while (at >= t0) {
+                    if (at < t0 + 16) see[x] |= 1u << (at - t0);
+                    const int up = __ldg(a.parent + (size_t)b * a.N + at);
+                    if (at == 0 ? up != -1 : (up < 0 || up >= at)) { fspad_report(a.status, FSPAD_ERR_BAD_TREE); break; }
+                    at = up;
                 }
             }
-            softmax(s);
+            float s[2][4];
 #pragma unroll
-            for (int st = 0; st < 2; ++st) {
-                uint32_t vw[4][8];                   // keys of columns 2c, 2c + 1, 2c + 8, 2c + 9: elements 16 g .. 16 g + 15
-                bool odd = false;
+            for (int t = 0; t < 2; ++t) {
 #pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    const int key = t0 + 16 * st + 8 * (y >> 1) + key_of(2 * c + (y & 1));
+                for (int x = 0; x < 4; ++x) s[t][x] = 0.f;
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const uint4 w = key < a.N ? __ldg(reinterpret_cast<const uint4 *>(tv + (size_t)key * D + 16 * g) + i) : make_uint4(0u, 0u, 0u, 0u);
-                        vw[y][4 * i] = w.x; vw[y][4 * i + 1] = w.y; vw[y][4 * i + 2] = w.z; vw[y][4 * i + 3] = w.w;
-                    }
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) odd |= odd_value(vw[y][i]);
+                for (int i = 0; i < 4; ++i) {
+                    mma16_bf(s[t], qf[2 * i], kw[t][i].x, kw[t][i].y);
+                    mma16_bf(s[t], qf[2 * i + 1], kw[t][i].z, kw[t][i].w);
                 }
-                // A row with an infinity or a NaN in it must not reach the queries that do not see it (0 times it is a NaN): it is taken
-                // out of the product, and the queries that do see it get NaN.
-                if (__any_sync(0xffffffffu, odd)) {
-                    uint32_t keys = 0;
 #pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-                        bool bad = false;
+                for (int x = 0; x < 4; ++x) s[t][x] = (see[x >> 1] >> (8 * t + key_of(2 * c + (x & 1)))) & 1u ? s[t][x] * a.scale_log2 : -INFINITY;
+            }
+            softmax(s, std::integral_constant<int, 2>());
+            // A row of V with an infinity or a NaN in it must not reach the queries that do not see it (0 times it is a NaN): it is taken
+            // out of the product, and the queries that do see it get NaN.
+            uint32_t keys = 0;
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) bad |= odd_value(vw[y][i]);
-                        if (bad) keys |= 1u << (16 * st + 8 * (y >> 1) + key_of(2 * c + (y & 1)));
-                    }
-                    keys = __reduce_or_sync(0xffffffffu, keys);
-#pragma unroll
-                    for (int y = 0; y < 4; ++y)
-                        if ((keys >> (16 * st + 8 * (y >> 1) + key_of(2 * c + (y & 1)))) & 1u)
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) vw[y][i] = 0u;
-#pragma unroll
-                    for (int x = 0; x < 2; ++x)
-                        if (see[x] & keys) l_run[x] = NAN;
+            for (int y = 0; y < 4; ++y) {
+                const uint4 w0 = vw[y][0], w1 = vw[y][1];
+                if (odd_value(w0.x) || odd_value(w0.y) || odd_value(w0.z) || odd_value(w0.w) || odd_value(w1.x) || odd_value(w1.y) || odd_value(w1.z) || odd_value(w1.w)) {
+                    keys |= 1u << (8 * (y >> 1) + key_of(2 * c + (y & 1)));
+                    vw[y][0] = vw[y][1] = make_uint4(0u, 0u, 0u, 0u);
                 }
-                const uint32_t p[4] = {umma::pack_bf16(s[2 * st][0], s[2 * st][1]), umma::pack_bf16(s[2 * st][2], s[2 * st][3]),
-                                       umma::pack_bf16(s[2 * st + 1][0], s[2 * st + 1][1]), umma::pack_bf16(s[2 * st + 1][2], s[2 * st + 1][3])};
+            }
+            keys = __reduce_or_sync(0xffffffffu, keys);
 #pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const uint32_t sel = j & 1 ? 0x7632u : 0x5410u;
-                    mma16_bf(o[j], p, __byte_perm(vw[0][j >> 1], vw[1][j >> 1], sel), __byte_perm(vw[2][j >> 1], vw[3][j >> 1], sel));
-                }
+            for (int x = 0; x < NX; ++x)
+                if (see[x] & keys) l_run[x] = NAN;
+            const uint32_t p[4] = {umma::pack_bf16(s[0][0], s[0][1]), WIDE ? umma::pack_bf16(s[0][2], s[0][3]) : 0u,
+                                   umma::pack_bf16(s[1][0], s[1][1]), WIDE ? umma::pack_bf16(s[1][2], s[1][3]) : 0u};
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const uint32_t sel = j & 1 ? 0x7632u : 0x5410u;
+                auto word = [&](int y) {
+                    const uint4 w = vw[y][j >> 3];
+                    return ((j >> 1) & 3) == 0 ? w.x : ((j >> 1) & 3) == 1 ? w.y : ((j >> 1) & 3) == 2 ? w.z : w.w;
+                };
+                mma16_bf(o[j], p, __byte_perm(word(0), word(1), sel), __byte_perm(word(2), word(3), sel));
             }
         }
 
+        // ---- queries as fp16, scaled by a power of two so that the row's largest magnitude lies in [2^14, 2^15): 8 significant bits
+        // stay exact down to 2^-31 of the largest ----
+        float cs[2] = {0.f, 0.f};                    // scores -> log2 units
+#pragma unroll
+        for (int x = 0; x < NX; ++x) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m = fspad_most2(m, fspad_most2(qf[i][x], qf[i][x + 2]));
+            m = fspad_most2(m, __shfl_xor_sync(0xffffffffu, m, 1));
+            m = fspad_most2(m, __shfl_xor_sync(0xffffffffu, m, 2));
+            m = max(m & 0xffffu, m >> 16);
+            // the largest magnitude is in [2^e, 2^(e+1)); of zeros, and of rows that are not finite (whose result is not either), as it is
+            const int e = m == 0u || m >= 0x7f80u ? 14 : max((int)(m >> 7) - 127, -100);
+            const float up = __uint_as_float((uint32_t)(127 + 14 - e) << 23);
+            cs[x] = a.scale_log2 * __uint_as_float((uint32_t)(127 - 14 + e) << 23);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int y = 0; y < 4; y += 2)
+                    qf[i][x + y] = pack_f16(__uint_as_float(qf[i][x + y] << 16) * up, __uint_as_float(qf[i][x + y] & 0xffff0000u) * up);
+        }
+
         // ---- units of the cache ----
+        bool failed = false;
+#pragma unroll 1
         for (int i = 0; i < n_kv; ++i) {
-            const int key0 = (first_kv + i * WARPS - nt) * UNIT, st = i % STAGES;
-            const uint32_t at = ring + (uint32_t)(st * STAGE);
-            if (!mbar_wait(bar0 + 8u * st, (phase >> st) & 1u)) {
-                failed = true;                       // what is under way gets another bounded time to land before the CTA leaves
-                for (int y = i; y < n_kv && y < i + STAGES; ++y) (void)mbar_wait(bar0 + 8u * (y % STAGES), (phase >> (y % STAGES)) & 1u);
+            const uint32_t st = n_use % STAGES, at = ring + st * STAGE;
+            if (!mbar_wait(bar0 + 8u * st, (n_use / STAGES) & 1u)) {
+                failed = true;
                 break;
             }
-            phase ^= 1u << st;
-            const int left = L - key0;               // keys of the unit that exist
+            ++n_use;
+            const int left = L - (kv0 + i) * UNIT;   // keys of the unit that exist
             float s[4][4];
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
@@ -328,7 +310,7 @@ tree_attn_packed_kernel(const Args a)
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int x = 0; x < 4; ++x) s[t][x] *= cs[x >> 1];
+                for (int x = 0; x < 2 * NX; ++x) s[t][x] *= cs[x >> 1];
             if (left < UNIT) {
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
@@ -336,11 +318,11 @@ tree_attn_packed_kernel(const Args a)
                     for (int x = 0; x < 4; ++x)
                         if (8 * t + key_of(2 * c + (x & 1)) >= left) s[t][x] = -INFINITY;
             }
-            softmax(s);
+            softmax(s, std::integral_constant<int, 4>());
 #pragma unroll
             for (int k2 = 0; k2 < 2; ++k2) {
-                const uint32_t p[4] = {pack_f16(s[2 * k2][0], s[2 * k2][1]), pack_f16(s[2 * k2][2], s[2 * k2][3]),
-                                       pack_f16(s[2 * k2 + 1][0], s[2 * k2 + 1][1]), pack_f16(s[2 * k2 + 1][2], s[2 * k2 + 1][3])};
+                const uint32_t p[4] = {pack_f16(s[2 * k2][0], s[2 * k2][1]), WIDE ? pack_f16(s[2 * k2][2], s[2 * k2][3]) : 0u,
+                                       pack_f16(s[2 * k2 + 1][0], s[2 * k2 + 1][1]), WIDE ? pack_f16(s[2 * k2 + 1][2], s[2 * k2 + 1][3]) : 0u};
                 uint2 w[4];
                 uint32_t sc[2];
 #pragma unroll
@@ -376,76 +358,48 @@ tree_attn_packed_kernel(const Args a)
                 }
             }
             __syncwarp();                            // every lane has read the stage
-            if (lane == 0 && i + STAGES < n_kv) fill(i + STAGES);
+            if (i + STAGES < n_kv) {
+                if (lane == 0) fill(i + STAGES);
+                ++n_fill;
+            }
         }
-        if (failed && lane == 0) s_fail = 1;
+        if (failed) {
+            // what is under way gets another bounded time to land before the warp leaves
+            for (; n_use < n_fill; ++n_use) (void)mbar_wait(bar0 + 8u * (n_use % STAGES), (n_use / STAGES) & 1u);
+            if (lane == 0) fspad_report(a.status, FSPAD_ERR_TIMEOUT);
+            return;
+        }
 
-        // ---- the warps' results together ----
+        // ---- the rows: lane (g, c) has elements 32 c + j in o[j][2 x], 32 c + 16 + j in o[j][2 x + 1] ----
+        const bool whole = u0 == 0 && u1 == n_run;
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
+        for (int x = 0; x < NX; ++x) {
             l_run[x] += __shfl_xor_sync(0xffffffffu, l_run[x], 1);
             l_run[x] += __shfl_xor_sync(0xffffffffu, l_run[x], 2);
-            if (c == 0) s_ml[warp][g + 8 * x] = make_float2(m_run[x], l_run[x]);
-        }
-        __syncthreads();
-        const bool any_fail = s_fail != 0;
+            if (node[x] < 0) continue;
+            if (whole) {
+                const float inv = 1.f / l_run[x];
+                uint4 *dst = reinterpret_cast<uint4 *>(a.out + (size_t)to_row[x] * D + 32 * c);
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            float m = -INFINITY;
+                for (int y = 0; y < 2; ++y)
 #pragma unroll
-            for (int w = 0; w < WARPS; ++w) m = fmaxf(m, s_ml[w][g + 8 * x].x);
-            const float f = m_run[x] == -INFINITY ? 0.f : ex2f(m_run[x] - m);
-            // lane (g, c): elements 32 c + j in o[j][2 x], 32 c + 16 + j in o[j][2 x + 1]
-            float4 *dst = reinterpret_cast<float4 *>(s_o + ((size_t)warp * BM + g + 8 * x) * OROW + c * 36);
+                    for (int j = 0; j < 16; j += 8)
+                        dst[2 * y + j / 8] = make_uint4(umma::pack_bf16(o[j][2 * x + y] * inv, o[j + 1][2 * x + y] * inv), umma::pack_bf16(o[j + 2][2 * x + y] * inv, o[j + 3][2 * x + y] * inv),
+                                                        umma::pack_bf16(o[j + 4][2 * x + y] * inv, o[j + 5][2 * x + y] * inv), umma::pack_bf16(o[j + 6][2 * x + y] * inv, o[j + 7][2 * x + y] * inv));
+            } else {
+                const size_t slot = ((size_t)slot0 * 2 + (u0 == 0 ? 1 : 0)) * BM + g + 8 * x;
+                float4 *dst = reinterpret_cast<float4 *>(a.part_o + slot * D + 32 * c);
 #pragma unroll
-            for (int y = 0; y < 2; ++y)
+                for (int y = 0; y < 2; ++y)
 #pragma unroll
-                for (int j = 0; j < 16; j += 4)
-                    dst[y * 4 + j / 4] = make_float4(o[j][2 * x + y] * f, o[j + 1][2 * x + y] * f, o[j + 2][2 * x + y] * f, o[j + 3][2 * x + y] * f);
-        }
-        __syncthreads();
-        {
-            // thread: row tid / 16, elements 8 (tid % 16) ..
-            const int row = tid >> 4, d0 = (tid & 15) * 8;
-            float m = -INFINITY, l = 0.f;
-#pragma unroll
-            for (int w = 0; w < WARPS; ++w) m = fmaxf(m, s_ml[w][row].x);
-            float acc[8];
-#pragma unroll
-            for (int x = 0; x < 8; ++x) acc[x] = 0.f;
-#pragma unroll
-            for (int w = 0; w < WARPS; ++w) {
-                const float2 ml = s_ml[w][row];
-                l += ml.x == -INFINITY ? ml.y : ml.y * ex2f(ml.x - m);       // (a sum without a maximum is zero, or a NaN)
-                const float4 *src = reinterpret_cast<const float4 *>(s_o + ((size_t)w * BM + row) * OROW + (d0 >> 5) * 36 + (d0 & 31));
-                const float4 lo = src[0], hi = src[1];
-                acc[0] += lo.x; acc[1] += lo.y; acc[2] += lo.z; acc[3] += lo.w;
-                acc[4] += hi.x; acc[5] += hi.y; acc[6] += hi.z; acc[7] += hi.w;
-            }
-            const int gr = row0 + row;
-            if (gr < a.M && !any_fail) {
-                if (u0 == 0 && u1 == n_run) {
-                    const float inv = 1.f / l;
-                    uint4 pk;
-                    pk.x = umma::pack_bf16(acc[0] * inv, acc[1] * inv); pk.y = umma::pack_bf16(acc[2] * inv, acc[3] * inv);
-                    pk.z = umma::pack_bf16(acc[4] * inv, acc[5] * inv); pk.w = umma::pack_bf16(acc[6] * inv, acc[7] * inv);
-                    *reinterpret_cast<uint4 *>(a.out + (((size_t)b * a.N + gr / a.G) * a.Hq + h * a.G + gr % a.G) * D + d0) = pk;
-                } else {
-                    const size_t slot = ((size_t)cta * 2 + (u0 == 0 ? 1 : 0)) * BM + row;
-                    float4 *dst = reinterpret_cast<float4 *>(a.part_o + slot * D + d0);
-                    dst[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
-                    dst[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
-                    if (d0 == 0) a.part_ml[slot] = make_float2(m, l);
-                }
+                    for (int j = 0; j < 16; j += 4) dst[4 * y + j / 4] = make_float4(o[j][2 * x + y], o[j + 1][2 * x + y], o[j + 2][2 * x + y], o[j + 3][2 * x + y]);
+                if (c == 0) a.part_ml[slot] = make_float2(m_run[x], l_run[x]);
             }
         }
-        if (any_fail) break;
-        __syncthreads();                             // the staged rows are read
         part.left -= u1 - u0;
         part.u = 0;
         if (++part.run == runs) { part.run = 0; ++part.b; }
     }
-    if (s_fail != 0 && tid == 0) fspad_report(a.status, FSPAD_ERR_TIMEOUT);
 }
 
 }  // namespace
@@ -457,7 +411,7 @@ size_t fspad_attn_packed_workspace(const fspad_ctx *ctx, int N, int B)
 {
     (void)B;
     if (many_rows(ctx, N)) return fspad_attn_packed_umma_workspace(ctx);
-    return scratch_bytes<BM>(ctx->sm_count);
+    return scratch_bytes<BM>(ctx->sm_count * WARPS);
 }
 
 cudaError_t fspad_launch_tree_attn_packed(fspad_ctx *ctx, const fspad_bf16 *q, const uint8_t *k_codes, const uint8_t *k_scales,
@@ -477,11 +431,14 @@ cudaError_t fspad_launch_tree_attn_packed(fspad_ctx *ctx, const fspad_bf16 *q, c
     a.out = out; a.status = ctx->d_status;
     if (many_rows(ctx, N)) return fspad_launch_attn_packed_umma(ctx, a, workspace, st);
     const int ctas = ctx->sm_count;
-    scratch_in<BM>(a, ctas, workspace);
-    cudaError_t e = cudaFuncSetAttribute(tree_attn_packed_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+    scratch_in<BM>(a, ctas * WARPS, workspace);
+    auto kernel = a.M > 8 ? tree_attn_packed_kernel<true> : tree_attn_packed_kernel<false>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
     if (e != cudaSuccess) return e;
     ctx->launches += 2;
-    e = fspad_launch(tree_attn_packed_kernel, dim3((unsigned)ctas), dim3(WARPS * 32), SMEM, st, 0, a);
+    e = fspad_launch(kernel, dim3((unsigned)ctas), dim3(WARPS * 32), SMEM, st, 0, a);
     if (e != cudaSuccess) return e;
-    return fspad_launch(tree_attn_packed_merge_kernel<BM, 2, 4>, dim3((unsigned)ctas, (unsigned)((a.M < BM ? a.M : BM) + 1) / 2), dim3(256), 0, st, 0, a);
+    int rows = 1;
+    while (rows < a.M && rows < BM) rows *= 2;
+    return fspad_launch(tree_attn_packed_merge_kernel<BM, 16>, dim3((unsigned)(ctas * WARPS)), dim3(512), 0, st, 0, a, rows);
 }

@@ -165,7 +165,7 @@ tree_attn_packed_umma_kernel(const Args a)
     tc_fence_before();
     const int cta = blockIdx.x;
     Parts parts;
-    Part part = cut_list<NT, UNIT>(a, cta, gridDim.x, parts, s_scan, cta == 0);      // (with a barrier in it)
+    Part part = cut_list<NT, UNIT, 1>(a, cta, gridDim.x, parts, s_scan, cta == 0);      // (with a barrier in it)
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
     const int nt = tree_units<UNIT>(a), runs = a.Hkv * a.mtiles;
@@ -322,46 +322,44 @@ tree_attn_packed_umma_kernel(const Args a)
             // ---- the group's last product, then the rows ----
             if (!first && !failed && !mbar_wait(bar(O_DONE + 2 * grp + (int)((n_done - 1) & 1u)), ((n_done - 1) >> 1) & 1u)) failed = true;
             tc_fence_after();
-            if (failed) s_soft_fail = s_fail = 1;
-            s_ml[grp][row] = make_float2(m_run, l_run);
             const bool whole = s.n_ch == s.n_run;
             const int slot = cta * 2 + (s.u0 == 0 ? 1 : 0);
-            s_to[grp][row] = !row_ok ? -1 : whole ? (s.b * a.N + node) * a.Hq + head : slot * BM + (gr - s.row0);
-            tc_fence_before();
-            asm volatile("bar.sync 1, 256;\n" ::: "memory");
-            tc_fence_after();
-            if (s_soft_fail != 0) break;
-            float f[2];                                      // factors of the accumulators that make up the row: the group's own, or both groups'
+            s_to[grp][row] = !row_ok ? -1 : (s.b * a.N + node) * a.Hq + head;
+            float f0 = 1.f, f1 = 0.f;                        // factors of the accumulators that make up the row: the group's own, or group 0's and group 1's
             float m_fin = m_run, l_fin = l_run;
-            f[grp] = 1.f;
-            f[grp ^ 1] = 0.f;
             if (!s.two) {
+                if (failed) s_soft_fail = s_fail = 1;
+                s_ml[grp][row] = make_float2(m_run, l_run);
+                tc_fence_before();
+                asm volatile("bar.sync 1, 256;\n" ::: "memory");
+                tc_fence_after();
+                if (s_soft_fail != 0) failed = true;
                 const float2 o = s_ml[grp ^ 1][row];
                 m_fin = fmaxf(m_run, o.x);
                 const float ref = m_fin == -INFINITY ? 0.f : m_fin;
-                f[grp] = ex2f(m_run - ref);
-                f[grp ^ 1] = ex2f(o.x - ref);
-                l_fin = (m_run == -INFINITY ? l_run : l_run * f[grp]) + (o.x == -INFINITY ? o.y : o.y * f[grp ^ 1]);     // (without a maximum: zero, or a NaN)
+                const float own = ex2f(m_run - ref), other = ex2f(o.x - ref);
+                l_fin = (m_run == -INFINITY ? l_run : l_run * own) + (o.x == -INFINITY ? o.y : o.y * other);     // (without a maximum: zero, or a NaN)
+                f0 = grp == 0 ? own : other;
+                f1 = grp == 0 ? other : own;
             }
+            __syncwarp();
             if (whole) {
                 const float inv = 1.f / l_fin;
-                f[0] *= inv;
-                f[1] *= inv;
+                f0 *= inv;
+                f1 *= inv;
             }
             if (!whole && row_ok && (s.two || grp == 0)) a.part_ml[(size_t)slot * BM + (gr - s.row0)] = make_float2(m_fin, l_fin);
             const bool both = !s.two && s.n_ch > 1;          // group 1 has had a chunk
-            const uint32_t stage = sQ + (uint32_t)grp * TILE;        // (the query tiles are read)
+            const uint32_t stage = sQ + (uint32_t)grp * TILE + (uint32_t)((warp & 3) * 8192);        // 8 KB a warp (the query tiles are read)
+            if (live && !failed) {
 #pragma unroll 1
-            for (int hf = s.two ? 0 : grp; hf < (s.two ? 2 : grp + 1); ++hf) {
-                // columns 64 hf ..: a row's pieces of 16 bytes lie in an order that depends on the row, so that neither side's accesses collide
-#pragma unroll 1
-                for (int x = 0; x < 2; ++x) {
+                for (int x = s.two ? 0 : 2 * grp; x < (s.two ? 4 : 2 * grp + 2); ++x) {
+                    // columns 32 x ..: a row's pieces of 16 bytes lie in an order that depends on the row, so that neither side's accesses collide
                     uint32_t r[32];
-                    const uint32_t own = tmem + lanes + 256u + (uint32_t)(hf * 64 + x * 32) + (s.two ? 128u * grp : 0u);
+                    const uint32_t own = tmem + lanes + 256u + 32u * x + (s.two ? 128u * grp : 0u);
                     __syncwarp();
                     tmem_ld32_issue(own, r);
                     tmem_ld_wait(r);
-                    const float f0 = s.two ? f[grp] : f[0];
 #pragma unroll
                     for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) * f0);
                     if (both) {
@@ -370,49 +368,48 @@ tree_attn_packed_umma_kernel(const Args a)
                         tmem_ld32_issue(own + 128u, r1);
                         tmem_ld_wait(r1);
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(fmaf(__uint_as_float(r1[j]), f[1], __uint_as_float(r[j])));
+                        for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(fmaf(__uint_as_float(r1[j]), f1, __uint_as_float(r[j])));
                     }
                     auto val = [&](int j) { return __uint_as_float(r[j]); };
                     if (whole) {
+                        // two quarters side by side, then whole pieces of 128 bytes: 4 rows at a time
 #pragma unroll
                         for (int j = 0; j < 32; j += 8)
-                            st_shared16(stage + (uint32_t)(row * 128 + (((x * 4 + j / 8) ^ (row & 7)) << 4)), pack_bf16(val(j), val(j + 1)),
+                            st_shared16(stage + (uint32_t)(lane * 128 + ((((x & 1) * 4 + j / 8) ^ (lane & 7)) << 4)), pack_bf16(val(j), val(j + 1)),
                                         pack_bf16(val(j + 2), val(j + 3)), pack_bf16(val(j + 4), val(j + 5)), pack_bf16(val(j + 6), val(j + 7)));
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 32; j += 4)
-                            st_shared16(stage + (uint32_t)(row * 256 + (((x * 8 + j / 4) ^ (row & 7)) << 4)), r[j], r[j + 1], r[j + 2], r[j + 3]);
-                    }
-                }
-                // a warp writes its own 32 rows, 4 of 128 bytes at a time
-                if (whole) {
-                    __syncwarp();
+                        if (x & 1) {
+                            __syncwarp();
 #pragma unroll 2
-                    for (int k = 0; k < 8; ++k) {
-                        const int r = (warp & 3) * 32 + 4 * k + (lane >> 3), to = s_to[grp][r];
-                        if (to >= 0)
-                            reinterpret_cast<uint4 *>(a.out + (size_t)to * D + hf * 64)[lane & 7] =
-                                ld_shared16(stage + (uint32_t)(r * 128 + (((lane & 7) ^ (r & 7)) << 4)));
-                    }
-                    __syncwarp();
-                } else {
-                    // the warp's 32 rows as they lie, 8 KB in one copy (rows that do not exist among them: nobody looks at those)
-                    if (live) {
+                            for (int k = 0; k < 8; ++k) {
+                                const int r4 = 4 * k + (lane >> 3), to = s_to[grp][(warp & 3) * 32 + r4];
+                                if (to >= 0)
+                                    reinterpret_cast<uint4 *>(a.out + (size_t)to * D + (x >> 1) * 64)[lane & 7] =
+                                        ld_shared16(stage + (uint32_t)(r4 * 128 + (((lane & 7) ^ (r4 & 7)) << 4)));
+                            }
+                            __syncwarp();
+                        }
+                    } else {
+                        // the warp's 32 rows as they lie, 4 KB in one copy, from one of two places in turn (rows that do not exist among them: nobody looks at those)
+                        const uint32_t at = stage + (uint32_t)((x & 1) * 4096);
+                        if (lane == 0) bulk_store_read_but_one();
+                        __syncwarp();
+#pragma unroll
+                        for (int j = 0; j < 32; j += 4) st_shared16(at + (uint32_t)(lane * 128 + (((j / 4) ^ (lane & 7)) << 4)), r[j], r[j + 1], r[j + 2], r[j + 3]);
                         fence_async_smem();
                         __syncwarp();
-                        if (lane == 0) {
-                            const int tile = s.two ? grp : 0;
-                            bulk_store(a.part_o + (((size_t)slot * 2 + tile) * 2 + hf) * (128 * 64) + (warp & 3) * (32 * 64), stage + (uint32_t)((warp & 3) * 32 * 256), 32 * 256);
-                            bulk_store_read();
-                        }
-                        __syncwarp();
+                        if (lane == 0)
+                            bulk_store(a.part_o + (((size_t)slot * 2 + (s.two ? grp : 0)) * 4 + x) * (128 * 32) + (warp & 3) * (32 * 32), at, 4096);
                     }
                 }
             }
-            // nobody goes on to the next stretch (whose queries, products and exchange use the same places) before all have read
-            tc_fence_before();
-            asm volatile("bar.sync 1, 256;\n" ::: "memory");
-            tc_fence_after();
+            if (failed) s_fail = 1;
+            // nobody goes on to the next stretch (whose queries, products, parents and exchange use the same places) before all have read
+            if (part.left > 0) {
+                if (lane == 0) bulk_store_read();
+                tc_fence_before();
+                asm volatile("bar.sync 1, 256;\n" ::: "memory");
+                tc_fence_after();
+            }
         }
         if (lane == 0) bulk_store_wait();                    // (the copies' memory is this CTA's)
     } else if (warp < 12) {
@@ -644,5 +641,5 @@ cudaError_t fspad_launch_attn_packed_umma(fspad_ctx *ctx, packed::Args a, void *
     ctx->launches += 2;
     e = fspad_launch(tree_attn_packed_umma_kernel, dim3((unsigned)ctas), dim3(NT), SMEM, st, 0, a);
     if (e != cudaSuccess) return e;
-    return fspad_launch(tree_attn_packed_merge_kernel<BM, 8, 1>, dim3((unsigned)ctas, (unsigned)((a.M < BM ? a.M : BM) + 7) / 8), dim3(256), 0, st, 0, a);
+    return fspad_launch(tree_attn_packed_merge_kernel<BM, 8>, dim3((unsigned)ctas, (unsigned)((a.M < BM ? a.M : BM) + 7) / 8), dim3(256), 0, st, 0, a, 8);
 }
