@@ -46,7 +46,8 @@ struct Args {
     float *part_o;                       // [parts][2][BM][D]: of the run that began before the part, of the one that goes on behind it.  Of 256 rows:
                                          // [..][2 row tiles][4 quarters of the columns][128][32], a row's 16-byte pieces in the order piece ^ (row & 7)
     float2 *part_ml;                     // [parts][2][BM]
-    int *cuts;                           // [parts][8]: runs that were cut (see tell_cut)
+    int *cuts;                           // [parts][8]: runs that were cut (see tell)
+    int entry_runs;                      // no more runs than parts there can be: an entry for every run
     int *status;
 };
 
@@ -216,28 +217,32 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
 // Whether one of the two bf16 of a word is an infinity or a NaN.
 __device__ __forceinline__ bool odd_value(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
 
-// One thread for every part: leaves word of the run that the part begins inside of, for the merge, if it holds the run's second piece: sequence, kv head, tile, and
-// the parts that hold the first and the last piece.  A sequence of -1: nothing to merge.
-template <int UNIT>
-__device__ __forceinline__ void tell_cut(const Args &a, const Parts &p, const Part &s, int cta)
+// Word of the runs that were cut, for the merge: sequence (-1: nothing to merge), kv head, tile, and the parts that hold the first and the last piece.
+// Where there is an entry for every run (a.entry_runs), the n-th is the n-th run's, and the part that holds the run's beginning, as its unit 0 comes, writes it; otherwise
+// the n-th is the n-th part's, of the run that the part begins inside of, if it holds the second piece.
+__device__ __forceinline__ void tell(const Args &a, int n, int b, int run, int i0, int i1)
 {
-    int4 what = make_int4(-1, 0, 0, 0);
-    int last = 0;
+    const int h = a.by_tiles.of(run);
+    reinterpret_cast<int4 *>(a.cuts)[2 * n] = make_int4(i1 > i0 ? b : -1, h, run - h * a.mtiles, i0);
+    a.cuts[8 * n + 4] = i1;
+}
+// One thread for every part, before anything of it is taken.
+template <int UNIT> __device__ __forceinline__ void tell_part(const Args &a, const Parts &p, const Part &s, int part)
+{
+    if (a.entry_runs) return;
+    int i0 = 0, i1 = 0;
     if (s.left > 0 && s.u > 0) {
-        int i0 = s.i0, i1 = s.i1;
-        if (!s.by_run) {
-            const int start = p.start(cta) - s.u;
-            i0 = p.owner(start);
-            i1 = p.owner(start + run_units<UNIT>(a, prefix_of(a, s.b, false)) - 1);
-        }
-        if (i0 == cta - 1) {
-            const int h = a.by_tiles.of(s.run);
-            what = make_int4(s.b, h, s.run - h * a.mtiles, i0);
-            last = i1;
-        }
+        const int start = p.start(part) - s.u;
+        i0 = p.owner(start);
+        i1 = i0 == part - 1 ? p.owner(start + run_units<UNIT>(a, prefix_of(a, s.b, false)) - 1) : i0;
     }
-    reinterpret_cast<int4 *>(a.cuts)[2 * cta] = what;
-    a.cuts[8 * cta + 4] = last;
+    tell(a, part, s.b, s.run, i0, i1);
+}
+// One thread, when the part comes to the beginning of a run (s.u = 0): `done` units of the part lie before it.
+__device__ __forceinline__ void tell_run(const Args &a, const Parts &p, const Part &s, int part, int done, int n_run)
+{
+    if (!a.entry_runs) return;
+    tell(a, (s.b * a.Hkv * a.mtiles) + s.run, s.b, s.run, part, s.by_run ? s.i1 : p.owner(p.start(part) + done + n_run - 1));
 }
 
 // The pieces of the runs that were cut, merged.  A CTA takes `rows` rows (a power of two, at most WARPS) of a run at a time, each by WARPS / rows warps that take its
@@ -247,49 +252,66 @@ __global__ void __launch_bounds__(WARPS * 32)
 tree_attn_packed_merge_kernel(const Args a, int rows)
 {
     __shared__ float4 s_acc[WARPS][32];
-    __shared__ float s_l[WARPS];
+    __shared__ float2 s_ml[WARPS];
     fspad_pdl_trigger();
     fspad_pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, wpr = WARPS / rows;
     const int4 run = __ldcg(reinterpret_cast<const int4 *>(a.cuts) + 2 * blockIdx.x);
-    if (run.x < 0) return;
     const int i0 = run.w, i1 = __ldcg(a.cuts + 8 * blockIdx.x + 4);
+    if (run.x < 0) return;
 #pragma unroll 1
     for (int row0 = blockIdx.y * rows; row0 < BM && run.z * BM + row0 < a.M; row0 += gridDim.y * rows) {
         const int row = row0 + warp % rows, gr = run.z * BM + row;
         const bool there = gr < a.M;
-        auto slot_of = [&](int i) { return ((size_t)i * 2 + (i == i0 ? 1 : 0)) * BM + row; };
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        float l = 0.f;
+        float l = 0.f, m = -INFINITY;
+        auto add = [&](float2 ml, float4 v, float m_new) {   // (without a maximum a piece's sum and row are zero, or NaN)
+            const float w = ml.x == -INFINITY ? 1.f : umma::ex2f(ml.x - m_new);
+            l += w * ml.y;
+            acc.x += w * v.x; acc.y += w * v.y; acc.z += w * v.z; acc.w += w * v.w;
+        };
+        auto move = [&](float m_new) {
+            const float w = m == -INFINITY ? 1.f : umma::ex2f(m - m_new);
+            l *= w;
+            acc.x *= w; acc.y *= w; acc.z *= w; acc.w *= w;
+            m = m_new;
+        };
+        constexpr int U = 8;                                 // pieces under way
         if (there) {
-            float m = -INFINITY;
-            for (int i = i0 + lane; i <= i1; i += 32) m = fmaxf(m, __ldcg(&a.part_ml[slot_of(i)]).x);
+#pragma unroll 1
+            for (int i = i0 + warp / rows; i <= i1; i += U * wpr) {
+                float2 ml[U];
+                float4 v[U];
+                float top = m;
 #pragma unroll
-            for (int off = 16; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
-#pragma unroll 8
-            for (int i = i0 + warp / rows; i <= i1; i += wpr) {
-                const size_t slot = slot_of(i);
-                const float2 ml = __ldcg(&a.part_ml[slot]);
-                const float4 v = __ldcg(reinterpret_cast<const float4 *>(a.part_o) + (BM == 256 ? (slot >> 7) * 4096 + (lane >> 3) * 1024 + (row & 127) * 8 + ((lane & 7) ^ (row & 7))
-                                                                                                  : slot * (D / 4) + lane));
-                const float w = ml.x == -INFINITY ? 1.f : umma::ex2f(ml.x - m);      // (without a maximum the sum and the row are zero, or NaN)
-                l += w * ml.y;
-                acc.x += w * v.x; acc.y += w * v.y; acc.z += w * v.z; acc.w += w * v.w;
+                for (int u = 0; u < U; ++u) {
+                    const int at = i + u * wpr;
+                    ml[u] = make_float2(-INFINITY, 0.f);
+                    v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (at <= i1) {
+                        const size_t slot = ((size_t)at * 2 + (at == i0 ? 1 : 0)) * BM + row;
+                        ml[u] = __ldcg(&a.part_ml[slot]);
+                        v[u] = __ldcg(reinterpret_cast<const float4 *>(a.part_o) + (BM == 256 ? (slot >> 7) * 4096 + (lane >> 3) * 1024 + (row & 127) * 8 + ((lane & 7) ^ (row & 7))
+                                                                                              : slot * (D / 4) + lane));
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u) top = fmaxf(top, ml[u].x);
+                move(top);
+#pragma unroll
+                for (int u = 0; u < U; ++u) add(ml[u], v[u], top);
             }
         }
         if (wpr > 1) {
             __syncthreads();
             s_acc[warp][lane] = acc;
-            if (lane == 0) s_l[warp] = l;
+            if (lane == 0) s_ml[warp] = make_float2(m, l);
             __syncthreads();
             if (warp < rows) {
-                l = 0.f;
-                acc = make_float4(0.f, 0.f, 0.f, 0.f);
-                for (int w = warp; w < WARPS; w += rows) {
-                    const float4 v = s_acc[w][lane];
-                    l += s_l[w];
-                    acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
-                }
+                float top = -INFINITY;
+                for (int w = warp; w < WARPS; w += rows) top = fmaxf(top, s_ml[w].x);
+                move(top);
+                for (int w = warp + rows; w < WARPS; w += rows) add(s_ml[w], s_acc[w][lane], top);
             }
         }
         if (warp < rows && there) {
@@ -311,6 +333,22 @@ template <int BM> static inline void scratch_in(Args &a, int parts, void *worksp
     a.part_o = static_cast<float *>(workspace);
     a.part_ml = reinterpret_cast<float2 *>(a.part_o + (size_t)parts * 2 * BM * D);
     a.cuts = reinterpret_cast<int *>(a.part_ml + (size_t)parts * 2 * BM);
+}
+
+// Parts there can be -> how the runs that were cut are told of; and the merge's launch: entries x groups of so many rows, so that there are a few CTAs for every SM.
+static inline int merge_entries(Args &a, int parts)
+{
+    const long long runs = (long long)a.B * a.Hkv * a.mtiles;
+    a.entry_runs = runs <= parts ? 1 : 0;
+    return a.entry_runs ? (int)runs : parts;
+}
+template <int BM, int WARPS> static inline cudaError_t launch_merge(fspad_ctx *ctx, const Args &a, int entries, cudaStream_t st)
+{
+    const int m = a.M < BM ? a.M : BM;
+    int rows = 1;
+    while (rows < WARPS && rows < m && (long long)entries * ((m + rows - 1) / rows) > 4 * ctx->sm_count) rows *= 2;
+    ctx->launches++;
+    return fspad_launch(tree_attn_packed_merge_kernel<BM, WARPS>, dim3((unsigned)entries, (unsigned)((m + rows - 1) / rows)), dim3(WARPS * 32), 0, st, 0, a, rows);
 }
 
 // Whether the units of a call, at most, can be counted in 32 bits (and 25 times as many as are cut into fewer parts than there are CTAs).

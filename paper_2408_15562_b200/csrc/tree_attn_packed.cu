@@ -26,12 +26,13 @@ using umma::mbar_wait;
 using umma::smem_u32;
 
 constexpr int UNIT = 32;                 // keys of a unit
-constexpr int BM = 16;                   // query rows of a tile
-constexpr int WARPS = 12;
-constexpr int STAGES = 4;
+constexpr int BM = 16;                   // query rows of a tile, at most
 constexpr int CODES = UNIT * FSPAD_PACKED_CODE_BYTES, SCALES = UNIT * FSPAD_PACKED_SCALE_BYTES;
 constexpr int STAGE = 2 * (CODES + SCALES);          // K codes | V codes | K scales | V scales
-constexpr int SMEM = WARPS * STAGES * STAGE;
+// With 8 rows a warp does with 128 registers.
+__host__ __device__ constexpr int warps_of(int nt) { return nt == 1 ? 16 : 12; }
+__host__ __device__ constexpr int stages_of(int nt) { return nt == 1 ? 3 : 4; }
+constexpr int MAX_WARPS = 16;
 
 __device__ __forceinline__ void mma16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
@@ -67,16 +68,25 @@ __device__ __forceinline__ uint32_t ld1(uint32_t at)
     asm volatile("ld.shared.u8 %0, [%1];\n" : "=r"(v) : "r"(at));
     return v;
 }
-// Columns 2c and 2c + 1 of a product's tile of eight keys are keys c and 4 + (c ^ 1): rows that the lanes read side by side then begin in
+// Eight by eight 16-bit values, a row's two in each lane, transposed.
+__device__ __forceinline__ uint32_t transpose8(uint32_t x)
+{
+    uint32_t y;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(y) : "r"(x));
+    return y;
+}
+
+// Rows 2c and 2c + 1 of eight keys of a product are keys c and 4 + (c ^ 1): rows that the lanes read side by side then begin in
 // different halves of the shared memory's 128-byte line.
 __device__ __forceinline__ int key_of(int column) { return (column & 1) ? 4 + ((column >> 1) ^ 1) : column >> 1; }
 
-// WIDE: tiles may have more than 8 rows.
-template <bool WIDE>
-__global__ void __launch_bounds__(WARPS * 32, 1)
+// NT: eights of query rows.  The products stand on their heads: scores S^T [keys][rows] = K Q^T, then O^T [elements][rows] += V^T P^T, so that K and V are the
+// operands with 16 rows and no half of an instruction goes to rows that do not exist.
+template <int NT>
+__global__ void __launch_bounds__(warps_of(NT) * 32, 1)
 tree_attn_packed_kernel(const Args a)
 {
-    constexpr int NX = WIDE ? 2 : 1;
+    constexpr int WARPS = warps_of(NT), STAGES = stages_of(NT);
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ __align__(8) unsigned long long s_bar[WARPS * STAGES];
     __shared__ int s_scan[WARPS + 2 * WARPS];
@@ -97,8 +107,9 @@ tree_attn_packed_kernel(const Args a)
     const int slot0 = blockIdx.x * WARPS + warp;
     Parts parts;
     Part part = cut_list<WARPS * 32, UNIT, WARPS>(a, blockIdx.x * WARPS, gridDim.x * WARPS, parts, s_scan, blockIdx.x == 0);
-    if (lane == 0) tell_cut<UNIT>(a, parts, part, slot0);
+    if (lane == 0) tell_part<UNIT>(a, parts, part, slot0);
     const int nt = tree_units<UNIT>(a), runs = a.Hkv * a.mtiles;
+    int done = 0;                                    // units of the part so far
     uint32_t n_fill = 0, n_use = 0;                  // stages filled and used so far
 
 #pragma unroll 1
@@ -127,57 +138,74 @@ tree_attn_packed_kernel(const Args a)
             if (lane == 0) fill(i);
             ++n_fill;
         }
+        if (u0 == 0 && lane == 0) tell_run(a, parts, part, slot0, done, n_run);
 
-        // ---- queries: rows g and g + 8 of the tile, elements 32 c .. 32 c + 31, as they are ----
-        uint32_t qf[8][4];                           // [product][a0, a1 (row + 8), a2 (column + 8), a3]
-        int node[2], to_row[2];
+        // ---- queries: row g of each eight, elements 32 c .. 32 c + 31, as they are ----
+        uint32_t qf[NT][8][2];                       // [eight][product][elements 4 s, 4 s + 1 / 4 s + 2, 4 s + 3 of the lane's 32]
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            const int gr = row0 + g + 8 * x;
-            const bool there = (WIDE || x == 0) && gr < a.M;
-            node[x] = there ? a.by_G.of(gr) : -1;
-            to_row[x] = there ? (b * a.N + node[x]) * a.Hq + h * a.G + (gr - node[x] * a.G) : -1;
+        for (int x = 0; x < NT; ++x) {
+            const int gr = row0 + g + 8 * x, node = a.by_G.of(gr);
+            const fspad_bf16 *q = a.q + ((size_t)(b * a.N + node) * a.Hq + h * a.G + (gr - node * a.G)) * D + 32 * c;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {            // pair 4 i + j of 16: product 2 i + j / 2, its columns 2c (j even) or 2c + 8
-                const uint4 w = there ? __ldg(reinterpret_cast<const uint4 *>(a.q + (size_t)to_row[x] * D + 32 * c) + i) : make_uint4(0u, 0u, 0u, 0u);
-                qf[2 * i][x] = w.x; qf[2 * i][x + 2] = w.y; qf[2 * i + 1][x] = w.z; qf[2 * i + 1][x + 2] = w.w;
+            for (int i = 0; i < 4; ++i) {
+                const uint4 w = gr < a.M ? __ldg(reinterpret_cast<const uint4 *>(q) + i) : make_uint4(0u, 0u, 0u, 0u);
+                qf[x][2 * i][0] = w.x; qf[x][2 * i][1] = w.y; qf[x][2 * i + 1][0] = w.z; qf[x][2 * i + 1][1] = w.w;
             }
         }
-        float o[16][4];
+        float o[NT][8][4];                           // elements 16 g + 2 j (0, 1) and 16 g + 2 j + 1 (2, 3) of rows 2 c and 2 c + 1
 #pragma unroll
-        for (int j = 0; j < 16; ++j)
+        for (int x = 0; x < NT; ++x)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) o[j][x] = 0.f;
-        float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int y = 0; y < 4; ++y) o[x][j][y] = 0.f;
+        float m_run[NT][2], l_run[NT][2];            // of rows 2 c, 2 c + 1; the sums of the lane's own keys alone
+#pragma unroll
+        for (int x = 0; x < NT; ++x) m_run[x][0] = m_run[x][1] = -INFINITY, l_run[x][0] = l_run[x][1] = 0.f;
 
-        // scores (log2 units, masked) of 8 T keys -> weights; the row's reference follows its maximum where that is far ahead of it
+        // scores (log2 units, masked) of 16 T keys -> weights; the row's reference follows its maximum where that is far ahead of it
         auto softmax = [&](auto &s, auto tiles) {
             constexpr int T = decltype(tiles)::value;
 #pragma unroll
-            for (int x = 0; x < NX; ++x) {
-                float mx = -INFINITY;
-#pragma unroll
-                for (int t = 0; t < T; ++t) mx = fmaxf(fmaxf(mx, s[t][2 * x]), s[t][2 * x + 1]);
-                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-                const bool move = mx > m_run[x] + kLazyLog2 || (m_run[x] == -INFINITY && mx > -INFINITY);
-                if (__any_sync(0xffffffffu, move)) {
-                    const float m_new = move ? mx : m_run[x];
-                    const float alpha = move ? ex2f(m_run[x] - m_new) : 1.f;
-                    m_run[x] = m_new;
-                    l_run[x] *= alpha;
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) { o[j][2 * x] *= alpha; o[j][2 * x + 1] *= alpha; }
-                }
-                const float ref = m_run[x] == -INFINITY ? 0.f : m_run[x] - kBiasLog2;
+            for (int x = 0; x < NT; ++x) {
+                float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
                 for (int t = 0; t < T; ++t)
 #pragma unroll
+                    for (int y = 0; y < 2; ++y) mx[y] = fmaxf(fmaxf(mx[y], s[t][x][y]), s[t][x][y + 2]);
+#pragma unroll
+                for (int off = 4; off < 32; off <<= 1)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) mx[y] = fmaxf(mx[y], __shfl_xor_sync(0xffffffffu, mx[y], off));
+                bool move[2];
+#pragma unroll
+                for (int y = 0; y < 2; ++y) move[y] = mx[y] > m_run[x][y] + kLazyLog2 || (m_run[x][y] == -INFINITY && mx[y] > -INFINITY);
+                if (__any_sync(0xffffffffu, move[0] || move[1])) {
+                    float alpha[2];
+#pragma unroll
                     for (int y = 0; y < 2; ++y) {
-                        const float p = ex2f(s[t][2 * x + y] - ref);
-                        s[t][2 * x + y] = p;
-                        l_run[x] += p;
+                        const float m_new = move[y] ? mx[y] : m_run[x][y];
+                        alpha[y] = move[y] ? ex2f(m_run[x][y] - m_new) : 1.f;
+                        m_run[x][y] = m_new;
+                        l_run[x][y] *= alpha[y];
                     }
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) o[x][j][y] *= alpha[y & 1];
+                }
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const float ref = m_run[x][y] == -INFINITY ? 0.f : m_run[x][y] - kBiasLog2;
+#pragma unroll
+                    for (int t = 0; t < T; ++t)
+#pragma unroll
+                        for (int z = 0; z < 4; z += 2) {
+                            const float p = ex2f(s[t][x][y + z] - ref);
+                            s[t][x][y + z] = p;
+                            l_run[x][y] += p;
+                        }
+                }
             }
         };
 
@@ -194,6 +222,18 @@ tree_attn_packed_kernel(const Args a)
                 for (int i = 0; i < 4; ++i)
                     kw[t][i] = t0 + key < a.N ? __ldg(reinterpret_cast<const uint4 *>(a.tk + first + key * D + 32 * c) + i) : make_uint4(0u, 0u, 0u, 0u);
             }
+            float s[1][NT][4];
+#pragma unroll
+            for (int x = 0; x < NT; ++x) {
+#pragma unroll
+                for (int y = 0; y < 4; ++y) s[0][x][y] = 0.f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t lo[4] = {kw[0][i].x, kw[1][i].x, kw[0][i].y, kw[1][i].y}, hi[4] = {kw[0][i].z, kw[1][i].z, kw[0][i].w, kw[1][i].w};
+                    mma16_bf(s[0][x], lo, qf[x][2 * i][0], qf[x][2 * i][1]);
+                    mma16_bf(s[0][x], hi, qf[x][2 * i + 1][0], qf[x][2 * i + 1][1]);
+                }
+            }
 #pragma unroll
             for (int y = 0; y < 4; ++y) {            // keys of columns 2c, 2c + 1, 2c + 8, 2c + 9: elements 16 g .. 16 g + 15
                 const int key = 8 * (y >> 1) + key_of(2 * c + (y & 1));
@@ -201,31 +241,24 @@ tree_attn_packed_kernel(const Args a)
                 for (int i = 0; i < 2; ++i)
                     vw[y][i] = t0 + key < a.N ? __ldg(reinterpret_cast<const uint4 *>(a.tv + first + key * D + 16 * g) + i) : make_uint4(0u, 0u, 0u, 0u);
             }
-            uint32_t see[2] = {0u, 0u};              // which of the 16 keys a row sees
+            uint32_t see[NT][2];                     // which of the 16 keys rows 2 c, 2 c + 1 see
 #pragma unroll
-            for (int x = 0; x < NX; ++x) {
-                int at = node[x];
-                while (at >= t0) {
-                    if (at < t0 + 16) see[x] |= 1u << (at - t0);
-                    const int up = __ldg(a.parent + (size_t)b * a.N + at);
-                    if (at == 0 ? up != -1 : (up < 0 || up >= at)) { fspad_report(a.status, FSPAD_ERR_BAD_TREE); break; }
-                    at = up;
+            for (int x = 0; x < NT; ++x)
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const int gr = row0 + 8 * x + 2 * c + y;
+                    see[x][y] = 0u;
+                    int at = gr < a.M ? a.by_G.of(gr) : -1;
+                    while (at >= t0) {
+                        if (at < t0 + 16) see[x][y] |= 1u << (at - t0);
+                        const int up = __ldg(a.parent + (size_t)b * a.N + at);
+                        if (at == 0 ? up != -1 : (up < 0 || up >= at)) { fspad_report(a.status, FSPAD_ERR_BAD_TREE); break; }
+                        at = up;
+                    }
+#pragma unroll
+                    for (int z = 0; z < 4; z += 2) s[0][x][y + z] = (see[x][y] >> (4 * z + key_of(g))) & 1u ? s[0][x][y + z] * a.scale_log2 : -INFINITY;
                 }
-            }
-            float s[2][4];
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-#pragma unroll
-                for (int x = 0; x < 4; ++x) s[t][x] = 0.f;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    mma16_bf(s[t], qf[2 * i], kw[t][i].x, kw[t][i].y);
-                    mma16_bf(s[t], qf[2 * i + 1], kw[t][i].z, kw[t][i].w);
-                }
-#pragma unroll
-                for (int x = 0; x < 4; ++x) s[t][x] = (see[x >> 1] >> (8 * t + key_of(2 * c + (x & 1)))) & 1u ? s[t][x] * a.scale_log2 : -INFINITY;
-            }
-            softmax(s, std::integral_constant<int, 2>());
+            softmax(s, std::integral_constant<int, 1>());
             // A row of V with an infinity or a NaN in it must not reach the queries that do not see it (0 times it is a NaN): it is taken
             // out of the product, and the queries that do see it get NaN.
             uint32_t keys = 0;
@@ -239,41 +272,45 @@ tree_attn_packed_kernel(const Args a)
             }
             keys = __reduce_or_sync(0xffffffffu, keys);
 #pragma unroll
-            for (int x = 0; x < NX; ++x)
-                if (see[x] & keys) l_run[x] = NAN;
-            const uint32_t p[4] = {umma::pack_bf16(s[0][0], s[0][1]), WIDE ? umma::pack_bf16(s[0][2], s[0][3]) : 0u,
-                                   umma::pack_bf16(s[1][0], s[1][1]), WIDE ? umma::pack_bf16(s[1][2], s[1][3]) : 0u};
+            for (int x = 0; x < NT; ++x) {
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                const uint32_t sel = j & 1 ? 0x7632u : 0x5410u;
-                auto word = [&](int y) {
-                    const uint4 w = vw[y][j >> 3];
-                    return ((j >> 1) & 3) == 0 ? w.x : ((j >> 1) & 3) == 1 ? w.y : ((j >> 1) & 3) == 2 ? w.z : w.w;
-                };
-                mma16_bf(o[j], p, __byte_perm(word(0), word(1), sel), __byte_perm(word(2), word(3), sel));
+                for (int y = 0; y < 2; ++y)
+                    if (see[x][y] & keys) l_run[x][y] = NAN;
+                const uint32_t p0 = transpose8(umma::pack_bf16(s[0][x][0], s[0][x][1])), p1 = transpose8(umma::pack_bf16(s[0][x][2], s[0][x][3]));
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    auto word = [&](int y) {
+                        const uint4 w = vw[y][j >> 2];
+                        return (j & 3) == 0 ? w.x : (j & 3) == 1 ? w.y : (j & 3) == 2 ? w.z : w.w;
+                    };
+                    const uint32_t v[4] = {__byte_perm(word(0), word(1), 0x5410), __byte_perm(word(0), word(1), 0x7632),
+                                           __byte_perm(word(2), word(3), 0x5410), __byte_perm(word(2), word(3), 0x7632)};
+                    mma16_bf(o[x][j], v, p0, p1);
+                }
             }
         }
 
         // ---- queries as fp16, scaled by a power of two so that the row's largest magnitude lies in [2^14, 2^15): 8 significant bits
         // stay exact down to 2^-31 of the largest ----
-        float cs[2] = {0.f, 0.f};                    // scores -> log2 units
+        float cs[NT][2];                             // scores -> log2 units, of rows 2 c, 2 c + 1
 #pragma unroll
-        for (int x = 0; x < NX; ++x) {
+        for (int x = 0; x < NT; ++x) {
             uint32_t m = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) m = fspad_most2(m, fspad_most2(qf[i][x], qf[i][x + 2]));
+            for (int i = 0; i < 8; ++i) m = fspad_most2(m, fspad_most2(qf[x][i][0], qf[x][i][1]));
             m = fspad_most2(m, __shfl_xor_sync(0xffffffffu, m, 1));
             m = fspad_most2(m, __shfl_xor_sync(0xffffffffu, m, 2));
             m = max(m & 0xffffu, m >> 16);
             // the largest magnitude is in [2^e, 2^(e+1)); of zeros, and of rows that are not finite (whose result is not either), as it is
             const int e = m == 0u || m >= 0x7f80u ? 14 : max((int)(m >> 7) - 127, -100);
             const float up = __uint_as_float((uint32_t)(127 + 14 - e) << 23);
-            cs[x] = a.scale_log2 * __uint_as_float((uint32_t)(127 - 14 + e) << 23);
+#pragma unroll
+            for (int y = 0; y < 2; ++y) cs[x][y] = a.scale_log2 * __uint_as_float((uint32_t)(127 - 14 + __shfl_sync(0xffffffffu, e, 4 * (2 * c + y))) << 23);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
 #pragma unroll
-                for (int y = 0; y < 4; y += 2)
-                    qf[i][x + y] = pack_f16(__uint_as_float(qf[i][x + y] << 16) * up, __uint_as_float(qf[i][x + y] & 0xffff0000u) * up);
+                for (int y = 0; y < 2; ++y)
+                    qf[x][i][y] = pack_f16(__uint_as_float(qf[x][i][y] << 16) * up, __uint_as_float(qf[x][i][y] & 0xffff0000u) * up);
         }
 
         // ---- units of the cache ----
@@ -287,47 +324,68 @@ tree_attn_packed_kernel(const Args a)
             }
             ++n_use;
             const int left = L - (kv0 + i) * UNIT;   // keys of the unit that exist
-            float s[4][4];
+            float s[2][NT][4];
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const int key = 8 * t + key_of(g);
-                const uint4 w = ld16(at + (uint32_t)(key * 64 + c * 16));
-                const uint32_t sc = fspad_e4m3_to_f16(ld2(at + 2 * CODES + (uint32_t)(key * 8 + c * 2)));
-                const uint32_t s0 = __byte_perm(sc, sc, 0x1010), s1 = __byte_perm(sc, sc, 0x3232);
-                const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+            for (int t = 0; t < 2; ++t) {
+                uint4 w[2];
+                uint32_t sc[2];
 #pragma unroll
-                for (int x = 0; x < 4; ++x) s[t][x] = 0.f;
+                for (int y = 0; y < 2; ++y) {
+                    const int key = 16 * t + 8 * y + key_of(g);
+                    w[y] = ld16(at + (uint32_t)(key * 64 + c * 16));
+                    sc[y] = fspad_e4m3_to_f16(ld2(at + 2 * CODES + (uint32_t)(key * 8 + c * 2)));
+                }
+#pragma unroll
+                for (int x = 0; x < NT; ++x)
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) s[t][x][y] = 0.f;
 #pragma unroll
                 for (int i2 = 0; i2 < 4; ++i2) {
-                    uint32_t f[4];
-                    fspad_e2m1_to_f16(ws[i2], f);
+                    uint32_t f[2][4];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) f[j] = fspad_hmul2(f[j], i2 < 2 ? s0 : s1);
-                    mma16(s[t], qf[2 * i2], f[0], f[1]);
-                    mma16(s[t], qf[2 * i2 + 1], f[2], f[3]);
+                    for (int y = 0; y < 2; ++y) {
+                        const uint32_t word = i2 == 0 ? w[y].x : i2 == 1 ? w[y].y : i2 == 2 ? w[y].z : w[y].w, s2 = __byte_perm(sc[y], sc[y], i2 < 2 ? 0x1010 : 0x3232);
+                        fspad_e2m1_to_f16(word, f[y]);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) f[y][j] = fspad_hmul2(f[y][j], s2);
+                    }
+                    const uint32_t lo[4] = {f[0][0], f[1][0], f[0][1], f[1][1]}, hi[4] = {f[0][2], f[1][2], f[0][3], f[1][3]};
+#pragma unroll
+                    for (int x = 0; x < NT; ++x) {
+                        mma16(s[t][x], lo, qf[x][2 * i2][0], qf[x][2 * i2][1]);
+                        mma16(s[t][x], hi, qf[x][2 * i2 + 1][0], qf[x][2 * i2 + 1][1]);
+                    }
                 }
             }
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int x = 0; x < 2 * NX; ++x) s[t][x] *= cs[x >> 1];
+                for (int x = 0; x < NT; ++x)
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) s[t][x][y] *= cs[x][y & 1];
             if (left < UNIT) {
 #pragma unroll
-                for (int t = 0; t < 4; ++t)
+                for (int t = 0; t < 2; ++t)
 #pragma unroll
-                    for (int x = 0; x < 4; ++x)
-                        if (8 * t + key_of(2 * c + (x & 1)) >= left) s[t][x] = -INFINITY;
+                    for (int y = 0; y < 4; ++y)
+                        if (16 * t + 4 * (y & 2) + key_of(g) >= left)
+#pragma unroll
+                            for (int x = 0; x < NT; ++x) s[t][x][y] = -INFINITY;
             }
-            softmax(s, std::integral_constant<int, 4>());
+            softmax(s, std::integral_constant<int, 2>());
 #pragma unroll
-            for (int k2 = 0; k2 < 2; ++k2) {
-                const uint32_t p[4] = {pack_f16(s[2 * k2][0], s[2 * k2][1]), WIDE ? pack_f16(s[2 * k2][2], s[2 * k2][3]) : 0u,
-                                       pack_f16(s[2 * k2 + 1][0], s[2 * k2 + 1][1]), WIDE ? pack_f16(s[2 * k2 + 1][2], s[2 * k2 + 1][3]) : 0u};
+            for (int t = 0; t < 2; ++t) {
+                uint32_t p[NT][2];
+#pragma unroll
+                for (int x = 0; x < NT; ++x) {
+                    p[x][0] = transpose8(pack_f16(s[t][x][0], s[t][x][1]));
+                    p[x][1] = transpose8(pack_f16(s[t][x][2], s[t][x][3]));
+                }
                 uint2 w[4];
                 uint32_t sc[2];
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
-                    const int ka = 16 * k2 + 8 * y + key_of(2 * c), kb = 16 * k2 + 8 * y + key_of(2 * c + 1);
+                    const int ka = 16 * t + 8 * y + key_of(2 * c), kb = 16 * t + 8 * y + key_of(2 * c + 1);
                     w[2 * y] = ld8(at + CODES + (uint32_t)(ka * 64 + g * 8));
                     w[2 * y + 1] = ld8(at + CODES + (uint32_t)(kb * 64 + g * 8));
                     uint32_t sa = ld1(at + 2 * CODES + SCALES + (uint32_t)(ka * 8 + g)), sb = ld1(at + 2 * CODES + SCALES + (uint32_t)(kb * 8 + g));
@@ -352,8 +410,9 @@ tree_attn_packed_kernel(const Args a)
                     }
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        mma16(o[8 * i2 + 2 * j], p, f[0][0][j], f[1][0][j]);
-                        mma16(o[8 * i2 + 2 * j + 1], p, f[0][1][j], f[1][1][j]);
+                        const uint32_t v[4] = {f[0][0][j], f[0][1][j], f[1][0][j], f[1][1][j]};
+#pragma unroll
+                        for (int x = 0; x < NT; ++x) mma16(o[x][4 * i2 + j], v, p[x][0], p[x][1]);
                     }
                 }
             }
@@ -370,36 +429,49 @@ tree_attn_packed_kernel(const Args a)
             return;
         }
 
-        // ---- the rows: lane (g, c) has elements 32 c + j in o[j][2 x], 32 c + 16 + j in o[j][2 x + 1] ----
+        // ---- the rows: of rows 2 c and 2 c + 1 the lane has elements 16 g .. 16 g + 15 ----
         const bool whole = u0 == 0 && u1 == n_run;
 #pragma unroll
-        for (int x = 0; x < NX; ++x) {
-            l_run[x] += __shfl_xor_sync(0xffffffffu, l_run[x], 1);
-            l_run[x] += __shfl_xor_sync(0xffffffffu, l_run[x], 2);
-            if (node[x] < 0) continue;
-            if (whole) {
-                const float inv = 1.f / l_run[x];
-                uint4 *dst = reinterpret_cast<uint4 *>(a.out + (size_t)to_row[x] * D + 32 * c);
+        for (int x = 0; x < NT; ++x)
 #pragma unroll
-                for (int y = 0; y < 2; ++y)
+            for (int y = 0; y < 2; ++y) {
+                float l = l_run[x][y];
 #pragma unroll
-                    for (int j = 0; j < 16; j += 8)
-                        dst[2 * y + j / 8] = make_uint4(umma::pack_bf16(o[j][2 * x + y] * inv, o[j + 1][2 * x + y] * inv), umma::pack_bf16(o[j + 2][2 * x + y] * inv, o[j + 3][2 * x + y] * inv),
-                                                        umma::pack_bf16(o[j + 4][2 * x + y] * inv, o[j + 5][2 * x + y] * inv), umma::pack_bf16(o[j + 6][2 * x + y] * inv, o[j + 7][2 * x + y] * inv));
-            } else {
-                const size_t slot = ((size_t)slot0 * 2 + (u0 == 0 ? 1 : 0)) * BM + g + 8 * x;
-                float4 *dst = reinterpret_cast<float4 *>(a.part_o + slot * D + 32 * c);
+                for (int off = 4; off < 32; off <<= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
+                const int r = 8 * x + 2 * c + y, gr = row0 + r;
+                if (gr >= a.M) continue;
+                if (whole) {
+                    const int node = a.by_G.of(gr);
+                    const float inv = 1.f / l;
+                    uint4 *dst = reinterpret_cast<uint4 *>(a.out + ((size_t)(b * a.N + node) * a.Hq + h * a.G + (gr - node * a.G)) * D + 16 * g);
 #pragma unroll
-                for (int y = 0; y < 2; ++y)
+                    for (int j = 0; j < 8; j += 4)
+                        dst[j / 4] = make_uint4(umma::pack_bf16(o[x][j][y] * inv, o[x][j][y + 2] * inv), umma::pack_bf16(o[x][j + 1][y] * inv, o[x][j + 1][y + 2] * inv),
+                                                umma::pack_bf16(o[x][j + 2][y] * inv, o[x][j + 2][y + 2] * inv), umma::pack_bf16(o[x][j + 3][y] * inv, o[x][j + 3][y + 2] * inv));
+                } else {
+                    const size_t slot = ((size_t)slot0 * 2 + (u0 == 0 ? 1 : 0)) * BM + r;
+                    float4 *dst = reinterpret_cast<float4 *>(a.part_o + slot * D + 16 * g);
 #pragma unroll
-                    for (int j = 0; j < 16; j += 4) dst[4 * y + j / 4] = make_float4(o[j][2 * x + y], o[j + 1][2 * x + y], o[j + 2][2 * x + y], o[j + 3][2 * x + y]);
-                if (c == 0) a.part_ml[slot] = make_float2(m_run[x], l_run[x]);
+                    for (int j = 0; j < 8; j += 2) dst[j / 2] = make_float4(o[x][j][y], o[x][j][y + 2], o[x][j + 1][y], o[x][j + 1][y + 2]);
+                    if (g == 0) a.part_ml[slot] = make_float2(m_run[x][y], l);
+                }
             }
-        }
+        done += u1 - u0;
         part.left -= u1 - u0;
         part.u = 0;
         if (++part.run == runs) { part.run = 0; ++part.b; }
     }
+}
+
+template <int NT> cudaError_t launch_few(fspad_ctx *ctx, Args &a, cudaStream_t st)
+{
+    const int ctas = ctx->sm_count, smem = warps_of(NT) * stages_of(NT) * STAGE;
+    cudaError_t e = cudaFuncSetAttribute(tree_attn_packed_kernel<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    const int entries = merge_entries(a, ctas * warps_of(NT));
+    ctx->launches++;
+    e = fspad_launch(tree_attn_packed_kernel<NT>, dim3((unsigned)ctas), dim3(warps_of(NT) * 32), smem, st, 0, a);
+    return e == cudaSuccess ? launch_merge<BM, 16>(ctx, a, entries, st) : e;
 }
 
 }  // namespace
@@ -411,7 +483,7 @@ size_t fspad_attn_packed_workspace(const fspad_ctx *ctx, int N, int B)
 {
     (void)B;
     if (many_rows(ctx, N)) return fspad_attn_packed_umma_workspace(ctx);
-    return scratch_bytes<BM>(ctx->sm_count * WARPS);
+    return scratch_bytes<BM>(ctx->sm_count * MAX_WARPS);
 }
 
 cudaError_t fspad_launch_tree_attn_packed(fspad_ctx *ctx, const fspad_bf16 *q, const uint8_t *k_codes, const uint8_t *k_scales,
@@ -430,15 +502,6 @@ cudaError_t fspad_launch_tree_attn_packed(fspad_ctx *ctx, const fspad_bf16 *q, c
     a.scale_log2 = ctx->scale * kLog2e;
     a.out = out; a.status = ctx->d_status;
     if (many_rows(ctx, N)) return fspad_launch_attn_packed_umma(ctx, a, workspace, st);
-    const int ctas = ctx->sm_count;
-    scratch_in<BM>(a, ctas * WARPS, workspace);
-    auto kernel = a.M > 8 ? tree_attn_packed_kernel<true> : tree_attn_packed_kernel<false>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
-    if (e != cudaSuccess) return e;
-    ctx->launches += 2;
-    e = fspad_launch(kernel, dim3((unsigned)ctas), dim3(WARPS * 32), SMEM, st, 0, a);
-    if (e != cudaSuccess) return e;
-    int rows = 1;
-    while (rows < a.M && rows < BM) rows *= 2;
-    return fspad_launch(tree_attn_packed_merge_kernel<BM, 16>, dim3((unsigned)(ctas * WARPS)), dim3(512), 0, st, 0, a, rows);
+    scratch_in<BM>(a, ctx->sm_count * MAX_WARPS, workspace);
+    return a.M <= 8 ? launch_few<1>(ctx, a, st) : launch_few<2>(ctx, a, st);
 }

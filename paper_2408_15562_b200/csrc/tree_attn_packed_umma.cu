@@ -170,7 +170,7 @@ tree_attn_packed_umma_kernel(const Args a)
     const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
     const int nt = tree_units<UNIT>(a), runs = a.Hkv * a.mtiles;
 
-    if (warp == 11 && lane == 0) tell_cut<UNIT>(a, parts, part, cta);    // (a warp without another job)
+    if (warp == 11 && lane == 0) tell_part<UNIT>(a, parts, part, cta);       // (a warp without another job)
 
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t sQ = base, sK = base + 2 * TILE, sV = base + 4 * TILE, sStage = base + 6 * TILE;
@@ -416,8 +416,11 @@ tree_attn_packed_umma_kernel(const Args a)
       asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
       if (warp == 8) {
         // ================= copies =================
-        int n = 0;                                           // stages filled so far
-        while (!failed && next(s)) {
+        int n = 0, done = 0;                                 // stages filled, chunks taken so far
+        for (;; done += s.n_ch) {
+            const Part at = part;
+            if (failed || !next(s)) break;
+            if (s.u0 == 0 && lane == 0) tell_run(a, parts, at, cta, done, s.n_run);
             const int *blocks = a.table + (size_t)s.b * a.table_stride;
             const int kv0 = s.u0 + s.n_tree - nt, n_kv = s.n_ch - s.n_tree;  // chunks of the cache
             int mine = 0;
@@ -638,8 +641,8 @@ cudaError_t fspad_launch_attn_packed_umma(fspad_ctx *ctx, packed::Args a, void *
     scratch_in<BM>(a, ctas, workspace);
     cudaError_t e = cudaFuncSetAttribute(tree_attn_packed_umma_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
     if (e != cudaSuccess) return e;
-    ctx->launches += 2;
+    const int entries = merge_entries(a, ctas);
+    ctx->launches++;
     e = fspad_launch(tree_attn_packed_umma_kernel, dim3((unsigned)ctas), dim3(NT), SMEM, st, 0, a);
-    if (e != cudaSuccess) return e;
-    return fspad_launch(tree_attn_packed_merge_kernel<BM, 8>, dim3((unsigned)ctas, (unsigned)((a.M < BM ? a.M : BM) + 7) / 8), dim3(256), 0, st, 0, a, 8);
+    return e == cudaSuccess ? launch_merge<BM, 8>(ctx, a, entries, st) : e;
 }
