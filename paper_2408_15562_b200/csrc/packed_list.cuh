@@ -62,6 +62,8 @@ __device__ __forceinline__ int prefix_of(const Args &a, int b, bool report)
 }
 template <int UNIT> __device__ __forceinline__ int tree_units(const Args &a) { return (a.N + UNIT - 1) / UNIT; }
 template <int UNIT> __device__ __forceinline__ int run_units(const Args &a, int L) { return tree_units<UNIT>(a) + (int)(((long long)L + UNIT - 1) / UNIT); }
+template <int UNIT> constexpr int kStretch = UNIT == 128 ? 4 : 2;
+
 // How many parts the list may be cut into.  With chunks of 128 keys for 256 rows a part of a cut run leaves 128 KB, which cost about a thirtieth of what a chunk
 // takes to write and read again: of few chunks, then, fewer parts than SMs (5 sqrt(total)).
 template <int UNIT> __device__ __forceinline__ int parts_of(int total, int ctas)
@@ -70,9 +72,9 @@ template <int UNIT> __device__ __forceinline__ int parts_of(int total, int ctas)
     return min(total, ctas);
 }
 
-// The list is cut in one of two ways.  With no more runs than parts (and no more than 32 sequences) every run is cut into pieces of at most `q` units, equal ones,
-// one to a CTA: a stretch of another run in a CTA costs as much as several units.  Otherwise into parts of q units or, the first r of them, q + 1, wherever
-// the cuts fall.  (Units are counted in 32 bits: the host has seen to it that they fit.)
+// The list is cut in one of two ways.  With no more runs than parts (and no more than 32 sequences) every run is cut into equal pieces, one to a part; or the list
+// into equal parts, wherever the cuts fall.  Equal parts are the shorter ones, but have stretches of two runs in them, and what a stretch costs besides
+// its units (queries, the rows' way out) is worth kStretch units: the first way is taken where its longest piece is not longer by more.  (Units are counted in 32 bits: the host has seen to it that they fit.)
 struct Parts {
     int n, q, r;                         // parts, units / parts, units % parts
     __device__ __forceinline__ int start(int i) const { return i * q + min(i, r); }
@@ -106,11 +108,11 @@ __device__ __forceinline__ Part cut_list(const Args &a, int part0, int slots, Pa
         p.n = parts_of<UNIT>(total, ctas);
         p.q = total / p.n;
         p.r = total - p.q * p.n;
-        int want = part < p.n ? p.start(part) : total;
+        const int want = part < p.n ? p.start(part) : total, most = p.q + kStretch<UNIT>;
         if (a.B * runs <= p.n) {
             // the smallest piece with which there are no more pieces than parts, from below, within a step or two
-            int k, sum, q = max(1, (total + p.n - 1) / p.n);
-            for (;;) {
+            int k = 0, sum = 0, q = max(1, (total + p.n - 1) / p.n), by_run = 0;
+            while (q <= most) {
                 k = lane < a.B ? (n + q - 1) / q : 0;
                 inc = runs * k;
 #pragma unroll
@@ -119,24 +121,34 @@ __device__ __forceinline__ Part cut_list(const Args &a, int part0, int slots, Pa
                     if (lane >= off) inc += o;
                 }
                 sum = __shfl_sync(0xffffffffu, inc, 31);
-                if (sum <= p.n) break;
-                q += max(1, (int)((float)q * (float)(sum - p.n) / (float)(2 * sum)));        // (ends: at q = n of the longest there is a piece a run)
+                if (sum <= p.n) { by_run = 1; break; }
+                q += max(1, (int)((float)q * (float)(sum - p.n) / (float)(2 * sum)));
             }
-            s.by_run = true;
-            p.n = sum;
-            want = part;
-            if (part < sum) {
-                s.b = __popc(__ballot_sync(0xffffffffu, inc <= part));
-                k = __shfl_sync(0xffffffffu, k, s.b);
-                const int nb = __shfl_sync(0xffffffffu, n, s.b), x = part - (s.b > 0 ? __shfl_sync(0xffffffffu, inc, s.b - 1) : 0);
-                s.run = x / k;
-                const int piece = x - s.run * k, w = nb / k, more = nb - w * k;              // the first `more` pieces are of w + 1 units
-                s.u = piece * w + min(piece, more);
-                s.left = w + (piece < more ? 1 : 0);
-                s.i0 = part - piece;
-                s.i1 = s.i0 + k - 1;
+            if (by_run) {
+                s.by_run = true;
+                p.n = sum;
+                if (part < sum) {
+                    s.b = __popc(__ballot_sync(0xffffffffu, inc <= part));
+                    k = __shfl_sync(0xffffffffu, k, s.b);
+                    const int nb = __shfl_sync(0xffffffffu, n, s.b), x = part - (s.b > 0 ? __shfl_sync(0xffffffffu, inc, s.b - 1) : 0);
+                    s.run = x / k;
+                    const int piece = x - s.run * k, w = nb / k, more = nb - w * k;          // the first `more` pieces are of w + 1 units
+                    s.u = piece * w + min(piece, more);
+                    s.left = w + (piece < more ? 1 : 0);
+                    s.i0 = part - piece;
+                    s.i1 = s.i0 + k - 1;
+                }
+                __syncthreads();
+                return s;
             }
-        } else if (part < p.n) {
+            inc = runs * n;
+#pragma unroll
+            for (int off = 1; off < 32; off <<= 1) {
+                const int o = __shfl_up_sync(0xffffffffu, inc, off);
+                if (lane >= off) inc += o;
+            }
+        }
+        if (part < p.n) {
             s.b = __popc(__ballot_sync(0xffffffffu, inc <= want));
             const int nb = __shfl_sync(0xffffffffu, n, s.b), x = want - (s.b > 0 ? __shfl_sync(0xffffffffu, inc, s.b - 1) : 0);
             s.run = x / nb;

@@ -109,6 +109,10 @@ tree_attn_packed_kernel(const Args a)
     Part part = cut_list<WARPS * 32, UNIT, WARPS>(a, blockIdx.x * WARPS, gridDim.x * WARPS, parts, s_scan, blockIdx.x == 0);
     if (lane == 0) tell_part<UNIT>(a, parts, part, slot0);
     const int nt = tree_units<UNIT>(a), runs = a.Hkv * a.mtiles;
+    // what lanes 0 .. 3 copy of a unit: from which array, of how many bytes a row, to where in the stage
+    const uint8_t *part_src = lane == 0 ? a.kc : lane == 1 ? a.vc : lane == 2 ? a.ks : a.vs;
+    const uint32_t part_row = lane < 2 ? FSPAD_PACKED_CODE_BYTES : FSPAD_PACKED_SCALE_BYTES;
+    const uint32_t part_at = lane < 2 ? lane * CODES : 2 * CODES + (lane - 2) * SCALES;
     int done = 0;                                    // units of the part so far
     uint32_t n_fill = 0, n_use = 0;                  // stages filled and used so far
 
@@ -119,25 +123,28 @@ tree_attn_packed_kernel(const Args a)
         const int h = a.by_tiles.of(part.run), row0 = (part.run - h * a.mtiles) * BM;
         const int *blocks = a.table + (size_t)b * a.table_stride;
 
-        // ---- the first fills ----
+        // ---- the first fills: lanes 0 .. 3 copy K codes, V codes, K scales, V scales; blocks are looked up 32 at a time ----
         const int kv0 = max(u0, nt) - nt, n_kv = max(0, u1 - nt - kv0);      // units of the cache
-        auto fill = [&](int i) {                     // lane 0
-            const int key0 = (kv0 + i) * UNIT;
-            int blk = __ldg(blocks + (key0 >> 7));
-            if (blk < 0 || blk >= a.n_blocks) { fspad_report(a.status, FSPAD_ERR_RANGE); blk = 0; }
-            const size_t row = ((size_t)blk * a.Hkv + h) * 128 + (key0 & 127);
-            const uint32_t st = n_fill % STAGES, to = ring + st * STAGE, bar = bar0 + 8u * st;
-            mbar_expect_tx(bar, STAGE);
-            bulk_load(to, a.kc + row * FSPAD_PACKED_CODE_BYTES, CODES, bar);
-            bulk_load(to + 2 * CODES, a.ks + row * FSPAD_PACKED_SCALE_BYTES, SCALES, bar);
-            bulk_load(to + CODES, a.vc + row * FSPAD_PACKED_CODE_BYTES, CODES, bar);
-            bulk_load(to + 2 * CODES + SCALES, a.vs + row * FSPAD_PACKED_SCALE_BYTES, SCALES, bar);
+        int block = 0, looked = -32;                 // of this lane, and lane 0's place in the table
+        auto fill = [&](int i) {
+            const int key0 = (kv0 + i) * UNIT, page = key0 >> 7;
+            if (page >= looked + 32) {
+                looked = page;
+                block = 0;
+                if ((long long)(page + lane) * 128 < L) {
+                    block = __ldg(blocks + page + lane);
+                    if (block < 0 || block >= a.n_blocks) { fspad_report(a.status, FSPAD_ERR_RANGE); block = 0; }
+                }
+            }
+            const int blk = __shfl_sync(0xffffffffu, block, page - looked);
+            const uint32_t st = n_fill % STAGES, bar = bar0 + 8u * st;
+            if (lane == 0) mbar_expect_tx(bar, STAGE);
+            __syncwarp();
+            if (lane < 4) bulk_load(ring + st * STAGE + part_at, part_src + ((size_t)(blk * a.Hkv + h) * 128 + (key0 & 127)) * part_row, part_row * UNIT, bar);
+            ++n_fill;
         };
 #pragma unroll 1
-        for (int i = 0; i < STAGES && i < n_kv; ++i) {
-            if (lane == 0) fill(i);
-            ++n_fill;
-        }
+        for (int i = 0; i < STAGES && i < n_kv; ++i) fill(i);
         if (u0 == 0 && lane == 0) tell_run(a, parts, part, slot0, done, n_run);
 
         // ---- queries: row g of each eight, elements 32 c .. 32 c + 31, as they are ----
@@ -163,8 +170,8 @@ tree_attn_packed_kernel(const Args a)
 #pragma unroll
         for (int x = 0; x < NT; ++x) m_run[x][0] = m_run[x][1] = -INFINITY, l_run[x][0] = l_run[x][1] = 0.f;
 
-        // scores (log2 units, masked) of 16 T keys -> weights; the row's reference follows its maximum where that is far ahead of it
-        auto softmax = [&](auto &s, auto tiles) {
+        // scores (masked; `to_log2` of each row's makes log2 units of them) of 16 T keys -> weights; the row's reference follows its maximum where that is far ahead of it
+        auto softmax = [&](auto &s, const float (&to_log2)[NT][2], auto tiles) {
             constexpr int T = decltype(tiles)::value;
 #pragma unroll
             for (int x = 0; x < NT; ++x) {
@@ -177,6 +184,8 @@ tree_attn_packed_kernel(const Args a)
                 for (int off = 4; off < 32; off <<= 1)
 #pragma unroll
                     for (int y = 0; y < 2; ++y) mx[y] = fmaxf(mx[y], __shfl_xor_sync(0xffffffffu, mx[y], off));
+#pragma unroll
+                for (int y = 0; y < 2; ++y) mx[y] *= to_log2[x][y];
                 bool move[2];
 #pragma unroll
                 for (int y = 0; y < 2; ++y) move[y] = mx[y] > m_run[x][y] + kLazyLog2 || (m_run[x][y] == -INFINITY && mx[y] > -INFINITY);
@@ -196,12 +205,12 @@ tree_attn_packed_kernel(const Args a)
                 }
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
-                    const float ref = m_run[x][y] == -INFINITY ? 0.f : m_run[x][y] - kBiasLog2;
+                    const float ref = m_run[x][y] == -INFINITY ? 0.f : kBiasLog2 - m_run[x][y];
 #pragma unroll
                     for (int t = 0; t < T; ++t)
 #pragma unroll
                         for (int z = 0; z < 4; z += 2) {
-                            const float p = ex2f(s[t][x][y + z] - ref);
+                            const float p = ex2f(fmaf(s[t][x][y + z], to_log2[x][y], ref));
                             s[t][x][y + z] = p;
                             l_run[x][y] += p;
                         }
@@ -256,9 +265,12 @@ tree_attn_packed_kernel(const Args a)
                         at = up;
                     }
 #pragma unroll
-                    for (int z = 0; z < 4; z += 2) s[0][x][y + z] = (see[x][y] >> (4 * z + key_of(g))) & 1u ? s[0][x][y + z] * a.scale_log2 : -INFINITY;
+                    for (int z = 0; z < 4; z += 2) s[0][x][y + z] = (see[x][y] >> (4 * z + key_of(g))) & 1u ? s[0][x][y + z] : -INFINITY;
                 }
-            softmax(s, std::integral_constant<int, 1>());
+            float plain[NT][2];
+#pragma unroll
+            for (int x = 0; x < NT; ++x) plain[x][0] = plain[x][1] = a.scale_log2;
+            softmax(s, plain, std::integral_constant<int, 1>());
             // A row of V with an infinity or a NaN in it must not reach the queries that do not see it (0 times it is a NaN): it is taken
             // out of the product, and the queries that do see it get NaN.
             uint32_t keys = 0;
@@ -357,12 +369,6 @@ tree_attn_packed_kernel(const Args a)
                     }
                 }
             }
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int x = 0; x < NT; ++x)
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) s[t][x][y] *= cs[x][y & 1];
             if (left < UNIT) {
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
@@ -372,7 +378,7 @@ tree_attn_packed_kernel(const Args a)
 #pragma unroll
                             for (int x = 0; x < NT; ++x) s[t][x][y] = -INFINITY;
             }
-            softmax(s, std::integral_constant<int, 2>());
+            softmax(s, cs, std::integral_constant<int, 2>());
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 uint32_t p[NT][2];
@@ -390,8 +396,10 @@ tree_attn_packed_kernel(const Args a)
                     w[2 * y + 1] = ld8(at + CODES + (uint32_t)(kb * 64 + g * 8));
                     uint32_t sa = ld1(at + 2 * CODES + SCALES + (uint32_t)(ka * 8 + g)), sb = ld1(at + 2 * CODES + SCALES + (uint32_t)(kb * 8 + g));
                     // what lies behind the sequence's end may be anything, and 0 times a NaN is one: its scale is zero
-                    if (ka >= left) sa = 0u;
-                    if (kb >= left) sb = 0u;
+                    if (left < UNIT) {
+                        if (ka >= left) sa = 0u;
+                        if (kb >= left) sb = 0u;
+                    }
                     sc[y] = fspad_e4m3_to_f16(sa | (sb << 8));
                 }
 #pragma unroll
@@ -417,10 +425,7 @@ tree_attn_packed_kernel(const Args a)
                 }
             }
             __syncwarp();                            // every lane has read the stage
-            if (i + STAGES < n_kv) {
-                if (lane == 0) fill(i + STAGES);
-                ++n_fill;
-            }
+            if (i + STAGES < n_kv) fill(i + STAGES);
         }
         if (failed) {
             // what is under way gets another bounded time to land before the warp leaves
