@@ -44,30 +44,41 @@ __device__ __forceinline__ void mma16_bf(float (&c)[4], const uint32_t (&a)[4], 
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ uint4 ld16(uint32_t at)
+// Shared loads at a register plus a constant (as operands of the instruction, no additions).
+template <int AT> __device__ __forceinline__ uint4 ld16(uint32_t at)
 {
     uint4 v;
-    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4 + %5];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at), "n"(AT));
     return v;
 }
-__device__ __forceinline__ uint2 ld8(uint32_t at)
+template <int AT> __device__ __forceinline__ uint2 ld8(uint32_t at)
 {
     uint2 v;
-    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];\n" : "=r"(v.x), "=r"(v.y) : "r"(at));
+    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2 + %3];\n" : "=r"(v.x), "=r"(v.y) : "r"(at), "n"(AT));
     return v;
 }
-__device__ __forceinline__ uint32_t ld2(uint32_t at)
+template <int AT> __device__ __forceinline__ uint32_t ld2(uint32_t at)
 {
     uint16_t v;
-    asm volatile("ld.shared.u16 %0, [%1];\n" : "=h"(v) : "r"(at));
+    asm volatile("ld.shared.u16 %0, [%1 + %2];\n" : "=h"(v) : "r"(at), "n"(AT));
     return v;
 }
-__device__ __forceinline__ uint32_t ld1(uint32_t at)
+template <int AT> __device__ __forceinline__ uint32_t ld1(uint32_t at)
 {
     uint32_t v;
-    asm volatile("ld.shared.u8 %0, [%1];\n" : "=r"(v) : "r"(at));
+    asm volatile("ld.shared.u8 %0, [%1 + %2];\n" : "=r"(v) : "r"(at), "n"(AT));
     return v;
 }
+
+// f(0), f(1), ... f(N - 1), each with its number as a constant
+template <int N, typename F> __device__ __forceinline__ void each(F &&f)
+{
+    if constexpr (N > 0) {
+        each<N - 1>(f);
+        f(std::integral_constant<int, N - 1>());
+    }
+}
+
 // Eight by eight 16-bit values, a row's two in each lane, transposed.
 __device__ __forceinline__ uint32_t transpose8(uint32_t x)
 {
@@ -113,6 +124,9 @@ tree_attn_packed_kernel(const Args a)
     const uint8_t *part_src = lane == 0 ? a.kc : lane == 1 ? a.vc : lane == 2 ? a.ks : a.vs;
     const uint32_t part_row = lane < 2 ? FSPAD_PACKED_CODE_BYTES : FSPAD_PACKED_SCALE_BYTES;
     const uint32_t part_at = lane < 2 ? lane * CODES : 2 * CODES + (lane - 2) * SCALES;
+    const uint32_t lane_k = key_of(g) * 64 + c * 16, lane_ks = 2 * CODES + key_of(g) * 8 + c * 2;
+    const uint32_t lane_va = CODES + key_of(2 * c) * 64 + g * 8, lane_vb = CODES + key_of(2 * c + 1) * 64 + g * 8;
+    const uint32_t lane_sa = 2 * CODES + SCALES + key_of(2 * c) * 8 + g, lane_sb = 2 * CODES + SCALES + key_of(2 * c + 1) * 8 + g;
     int done = 0;                                    // units of the part so far
     uint32_t n_fill = 0, n_use = 0;                  // stages filled and used so far
 
@@ -336,17 +350,13 @@ tree_attn_packed_kernel(const Args a)
             }
             ++n_use;
             const int left = L - (kv0 + i) * UNIT;   // keys of the unit that exist
+            // the lane's places: its row of K, its scales; the rows of V of columns 2 c and 2 c + 1, their scales
+            const uint32_t at_k = at + lane_k, at_ks = at + lane_ks, at_va = at + lane_va, at_vb = at + lane_vb, at_sa = at + lane_sa, at_sb = at + lane_sb;
             float s[2][NT][4];
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                uint4 w[2];
-                uint32_t sc[2];
-#pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    const int key = 16 * t + 8 * y + key_of(g);
-                    w[y] = ld16(at + (uint32_t)(key * 64 + c * 16));
-                    sc[y] = fspad_e4m3_to_f16(ld2(at + 2 * CODES + (uint32_t)(key * 8 + c * 2)));
-                }
+            each<2>([&](auto t_) {
+                constexpr int t = decltype(t_)::value;
+                uint4 w[2] = {ld16<t * 1024>(at_k), ld16<t * 1024 + 512>(at_k)};
+                uint32_t sc[2] = {fspad_e4m3_to_f16(ld2<t * 128>(at_ks)), fspad_e4m3_to_f16(ld2<t * 128 + 64>(at_ks))};
 #pragma unroll
                 for (int x = 0; x < NT; ++x)
 #pragma unroll
@@ -368,7 +378,7 @@ tree_attn_packed_kernel(const Args a)
                         mma16(s[t][x], hi, qf[x][2 * i2 + 1][0], qf[x][2 * i2 + 1][1]);
                     }
                 }
-            }
+            });
             if (left < UNIT) {
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
@@ -379,28 +389,24 @@ tree_attn_packed_kernel(const Args a)
                             for (int x = 0; x < NT; ++x) s[t][x][y] = -INFINITY;
             }
             softmax(s, cs, std::integral_constant<int, 2>());
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
+            each<2>([&](auto t_) {
+                constexpr int t = decltype(t_)::value;
                 uint32_t p[NT][2];
 #pragma unroll
                 for (int x = 0; x < NT; ++x) {
                     p[x][0] = transpose8(pack_f16(s[t][x][0], s[t][x][1]));
                     p[x][1] = transpose8(pack_f16(s[t][x][2], s[t][x][3]));
                 }
-                uint2 w[4];
-                uint32_t sc[2];
+                const uint2 w[4] = {ld8<t * 1024>(at_va), ld8<t * 1024>(at_vb), ld8<t * 1024 + 512>(at_va), ld8<t * 1024 + 512>(at_vb)};
+                uint32_t sa[2] = {ld1<t * 128>(at_sa), ld1<t * 128 + 64>(at_sa)}, sb[2] = {ld1<t * 128>(at_sb), ld1<t * 128 + 64>(at_sb)}, sc[2];
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
-                    const int ka = 16 * t + 8 * y + key_of(2 * c), kb = 16 * t + 8 * y + key_of(2 * c + 1);
-                    w[2 * y] = ld8(at + CODES + (uint32_t)(ka * 64 + g * 8));
-                    w[2 * y + 1] = ld8(at + CODES + (uint32_t)(kb * 64 + g * 8));
-                    uint32_t sa = ld1(at + 2 * CODES + SCALES + (uint32_t)(ka * 8 + g)), sb = ld1(at + 2 * CODES + SCALES + (uint32_t)(kb * 8 + g));
                     // what lies behind the sequence's end may be anything, and 0 times a NaN is one: its scale is zero
                     if (left < UNIT) {
-                        if (ka >= left) sa = 0u;
-                        if (kb >= left) sb = 0u;
+                        if (16 * t + 8 * y + key_of(2 * c) >= left) sa[y] = 0u;
+                        if (16 * t + 8 * y + key_of(2 * c + 1) >= left) sb[y] = 0u;
                     }
-                    sc[y] = fspad_e4m3_to_f16(sa | (sb << 8));
+                    sc[y] = fspad_e4m3_to_f16(sb[y] * 256u + sa[y]);
                 }
 #pragma unroll
                 for (int i2 = 0; i2 < 2; ++i2) {     // elements 16 g + 8 i2 ..
@@ -423,7 +429,7 @@ tree_attn_packed_kernel(const Args a)
                         for (int x = 0; x < NT; ++x) mma16(o[x][4 * i2 + j], v, p[x][0], p[x][1]);
                     }
                 }
-            }
+            });
             __syncwarp();                            // every lane has read the stage
             if (i + STAGES < n_kv) fill(i + STAGES);
         }
