@@ -127,11 +127,6 @@ def _stream(stream: Optional[torch.cuda.Stream]):
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
-def _shaped(name: str, t: Optional[torch.Tensor], *shape):
-    if t is not None and t.shape != shape:
-        raise ValueError("%s: expected shape %s, got %s" % (name, shape, tuple(t.shape)))
-
-
 class Context:
     """Owns an `fspad_ctx` on the current CUDA device."""
 
@@ -383,128 +378,49 @@ class Context:
         shape = (self.cfg.n_layers, 2, n_blocks, self.cfg.n_kv_heads, 128)
         return (torch.zeros(shape + (64,), dtype=torch.uint8, device=device), torch.zeros(shape + (8,), dtype=torch.uint8, device=device))
 
-    def _packed(self, codes, scales):
-        nb = codes.shape[2] if codes.dim() == 6 else 0
-        shape = (self.cfg.n_layers, 2, nb, self.cfg.n_kv_heads, 128)
-        _shaped("codes", codes, *shape, 64)
-        _shaped("scales", scales, *shape, 8)
-        return nb
+    # (These calls' arguments are looked at, and outputs that are not given made, by the native code.)
+    def _packed_call(self, name, stream, *args):
+        if stream is not None and stream.cuda_stream != _stream(None):
+            with torch.cuda.stream(stream):      # what is made for the call is the stream's own
+                return self._packed_call(name, None, *args)
+        c = self.cfg
+        r = getattr(_calls(), name)(self._h.value, c.n_q_heads, c.n_kv_heads, c.n_layers, c.max_nodes, _stream(stream), *args)
+        if type(r) is int:
+            raise FspadError(r, "fspad_" + name)
+        return r
 
     def rope_qkv(self, qkv, theta, sections=(64, 0, 0), parent=None, start=None, positions=None, adjacent=False, q=None, k=None, v=None,
                  stream=None):
         """Rows of the QKV product [B][N][(Hq + 2 Hkv) * 128] (bf16, device; rows may stand further apart) -> q [B][N][Hq][128] and k, v
         [B][Hkv][N][128], queries and keys turned by positions of up to three axes: `positions` [B][N][3], or of tree nodes `start`
         [B][3] plus the depth in `parent` [B][N].  `sections`: how many of the 64 pairs go by time, height and width."""
-        B, N, width = qkv.shape
-        hq, hkv = self.cfg.n_q_heads, self.cfg.n_kv_heads
-        if width != (hq + 2 * hkv) * 128:
-            raise ValueError("qkv: expected rows of %d elements, got %d" % ((hq + 2 * hkv) * 128, width))
-        rows, row, one = qkv.stride()
-        if N == 1:
-            row = rows if B > 1 else width
-        elif B > 1 and rows != N * row:
-            one = 0
-        if one != 1:
-            raise ValueError("qkv: rows must be contiguous and evenly spaced, got strides %s" % (qkv.stride(),))
-        _shaped("parent", parent, B, N)
-        _shaped("start", start, B, 3)
-        _shaped("positions", positions, B, N, 3)
-        _shaped("q", q, B, N, hq, 128)
-        _shaped("k", k, B, hkv, N, 128)
-        _shaped("v", v, B, hkv, N, 128)
-        bf, dev = torch.bfloat16, qkv.device
-        if q is None:
-            q = torch.empty((B, N, hq, 128), dtype=bf, device=dev)
-        if k is None:
-            k = torch.empty((B, hkv, N, 128), dtype=bf, device=dev)
-        if v is None:
-            v = torch.empty((B, hkv, N, 128), dtype=bf, device=dev)
-        rc = _calls().rope_qkv(self._h.value, qkv, row, positions, start, parent, N, B, theta, sections[0], sections[1], sections[2],
-                               int(adjacent), q, k, v, _stream(stream))
-        if rc != 0:
-            raise FspadError(rc, "fspad_rope_qkv")
-        return q, k, v
+        return self._packed_call("rope_qkv", stream, qkv, theta, *sections, parent, start, positions, adjacent, q, k, v)
 
-    def block_plan(self, length, add, block_table, held, free_blocks, n_free, max_rows, drop=None, out=None, stream=None):
+    def block_plan(self, length, add, block_table, held, free_blocks, n_free, max_rows, drop=None, out=(None, None, None, None), stream=None):
         """Blocks for add[b] rows behind the length[b] that sequence b holds; block_table [B][blocks], held [B], free_blocks [n_blocks] and
         n_free [1] (int32, device) are updated.  Returns (row_start [B + 1], slots [max_rows] int64, row_seq, row_pos [max_rows])."""
-        B, bps = block_table.shape
-        _shaped("length", length, B)
-        _shaped("add", add, B)
-        _shaped("drop", drop, B)
-        _shaped("held", held, B)
-        _shaped("n_free", n_free, 1)
-        if out is None:
-            dev, i32 = block_table.device, torch.int32
-            out = (torch.empty((B + 1,), dtype=i32, device=dev), torch.empty((max_rows,), dtype=torch.int64, device=dev),
-                   torch.empty((max_rows,), dtype=i32, device=dev), torch.empty((max_rows,), dtype=i32, device=dev))
-        row_start, slots, row_seq, row_pos = out
-        _shaped("row_start", row_start, B + 1)
-        _shaped("slots", slots, max_rows)
-        _shaped("row_seq", row_seq, max_rows)
-        _shaped("row_pos", row_pos, max_rows)
-        rc = _calls().block_plan(self._h.value, length, add, drop, B, bps, free_blocks.shape[0], block_table, held, free_blocks, n_free,
-                                 max_rows, row_start, slots, row_seq, row_pos, _stream(stream))
-        if rc != 0:
-            raise FspadError(rc, "fspad_block_plan")
-        return out
+        return self._packed_call("block_plan", stream, length, add, drop, block_table, held, free_blocks, n_free, max_rows, *out)
 
     def kv_write_packed(self, k, v, slots, codes, scales, layer=0, k_rounded=None, v_rounded=None, stream=None):
         """Rows k, v [Hkv][rows][128] (bf16, device; a leading axis of one is allowed) into the slots [rows] (int64; -1: left out) of a layer."""
-        hkv, (rows,) = self.cfg.n_kv_heads, slots.shape
-        nb = self._packed(codes, scales)
-        for name, t in (("k", k), ("v", v), ("k_rounded", k_rounded), ("v_rounded", v_rounded)):
-            if t is not None and t.shape != (hkv, rows, 128) and t.shape != (1, hkv, rows, 128):
-                raise ValueError("%s: expected shape %s, got %s" % (name, (hkv, rows, 128), tuple(t.shape)))
-        rc = _calls().kv_write_packed(self._h.value, k, v, slots, rows, layer, codes, scales, nb, k_rounded, v_rounded, _stream(stream))
-        if rc != 0:
-            raise FspadError(rc, "fspad_kv_write_packed")
+        self._packed_call("kv_write_packed", stream, k, v, slots, codes, scales, layer, k_rounded, v_rounded)
 
     def kv_append_packed(self, codes, scales, block_table, tree_kv, accepted_path, n_accepted, prefix_len, rounded=None, new_len=None,
                          stream=None):
         """tree_kv [layers][2][B][Hkv][N][128] (bf16): rows of the accepted path written behind the prefix of the 4-bit cache."""
-        (B, bps), N = block_table.shape, tree_kv.shape[4] if tree_kv.dim() == 6 else 0
-        shape = (self.cfg.n_layers, 2, B, self.cfg.n_kv_heads, N, 128)
-        nb = self._packed(codes, scales)
-        _shaped("tree_kv", tree_kv, *shape)
-        _shaped("rounded", rounded, *shape)
-        _shaped("accepted_path", accepted_path, B, self.cfg.max_nodes)
-        _shaped("n_accepted", n_accepted, B)
-        _shaped("prefix_len", prefix_len, B)
-        _shaped("new_len", new_len, B)
-        if new_len is None:
-            new_len = torch.empty((B,), dtype=torch.int32, device=codes.device)
-        rc = _calls().kv_append_packed(self._h.value, codes, scales, block_table, bps, nb, tree_kv, accepted_path, n_accepted, prefix_len,
-                                       N, B, rounded, new_len, _stream(stream))
-        if rc != 0:
-            raise FspadError(rc, "fspad_kv_append_packed")
-        return new_len
+        return self._packed_call("kv_append_packed", stream, codes, scales, block_table, tree_kv, accepted_path, n_accepted, prefix_len, rounded, new_len)
 
     def tree_attn_packed(self, q, codes, scales, block_table, tree_k, tree_v, parent, prefix_len, layer=0, out=None, workspace=None,
                          stream=None):
         """Tree-masked attention of q [B][N][Hq][128] over a layer of the 4-bit cache and the tree's bf16 rows [B][Hkv][N][128].  Without
         `workspace` (uint8) the context's own is used, which calls on one stream at a time may share."""
-        B, N = q.shape[0], q.shape[1]
-        hq, hkv = self.cfg.n_q_heads, self.cfg.n_kv_heads
-        nb = self._packed(codes, scales)
-        _shaped("q", q, B, N, hq, 128)
-        _shaped("tree_k", tree_k, B, hkv, N, 128)
-        _shaped("tree_v", tree_v, B, hkv, N, 128)
-        _shaped("parent", parent, B, N)
-        _shaped("prefix_len", prefix_len, B)
-        _shaped("out", out, B, N, hq, 128)
-        rows, bps = block_table.shape
-        if rows != B:
-            raise ValueError("block_table: expected %d sequences, got %d" % (B, rows))
-        if out is None:
-            out = torch.empty_like(q)
         if workspace is None:
-            workspace = self._workspace(N, B, q.device)
-        rc = _calls().tree_attn_packed(self._h.value, q, codes, scales, layer, block_table, bps, nb, tree_k, tree_v, parent, prefix_len,
-                                       N, B, out, workspace, workspace.numel(), _stream(stream))
-        if rc != 0:
-            raise FspadError(rc, "fspad_tree_attn_packed")
-        return out
+            if stream is not None:
+                with torch.cuda.stream(stream):
+                    workspace = self._workspace(q.shape[1], q.shape[0], q.device)
+            else:
+                workspace = self._workspace(q.shape[1], q.shape[0], q.device)
+        return self._packed_call("tree_attn_packed", stream, q, codes, scales, block_table, tree_k, tree_v, parent, prefix_len, layer, out, workspace)
 
     def tree_attn_packed_workspace_bytes(self, n_nodes: int, batch: int) -> int:
         return int(load().fspad_tree_attn_packed_workspace_bytes(self._h, n_nodes, batch))

@@ -1,6 +1,7 @@
 // C ABI of the operators around the cache held in 4 bits: argument validation.  (The calls of the verify step: api.cu.)
 #include <climits>
 #include <cmath>
+#include <cstring>
 
 #include "packed.cuh"
 
@@ -60,7 +61,11 @@ int fspad_rope_qkv(fspad_ctx *ctx, const fspad_bf16 *qkv, int64_t row_stride, co
     if ((int64_t)n_nodes * batch > INT_MAX || batch > 65535) return FSPAD_ERR_TOO_LARGE;
     if (batch == 0) return FSPAD_OK;
     FspadRopeTable t;
-    for (int i = 0; i < half; ++i) t.turns[i] = std::pow(theta, -2.0 * i / FSPAD_HEAD_DIM) / (2.0 * 3.14159265358979323846);
+    if (ctx->rope_theta != theta) {
+        for (int i = 0; i < half; ++i) ctx->rope_turns[i] = std::pow(theta, -2.0 * i / FSPAD_HEAD_DIM) / (2.0 * 3.14159265358979323846);
+        ctx->rope_theta = theta;
+    }
+    std::memcpy(t.turns, ctx->rope_turns, sizeof t.turns);
     t.split0 = sec_t;
     t.split1 = sec_t + sec_h;
     return result(fspad_launch_rope_qkv(ctx, qkv, row_stride, positions, start, parent, n_nodes, batch, t, adjacent != 0, q, k, v,

@@ -477,7 +477,7 @@ tree_attn_packed_kernel(const Args a)
 template <int NT> cudaError_t launch_few(fspad_ctx *ctx, Args &a, cudaStream_t st)
 {
     const int ctas = ctx->sm_count, smem = warps_of(NT) * stages_of(NT) * STAGE;
-    cudaError_t e = cudaFuncSetAttribute(tree_attn_packed_kernel<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    cudaError_t e = raise_shared(ctx, NT, reinterpret_cast<const void *>(&tree_attn_packed_kernel<NT>), smem);
     if (e != cudaSuccess) return e;
     const int entries = merge_entries(a, ctas * warps_of(NT));
     ctx->launches++;

@@ -639,7 +639,7 @@ cudaError_t fspad_launch_attn_packed_umma(fspad_ctx *ctx, packed::Args a, void *
     a.mtiles = (a.M + BM - 1) / BM;
     a.by_tiles.set((unsigned)a.mtiles);
     scratch_in<BM>(a, ctas, workspace);
-    cudaError_t e = cudaFuncSetAttribute(tree_attn_packed_umma_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+    cudaError_t e = raise_shared(ctx, 0, reinterpret_cast<const void *>(&tree_attn_packed_umma_kernel), SMEM);
     if (e != cudaSuccess) return e;
     const int entries = merge_entries(a, ctas);
     ctx->launches++;
