@@ -64,11 +64,11 @@ template <int UNIT> __device__ __forceinline__ int tree_units(const Args &a) { r
 template <int UNIT> __device__ __forceinline__ int run_units(const Args &a, int L) { return tree_units<UNIT>(a) + (int)(((long long)L + UNIT - 1) / UNIT); }
 template <int UNIT> constexpr int kStretch = UNIT == 128 ? 4 : 2;
 
-// How many parts the list may be cut into.  With chunks of 128 keys for 256 rows a part of a cut run leaves 128 KB, which cost about a thirtieth of what a chunk
-// takes to write and read again: of few chunks, then, fewer parts than SMs (5 sqrt(total)).
+// How many parts the list may be cut into.  With chunks of 128 keys for 256 rows a part of a cut run leaves 128 KB, which cost about a hundredth of what a chunk
+// takes to write and read again: of few chunks, then, fewer parts than SMs (12 sqrt(total); with 5 sqrt(total) 60 nodes over 2K keys took 25.2 us, not 20.4).
 template <int UNIT> __device__ __forceinline__ int parts_of(int total, int ctas)
 {
-    if (UNIT == 128 && total < (ctas * ctas) / 25) ctas = max(1, (int)sqrtf((float)(total * 25)));
+    if (UNIT == 128 && total < (ctas * ctas) / 150) ctas = max(1, (int)sqrtf((float)(total * 150)));
     return min(total, ctas);
 }
 

@@ -261,10 +261,13 @@ tree_attn_packed_umma_kernel(const Args a)
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(Q_FULL + t));
             };
-            // one row tile: group 0's as it is, group 1's as fp16; two: fp16, or first as they are for the tree
+            // one row tile: group 0's as it is, for the tree, group 1's as fp16; two: fp16, or first as they are for the tree
             fetch_q(grp);
-            scale_q(grp, s.two ? s.n_tree == 0 : grp == 1);
+            const bool raw = s.two ? s.n_tree > 0 : grp == 0;
+            if (!raw) scale_q(grp, true);
             tell_q(grp);
+            // (group 0's own chunks of the cache, if there are any, need the factors all the same)
+            if (raw && !s.two && s.n_ch > s.n_tree + (s.n_tree & 1)) scale_q(grp, false);
             if (s.n_tree > 0) {
                 for (int i = tid; i < a.N; i += 256) {
                     int p = a.parent[(size_t)s.b * a.N + i];
@@ -468,14 +471,19 @@ tree_attn_packed_umma_kernel(const Args a)
                 if (!failed && !mbar_wait(bar(Q_FULL + t), ph_q[t])) failed = true;
                 ph_q[t] ^= 1u;
             };
+            bool have_q[2] = {false, false};                 // of one row tile: its two forms
             // item i: group i & 1, chunk i / 2 or, of one row tile, i
             auto issue_s = [&](int i) {
                 const int g = i & 1, c = s.two ? i >> 1 : i;
                 const bool tree = c < s.n_tree;
                 if (s.two && c == s.n_tree && c > 0) wait_q(g);              // the tile again, as fp16
                 const uint32_t at = cc + (uint32_t)c, slot = at & 1u;
-                if ((!s.two || g == 0) && !failed && !mbar_wait(bar(K_FULL + slot), (at >> 1) & 1u)) failed = true;
                 const int t = s.two ? g : tree ? 0 : 1;
+                if (!s.two && !have_q[t]) {
+                    wait_q(t);
+                    have_q[t] = true;
+                }
+                if ((!s.two || g == 0) && !failed && !mbar_wait(bar(K_FULL + slot), (at >> 1) & 1u)) failed = true;
                 if (!failed && issuer) {
                     tc_fence_after();
                     const uint32_t kb = k_lo + slot * (TILE >> 4), qb = q_lo + (uint32_t)t * (TILE >> 4), d = tmem + 128u * g;
@@ -490,14 +498,18 @@ tree_attn_packed_umma_kernel(const Args a)
                 }
                 __syncwarp();
             };
-            wait_q(0);
-            if (!s.two) wait_q(1);
+            if (s.two) wait_q(0);
 #pragma unroll 1
             for (int i = -2; i < n_items; ++i) {
                 if (i >= 0) {
                     const int g = i & 1, c = s.two ? i >> 1 : i;
                     const bool tree = c < s.n_tree;
                     const uint32_t at = cc + (uint32_t)c, slot = at & 1u;
+                    // (a form that no chunk needs is written all the same; its phase is over before the stretch can be)
+                    if (!s.two && i == n_items - 1) {
+                        if (!have_q[0]) wait_q(0);
+                        if (!have_q[1]) wait_q(1);
+                    }
                     if ((!s.two || g == 0) && !failed && !mbar_wait(bar(V_FULL + slot), (at >> 1) & 1u)) failed = true;
                     if (!failed && !mbar_wait(bar(P_FULL + g), n_p[g] & 1u)) failed = true;
                     if (!failed && issuer) {
