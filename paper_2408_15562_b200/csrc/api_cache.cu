@@ -142,6 +142,7 @@ int fspad_tree_attn_packed(fspad_ctx *ctx, const fspad_bf16 *q, const uint8_t *c
     if ((rc = check_blocks(blocks_per_seq, n_blocks)) != 0) return rc;
     if (batch == 0) return FSPAD_OK;
     if (workspace_bytes < fspad_attn_packed_workspace(ctx, n_nodes, batch)) return FSPAD_ERR_RANGE;
+    if (!fspad_attn_packed_fits(ctx, n_nodes, batch, blocks_per_seq)) return FSPAD_ERR_TOO_LARGE;
     const size_t rows = (size_t)n_blocks * ctx->cfg.n_kv_heads * 128, first = (size_t)layer * 2 * rows;
     const uint8_t *kc = codes + first * FSPAD_PACKED_CODE_BYTES, *ks = scales + first * FSPAD_PACKED_SCALE_BYTES;
     const FspadPaged pg{block_table, blocks_per_seq, n_blocks};

@@ -34,6 +34,7 @@ cudaError_t fspad_launch_kv_append_packed(fspad_ctx *ctx, uint8_t *codes, uint8_
                                           const int *path, const int *n_acc, const int *prefix_len, int N, int B,
                                           fspad_bf16 *rounded, int *new_len, cudaStream_t st);
 size_t fspad_attn_packed_workspace(const fspad_ctx *ctx, int N, int B);
+bool fspad_attn_packed_fits(const fspad_ctx *ctx, int N, int B, int bps);
 cudaError_t fspad_launch_tree_attn_packed(fspad_ctx *ctx, const fspad_bf16 *q, const uint8_t *k_codes, const uint8_t *k_scales,
                                           const uint8_t *v_codes, const uint8_t *v_scales, FspadPaged paged, const fspad_bf16 *tk,
                                           const fspad_bf16 *tv, const int *parent, const int *prefix_len, int N, int B,

@@ -89,11 +89,11 @@ struct Part {
 };
 
 // All T threads of the CTA call it, and there is a CTA barrier in it; scratch holds T / 32 + 2 W values.  W: how many parts a CTA takes: one, which all its
-// threads ask for, or one for each of its W = T / 32 warps (part0: the CTA's first, of `slots` that there may be).
+// threads ask for, or one for each of its W = T / 32 warps: part0 + w * gridDim.x, so that few parts are on as many SMs.  slots: how many there may be.
 template <int T, int UNIT, int W>
 __device__ __forceinline__ Part cut_list(const Args &a, int part0, int slots, Parts &p, int *scratch, bool report)
 {
-    const int part = part0 + (W > 1 ? (int)(threadIdx.x >> 5) : 0), ctas = slots;
+    const int part = part0 + (W > 1 ? (int)(threadIdx.x >> 5) * (int)gridDim.x : 0), ctas = slots;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, runs = a.Hkv * a.mtiles;
     Part s = {0, 0, 0, 0, 0, 0, false};
     if (a.B <= 32) {                     // every warp for itself
@@ -183,7 +183,7 @@ __device__ __forceinline__ Part cut_list(const Args &a, int part0, int slots, Pa
     int x = inc - mine;
 #pragma unroll 1
     for (int w = 0; w < W; ++w) {
-        const int want = part0 + w < p.n ? p.start(part0 + w) : total;
+        const int its = part0 + w * (int)gridDim.x, want = its < p.n ? p.start(its) : total;
         if (x <= want && want < inc) {
             int b = b0, y = x;
 #pragma unroll 1
@@ -198,7 +198,7 @@ __device__ __forceinline__ Part cut_list(const Args &a, int part0, int slots, Pa
     }
     __syncthreads();
     if (part < p.n) {
-        const int at = T / 32 + 2 * (part - part0);
+        const int at = T / 32 + (W > 1 ? 2 * warp : 0);
         s.b = scratch[at];
         const int nb = run_units<UNIT>(a, prefix_of(a, s.b, false));
         s.run = scratch[at + 1] / nb;
@@ -260,7 +260,7 @@ __device__ __forceinline__ void tell_run(const Args &a, const Parts &p, const Pa
 // The pieces of the runs that were cut, merged.  A CTA takes `rows` rows (a power of two, at most WARPS) of a run at a time, each by WARPS / rows warps that take its
 // pieces in turn, four elements a lane.
 template <int BM, int WARPS>
-__global__ void __launch_bounds__(WARPS * 32)
+__global__ void __launch_bounds__(WARPS * 32, WARPS > 8 ? 1 : 3)
 tree_attn_packed_merge_kernel(const Args a, int rows)
 {
     __shared__ float4 s_acc[WARPS][32];
@@ -356,20 +356,23 @@ static inline cudaError_t raise_shared(fspad_ctx *ctx, int bit, const void *kern
     return e;
 }
 
-// Parts there can be -> how the runs that were cut are told of; and the merge's launch: entries x groups of so many rows, so that there are a few CTAs for every SM.
+// Parts there can be -> how the runs that were cut are told of; and the merge's launch: entries x groups of so many rows, so that they are all there at once (three CTAs an SM).
 static inline int merge_entries(Args &a, int parts)
 {
     const long long runs = (long long)a.B * a.Hkv * a.mtiles;
     a.entry_runs = runs <= parts ? 1 : 0;
     return a.entry_runs ? (int)runs : parts;
 }
-template <int BM, int WARPS> static inline cudaError_t launch_merge(fspad_ctx *ctx, const Args &a, int entries, cudaStream_t st)
+template <int BM> static inline cudaError_t launch_merge(fspad_ctx *ctx, const Args &a, int entries, cudaStream_t st)
 {
     const int m = a.M < BM ? a.M : BM;
-    int rows = 1;
-    while (rows < WARPS && rows < m && (long long)entries * ((m + rows - 1) / rows) > 4 * ctx->sm_count) rows *= 2;
     ctx->launches++;
-    return fspad_launch(tree_attn_packed_merge_kernel<BM, WARPS>, dim3((unsigned)entries, (unsigned)((m + rows - 1) / rows)), dim3(WARPS * 32), 0, st, 0, a, rows);
+    // a row a CTA, with twice the warps, where that is no more than a CTA an SM (long runs in many pieces: 21.6 us against 24.9 on one token over 32K keys)
+    if ((long long)entries * m <= ctx->sm_count)
+        return fspad_launch(tree_attn_packed_merge_kernel<BM, 16>, dim3((unsigned)entries, (unsigned)m), dim3(512), 0, st, 0, a, 1);
+    int rows = 1;
+    while (rows < 8 && rows < m && (long long)entries * ((m + rows - 1) / rows) > 3 * ctx->sm_count) rows *= 2;
+    return fspad_launch(tree_attn_packed_merge_kernel<BM, 8>, dim3((unsigned)entries, (unsigned)((m + rows - 1) / rows)), dim3(256), 0, st, 0, a, rows);
 }
 
 // Whether the units of a call, at most, can be counted in 32 bits (and 25 times as many as are cut into fewer parts than there are CTAs).

@@ -115,9 +115,9 @@ tree_attn_packed_kernel(const Args a)
     fspad_pdl_trigger();
     fspad_pdl_wait();
 
-    const int slot0 = blockIdx.x * WARPS + warp;
+    const int slot0 = warp * gridDim.x + blockIdx.x;
     Parts parts;
-    Part part = cut_list<WARPS * 32, UNIT, WARPS>(a, blockIdx.x * WARPS, gridDim.x * WARPS, parts, s_scan, blockIdx.x == 0);
+    Part part = cut_list<WARPS * 32, UNIT, WARPS>(a, blockIdx.x, gridDim.x * WARPS, parts, s_scan, blockIdx.x == 0);
     if (lane == 0) tell_part<UNIT>(a, parts, part, slot0);
     const int nt = tree_units<UNIT>(a), runs = a.Hkv * a.mtiles;
     // what lanes 0 .. 3 copy of a unit: from which array, of how many bytes a row, to where in the stage
@@ -482,19 +482,37 @@ template <int NT> cudaError_t launch_few(fspad_ctx *ctx, Args &a, cudaStream_t s
     const int entries = merge_entries(a, ctas * warps_of(NT));
     ctx->launches++;
     e = fspad_launch(tree_attn_packed_kernel<NT>, dim3((unsigned)ctas), dim3(warps_of(NT) * 32), smem, st, 0, a);
-    return e == cudaSuccess ? launch_merge<BM, 16>(ctx, a, entries, st) : e;
+    return e == cudaSuccess ? launch_merge<BM>(ctx, a, entries, st) : e;
 }
 
 }  // namespace
 
-// Which of the two kernels takes a call, by the query rows of a kv head.
-static bool many_rows(const fspad_ctx *ctx, int N) { return (long long)N * (ctx->cfg.n_q_heads / ctx->cfg.n_kv_heads) > BM; }
+// Which of the two kernels takes a call.  Up to 16 query rows a kv head this one does; up to 32, in two tiles, each of which takes the cache's codes apart for itself,
+// where the list is short, by what the table has room for (lengths are not known here).  us, this kernel and the other, 8 kv heads: 24 rows, one sequence 10 - 14
+// and 13 - 17 (32 to 4000 keys), four 11 - 24 and 14 - 27, sixteen of 700 keys (5900 units) 20 and 21, of 1500 30 and 29; 48 rows, sixteen of 300 keys 22 and 17;
+// 100 rows, one of 700 keys 19 and 16; 12 rows, sixteen of 32 to 1500 keys 12 - 22 and 13 - 29.
+static bool many_rows(const fspad_ctx *ctx, int N, int B, int bps)
+{
+    const fspad_config &c = ctx->cfg;
+    const long long M = (long long)N * (c.n_q_heads / c.n_kv_heads), units = 2ll * B * c.n_kv_heads * ((N + UNIT - 1) / UNIT + 4ll * bps);
+    return M > 32 || (M > 16 && units > 6000);
+}
 
 size_t fspad_attn_packed_workspace(const fspad_ctx *ctx, int N, int B)
 {
-    (void)B;
-    if (many_rows(ctx, N)) return fspad_attn_packed_umma_workspace(ctx);
-    return scratch_bytes<BM>(ctx->sm_count * MAX_WARPS);
+    // of either kernel: the choice depends on the table's width, too
+    (void)N; (void)B;
+    const size_t few = scratch_bytes<BM>(ctx->sm_count * MAX_WARPS), many = fspad_attn_packed_umma_workspace(ctx);
+    return few > many ? few : many;
+}
+
+// Whether a call's list can be counted in 32 bits.
+bool fspad_attn_packed_fits(const fspad_ctx *ctx, int N, int B, int bps)
+{
+    const fspad_config &c = ctx->cfg;
+    Args a;
+    a.N = N; a.B = B; a.Hkv = c.n_kv_heads; a.M = N * (c.n_q_heads / c.n_kv_heads); a.mtiles = (a.M + BM - 1) / BM; a.table_stride = bps;
+    return units_fit<UNIT>(a);
 }
 
 cudaError_t fspad_launch_tree_attn_packed(fspad_ctx *ctx, const fspad_bf16 *q, const uint8_t *k_codes, const uint8_t *k_scales,
@@ -512,7 +530,7 @@ cudaError_t fspad_launch_tree_attn_packed(fspad_ctx *ctx, const fspad_bf16 *q, c
     a.by_G.set((unsigned)a.G); a.by_tiles.set((unsigned)a.mtiles);
     a.scale_log2 = ctx->scale * kLog2e;
     a.out = out; a.status = ctx->d_status;
-    if (many_rows(ctx, N)) return fspad_launch_attn_packed_umma(ctx, a, workspace, st);
+    if (many_rows(ctx, N, B, paged.stride)) return fspad_launch_attn_packed_umma(ctx, a, workspace, st);
     scratch_in<BM>(a, ctx->sm_count * MAX_WARPS, workspace);
     return a.M <= 8 ? launch_few<1>(ctx, a, st) : launch_few<2>(ctx, a, st);
 }
