@@ -449,7 +449,7 @@ int fspad_device(const fspad_ctx *ctx);
  *   start [batch][3] int32 and parent [batch][n_nodes] int32, with positions NULL: node i of tree b stands at start[b][a] + depth(i) on axis a
  *   q         [batch][n_nodes][Hq][128], k and v [batch][Hkv][n_nodes][128]: what fspad_tree_attn* and the cache calls take
  * The outputs must not overlap qkv or one another.  Errors: FSPAD_ERR_NULL also where neither or both kinds of positions are given; FSPAD_ERR_SHAPE for sections
- * that do not sum to 64 and strides outside these rules; FSPAD_ERR_RANGE for a theta that is not finite and positive; FSPAD_ERR_TOO_LARGE
+ * that do not sum to 64 and strides outside these rules; FSPAD_ERR_RANGE for a theta that is not finite and positive, or so small that its powers are not finite; FSPAD_ERR_TOO_LARGE
  * for more than 65535 sequences or 2^31 - 1 rows; a malformed parent[] sets FSPAD_ERR_BAD_TREE in the status word.
  */
 int fspad_rope_qkv(fspad_ctx *ctx, const fspad_bf16 *qkv, int64_t row_stride, const int32_t *positions, const int32_t *start,

@@ -57,7 +57,7 @@ int fspad_rope_qkv(fspad_ctx *ctx, const fspad_bf16 *qkv, int64_t row_stride, co
     const int64_t width = ((int64_t)c.n_q_heads + 2 * (int64_t)c.n_kv_heads) * FSPAD_HEAD_DIM;
     if (sec_t < 0 || sec_h < 0 || sec_w < 0 || sec_t > half || sec_h > half || sec_w > half || sec_t + sec_h + sec_w != half) return FSPAD_ERR_SHAPE;
     if (row_stride < width || row_stride % 8 != 0) return FSPAD_ERR_SHAPE;
-    if (!(theta > 0.0) || std::isinf(theta)) return FSPAD_ERR_RANGE;
+    if (!(theta > 0.0) || std::isinf(theta) || std::isinf(std::pow(theta, -2.0 * (half - 1) / FSPAD_HEAD_DIM))) return FSPAD_ERR_RANGE;
     if ((int64_t)n_nodes * batch > INT_MAX || batch > 65535) return FSPAD_ERR_TOO_LARGE;
     if (batch == 0) return FSPAD_OK;
     FspadRopeTable t;
@@ -81,8 +81,7 @@ int fspad_block_plan(fspad_ctx *ctx, const int32_t *len, const int32_t *add, con
     if (!len || !add || !block_table || !held || !free_blocks || !n_free || !row_start || !slots) return FSPAD_ERR_NULL;
     if (batch < 0 || batch > ctx->cfg.max_batch || max_rows < 0) return FSPAD_ERR_SHAPE;
     if ((rc = check_blocks(blocks_per_seq, n_blocks)) != 0) return rc;
-    if (batch > FSPAD_PLAN_MAX_BATCH) return FSPAD_ERR_TOO_LARGE;
-    if (batch == 0) return FSPAD_OK;
+    if (batch > FSPAD_PLAN_MAX_BATCH) return FSPAD_ERR_TOO_LARGE;      // (no sequences: row_start[0] and the slots are written all the same)
     static_assert(sizeof(long long) == sizeof(int64_t), "slots");
     return result(fspad_launch_block_plan(ctx, len, add, drop, batch, blocks_per_seq, n_blocks, block_table, held, free_blocks, n_free,
                                           max_rows, row_start, reinterpret_cast<long long *>(slots), row_seq, row_pos, fspad_stream(stream)));

@@ -134,6 +134,11 @@ FSPAD_CALL(verify_step_host, 2)
 
 // ---- the calls around the 4-bit cache: they know the context's sizes, look at every tensor's shape and device, and make the outputs that are
 // not given (in Python that took longer than the launches: a single-token step 11.1 -> 8 us, rotary rows of a tree 13.8 -> 6.5) ----
+// A tensor's address; an empty one has none, and nothing is read or written there: it gets one that is aligned.
+alignas(16) char kNothing[16];
+void *address(const at::Tensor &t) { return t.numel() ? t.data_ptr() : kNothing; }
+template <typename T> T *as(const at::Tensor &t) { return static_cast<T *>(address(t)); }
+
 struct Call {
     fspad_ctx *ctx;
     int device;
@@ -192,7 +197,7 @@ struct Call {
     {
         if (!ok || (optional && o == Py_None)) return nullptr;
         const at::Tensor *t = tensor(name, o, type);
-        return t && shaped(name, t, want) ? t->data_ptr() : nullptr;
+        return t && shaped(name, t, want) ? address(*t) : nullptr;
     }
     // An output: the tensor that was given, or a new one.
     at::Tensor out(const char *name, PyObject *o, at::ScalarType type, std::initializer_list<long long> want)
@@ -218,7 +223,6 @@ struct Call {
         return (int)nb;
     }
 };
-template <typename T> T *as(const at::Tensor &t) { return static_cast<T *>(t.data_ptr()); }
 
 // (handle, Hq, Hkv, layers, max_nodes, stream) come first.  `body` gives the arguments' checks and the call: its status, and what it returns.
 template <typename F> PyObject *packed_call(PyObject *const *args, Py_ssize_t n, Py_ssize_t want, F body)
@@ -287,7 +291,7 @@ PyObject *call_rope_qkv(PyObject *, PyObject *const *args, Py_ssize_t n)
         const int adjacent = c.ok ? PyObject_IsTrue(a[8]) : 0;
         const at::Tensor q = c.out("q", a[9], kBf, {B, N, c.hq, 128}), k = c.out("k", a[10], kBf, {B, c.hkv, N, 128}), v = c.out("v", a[11], kBf, {B, c.hkv, N, 128});
         if (!c.ok) return nullptr;
-        const auto *x = static_cast<const fspad_bf16 *>(qkv->data_ptr());
+        const auto *x = as<fspad_bf16>(*qkv);
         rc = unlocked([&] { return fspad_rope_qkv(c.ctx, x, row, positions, start, parent, (int)N, (int)B, theta, st, sh, sw, adjacent, as<fspad_bf16>(q), as<fspad_bf16>(k), as<fspad_bf16>(v), c.stream); });
         return rc ? nullptr : Py_BuildValue("(NNN)", THPVariable_Wrap(q), THPVariable_Wrap(k), THPVariable_Wrap(v));
     });
@@ -311,11 +315,8 @@ PyObject *call_block_plan(PyObject *, PyObject *const *args, Py_ssize_t n)
         const at::Tensor row_start = c.out("row_start", a[8], kI32, {B + 1}), slots = c.out("slots", a[9], at::kLong, {max_rows}),
                          row_seq = c.out("row_seq", a[10], kI32, {max_rows}), row_pos = c.out("row_pos", a[11], kI32, {max_rows});
         if (!c.ok) return nullptr;
-        // (an empty tensor has no address, and nothing is written to it)
-        int32_t none;
-        auto *to = max_rows > 0 ? as<int64_t>(slots) : reinterpret_cast<int64_t *>(&none);
         rc = unlocked([&] { return fspad_block_plan(c.ctx, len, add, drop, (int)B, (int)bps, (int)nb, as<int32_t>(*table), held, as<int32_t>(*free_blocks), n_free, max_rows, as<int32_t>(row_start),
-                                                     to, as<int32_t>(row_seq), as<int32_t>(row_pos), c.stream); });
+                                                     as<int64_t>(slots), as<int32_t>(row_seq), as<int32_t>(row_pos), c.stream); });
         return rc ? nullptr : Py_BuildValue("(NNNN)", THPVariable_Wrap(row_start), THPVariable_Wrap(slots), THPVariable_Wrap(row_seq), THPVariable_Wrap(row_pos));
     });
 }
@@ -342,7 +343,6 @@ PyObject *call_kv_write_packed(PyObject *, PyObject *const *args, Py_ssize_t n)
         const auto *k = rows_of("k", a[0], false), *v = rows_of("v", a[1], false);
         auto *kr = rows_of("k_rounded", a[6], true), *vr = rows_of("v_rounded", a[7], true);
         if (!c.ok) return nullptr;
-        if (rows == 0) Py_RETURN_NONE;
         rc = unlocked([&] { return fspad_kv_write_packed(c.ctx, k, v, as<int64_t>(*slots), (int)rows, layer, codes, scales, nb, kr, vr, c.stream); });
         if (rc) return nullptr;
         Py_RETURN_NONE;
@@ -402,7 +402,7 @@ PyObject *call_tree_attn_packed(PyObject *, PyObject *const *args, Py_ssize_t n)
         const at::Tensor out = c.out("out", a[9], kBf, {B, N, c.hq, 128});
         const at::Tensor *ws = c.tensor("workspace", a[10], at::kByte);
         if (!c.ok) return nullptr;
-        rc = unlocked([&] { return fspad_tree_attn_packed(c.ctx, as<fspad_bf16>(*q), codes, scales, layer, table, bps, nb, tk, tv, parent, len, (int)N, (int)B, as<fspad_bf16>(out), ws->data_ptr(),
+        rc = unlocked([&] { return fspad_tree_attn_packed(c.ctx, as<fspad_bf16>(*q), codes, scales, layer, table, bps, nb, tk, tv, parent, len, (int)N, (int)B, as<fspad_bf16>(out), address(*ws),
                                                            (size_t)ws->numel(), c.stream); });
         return rc ? nullptr : THPVariable_Wrap(out);
     });

@@ -280,3 +280,53 @@ def test_append_leaves_out_what_does_not_fit(what):
     assert changed[0, 100:103].any() and not changed[0, :100].any() and not changed[1].any()
     left = {tuple(i) for i in np.argwhere(changed[2:])}
     assert left <= ({(0, 127), (1, 1)} if what == "node" else set())
+
+
+def test_calls_with_nothing_to_do():
+    ctx = binding.Context(8, 2, 16, 512, n_layers=2, max_batch=4)
+    codes, scales = ctx.new_packed_cache(3)
+    i32, bf = dict(dtype=torch.int32, device="cuda"), dict(dtype=torch.bfloat16, device="cuda")
+    none = torch.empty((0, 5, 3), **i32)
+    q, k, v = ctx.rope_qkv(torch.empty((0, 5, 12 * 128), **bf), 1e4, positions=none)
+    assert q.shape == (0, 5, 8, 128) and k.shape == v.shape == (0, 2, 5, 128)
+    ctx.kv_write_packed(torch.empty((2, 0, 128), **bf), torch.empty((2, 0, 128), **bf), torch.empty((0,), dtype=torch.int64, device="cuda"), codes, scales)
+    new = ctx.kv_append_packed(codes, scales, torch.empty((0, 2), **i32), torch.empty((2, 2, 0, 2, 4, 128), **bf), torch.empty((0, 16), **i32),
+                               torch.empty((0,), **i32), torch.empty((0,), **i32))
+    assert new.shape == (0,)
+    out = ctx.tree_attn_packed(torch.empty((0, 4, 8, 128), **bf), codes, scales, torch.empty((0, 2), **i32), torch.empty((0, 2, 4, 128), **bf),
+                               torch.empty((0, 2, 4, 128), **bf), torch.empty((0, 4), **i32), torch.empty((0,), **i32))
+    assert out.shape == (0, 4, 8, 128)
+    free, n_free = torch.arange(3, **i32), torch.tensor([3], **i32)
+    row_start, slots, seq, pos = ctx.block_plan(torch.empty((0,), **i32), torch.empty((0,), **i32), torch.empty((0, 2), **i32), torch.empty((0,), **i32), free, n_free, 5)
+    assert row_start.tolist() == [0] and slots.tolist() == seq.tolist() == pos.tolist() == [-1] * 5 and n_free.item() == 3
+    table, held = torch.zeros((2, 2), **i32), torch.zeros((2,), **i32)
+    row_start, slots, seq, pos = ctx.block_plan(torch.tensor([128, 0], **i32), torch.zeros((2,), **i32), table, held, free, n_free, 0)
+    assert row_start.tolist() == [0, 0, 0] and slots.numel() == 0 and held.tolist() == [1, 0] and table.tolist() == [[2, 0], [0, 0]] and n_free.item() == 2
+    ctx.check()
+    assert not codes.any() and not scales.any()
+
+
+def test_refused_arguments_leave_the_context_usable():
+    ctx = binding.Context(8, 2, 16, 512, n_layers=2, max_batch=4)
+    codes, scales = ctx.new_packed_cache(3)
+    i32, bf = dict(dtype=torch.int32, device="cuda"), dict(dtype=torch.bfloat16, device="cuda")
+    qkv, start, parent = torch.zeros((1, 4, 12 * 128), **bf), torch.zeros((1, 3), **i32), torch.arange(-1, 3, **i32)[None].contiguous()
+    k, slots = torch.zeros((2, 5, 128), **bf), torch.arange(5, device="cuda")
+    for kind, call in [
+            (binding.FspadError, lambda: ctx.rope_qkv(qkv, 0.0, start=start, parent=parent)),
+            (binding.FspadError, lambda: ctx.rope_qkv(qkv, 1e4, (64, 1, 0), start=start, parent=parent)),
+            (binding.FspadError, lambda: ctx.rope_qkv(qkv, 1e4, start=start)),
+            (ValueError, lambda: ctx.rope_qkv(qkv[:, :, :-128], 1e4, start=start, parent=parent)),
+            (ValueError, lambda: ctx.rope_qkv(qkv, 1e4, start=start.cpu(), parent=parent)),
+            (TypeError, lambda: ctx.rope_qkv(qkv, 1e4, start=start.long(), parent=parent)),
+            (ValueError, lambda: ctx.rope_qkv(qkv, 1e4, start=start, parent=parent, q=torch.zeros((1, 4, 8, 64), **bf))),
+            (binding.FspadError, lambda: ctx.kv_write_packed(k, k, slots, codes, scales, layer=2)),
+            (binding.FspadError, lambda: ctx.kv_write_packed(k, k, slots, codes, scales, k_rounded=k)),
+            (ValueError, lambda: ctx.kv_write_packed(k, k[:, :4], slots, codes, scales)),
+            (ValueError, lambda: ctx.kv_write_packed(k, k, slots, codes, scales[:, :, :2])),
+            (ValueError, lambda: ctx.kv_write_packed(k.transpose(0, 1), k, slots, codes, scales))]:
+        with pytest.raises(kind):
+            call()
+    assert not codes.any() and not scales.any()
+    ctx.kv_write_packed(k, k, slots, codes, scales, layer=1)
+    ctx.check()
