@@ -290,7 +290,7 @@ def test_calls_with_nothing_to_do():
     q, k, v = ctx.rope_qkv(torch.empty((0, 5, 12 * 128), **bf), 1e4, positions=none)
     assert q.shape == (0, 5, 8, 128) and k.shape == v.shape == (0, 2, 5, 128)
     ctx.kv_write_packed(torch.empty((2, 0, 128), **bf), torch.empty((2, 0, 128), **bf), torch.empty((0,), dtype=torch.int64, device="cuda"), codes, scales)
-    new = ctx.kv_append_packed(codes, scales, torch.empty((0, 2), **i32), torch.empty((2, 2, 0, 2, 4, 128), **bf), torch.empty((0, 16), **i32),
+    new = ctx.kv_append_packed(codes, scales, torch.empty((0, 2), **i32), torch.empty((2, 2, 0, 2, 4, 128), **bf), torch.empty((0, 64), **i32),
                                torch.empty((0,), **i32), torch.empty((0,), **i32))
     assert new.shape == (0,)
     out = ctx.tree_attn_packed(torch.empty((0, 4, 8, 128), **bf), codes, scales, torch.empty((0, 2), **i32), torch.empty((0, 2, 4, 128), **bf),
