@@ -137,8 +137,8 @@ class Context:
         self.cfg = FspadConfig(n_q_heads, n_kv_heads, head_dim, max_nodes, vocab, n_layers, max_len,
                                max_batch, softmax_scale)
         self._h = ctypes.c_void_p()
-        self._workspaces = []       # of the attention over the 4-bit cache; an outgrown one stays, a captured graph may hold its address
-        self._workspace_sizes = {}
+        self._workspace = None      # of the attention over the 4-bit cache
+        self._sizes = (n_q_heads, n_kv_heads, n_layers, max_nodes)
         rc = load().fspad_create(ctypes.byref(self.cfg), ctypes.byref(self._h))
         if rc != 0:
             raise FspadError(rc, "fspad_create")
@@ -383,8 +383,7 @@ class Context:
         if stream is not None and stream.cuda_stream != _stream(None):
             with torch.cuda.stream(stream):      # what is made for the call is the stream's own
                 return self._packed_call(name, None, *args)
-        c = self.cfg
-        r = getattr(_calls(), name)(self._h.value, c.n_q_heads, c.n_kv_heads, c.n_layers, c.max_nodes, _stream(stream), *args)
+        r = getattr(_native or _calls(), name)(self._h.value, *self._sizes, _stream(None), *args)
         if type(r) is int:
             raise FspadError(r, "fspad_" + name)
         return r
@@ -415,23 +414,18 @@ class Context:
         """Tree-masked attention of q [B][N][Hq][128] over a layer of the 4-bit cache and the tree's bf16 rows [B][Hkv][N][128].  Without
         `workspace` (uint8) the context's own is used, which calls on one stream at a time may share."""
         if workspace is None:
-            if stream is not None:
-                with torch.cuda.stream(stream):
-                    workspace = self._workspace(q.shape[1], q.shape[0], q.device)
-            else:
-                workspace = self._workspace(q.shape[1], q.shape[0], q.device)
+            workspace = self._workspace
+            if workspace is None:
+                workspace = self._workspace = self._make_workspace(q.device, stream)
         return self._packed_call("tree_attn_packed", stream, q, codes, scales, block_table, tree_k, tree_v, parent, prefix_len, layer, out, workspace)
 
     def tree_attn_packed_workspace_bytes(self, n_nodes: int, batch: int) -> int:
         return int(load().fspad_tree_attn_packed_workspace_bytes(self._h, n_nodes, batch))
 
-    def _workspace(self, n_nodes, batch, device):
-        need = self._workspace_sizes.get((n_nodes, batch))
-        if need is None:
-            need = self._workspace_sizes[n_nodes, batch] = self.tree_attn_packed_workspace_bytes(n_nodes, batch)
-        if not self._workspaces or self._workspaces[-1].numel() < need:
-            self._workspaces.append(torch.empty((max(need, 16),), dtype=torch.uint8, device=device))
-        return self._workspaces[-1]
+    def _make_workspace(self, device, stream):
+        """Of the largest call; it lives as long as the context, so that a captured call's stays where it is."""
+        with torch.cuda.stream(stream):          # (None: the current one)
+            return torch.empty((max(self.tree_attn_packed_workspace_bytes(self.cfg.max_nodes, self.cfg.max_batch), 16),), dtype=torch.uint8, device=device)
 
 
 def accept_stats_noalloc(logits, temperature, rows_per_seq, out, stream=None) -> int:

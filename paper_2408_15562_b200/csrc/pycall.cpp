@@ -139,6 +139,19 @@ alignas(16) char kNothing[16];
 void *address(const at::Tensor &t) { return t.numel() ? t.data_ptr() : kNothing; }
 template <typename T> T *as(const at::Tensor &t) { return static_cast<T *>(address(t)); }
 
+struct Output {
+    const char *name;
+    PyObject *given;
+    at::ScalarType type;
+    std::initializer_list<long long> size;
+    size_t bytes() const                                     // in whole steps of 256, so that each starts as an allocation does
+    {
+        size_t n = c10::elementSize(type);
+        for (long long x : size) n *= (size_t)x;
+        return n == 0 ? 256 : (n + 255) / 256 * 256;
+    }
+};
+
 struct Call {
     fspad_ctx *ctx;
     int device;
@@ -199,17 +212,37 @@ struct Call {
         const at::Tensor *t = tensor(name, o, type);
         return t && shaped(name, t, want) ? address(*t) : nullptr;
     }
-    // An output: the tensor that was given, or a new one.
-    at::Tensor out(const char *name, PyObject *o, at::ScalarType type, std::initializer_list<long long> want)
+    // Outputs: the tensors that were given; the others are new and share one allocation of the current stream's (on the current device, which
+    // the library then checks).  An allocation for each took 0.9 us of a call's 8.
+    void outputs(at::Tensor *to, std::initializer_list<Output> wanted)
     {
-        if (!ok) return at::Tensor();
-        if (o != Py_None) {
-            const at::Tensor *t = tensor(name, o, type);
-            return t && shaped(name, t, want) ? *t : at::Tensor();
+        size_t bytes = 0;
+        at::Tensor *t = to;
+        for (const Output &w : wanted) {
+            if (!ok) return;
+            if (w.given != Py_None) {
+                const at::Tensor *x = tensor(w.name, w.given, w.type);
+                if (x && shaped(w.name, x, w.size)) *t = *x;
+            } else {
+                bytes += w.bytes();
+            }
+            ++t;
         }
-        int64_t size[8];
-        std::copy(want.begin(), want.end(), size);
-        return at::empty(at::IntArrayRef(size, want.size()), at::TensorOptions().dtype(type).device(at::kCUDA, (c10::DeviceIndex)device));
+        if (!ok || bytes == 0) return;
+        auto storage = c10::make_intrusive<c10::StorageImpl>(c10::StorageImpl::use_byte_size_t(), bytes, c10::GetAllocator(c10::kCUDA), true);
+        size_t at = 0;
+        t = to;
+        for (const Output &w : wanted) {
+            if (w.given == Py_None) {
+                int64_t size[8];
+                std::copy(w.size.begin(), w.size.end(), size);
+                *t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(storage), c10::DispatchKeySet(c10::DispatchKey::CUDA), caffe2::TypeMeta::fromScalarType(w.type));
+                t->unsafeGetTensorImpl()->set_sizes_contiguous(at::IntArrayRef(size, w.size.size()));
+                t->unsafeGetTensorImpl()->set_storage_offset((int64_t)(at / c10::elementSize(w.type)));
+                at += w.bytes();
+            }
+            ++t;
+        }
     }
     // Codes and scales of the cache: its blocks.
     int cache(PyObject *codes, PyObject *scales, uint8_t **c, uint8_t **s)
@@ -289,11 +322,12 @@ PyObject *call_rope_qkv(PyObject *, PyObject *const *args, Py_ssize_t n)
         const auto *start = static_cast<const int32_t *>(c.data("start", a[6], kI32, {B, 3}, true));
         const auto *positions = static_cast<const int32_t *>(c.data("positions", a[7], kI32, {B, N, 3}, true));
         const int adjacent = c.ok ? PyObject_IsTrue(a[8]) : 0;
-        const at::Tensor q = c.out("q", a[9], kBf, {B, N, c.hq, 128}), k = c.out("k", a[10], kBf, {B, c.hkv, N, 128}), v = c.out("v", a[11], kBf, {B, c.hkv, N, 128});
+        at::Tensor o[3];
+        c.outputs(o, {{"q", a[9], kBf, {B, N, c.hq, 128}}, {"k", a[10], kBf, {B, c.hkv, N, 128}}, {"v", a[11], kBf, {B, c.hkv, N, 128}}});
         if (!c.ok) return nullptr;
         const auto *x = as<fspad_bf16>(*qkv);
-        rc = unlocked([&] { return fspad_rope_qkv(c.ctx, x, row, positions, start, parent, (int)N, (int)B, theta, st, sh, sw, adjacent, as<fspad_bf16>(q), as<fspad_bf16>(k), as<fspad_bf16>(v), c.stream); });
-        return rc ? nullptr : Py_BuildValue("(NNN)", THPVariable_Wrap(q), THPVariable_Wrap(k), THPVariable_Wrap(v));
+        rc = unlocked([&] { return fspad_rope_qkv(c.ctx, x, row, positions, start, parent, (int)N, (int)B, theta, st, sh, sw, adjacent, as<fspad_bf16>(o[0]), as<fspad_bf16>(o[1]), as<fspad_bf16>(o[2]), c.stream); });
+        return rc ? nullptr : Py_BuildValue("(NNN)", THPVariable_Wrap(o[0]), THPVariable_Wrap(o[1]), THPVariable_Wrap(o[2]));
     });
 }
 
@@ -312,12 +346,12 @@ PyObject *call_block_plan(PyObject *, PyObject *const *args, Py_ssize_t n)
         const auto *len = static_cast<const int32_t *>(c.data("length", a[0], kI32, {B})), *add = static_cast<const int32_t *>(c.data("add", a[1], kI32, {B}));
         const auto *drop = static_cast<const int32_t *>(c.data("drop", a[2], kI32, {B}, true));
         auto *held = static_cast<int32_t *>(c.data("held", a[4], kI32, {B})), *n_free = static_cast<int32_t *>(c.data("n_free", a[6], kI32, {1}));
-        const at::Tensor row_start = c.out("row_start", a[8], kI32, {B + 1}), slots = c.out("slots", a[9], at::kLong, {max_rows}),
-                         row_seq = c.out("row_seq", a[10], kI32, {max_rows}), row_pos = c.out("row_pos", a[11], kI32, {max_rows});
+        at::Tensor o[4];
+        c.outputs(o, {{"row_start", a[8], kI32, {B + 1}}, {"slots", a[9], at::kLong, {max_rows}}, {"row_seq", a[10], kI32, {max_rows}}, {"row_pos", a[11], kI32, {max_rows}}});
         if (!c.ok) return nullptr;
-        rc = unlocked([&] { return fspad_block_plan(c.ctx, len, add, drop, (int)B, (int)bps, (int)nb, as<int32_t>(*table), held, as<int32_t>(*free_blocks), n_free, max_rows, as<int32_t>(row_start),
-                                                     as<int64_t>(slots), as<int32_t>(row_seq), as<int32_t>(row_pos), c.stream); });
-        return rc ? nullptr : Py_BuildValue("(NNNN)", THPVariable_Wrap(row_start), THPVariable_Wrap(slots), THPVariable_Wrap(row_seq), THPVariable_Wrap(row_pos));
+        rc = unlocked([&] { return fspad_block_plan(c.ctx, len, add, drop, (int)B, (int)bps, (int)nb, as<int32_t>(*table), held, as<int32_t>(*free_blocks), n_free, max_rows, as<int32_t>(o[0]),
+                                                     as<int64_t>(o[1]), as<int32_t>(o[2]), as<int32_t>(o[3]), c.stream); });
+        return rc ? nullptr : Py_BuildValue("(NNNN)", THPVariable_Wrap(o[0]), THPVariable_Wrap(o[1]), THPVariable_Wrap(o[2]), THPVariable_Wrap(o[3]));
     });
 }
 
@@ -378,7 +412,8 @@ PyObject *call_kv_append_packed(PyObject *, PyObject *const *args, Py_ssize_t n)
         const auto *path = static_cast<const int32_t *>(c.data("accepted_path", a[4], kI32, {B, c.max_nodes}));
         const auto *count = static_cast<const int32_t *>(c.data("n_accepted", a[5], kI32, {B})), *len = static_cast<const int32_t *>(c.data("prefix_len", a[6], kI32, {B}));
         auto *rounded = static_cast<fspad_bf16 *>(c.data("rounded", a[7], kBf, {c.layers, 2, B, c.hkv, N, 128}, true));
-        const at::Tensor new_len = c.out("new_len", a[8], kI32, {B});
+        at::Tensor new_len;
+        c.outputs(&new_len, {{"new_len", a[8], kI32, {B}}});
         if (!c.ok) return nullptr;
         rc = unlocked([&] { return fspad_kv_append_packed(c.ctx, codes, scales, table, bps, nb, kv, path, count, len, (int)N, (int)B, rounded, as<int32_t>(new_len), c.stream); });
         return rc ? nullptr : THPVariable_Wrap(new_len);
@@ -399,7 +434,8 @@ PyObject *call_tree_attn_packed(PyObject *, PyObject *const *args, Py_ssize_t n)
         c.shaped("q", q, {B, N, c.hq, 128});
         const auto *tk = static_cast<const fspad_bf16 *>(c.data("tree_k", a[4], kBf, {B, c.hkv, N, 128})), *tv = static_cast<const fspad_bf16 *>(c.data("tree_v", a[5], kBf, {B, c.hkv, N, 128}));
         const auto *parent = static_cast<const int32_t *>(c.data("parent", a[6], kI32, {B, N})), *len = static_cast<const int32_t *>(c.data("prefix_len", a[7], kI32, {B}));
-        const at::Tensor out = c.out("out", a[9], kBf, {B, N, c.hq, 128});
+        at::Tensor out;
+        c.outputs(&out, {{"out", a[9], kBf, {B, N, c.hq, 128}}});
         const at::Tensor *ws = c.tensor("workspace", a[10], at::kByte);
         if (!c.ok) return nullptr;
         rc = unlocked([&] { return fspad_tree_attn_packed(c.ctx, as<fspad_bf16>(*q), codes, scales, layer, table, bps, nb, tk, tv, parent, len, (int)N, (int)B, as<fspad_bf16>(out), address(*ws),

@@ -166,7 +166,7 @@ import torch
 from paper_2408_15562_b200 import binding
 what = sys.argv[1]
 bf, i32, u8 = torch.bfloat16, torch.int32, torch.uint8
-ctx = types.SimpleNamespace(_h=ctypes.c_void_p(), cfg=types.SimpleNamespace(n_q_heads=8, n_kv_heads=2, n_layers=1, max_nodes=4))
+ctx = types.SimpleNamespace(_h=ctypes.c_void_p(), _sizes=(8, 2, 1, 4))
 ctx._packed_call = lambda *a: binding.Context._packed_call(ctx, *a)
 binding._stream = lambda s: 0
 C = binding.Context
