@@ -151,6 +151,9 @@ cudaError_t fspad_launch_rope_qkv(fspad_ctx *ctx, const fspad_bf16 *qkv, long lo
     if (groups > heads) groups = heads;
     if (groups > 65535) groups = 65535;
     a.heads_per = (int)((heads + groups - 1) / groups);
+    // many rows: shorter CTAs, for the last ones leave SMs idle (8201 rows of 48 heads: 39.9 us with 16 heads a thread, 36.9 with 8, 36.0 with 4 and 40.4
+    // with 3; trees, whose CTAs all take the depths again, do not gain: 64 of 60 nodes 21.8 us with 10 heads and 23.3 with 5)
+    if (!tree && a.heads_per > 4) a.heads_per = 4;
     const dim3 grid((unsigned)tiles, (unsigned)((heads + a.heads_per - 1) / a.heads_per), (unsigned)seqs);
     auto kernel = tree ? (adjacent ? rope_qkv_kernel<true, true> : rope_qkv_kernel<true, false>)
                        : (adjacent ? rope_qkv_kernel<false, true> : rope_qkv_kernel<false, false>);
