@@ -259,8 +259,8 @@ __device__ __forceinline__ void tell_run(const Args &a, const Parts &p, const Pa
 
 // The pieces of the runs that were cut, merged.  A CTA takes `rows` rows (a power of two, at most WARPS) of a run at a time, each by WARPS / rows warps that take its
 // pieces in turn, four elements a lane.
-template <int BM, int WARPS>
-__global__ void __launch_bounds__(WARPS * 32, WARPS > 8 ? 1 : 3)
+template <int BM, int WARPS, int U>           // U: pieces of a row under way
+__global__ void __launch_bounds__(WARPS * 32, WARPS > 8 ? 1 : U > 2 ? 3 : 6)
 tree_attn_packed_merge_kernel(const Args a, int rows)
 {
     __shared__ float4 s_acc[WARPS][32];
@@ -288,7 +288,6 @@ tree_attn_packed_merge_kernel(const Args a, int rows)
             acc.x *= w; acc.y *= w; acc.z *= w; acc.w *= w;
             m = m_new;
         };
-        constexpr int U = 8;                                 // pieces under way
         if (there) {
 #pragma unroll 1
             for (int i = i0 + warp / rows; i <= i1; i += U * wpr) {
@@ -363,16 +362,20 @@ static inline int merge_entries(Args &a, int parts)
     a.entry_runs = runs <= parts ? 1 : 0;
     return a.entry_runs ? (int)runs : parts;
 }
-template <int BM> static inline cudaError_t launch_merge(fspad_ctx *ctx, const Args &a, int entries, cudaStream_t st)
+template <int BM> static inline cudaError_t launch_merge(fspad_ctx *ctx, const Args &a, int entries, int parts, cudaStream_t st)
 {
     const int m = a.M < BM ? a.M : BM;
     ctx->launches++;
     // a row a CTA, with twice the warps, where that is no more than a CTA an SM (long runs in many pieces: 21.6 us against 24.9 on one token over 32K keys)
     if ((long long)entries * m <= ctx->sm_count)
-        return fspad_launch(tree_attn_packed_merge_kernel<BM, 16>, dim3((unsigned)entries, (unsigned)m), dim3(512), 0, st, 0, a, 1);
+        return fspad_launch(tree_attn_packed_merge_kernel<BM, 16, 8>, dim3((unsigned)entries, (unsigned)m), dim3(512), 0, st, 0, a, 1);
     int rows = 1;
     while (rows < 8 && rows < m && (long long)entries * ((m + rows - 1) / rows) > 3 * ctx->sm_count) rows *= 2;
-    return fspad_launch(tree_attn_packed_merge_kernel<BM, 8>, dim3((unsigned)entries, (unsigned)((m + rows - 1) / rows)), dim3(256), 0, st, 0, a, rows);
+    const dim3 grid((unsigned)entries, (unsigned)((m + rows - 1) / rows));
+    // runs in two pieces or three: fewer loads a row and twice the rows on an SM (16 trees of 60 nodes, 32 heads over 8, 512 to 4096 keys 95.6 -> 87.7 us, but
+    // one tree over 2K keys, in 19 pieces a run, 19.6 -> 23.9)
+    if ((long long)a.B * a.Hkv * a.mtiles * 2 >= parts) return fspad_launch(tree_attn_packed_merge_kernel<BM, 8, 2>, grid, dim3(256), 0, st, 0, a, rows);
+    return fspad_launch(tree_attn_packed_merge_kernel<BM, 8, 8>, grid, dim3(256), 0, st, 0, a, rows);
 }
 
 // Whether the units of a call, at most, can be counted in 32 bits (and 25 times as many as are cut into fewer parts than there are CTAs).

@@ -482,7 +482,7 @@ template <int NT> cudaError_t launch_few(fspad_ctx *ctx, Args &a, cudaStream_t s
     const int entries = merge_entries(a, ctas * warps_of(NT));
     ctx->launches++;
     e = fspad_launch(tree_attn_packed_kernel<NT>, dim3((unsigned)ctas), dim3(warps_of(NT) * 32), smem, st, 0, a);
-    return e == cudaSuccess ? launch_merge<BM>(ctx, a, entries, st) : e;
+    return e == cudaSuccess ? launch_merge<BM>(ctx, a, entries, ctas * warps_of(NT), st) : e;
 }
 
 }  // namespace

@@ -656,5 +656,5 @@ cudaError_t fspad_launch_attn_packed_umma(fspad_ctx *ctx, packed::Args a, void *
     const int entries = merge_entries(a, ctas);
     ctx->launches++;
     e = fspad_launch(tree_attn_packed_umma_kernel, dim3((unsigned)ctas), dim3(NT), SMEM, st, 0, a);
-    return e == cudaSuccess ? launch_merge<BM>(ctx, a, entries, st) : e;
+    return e == cudaSuccess ? launch_merge<BM>(ctx, a, entries, ctas, st) : e;
 }
