@@ -261,7 +261,7 @@ __device__ __forceinline__ void tell_run(const Args &a, const Parts &p, const Pa
 // pieces in turn, four elements a lane.
 template <int BM, int WARPS, int U>           // U: pieces of a row under way
 __global__ void __launch_bounds__(WARPS * 32, WARPS > 8 ? 1 : U > 2 ? 3 : 6)
-tree_attn_packed_merge_kernel(const Args a, int rows)
+tree_attn_packed_merge_kernel(const Args a, int rows, int parts)
 {
     __shared__ float4 s_acc[WARPS][32];
     __shared__ float2 s_ml[WARPS];
@@ -270,7 +270,8 @@ tree_attn_packed_merge_kernel(const Args a, int rows)
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, wpr = WARPS / rows;
     const int4 run = __ldcg(reinterpret_cast<const int4 *>(a.cuts) + 2 * blockIdx.x);
     const int i0 = run.w, i1 = __ldcg(a.cuts + 8 * blockIdx.x + 4);
-    if (run.x < 0) return;
+    // (-1: nothing to merge; and should a part have given up, its runs were never told of, and what is read is no run)
+    if ((unsigned)run.x >= (unsigned)a.B || (unsigned)run.y >= (unsigned)a.Hkv || (unsigned)run.z >= (unsigned)a.mtiles || i0 < 0 || i1 < i0 || i1 >= parts) return;
 #pragma unroll 1
     for (int row0 = blockIdx.y * rows; row0 < BM && run.z * BM + row0 < a.M; row0 += gridDim.y * rows) {
         const int row = row0 + warp % rows, gr = run.z * BM + row;
@@ -368,14 +369,14 @@ template <int BM> static inline cudaError_t launch_merge(fspad_ctx *ctx, const A
     ctx->launches++;
     // a row a CTA, with twice the warps, where that is no more than a CTA an SM (long runs in many pieces: 21.6 us against 24.9 on one token over 32K keys)
     if ((long long)entries * m <= ctx->sm_count)
-        return fspad_launch(tree_attn_packed_merge_kernel<BM, 16, 8>, dim3((unsigned)entries, (unsigned)m), dim3(512), 0, st, 0, a, 1);
+        return fspad_launch(tree_attn_packed_merge_kernel<BM, 16, 8>, dim3((unsigned)entries, (unsigned)m), dim3(512), 0, st, 0, a, 1, parts);
     int rows = 1;
     while (rows < 8 && rows < m && (long long)entries * ((m + rows - 1) / rows) > 3 * ctx->sm_count) rows *= 2;
     const dim3 grid((unsigned)entries, (unsigned)((m + rows - 1) / rows));
     // runs in two pieces or three: fewer loads a row and twice the rows on an SM (16 trees of 60 nodes, 32 heads over 8, 512 to 4096 keys 95.6 -> 87.7 us, but
     // one tree over 2K keys, in 19 pieces a run, 19.6 -> 23.9)
-    if ((long long)a.B * a.Hkv * a.mtiles * 2 >= parts) return fspad_launch(tree_attn_packed_merge_kernel<BM, 8, 2>, grid, dim3(256), 0, st, 0, a, rows);
-    return fspad_launch(tree_attn_packed_merge_kernel<BM, 8, 8>, grid, dim3(256), 0, st, 0, a, rows);
+    if ((long long)a.B * a.Hkv * a.mtiles * 2 >= parts) return fspad_launch(tree_attn_packed_merge_kernel<BM, 8, 2>, grid, dim3(256), 0, st, 0, a, rows, parts);
+    return fspad_launch(tree_attn_packed_merge_kernel<BM, 8, 8>, grid, dim3(256), 0, st, 0, a, rows, parts);
 }
 
 // Whether the units of a call, at most, can be counted in 32 bits (and 25 times as many as are cut into fewer parts than there are CTAs).
