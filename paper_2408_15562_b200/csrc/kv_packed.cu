@@ -2,9 +2,11 @@
 // tokens continue the sequence, the others and their descendants are discarded).
 //
 // Of every 16 elements: scale s = e4m3(max |x| / 6), codes e2m1(x / s), both to the nearest value, ties to the even code, a larger
-// magnitude than the type has to its largest.  The division is a product with 1/s whose result is rounded once more, to a multiple of
-// 2^-13: an exact tie (a multiple of 1/4) is met again that way, and nothing else can come to look like one, because x has 8 significant bits, s four
-// and a tie three, so that a quotient that is no tie lies at least 1/256 of its value away from one.
+// magnitude than the type has to its largest.  A division here is a product with a reciprocal that is 2^-20 too large, cut to 12 significant bits: a quotient
+// that is a tie of the type (three bits, of a scale five) comes out a little above it and is met again, and nothing else can come to look like one, because
+// x has 8 significant bits, s four and a tie three, so that a quotient that is no tie lies at least 1/256 of its value away from one.  (Divisions, and
+// quotients rounded by an addition and given their sign back, took half as many instructions again, and the instructions bounded the kernels: 16K rows
+// of 8 heads 33.0 us.)
 // A block with an infinity or a NaN gets a scale that is no number and codes of zero: it reads as NaN.
 //
 // Bound by memory: 256 bytes read and 72 written a row (256 more where the caller asks for the values that are kept).  Half a warp
@@ -16,6 +18,10 @@ namespace {
 constexpr int kWarpsPerCta = 8;
 constexpr int kInFlight = 4;             // row pairs
 
+// See above: what reciprocals are too large by, and a quotient's first 12 bits.
+constexpr float kUp = 1.0f + 0x1p-20f;
+__device__ __forceinline__ float cut(float x) { return __uint_as_float(__float_as_uint(x) & 0xfffff000u); }
+
 // Eight elements of a row (two bf16 a word) -> their codes; `scale` is the block's, which the neighbouring lane (lane ^ 1) shares.
 // With `rounded` the kept values come back in x.
 __device__ __forceinline__ uint32_t quantise(uint4 &x, uint32_t &scale, bool rounded)
@@ -25,24 +31,25 @@ __device__ __forceinline__ uint32_t quantise(uint4 &x, uint32_t &scale, bool rou
     m = max(m & 0xffffu, m >> 16);       // (magnitudes of bf16 order like whole numbers, infinities and NaN on top)
     m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
     const bool finite = m < 0x7f80u;
-    const float most = __uint_as_float(m << 16) / 6.0f;
+    const float most = cut(__uint_as_float(m << 16) * (kUp / 6.0f));
     uint16_t two;
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;\n" : "=h"(two) : "f"(0.0f), "f"(finite ? most : 0.0f));
     const uint32_t f16 = fspad_e4m3_to_f16(two);
     const float s = __half2float(__ushort_as_half((unsigned short)f16));
-    const float r = s > 0.0f ? 1.0f / s : 0.0f;
+    const float r = s > 0.0f ? __fdividef(kUp, s) : 0.0f;
     scale = finite ? (two & 0xffu) : 0x7fu;
-    uint32_t codes = 0;
-    const float big = 1536.0f;           // its neighbours are 2^-13 apart
+    float q[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float a = __uint_as_float(w[i] << 16), b = __uint_as_float(w[i] & 0xffff0000u);
-        // (the sign comes from the element: a quotient rounded to zero has lost it)
-        const float qa = copysignf(__fsub_rn(__fadd_rn(fabsf(a) * r, big), big), a), qb = copysignf(__fsub_rn(__fadd_rn(fabsf(b) * r, big), big), b);
-        uint32_t byte;
-        asm("{\n\t.reg .b8 c;\n\tcvt.rn.satfinite.e2m1x2.f32 c, %1, %2;\n\tcvt.u32.u8 %0, c;\n\t}\n" : "=r"(byte) : "f"(qb), "f"(qa));
-        codes |= byte << (8 * i);
+        q[2 * i] = cut(__uint_as_float(w[i] << 16) * r);
+        q[2 * i + 1] = cut(__uint_as_float(w[i] & 0xffff0000u) * r);
     }
+    uint32_t codes;
+    asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n\tcvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n\t"
+        "mov.b32 %0, {b0, b1, b2, b3};\n\t}\n"
+        : "=r"(codes) : "f"(q[0]), "f"(q[1]), "f"(q[2]), "f"(q[3]), "f"(q[4]), "f"(q[5]), "f"(q[6]), "f"(q[7]));
     if (!finite) codes = 0;
     if (rounded) {
         uint32_t h[4];
@@ -69,11 +76,12 @@ kv_write_packed_kernel(const uint4 *k, const uint4 *v, const long long *__restri
     fspad_pdl_trigger();
     fspad_pdl_wait();
     const int lane = threadIdx.x & 31, piece = lane & 15, half = lane >> 4;
-    const int groups = (rows + 2 * kInFlight - 1) / (2 * kInFlight);
-    const long long job = (long long)blockIdx.x * kWarpsPerCta + (threadIdx.x >> 5);
-    if (job >= (long long)groups * Hkv * 2) return;
-    const int group = (int)(job % groups);
-    const int head = (int)((job / groups) % Hkv), plane = (int)(job / groups / Hkv);
+    // (32 bits are enough for the number, and a division of 64 takes a hundred instructions)
+    const unsigned groups = (unsigned)(rows + 2 * kInFlight - 1) / (2 * kInFlight), job = blockIdx.x * kWarpsPerCta + (threadIdx.x >> 5);
+    const unsigned of_head = job / groups;
+    if (of_head >= 2u * Hkv) return;
+    const int group = (int)(job - of_head * groups), plane = of_head >= (unsigned)Hkv ? 1 : 0, head = (int)of_head - plane * Hkv;
+    const long long first = ((long long)plane * n_blocks * Hkv + head) * 128;        // the head's rows of a block: 128 Hkv to the next block's
     const uint4 *src = (plane ? v : k) + (long long)head * rows * 16;
     uint4 *back = plane ? v_rounded : k_rounded;
     uint4 x[kInFlight];
@@ -98,7 +106,7 @@ kv_write_packed_kernel(const uint4 *k, const uint4 *v, const long long *__restri
         uint32_t scale;
         const uint32_t c = quantise(x[u], scale, back != nullptr);
         if (slot[u] < 0) continue;
-        const long long to = ((((long long)plane * n_blocks + (slot[u] >> 7)) * Hkv + head) << 7) + (slot[u] & 127);
+        const long long to = first + (long long)(int)(slot[u] >> 7) * (Hkv * 128) + (slot[u] & 127);
         reinterpret_cast<uint32_t *>(codes)[to * 16 + piece] = c;
         if (!(piece & 1)) scales[to * 8 + (piece >> 1)] = (uint8_t)scale;
         if (back) back[((long long)head * rows + r) * 16 + piece] = x[u];
@@ -115,10 +123,11 @@ kv_append_packed_kernel(uint8_t *__restrict__ codes, uint8_t *__restrict__ scale
     fspad_pdl_trigger();
     fspad_pdl_wait();
     const int lane = threadIdx.x & 31, piece = lane & 15, half = lane >> 4;
-    const long long slice = (long long)blockIdx.x * kWarpsPerCta + (threadIdx.x >> 5);
-    if (slice >= (long long)n_layers * 2 * B * Hkv) return;
-    const int h = (int)(slice % Hkv), b = (int)((slice / Hkv) % B);
-    const long long lk = slice / ((long long)Hkv * B);              // layer * 2 + (K or V)
+    // (a slice has 256 bytes of tree_kv at least: 32 bits are enough for the number)
+    const unsigned number = blockIdx.x * kWarpsPerCta + (threadIdx.x >> 5), of_seq = number / (unsigned)Hkv, lk = of_seq / (unsigned)B;  // lk: layer * 2 + (K or V)
+    if (lk >= 2u * n_layers) return;
+    const int h = (int)(number - of_seq * Hkv), b = (int)(of_seq - lk * B);
+    const long long slice = number, first = ((long long)lk * n_blocks * Hkv + h) * 128;      // the head's rows of a block: 128 Hkv to the next block's
     int L = prefix_len[b], n = n_acc[b];
     const int *pth = path + (size_t)b * path_stride;
     bool bad = false;
@@ -150,7 +159,7 @@ kv_append_packed_kernel(uint8_t *__restrict__ codes, uint8_t *__restrict__ scale
                 uint32_t scale;
                 const uint32_t c = quantise(x[u], scale, rounded != nullptr);
                 if (node[u] < 0) continue;
-                const long long to = (((lk * n_blocks + block) * Hkv + h) << 7) + ((L + j0 + j1 + 2 * u + half) & 127);
+                const long long to = first + (long long)block * (Hkv * 128) + ((L + j0 + j1 + 2 * u + half) & 127);
                 reinterpret_cast<uint32_t *>(codes)[to * 16 + piece] = c;
                 if (!(piece & 1)) scales[to * 8 + (piece >> 1)] = (uint8_t)scale;
                 if (rounded) rounded[(slice * N + node[u]) * 16 + piece] = x[u];

@@ -45,13 +45,34 @@ rope_qkv_kernel(const __grid_constant__ RopeArgs a)
     const long long r = (long long)blockIdx.x * kRows + (threadIdx.x >> 3);
     long long row;                       // of all rows
     int b, i;
-    double pos[3] = {0.0, 0.0, 0.0};
-    bool ok;
     if (TREE) {
         b = blockIdx.z;
         i = (int)r;
-        ok = i < a.N;
         row = (long long)b * a.N + i;
+    } else {
+        row = r;
+        b = (int)((unsigned)r / (unsigned)a.N);      // (at most 2^31 rows, and the last CTA's)
+        i = (int)((unsigned)r - (unsigned)b * (unsigned)a.N);
+    }
+    const bool ok = TREE ? i < a.N : r < (long long)a.B * a.N;
+    const int heads = a.Hq + 2 * a.Hkv;
+    const int h0 = blockIdx.y * a.heads_per, h1 = min(heads, h0 + a.heads_per);
+    const uint4 *src = reinterpret_cast<const uint4 *>(a.qkv + row * a.row_stride);
+    // the thread's 16-byte pieces of a head: elements 8c .. and 64 + 8c .. (pairs across the halves), or 16c .. (neighbours)
+    const int p0 = ADJACENT ? 2 * c : c, p1 = ADJACENT ? 2 * c + 1 : c + 8;
+    constexpr int U = 4;                 // heads under way: the first are asked for before the positions and their sines are taken
+    uint4 first[U], second[U];
+    auto fetch = [&](int h) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (ok && h + u < h1) {
+                first[u] = __ldg(src + (h + u) * 16 + p0);
+                second[u] = __ldg(src + (h + u) * 16 + p1);
+            }
+    };
+    fetch(h0);
+    double pos[3] = {0.0, 0.0, 0.0};
+    if (TREE) {
         // depth by doubling: after round t every node knows its ancestor 2^t up and how far that is
         for (int n = threadIdx.x; n < a.N; n += kThreads) {
             int p = a.parent[(size_t)b * a.N + n];
@@ -75,15 +96,9 @@ rope_qkv_kernel(const __grid_constant__ RopeArgs a)
 #pragma unroll
             for (int x = 0; x < 3; ++x) pos[x] = (double)a.start[b * 3 + x] + (double)d;
         }
-    } else {
-        row = r;
-        ok = r < (long long)a.B * a.N;
-        b = (int)(r / a.N);
-        i = (int)(r - (long long)b * a.N);
-        if (ok) {
+    } else if (ok) {
 #pragma unroll
-            for (int x = 0; x < 3; ++x) pos[x] = (double)a.positions[row * 3 + x];
-        }
+        for (int x = 0; x < 3; ++x) pos[x] = (double)a.positions[row * 3 + x];
     }
     if (!ok) return;
     float co[8], si[8];
@@ -93,14 +108,14 @@ rope_qkv_kernel(const __grid_constant__ RopeArgs a)
         const double t = (p < a.table.split0 ? pos[0] : p < a.table.split1 ? pos[1] : pos[2]) * a.table.turns[p];
         sincospif(2.0f * (float)(t - rint(t)), &si[j], &co[j]);
     }
-    const int heads = a.Hq + 2 * a.Hkv;
-    const int h0 = blockIdx.y * a.heads_per, h1 = min(heads, h0 + a.heads_per);
-    const uint4 *src = reinterpret_cast<const uint4 *>(a.qkv + row * a.row_stride);
-    // the thread's 16-byte pieces of a head: elements 8c .. and 64 + 8c .. (pairs across the halves), or 16c .. (neighbours)
-    const int p0 = ADJACENT ? 2 * c : c, p1 = ADJACENT ? 2 * c + 1 : c + 8;
-#pragma unroll 4
-    for (int h = h0; h < h1; ++h) {
-        const uint4 lo = __ldg(src + h * 16 + p0), hi = __ldg(src + h * 16 + p1);
+#pragma unroll 1
+    for (int h4 = h0; h4 < h1; h4 += U) {
+      if (h4 > h0) fetch(h4);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int h = h4 + u;
+        if (h >= h1) break;
+        const uint4 lo = first[u], hi = second[u];
         uint4 o0, o1;
         fspad_bf16 *to;
         if (h < a.Hq) to = a.q + (row * a.Hq + h) * FSPAD_HEAD_DIM;
@@ -110,11 +125,11 @@ rope_qkv_kernel(const __grid_constant__ RopeArgs a)
             o0 = lo;
             o1 = hi;
         } else {
-            const uint32_t l[4] = {lo.x, lo.y, lo.z, lo.w}, u[4] = {hi.x, hi.y, hi.z, hi.w};
+            const uint32_t wl[4] = {lo.x, lo.y, lo.z, lo.w}, wh[4] = {hi.x, hi.y, hi.z, hi.w};
             uint32_t y0[4], y1[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float2 x = unpack(l[j]), z = unpack(u[j]);
+                const float2 x = unpack(wl[j]), z = unpack(wh[j]);
                 if (ADJACENT) {          // (x.x, x.y) is pair j, (z.x, z.y) pair 4 + j
                     y0[j] = pack(x.x * co[j] - x.y * si[j], x.y * co[j] + x.x * si[j]);
                     y1[j] = pack(z.x * co[4 + j] - z.y * si[4 + j], z.y * co[4 + j] + z.x * si[4 + j]);
@@ -128,6 +143,7 @@ rope_qkv_kernel(const __grid_constant__ RopeArgs a)
         }
         reinterpret_cast<uint4 *>(to)[p0] = o0;
         reinterpret_cast<uint4 *>(to)[p1] = o1;
+      }
     }
 }
 
@@ -151,8 +167,8 @@ cudaError_t fspad_launch_rope_qkv(fspad_ctx *ctx, const fspad_bf16 *qkv, long lo
     if (groups > heads) groups = heads;
     if (groups > 65535) groups = 65535;
     a.heads_per = (int)((heads + groups - 1) / groups);
-    // many rows: shorter CTAs, for the last ones leave SMs idle (8201 rows of 48 heads: 39.9 us with 16 heads a thread, 36.9 with 8, 36.0 with 4 and 40.4
-    // with 3; trees, whose CTAs all take the depths again, do not gain: 64 of 60 nodes 21.8 us with 10 heads and 23.3 with 5)
+    // many rows: shorter CTAs, for the last ones leave SMs idle (8201 rows of 48 heads: 39.9 us with 16 heads a thread, 36.0 with 4 and 40.4 with 3, before the
+    // loads went ahead of the sines; trees, whose CTAs all take the depths again, do not gain: 64 of 60 nodes 21.8 us with 10 heads and 23.3 with 5)
     if (!tree && a.heads_per > 4) a.heads_per = 4;
     const dim3 grid((unsigned)tiles, (unsigned)((heads + a.heads_per - 1) / a.heads_per), (unsigned)seqs);
     auto kernel = tree ? (adjacent ? rope_qkv_kernel<true, true> : rope_qkv_kernel<true, false>)
