@@ -392,12 +392,14 @@ class Context:
                  stream=None):
         """Rows of the QKV product [B][N][(Hq + 2 Hkv) * 128] (bf16, device; rows may stand further apart) -> q [B][N][Hq][128] and k, v
         [B][Hkv][N][128], queries and keys turned by positions of up to three axes: `positions` [B][N][3], or of tree nodes `start`
-        [B][3] plus the depth in `parent` [B][N].  `sections`: how many of the 64 pairs go by time, height and width."""
+        [B][3] plus the depth in `parent` [B][N].  `sections`: how many of the 64 pairs go by time, height and width.  New outputs of a call
+        share one allocation."""
         return self._packed_call("rope_qkv", stream, qkv, theta, *sections, parent, start, positions, adjacent, q, k, v)
 
     def block_plan(self, length, add, block_table, held, free_blocks, n_free, max_rows, drop=None, out=(None, None, None, None), stream=None):
         """Blocks for add[b] rows behind the length[b] that sequence b holds; block_table [B][blocks], held [B], free_blocks [n_blocks] and
-        n_free [1] (int32, device) are updated.  Returns (row_start [B + 1], slots [max_rows] int64, row_seq, row_pos [max_rows])."""
+        n_free [1] (int32, device) are updated.  Returns (row_start [B + 1], slots [max_rows] int64, row_seq, row_pos [max_rows]; new
+        ones share one allocation)."""
         return self._packed_call("block_plan", stream, length, add, drop, block_table, held, free_blocks, n_free, max_rows, *out)
 
     def kv_write_packed(self, k, v, slots, codes, scales, layer=0, k_rounded=None, v_rounded=None, stream=None):
@@ -412,7 +414,7 @@ class Context:
     def tree_attn_packed(self, q, codes, scales, block_table, tree_k, tree_v, parent, prefix_len, layer=0, out=None, workspace=None,
                          stream=None):
         """Tree-masked attention of q [B][N][Hq][128] over a layer of the 4-bit cache and the tree's bf16 rows [B][Hkv][N][128].  Without
-        `workspace` (uint8) the context's own is used, which calls on one stream at a time may share."""
+        `workspace` (uint8) the context's own is used: no two such calls, captured ones among them, may then run at the same time."""
         if workspace is None:
             workspace = self._workspace
             if workspace is None:

@@ -9,8 +9,10 @@
 // of 8 heads 33.0 us.)
 // A block with an infinity or a NaN gets a scale that is no number and codes of zero: it reads as NaN.
 //
-// Bound by memory: 256 bytes read and 72 written a row (256 more where the caller asks for the values that are kept).  Half a warp
-// takes a row, 16 bytes a lane, so that two lanes share a scale; four pairs of rows are in flight.
+// Bound by memory in the end, 256 bytes read and 72 written a row (256 more where the caller asks for the values that are kept), and by the issue of
+// instructions nearly as much (some 80 for eight elements; 84 % of the slots taken when they were 130).  Half a warp
+// takes a row, 16 bytes a lane, so that two lanes share a scale; four pairs of rows are in flight (two: 30.7 us against 29.4 on 16K rows of 8 heads, eight:
+// 33.7 against 33.1 when both were slower).  16K rows with the values kept 29.4 us, 5.2 TB/s; 64 paths of 24 nodes in 16 layers 45.3 us, 5.1 TB/s.
 #include "packed.cuh"
 
 namespace {

@@ -12,6 +12,11 @@
 // scales come by bulk copies into a ring of the warp's own; they go from shared memory straight into the registers of the operands (no
 // second trip through shared memory): the order of the elements within a product and of the keys within a unit is chosen so
 // that every lane reads 16 bytes of a row of K, and 8 of a row of V, and finds its operands in them.  The tree's rows are taken as bf16.
+//
+// What bounds it.  Long contexts: 32 tokens of 64 heads over 8, 4000 to 32000 keys, 136 us with the merge, 645 MB read at 4.7 TB/s (72 % of the measured copy
+// rate).  The integer pipe is 59 % busy and 65 % of the issue slots are taken: a unit of 32 keys takes some 660 instructions, 140 of them conversions of codes
+// and scales, which each element needs once however few rows there are; 16 warps an SM, with all registers taken, do not hide the rest.  Short ones:
+// one token over 2000 keys 8.4 us, of which the two launches, the list and the first trips to memory in turn are the most.
 #include <type_traits>
 
 #include "packed_list.cuh"

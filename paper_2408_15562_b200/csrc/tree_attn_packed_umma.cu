@@ -15,6 +15,13 @@
 // they are: the tree's chunks come first, with bf16 operands (one product's operands have one type), and the query tile is then written
 // again.  With one row tile its two forms lie in the two tiles' places.
 //
+// What bounds it: with two row tiles a chunk takes 4450 cycles, in which the products take 2900 (128 x 128 x 16 with both operands in shared memory 108 cycles, with
+// one in tensor memory 75) and each group goes through a chain: exponentials 2050, its product with V 600, the next scores 860, the handing over between
+// the warps the rest.  One tree of 60 nodes, 64 heads over 8, over 32700 keys: 87.7 us (64 GFLOP, 730 TFLOP/s).  With one row tile the codes' warps are the
+// slowest, 3150 cycles a chunk.  What a stretch takes besides (queries, the tree's rows in bf16, the rows' way out, code that is fetched cold: 15000 to 20000 cycles) bounds
+// short runs: 16 trees of 60 nodes, 32 heads over 8, 512 to 4096 keys 87.7 us, with the merge (16 by itself, from a cold cache).  Not kept: weights handed over in halves (91.4 us for the first of
+// these), the products told of behind the next scores (one row tile 10 % longer).
+//
 // Every wait is bounded; on expiry the CTA records FSPAD_ERR_TIMEOUT, lets what is under way land and frees its tensor memory.
 #include "packed_list.cuh"
 
