@@ -563,30 +563,27 @@ tree_attn_packed_umma_kernel(const Args a)
                     if (cc >= 2 && !mbar_wait(bar(K_FREE + slot), ((cc >> 1) - 1u) & 1u)) { failed = true; break; }
                     if (lane == 0) odd[w4] = 0u;             // (a warp's 32 rows are a word)
 #pragma unroll 4
-                    for (int r = w4 * 32 + (lane >> 4); r < w4 * 32 + 32; r += 2)
-                        cp_async16(sK + slot * TILE + tile_off(r, piece), a.tk + (r < rows ? first + (size_t)r * D : 0), r < rows);
+                    for (int r = w4 * 32 + (lane >> 4); r < w4 * 32 + 32; r += 2) {
+                        const size_t at = r < rows ? first + (size_t)r * D : 0;
+                        cp_async16(sV + slot * TILE + tile_off(r, piece), a.tv + at, r < rows);
+                        cp_async16(sK + slot * TILE + tile_off(r, piece), a.tk + at, r < rows);
+                    }
                     cp_async_commit();
+                    cp_async_wait<0>();
+                    __syncwarp();                            // (the word is zero)
 #pragma unroll 1
-                    for (int r8 = 0; r8 < 32; r8 += 16) {
+                    for (int r8 = 0; r8 < 32; r8 += 16) {    // V, as this lane has copied it
                         uint4 x[8];
 #pragma unroll
-                        for (int y = 0; y < 8; ++y) {
-                            const int r = w4 * 32 + r8 + 2 * y + (lane >> 4);
-                            x[y] = make_uint4(0u, 0u, 0u, 0u);
-                            if (r < rows) x[y] = __ldg(reinterpret_cast<const uint4 *>(a.tv + first + (size_t)r * D));
-                        }
-                        __syncwarp();
+                        for (int y = 0; y < 8; ++y) x[y] = ld_shared16(sV + slot * TILE + tile_off(w4 * 32 + r8 + 2 * y + (lane >> 4), piece));
 #pragma unroll
-                        for (int y = 0; y < 8; ++y) {
-                            const int r = r8 + 2 * y + (lane >> 4);
+                        for (int y = 0; y < 8; ++y)
                             if (odd_value(x[y].x) || odd_value(x[y].y) || odd_value(x[y].z) || odd_value(x[y].w)) {
+                                const int r = r8 + 2 * y + (lane >> 4);
                                 atomicOr(&odd[w4], 1u << r);         // out of the product: see softmax
-                                x[y] = make_uint4(0u, 0u, 0u, 0u);
+                                st_shared(sV + slot * TILE + tile_off(w4 * 32 + r, piece), make_uint4(0u, 0u, 0u, 0u));
                             }
-                            st_shared(sV + slot * TILE + tile_off(w4 * 32 + r, piece), x[y]);
-                        }
                     }
-                    cp_async_wait<0>();
                     fence_async_smem();
                     __syncwarp();
                     if (lane == 0) {
