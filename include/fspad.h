@@ -448,7 +448,7 @@ int fspad_device(const fspad_ctx *ctx);
  *   positions [batch][n_nodes][3] int32, with start and parent NULL; n_nodes may then be any number of rows (a prompt), batch * n_nodes < 2^31
  *   start [batch][3] int32 and parent [batch][n_nodes] int32, with positions NULL: node i of tree b stands at start[b][a] + depth(i) on axis a
  *   q         [batch][n_nodes][Hq][128], k and v [batch][Hkv][n_nodes][128]: what fspad_tree_attn* and the cache calls take
- * The outputs must not overlap qkv or one another.  Errors: FSPAD_ERR_NULL also where neither or both kinds of positions are given; FSPAD_ERR_SHAPE for sections
+ * The outputs must not overlap qkv or one another (FSPAD_ERR_RANGE where they begin at the same address).  Errors: FSPAD_ERR_NULL also where neither or both kinds of positions are given; FSPAD_ERR_SHAPE for sections
  * that do not sum to 64 and strides outside these rules; FSPAD_ERR_RANGE for a theta that is not finite and positive, or so small that its powers are not finite; FSPAD_ERR_TOO_LARGE
  * for more than 65535 sequences or 2^31 - 1 rows; a malformed parent[] sets FSPAD_ERR_BAD_TREE in the status word.
  */
@@ -495,7 +495,8 @@ int fspad_kv_write_packed(fspad_ctx *ctx, const fspad_bf16 *k, const fspad_bf16 
 
 /*
  * fspad_kv_append for the 4-bit cache: for every layer, K and V, sequence b and kv head, cache row L_b + j receives
- * tree_kv[..][accepted_path[b][j]], j = 0 .. n_accepted[b] - 1.  new_len[b] = L_b + n_accepted[b] (may be NULL).
+ * tree_kv[..][accepted_path[b][j]], j = 0 .. n_accepted[b] - 1.  new_len[b] = L_b + n_accepted[b] (may be NULL, but not
+ * prefix_len: FSPAD_ERR_RANGE).
  *
  *   tree_kv [n_layers][2][batch][Hkv][n_nodes][128] bf16;  accepted_path [batch][max_nodes], n_accepted, prefix_len, new_len [batch] int32
  *   rounded as tree_kv or NULL: receives the values that are kept, at the nodes' own places (other nodes: unchanged); may be tree_kv, if no node
@@ -512,7 +513,8 @@ int fspad_kv_append_packed(fspad_ctx *ctx, uint8_t *codes, uint8_t *scales, cons
  * fspad_tree_attn_paged over the 4-bit cache: the keys of node i of sequence b are cache rows 0 .. L_b - 1 and, in bf16, the rows of the
  * node itself and of its ancestors in tree_k / tree_v.  n_nodes = 1 is the single-token step.
  *
- *   q, out [batch][n_nodes][Hq][128] bf16;  tree_k, tree_v [batch][Hkv][n_nodes][128] bf16 (required)
+ *   q, out [batch][n_nodes][Hq][128] bf16;  tree_k, tree_v [batch][Hkv][n_nodes][128] bf16 (required).  out must not overlap an input
+ *              (FSPAD_ERR_RANGE where it begins at the same address)
  *   layer  of the cache;  parent [batch][n_nodes], prefix_len [batch] int32, 0 <= L_b <= 128 * blocks_per_seq
  *   workspace  of at least fspad_tree_attn_packed_workspace_bytes(ctx, n_nodes, batch) bytes, scratch: no other call may use it
  *              until this one is done

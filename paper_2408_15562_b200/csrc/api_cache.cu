@@ -60,6 +60,7 @@ int fspad_rope_qkv(fspad_ctx *ctx, const fspad_bf16 *qkv, int64_t row_stride, co
     if (!(theta > 0.0) || std::isinf(theta) || std::isinf(std::pow(theta, -2.0 * (half - 1) / FSPAD_HEAD_DIM))) return FSPAD_ERR_RANGE;
     if ((int64_t)n_nodes * batch > INT_MAX || batch > 65535) return FSPAD_ERR_TOO_LARGE;
     if (batch == 0) return FSPAD_OK;
+    if (q == qkv || k == qkv || v == qkv || q == k || q == v || k == v) return FSPAD_ERR_RANGE;
     FspadRopeTable t;
     if (ctx->rope_theta != theta) {
         for (int i = 0; i < half; ++i) ctx->rope_turns[i] = std::pow(theta, -2.0 * i / FSPAD_HEAD_DIM) / (2.0 * 3.14159265358979323846);
@@ -114,6 +115,7 @@ int fspad_kv_append_packed(fspad_ctx *ctx, uint8_t *codes, uint8_t *scales, cons
     if (misaligned(codes) || misaligned(scales) || misaligned(tree_kv) || misaligned(rounded)) return FSPAD_ERR_ALIGN;
     if ((rc = check_blocks(blocks_per_seq, n_blocks)) != 0) return rc;
     if (batch == 0) return FSPAD_OK;
+    if (new_len == prefix_len) return FSPAD_ERR_RANGE;         // (other warps still read it)
     const FspadPaged pg{block_table, blocks_per_seq, n_blocks};
     return result(fspad_launch_kv_append_packed(ctx, codes, scales, pg, tree_kv, accepted_path, n_accepted, prefix_len, n_nodes, batch,
                                                 rounded, new_len, fspad_stream(stream)));
@@ -140,6 +142,7 @@ int fspad_tree_attn_packed(fspad_ctx *ctx, const fspad_bf16 *q, const uint8_t *c
     if (layer < 0 || layer >= ctx->cfg.n_layers) return FSPAD_ERR_SHAPE;
     if ((rc = check_blocks(blocks_per_seq, n_blocks)) != 0) return rc;
     if (batch == 0) return FSPAD_OK;
+    if (out == q || out == tree_k || out == tree_v) return FSPAD_ERR_RANGE;
     if (workspace_bytes < fspad_attn_packed_workspace(ctx, n_nodes, batch)) return FSPAD_ERR_RANGE;
     if (!fspad_attn_packed_fits(ctx, n_nodes, batch, blocks_per_seq)) return FSPAD_ERR_TOO_LARGE;
     const size_t rows = (size_t)n_blocks * ctx->cfg.n_kv_heads * 128, first = (size_t)layer * 2 * rows;

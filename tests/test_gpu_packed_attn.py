@@ -224,6 +224,25 @@ def test_captured_replayed_and_on_another_stream(nodes):
 
 
 @pytest.mark.parametrize("nodes", [1, 60])
+def test_two_calls_at_once_with_a_workspace_each(nodes):
+    cases = [Case(18, 4, nodes, 8, 2, [3000, 64, 333, 1500]), Case(19, 4, nodes, 8, 2, [0, 2500, 700, 129])]
+    ctx = cases[0].context()
+    args = [c.arguments() for c in cases]
+    want = [ctx.tree_attn_packed(*a) for a in args]
+    size = ctx.tree_attn_packed_workspace_bytes(nodes, 4)
+    own = [torch.empty(size, dtype=torch.uint8, device="cuda") for _ in cases]
+    out = [[torch.full_like(w, 9) for _ in range(8)] for w in want]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    for i in range(8):
+        for a, o, ws, st in zip(args, out, own, streams):
+            ctx.tree_attn_packed(*a, out=o[i], workspace=ws, stream=st)
+    torch.cuda.synchronize()
+    ctx.check()
+    assert all(torch.equal(x, w) for o, w in zip(out, want) for x in o)
+
+
+@pytest.mark.parametrize("nodes", [1, 60])
 def test_results_do_not_depend_on_the_run(nodes):
     case = Case(16, 5, nodes, 8, 2, [900, 64, 333, 0, 1700])
     args, ctx = case.arguments(), case.context()

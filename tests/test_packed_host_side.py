@@ -13,6 +13,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(ROOT, "paper_2408_15562_b200", "csrc")
 NULL, CUDA, TREE, SHAPE, ALIGN, RANGE, LARGE, DEVICE = "NULL", "CUDA", "TREE_TOO_LARGE", "SHAPE", "ALIGN", "RANGE", "TOO_LARGE", "DEVICE"
 P, ODD = 0x10000, 0x10008                  # a 16-byte aligned address that nothing reads, and one that is not
+P1, P2, P3 = 0x20000, 0x30000, 0x40000     # further ones
 HQ, HKV, NODES, LAYERS, BATCH = 8, 2, 64, 3, 2000
 
 
@@ -55,14 +56,14 @@ def lib(tmp_path_factory):
 # the arguments of each call, in order, with values that are accepted
 CALLS = {
     "rope_qkv": dict(qkv=P, row_stride=(HQ + 2 * HKV) * 128, positions=None, start=P, parent=P, n_nodes=NODES, batch=2, theta=1e4, sec_t=16, sec_h=24,
-                     sec_w=24, adjacent=0, q=P, k=P, v=P, stream=None),
+                     sec_w=24, adjacent=0, q=P1, k=P2, v=P3, stream=None),
     "block_plan": dict(len=P, add=P, drop=None, batch=5, blocks_per_seq=4, n_blocks=9, block_table=P, held=P, free_blocks=P, n_free=P, max_rows=7,
                        row_start=P, slots=P, row_seq=None, row_pos=None, stream=None),
     "kv_write_packed": dict(k=P, v=P, slots=P, rows=7, layer=2, codes=P, scales=P, n_blocks=9, k_rounded=None, v_rounded=None, stream=None),
     "kv_append_packed": dict(codes=P, scales=P, block_table=P, blocks_per_seq=4, n_blocks=9, tree_kv=P, accepted_path=P, n_accepted=P, prefix_len=P,
                              n_nodes=NODES, batch=2, rounded=None, new_len=None, stream=None),
     "tree_attn_packed": dict(q=P, codes=P, scales=P, layer=1, block_table=P, blocks_per_seq=4, n_blocks=9, tree_k=P, tree_v=P, parent=P, prefix_len=P,
-                             n_nodes=NODES, batch=2, out=P, workspace=P, workspace_bytes=NODES * 2 * 1000, stream=None),
+                             n_nodes=NODES, batch=2, out=P1, workspace=P, workspace_bytes=NODES * 2 * 1000, stream=None),
 }
 
 
@@ -94,17 +95,17 @@ REFUSED = {
         (dict(positions=P, start=None, parent=None, n_nodes=1 << 30, batch=2), LARGE),
         (dict(sec_t=17), SHAPE), (dict(sec_t=0), SHAPE), (dict(sec_t=65, sec_h=-1, sec_w=0), SHAPE), (dict(sec_t=-8, sec_h=48), SHAPE),
         (dict(row_stride=(HQ + 2 * HKV) * 128 - 8), SHAPE), (dict(row_stride=(HQ + 2 * HKV) * 128 + 4), SHAPE), (dict(row_stride=0), SHAPE),
-        (dict(theta=0.0), RANGE), (dict(theta=-1.0), RANGE), (dict(theta=math.nan), RANGE), (dict(theta=math.inf), RANGE), (dict(theta=5e-324), RANGE)],
+        (dict(theta=0.0), RANGE), (dict(theta=-1.0), RANGE), (dict(theta=math.nan), RANGE), (dict(theta=math.inf), RANGE), (dict(theta=5e-324), RANGE)] + [(dict([c]), RANGE) for c in [("q", P), ("k", P), ("v", P), ("q", P2), ("k", P3), ("v", P1)]],
     "block_plan": _null("len", "add", "block_table", "held", "free_blocks", "n_free", "row_start", "slots") + BLOCKS + [
         (dict(batch=-1), SHAPE), (dict(batch=BATCH + 1), SHAPE), (dict(max_rows=-1), SHAPE), (dict(batch=1025), LARGE)],
     "kv_write_packed": _null("k", "v", "slots", "codes", "scales") + _odd("k", "v", "codes", "scales") + [
         (dict(k_rounded=P), NULL), (dict(v_rounded=P), NULL), (dict(k_rounded=ODD, v_rounded=P), ALIGN), (dict(k_rounded=P, v_rounded=ODD), ALIGN),
         (dict(rows=-1), SHAPE), (dict(layer=-1), SHAPE), (dict(layer=LAYERS), SHAPE), (dict(n_blocks=0), SHAPE), (dict(rows=1 << 30), LARGE)],
     "kv_append_packed": _null("codes", "scales", "block_table", "tree_kv", "accepted_path", "n_accepted", "prefix_len") +
-        _odd("codes", "scales", "tree_kv", "rounded") + TREE_SIZES + BLOCKS,
+        _odd("codes", "scales", "tree_kv", "rounded") + TREE_SIZES + BLOCKS + [(dict(new_len=P), RANGE)],
     "tree_attn_packed": _null("q", "codes", "scales", "block_table", "tree_k", "tree_v", "parent", "prefix_len", "out", "workspace") +
         _odd("q", "codes", "scales", "tree_k", "tree_v", "out", "workspace") + TREE_SIZES + BLOCKS + [
-        (dict(layer=-1), SHAPE), (dict(layer=LAYERS), SHAPE), (dict(workspace_bytes=NODES * 2 * 1000 - 1), RANGE), (dict(fits=0), LARGE)],
+        (dict(layer=-1), SHAPE), (dict(layer=LAYERS), SHAPE), (dict(workspace_bytes=NODES * 2 * 1000 - 1), RANGE), (dict(fits=0), LARGE), (dict(out=P), RANGE)],
 }
 
 
