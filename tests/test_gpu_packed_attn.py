@@ -316,3 +316,49 @@ def test_from_the_product_to_the_cache_and_back():
             paths[b, :len(p)], n_acc[b] = p, len(p)
         length = ctx.kv_append_packed(codes, scales, table, tree, dev(paths), dev(n_acc), length)
         ctx.check()
+
+
+def test_a_captured_step_replayed_is_the_step_called():
+    """Blocks, rotary positions, attention and append of a step in one graph, replayed over growing lengths."""
+    rng = np.random.default_rng(21)
+    B, hq, hkv, N, bps = 3, 8, 2, 9, 6
+    width, nb = (hq + 2 * hkv) * 128, 3 * 6
+    parent = dev(np.stack([np.array([-1] + [int(rng.integers(0, i)) for i in range(1, N)], np.int32) for _ in range(B)]))
+    path = np.full((B, N), -1, np.int32)
+    count = np.array([2, 1, 0], np.int32)
+    p = parent.cpu().numpy()
+    for b in range(B):
+        path[b, 0] = 0
+        path[b, 1] = int(np.flatnonzero(p[b] == 0)[0])
+    path, count, free = dev(path), dev(count), rng.permutation(nb).astype(np.int32)
+    qkv = b16(synth.normal_bf16(rng, (B, N, width)))
+
+    class State:
+        def __init__(self):
+            self.ctx = binding.Context(hq, hkv, 16, 512, max_nodes=N, max_batch=B)
+            self.codes, self.scales = self.ctx.new_packed_cache(nb)
+            self.table, self.held = dev(np.zeros((B, bps), np.int32)), dev(np.zeros(B, np.int32))
+            self.free, self.n_free, self.length = dev(free), dev(np.array([nb], np.int32)), dev(np.array([0, 126, 255], np.int32))
+            self.add, self.tree = dev(np.full(B, N, np.int32)), torch.empty((1, 2, B, hkv, N, 128), dtype=torch.bfloat16, device="cuda")
+
+        def step(self):
+            plan = self.ctx.block_plan(self.length, self.add, self.table, self.held, self.free, self.n_free, B * N)
+            start = self.length[:, None].repeat(1, 3)
+            q, _, _ = self.ctx.rope_qkv(qkv, 1e4, (20, 20, 24), parent=parent, start=start, k=self.tree[0, 0], v=self.tree[0, 1])
+            out = self.ctx.tree_attn_packed(q, self.codes, self.scales, self.table, self.tree[0, 0], self.tree[0, 1], parent, self.length)
+            self.length.copy_(self.ctx.kv_append_packed(self.codes, self.scales, self.table, self.tree, path, count, self.length))
+            return (out,) + plan
+
+    called, replayed = State(), State()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = replayed.step()
+    for _ in range(5):
+        want = called.step()
+        graph.replay()
+        for name in ("codes", "scales", "table", "held", "free", "n_free", "length"):
+            assert torch.equal(getattr(called, name), getattr(replayed, name)), name
+        assert all(torch.equal(x, y) for x, y in zip(want, out))
+    called.ctx.check()
+    replayed.ctx.check()
+    assert replayed.length.tolist() == [10, 131, 255]
