@@ -133,7 +133,7 @@ FSPAD_CALL(verify_step_host, 2)
 #undef FSPAD_CALL
 
 // ---- the calls around the 4-bit cache: they know the context's sizes, look at every tensor's shape and device, and make the outputs that are
-// not given (in Python that took longer than the launches: a single-token step 11.1 -> 8 us, rotary rows of a tree 13.8 -> 6.5) ----
+// not given (in Python that took longer than the launches: a single-token step 11.1 -> 7.5 us, rotary rows of a tree 13.8 -> 5.8) ----
 // A tensor's address; an empty one has none, and nothing is read or written there: it gets one that is aligned.
 alignas(16) char kNothing[16];
 void *address(const at::Tensor &t) { return t.numel() ? t.data_ptr() : kNothing; }

@@ -5,7 +5,7 @@
 //   s_j = c q_i . k_j,   out_i = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m)
 // over the L_b cached keys, whose rows are code * scale, and over the node itself and its ancestors among the bf16 tree rows.
 //
-// Few query rows a kv head (up to 16; more: tree_attn_packed_umma.cu).  Every warp takes a part of the list of work (packed_list.cuh) by itself, in units of 32 keys,
+// Few query rows a kv head (up to 16, up to 32 of a short list; more: tree_attn_packed_umma.cu).  Every warp takes a part of the list of work (packed_list.cuh) by itself, in units of 32 keys,
 // with its own maximum, sum and accumulators; nothing in a CTA waits for anything else of it.
 //
 // A warp keeps its queries in registers as tensor-core operands (fp16, each row scaled by a power of two, which is exact).  A unit's codes and
