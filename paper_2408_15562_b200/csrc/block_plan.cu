@@ -109,7 +109,7 @@ block_plan_kernel(const PlanArgs a)
     const bool fits = s_bad == 0 && free0 >= 0 && free0 + total[2] <= a.n_blocks && total[1] <= free0 + total[2] && total[0] <= a.max_rows;
     __syncthreads();
     const int step = n_cta * kPlanThreads, first = cta * kPlanThreads + tid;
-    if (!fits) {                         // the same verdict in every CTA: nothing is changed, no row has a slot
+    if (!fits) {                         // the same answer in every CTA: nothing is changed, no row has a slot
         if (first == 0) fspad_report(a.status, FSPAD_ERR_RANGE);
         for (int b = first; b <= a.B; b += step) a.row_start[b] = 0;
         for (long long r = first; r < a.max_rows; r += step) {
