@@ -5,7 +5,7 @@
 //   s_j = c q_i . k_j,   out_i = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m)
 // over the L_b cached keys, whose rows are code * scale, and over the node itself and its ancestors among the bf16 tree rows.
 //
-// Few query rows a kv head (up to 16, up to 32 of a short list; more: tree_attn_packed_umma.cu).  Every warp takes a part of the list of work (packed_list.cuh) by itself, in units of 32 keys,
+// Few query rows a kv head (up to 32, in tiles of 16; more: tree_attn_packed_umma.cu).  Every warp takes a part of the list of work (packed_list.cuh) by itself, in units of 32 keys,
 // with its own maximum, sum and accumulators; nothing in a CTA waits for anything else of it.
 //
 // A warp keeps its queries in registers as tensor-core operands (fp16, each row scaled by a power of two, which is exact).  A unit's codes and
@@ -492,20 +492,21 @@ template <int NT> cudaError_t launch_few(fspad_ctx *ctx, Args &a, cudaStream_t s
 
 }  // namespace
 
-// Which of the two kernels takes a call.  Up to 16 query rows a kv head this one does; up to 32, in two tiles, each of which takes the cache's codes apart for itself,
-// where the list is short, by what the table has room for (lengths are not known here).  us, this kernel and the other, 8 kv heads: 24 rows, one sequence 10 - 14
-// and 13 - 17 (32 to 4000 keys), four 11 - 24 and 14 - 27, sixteen of 700 keys (5900 units) 20 and 21, of 1500 30 and 29; 48 rows, sixteen of 300 keys 22 and 17;
-// 100 rows, one of 700 keys 19 and 16; 12 rows, sixteen of 32 to 1500 keys 12 - 22 and 13 - 29.
-static bool many_rows(const fspad_ctx *ctx, int N, int B, int bps)
+// Which of the two kernels takes a call.  Up to 32 query rows a kv head this one does (above 16 in two tiles, each of which takes the cache's codes apart for itself):
+// the other's fixed costs are for 128 rows, and paid for every (sequence, kv head).  us, this kernel and the other, 20 to 32 rows: one sequence of 8 kv heads, 300 to
+// 4000 keys 11 - 15 and 14 - 17, sixteen of 1500 27 and 36, thirty-two 43 and 59; sixteen of 32 heads and 300 keys 37 and 61; but thirty-two of 12000 keys 204
+// and 191.  A tree of more than 24 nodes without shared heads has so many keys of its own that few runs are better off there: 32 nodes, 8 heads, one
+// sequence of 300 to 4000 keys 17 - 21 and 15 - 17, four 18 - 28 and 15 - 23, but thirty-two 28 - 91 and 35 - 93.  48 rows: 32 heads, sixteen of 1500 keys 120 and 103, of 300 61 and 63.
+static bool many_rows(const fspad_ctx *ctx, int N, int B)
 {
     const fspad_config &c = ctx->cfg;
-    const long long M = (long long)N * (c.n_q_heads / c.n_kv_heads), units = 2ll * B * c.n_kv_heads * ((N + UNIT - 1) / UNIT + 4ll * bps);
-    return M > 32 || (M > 16 && units > 6000);
+    const long long M = (long long)N * (c.n_q_heads / c.n_kv_heads);
+    return M > 32 || (M > 16 && N > 24 && (long long)B * c.n_kv_heads <= ctx->sm_count);
 }
 
 size_t fspad_attn_packed_workspace(const fspad_ctx *ctx, int N, int B)
 {
-    // of either kernel: the choice depends on the table's width, too
+    // of either kernel, so that a workspace made for one call serves every other
     (void)N; (void)B;
     const size_t few = scratch_bytes<BM>(ctx->sm_count * MAX_WARPS), many = fspad_attn_packed_umma_workspace(ctx);
     return few > many ? few : many;
@@ -535,7 +536,7 @@ cudaError_t fspad_launch_tree_attn_packed(fspad_ctx *ctx, const fspad_bf16 *q, c
     a.by_G.set((unsigned)a.G); a.by_tiles.set((unsigned)a.mtiles);
     a.scale_log2 = ctx->scale * kLog2e;
     a.out = out; a.status = ctx->d_status;
-    if (many_rows(ctx, N, B, paged.stride)) return fspad_launch_attn_packed_umma(ctx, a, workspace, st);
+    if (many_rows(ctx, N, B)) return fspad_launch_attn_packed_umma(ctx, a, workspace, st);
     scratch_in<BM>(a, ctx->sm_count * MAX_WARPS, workspace);
     return a.M <= 8 ? launch_few<1>(ctx, a, st) : launch_few<2>(ctx, a, st);
 }
