@@ -292,20 +292,23 @@ tree_attn_packed_umma_kernel(const Args a)
                 const int key0 = tree ? u * UNIT : (u - nt) * UNIT;
                 const bool masked = tree || key0 + UNIT > s.L;
                 uint32_t see[4] = {~0u, ~0u, ~0u, ~0u};
-                if (masked) {
-                    unsigned long long see0 = 0ull, see1 = 0ull;
-                    if (tree) {
-                        for (int at = node; at >= key0; at = s_par[at]) {
-                            const unsigned o = (unsigned)(at - key0);
-                            if (o < 64u) see0 |= 1ull << o;
-                            else if (o < 128u) see1 |= 1ull << (o - 64u);
+                if (tree) {
+                    // from the node up, word by word, for an ancestor comes before its descendants (with two words of 64 bits a step took three times as long:
+                    // 22 chains of 156 nodes, 32 heads, 186 us against 117; trees of ten nodes' depth 54 and 51)
+                    int at = node;
+                    while (at >= key0 + 128) at = s_par[at];
+#pragma unroll
+                    for (int x = 3; x >= 0; --x) {
+                        see[x] = 0u;
+                        while (at >= key0 + 32 * x) {
+                            see[x] |= 1u << (at & 31);
+                            at = s_par[at];
                         }
-                    } else {
-                        const int left = s.L - key0;         // 1 .. 127
-                        see0 = left >= 64 ? ~0ull : (1ull << left) - 1ull;
-                        see1 = left > 64 ? (1ull << (left - 64)) - 1ull : 0ull;
                     }
-                    see[0] = (uint32_t)see0; see[1] = (uint32_t)(see0 >> 32); see[2] = (uint32_t)see1; see[3] = (uint32_t)(see1 >> 32);
+                } else if (masked) {
+                    const int left = s.L - key0;             // 1 .. 127
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) see[x] = left >= 32 * x + 32 ? ~0u : left > 32 * x ? (1u << (left - 32 * x)) - 1u : 0u;
                 }
                 if (!failed && !mbar_wait(bar(S_FULL + grp), ph_s)) failed = true;
                 ph_s ^= 1u;

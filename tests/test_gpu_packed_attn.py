@@ -362,3 +362,12 @@ def test_a_captured_step_replayed_is_the_step_called():
     called.ctx.check()
     replayed.ctx.check()
     assert replayed.length.tolist() == [10, 131, 255]
+
+
+@pytest.mark.parametrize("nodes", [8, 15, 16, 17, 24, 25, 32, 33])
+@pytest.mark.parametrize("tree", ["random", "chain"])
+@pytest.mark.parametrize("batch", [2, 170])
+def test_around_the_line_between_the_kernels(nodes, tree, batch):
+    """Up to 32 rows a kv head, and from 25 nodes on by the number of runs: on both sides of it."""
+    case = Case(22, batch, nodes, 2, 2, [(37 * b) % 140 for b in range(batch)], tree=tree)
+    case.check(_run(case))
