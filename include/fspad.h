@@ -520,8 +520,8 @@ int fspad_kv_append_packed(fspad_ctx *ctx, uint8_t *codes, uint8_t *scales, cons
  *              until this one is done
  * Single-precision accumulation and softmax.  A tree row of V with an infinity or a NaN makes the outputs of the nodes that see it NaN, and of
  * no others; so does such a row of K.  Errors: FSPAD_ERR_RANGE for a workspace that is too small, and, in the status word, for a
- * prefix length or a table entry out of range; FSPAD_ERR_TOO_LARGE where batch * Hkv * ceil(n_nodes * Hq / Hkv / 16) * (4 blocks_per_seq + ceil(n_nodes / 32)) does not fit
- * 32 bits; otherwise as fspad_tree_attn_paged.
+ * prefix length or a table entry out of range; FSPAD_ERR_TOO_LARGE where batch * Hkv * ceil(n_nodes * Hq / Hkv / 16) * (4 blocks_per_seq + ceil(n_nodes / 32)) is not below
+ * 2^31 - 10^6; otherwise as fspad_tree_attn_paged.
  */
 size_t fspad_tree_attn_packed_workspace_bytes(const fspad_ctx *ctx, int n_nodes, int batch);
 int fspad_tree_attn_packed(fspad_ctx *ctx, const fspad_bf16 *q, const uint8_t *codes, const uint8_t *scales, int layer,
