@@ -415,19 +415,14 @@ class Context:
                          stream=None):
         """Tree-masked attention of q [B][N][Hq][128] over a layer of the 4-bit cache and the tree's bf16 rows [B][Hkv][N][128].  Without
         `workspace` (uint8) the context's own is used: no two such calls, captured ones among them, may then run at the same time."""
-        if workspace is None:
-            workspace = self._workspace
-            if workspace is None:
-                workspace = self._workspace = self._make_workspace(q.device, stream)
-        return self._packed_call("tree_attn_packed", stream, q, codes, scales, block_table, tree_k, tree_v, parent, prefix_len, layer, out, workspace)
+        r = self._packed_call("tree_attn_packed", stream, q, codes, scales, block_table, tree_k, tree_v, parent, prefix_len, layer, out,
+                              self._workspace if workspace is None else workspace)
+        if type(r) is tuple:         # (the first call's: it lives as long as the context, so that a captured call's stays where it is)
+            r, self._workspace = r
+        return r
 
     def tree_attn_packed_workspace_bytes(self, n_nodes: int, batch: int) -> int:
         return int(load().fspad_tree_attn_packed_workspace_bytes(self._h, n_nodes, batch))
-
-    def _make_workspace(self, device, stream):
-        """Of the largest call; it lives as long as the context, so that a captured call's stays where it is."""
-        with torch.cuda.stream(stream):          # (None: the current one)
-            return torch.empty((max(self.tree_attn_packed_workspace_bytes(self.cfg.max_nodes, self.cfg.max_batch), 16),), dtype=torch.uint8, device=device)
 
 
 def accept_stats_noalloc(logits, temperature, rows_per_seq, out, stream=None) -> int:

@@ -436,11 +436,21 @@ PyObject *call_tree_attn_packed(PyObject *, PyObject *const *args, Py_ssize_t n)
         const auto *parent = static_cast<const int32_t *>(c.data("parent", a[6], kI32, {B, N})), *len = static_cast<const int32_t *>(c.data("prefix_len", a[7], kI32, {B}));
         at::Tensor out;
         c.outputs(&out, {{"out", a[9], kBf, {B, N, c.hq, 128}}});
-        const at::Tensor *ws = c.tensor("workspace", a[10], at::kByte);
+        // none given: one is made, once everything else has been looked at, and goes back with the output (its size is the same for every call of a context;
+        // a context that is none has none, and the library refuses the call)
+        at::Tensor ws;
+        const bool make = a[10] == Py_None;
+        if (make) {
+            const long long bytes = (long long)fspad_tree_attn_packed_workspace_bytes(c.ctx, (int)c.max_nodes, 0);
+            if (bytes > 0) c.outputs(&ws, {{"workspace", Py_None, at::kByte, {bytes}}});
+        } else if (const at::Tensor *t = c.tensor("workspace", a[10], at::kByte)) {
+            ws = *t;
+        }
         if (!c.ok) return nullptr;
-        rc = unlocked([&] { return fspad_tree_attn_packed(c.ctx, as<fspad_bf16>(*q), codes, scales, layer, table, bps, nb, tk, tv, parent, len, (int)N, (int)B, as<fspad_bf16>(out), address(*ws),
-                                                           (size_t)ws->numel(), c.stream); });
-        return rc ? nullptr : THPVariable_Wrap(out);
+        rc = unlocked([&] { return fspad_tree_attn_packed(c.ctx, as<fspad_bf16>(*q), codes, scales, layer, table, bps, nb, tk, tv, parent, len, (int)N, (int)B, as<fspad_bf16>(out),
+                                                           ws.defined() ? address(ws) : nullptr, ws.defined() ? (size_t)ws.numel() : 0, c.stream); });
+        if (rc) return nullptr;
+        return make ? Py_BuildValue("(NN)", THPVariable_Wrap(out), THPVariable_Wrap(ws)) : THPVariable_Wrap(out);
     });
 }
 
