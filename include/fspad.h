@@ -495,8 +495,8 @@ int fspad_kv_write_packed(fspad_ctx *ctx, const fspad_bf16 *k, const fspad_bf16 
 
 /*
  * fspad_kv_append for the 4-bit cache: for every layer, K and V, sequence b and kv head, cache row L_b + j receives
- * tree_kv[..][accepted_path[b][j]], j = 0 .. n_accepted[b] - 1.  new_len[b] = L_b + n_accepted[b] (may be NULL, but not
- * prefix_len: FSPAD_ERR_RANGE).
+ * tree_kv[..][accepted_path[b][j]], j = 0 .. n_accepted[b] - 1.  new_len[b] = L_b + n_accepted[b] (may be NULL, but must not
+ * overlap prefix_len, n_accepted, accepted_path or block_table: FSPAD_ERR_RANGE).
  *
  *   tree_kv [n_layers][2][batch][Hkv][n_nodes][128] bf16;  accepted_path [batch][max_nodes], n_accepted, prefix_len, new_len [batch] int32
  *   rounded as tree_kv or NULL: receives the values that are kept, at the nodes' own places (other nodes: unchanged); may be tree_kv, if no node

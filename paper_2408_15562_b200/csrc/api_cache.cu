@@ -17,6 +17,12 @@ int check_device(const fspad_ctx *ctx)
     if (cudaGetDevice(&d) != cudaSuccess) return FSPAD_ERR_CUDA;
     return d == ctx->device ? FSPAD_OK : FSPAD_ERR_DEVICE;
 }
+// Whether two arrays of so many bytes share any.
+bool overlap(const void *a, size_t na, const void *b, size_t nb)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return na > 0 && nb > 0 && (x < y ? y - x < na : x - y < nb);
+}
 int result(cudaError_t e) { return e == cudaSuccess ? FSPAD_OK : FSPAD_ERR_CUDA; }
 
 int check_tree(const fspad_ctx *ctx, int n_nodes, int batch)
@@ -115,7 +121,10 @@ int fspad_kv_append_packed(fspad_ctx *ctx, uint8_t *codes, uint8_t *scales, cons
     if (misaligned(codes) || misaligned(scales) || misaligned(tree_kv) || misaligned(rounded)) return FSPAD_ERR_ALIGN;
     if ((rc = check_blocks(blocks_per_seq, n_blocks)) != 0) return rc;
     if (batch == 0) return FSPAD_OK;
-    if (new_len == prefix_len) return FSPAD_ERR_RANGE;         // (other warps still read it)
+    const size_t word = sizeof(int32_t), seqs = word * batch;
+    if (new_len && (overlap(new_len, seqs, prefix_len, seqs) || overlap(new_len, seqs, n_accepted, seqs) ||         // (other warps still read them)
+                    overlap(new_len, seqs, accepted_path, seqs * ctx->cfg.max_nodes) || overlap(new_len, seqs, block_table, seqs * blocks_per_seq)))
+        return FSPAD_ERR_RANGE;
     const FspadPaged pg{block_table, blocks_per_seq, n_blocks};
     return result(fspad_launch_kv_append_packed(ctx, codes, scales, pg, tree_kv, accepted_path, n_accepted, prefix_len, n_nodes, batch,
                                                 rounded, new_len, fspad_stream(stream)));
