@@ -487,7 +487,8 @@ int fspad_block_plan(fspad_ctx *ctx, const int32_t *len, const int32_t *add, con
  *   k, v   [Hkv][rows][128] bf16 (what fspad_rope_qkv writes for batch = 1)
  *   slots  [rows] int64: block * 128 + row of the block (fspad_block_plan); -1: the row is left out.  No slot may occur twice.
  *   layer  0 .. n_layers - 1;  codes, scales, n_blocks as above
- *   k_rounded, v_rounded [Hkv][rows][128] bf16 or both NULL: receive the values that are kept (rows left out: unchanged); may be k and v
+ *   k_rounded, v_rounded [Hkv][rows][128] bf16 or both NULL: receive the values that are kept (rows left out: unchanged); may be k and v, in this order;
+ *          otherwise they must not overlap k, v or one another (FSPAD_ERR_RANGE)
  * A slot outside the cache sets FSPAD_ERR_RANGE in the status word and its row is left out.
  */
 int fspad_kv_write_packed(fspad_ctx *ctx, const fspad_bf16 *k, const fspad_bf16 *v, const int64_t *slots, int rows, int layer,

@@ -106,6 +106,10 @@ int fspad_kv_write_packed(fspad_ctx *ctx, const fspad_bf16 *k, const fspad_bf16 
     if (rows < 0 || layer < 0 || layer >= ctx->cfg.n_layers || n_blocks < 1) return FSPAD_ERR_SHAPE;
     if ((int64_t)rows * ctx->cfg.n_kv_heads > INT_MAX) return FSPAD_ERR_TOO_LARGE;
     if (rows == 0) return FSPAD_OK;
+    const size_t n = (size_t)rows * ctx->cfg.n_kv_heads * FSPAD_HEAD_DIM * sizeof(fspad_bf16);
+    if (k_rounded && (overlap(k_rounded, n, v, n) || overlap(v_rounded, n, k, n) || overlap(k_rounded, n, v_rounded, n) ||       // (K and V go at the same time)
+                      (k_rounded != k && overlap(k_rounded, n, k, n)) || (v_rounded != v && overlap(v_rounded, n, v, n))))
+        return FSPAD_ERR_RANGE;
     return result(fspad_launch_kv_write_packed(ctx, k, v, reinterpret_cast<const long long *>(slots), rows, layer, codes, scales, n_blocks,
                                                k_rounded, v_rounded, fspad_stream(stream)));
 }
