@@ -501,7 +501,7 @@ int fspad_kv_write_packed(fspad_ctx *ctx, const fspad_bf16 *k, const fspad_bf16 
  *
  *   tree_kv [n_layers][2][batch][Hkv][n_nodes][128] bf16;  accepted_path [batch][max_nodes], n_accepted, prefix_len, new_len [batch] int32
  *   rounded as tree_kv or NULL: receives the values that are kept, at the nodes' own places (other nodes: unchanged); may be tree_kv, if no node
- *   occurs twice in a path (on a path of a tree none does)
+ *   occurs twice in a path (on a path of a tree none does), and must not overlap it otherwise (FSPAD_ERR_RANGE)
  * Blocks of the written rows must not be shared.  A path entry outside [0, n_nodes), n_accepted outside [0, n_nodes],
  * L_b + n_accepted[b] > 128 * blocks_per_seq or a table entry out of range set FSPAD_ERR_RANGE in the status word and the rows
  * concerned are left out.

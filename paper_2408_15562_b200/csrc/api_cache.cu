@@ -129,6 +129,8 @@ int fspad_kv_append_packed(fspad_ctx *ctx, uint8_t *codes, uint8_t *scales, cons
     if (new_len && (overlap(new_len, seqs, prefix_len, seqs) || overlap(new_len, seqs, n_accepted, seqs) ||         // (other warps still read them)
                     overlap(new_len, seqs, accepted_path, seqs * ctx->cfg.max_nodes) || overlap(new_len, seqs, block_table, seqs * blocks_per_seq)))
         return FSPAD_ERR_RANGE;
+    const size_t tree = (size_t)ctx->cfg.n_layers * 2 * batch * ctx->cfg.n_kv_heads * n_nodes * FSPAD_HEAD_DIM * sizeof(fspad_bf16);
+    if (rounded && rounded != tree_kv && overlap(rounded, tree, tree_kv, tree)) return FSPAD_ERR_RANGE;
     const FspadPaged pg{block_table, blocks_per_seq, n_blocks};
     return result(fspad_launch_kv_append_packed(ctx, codes, scales, pg, tree_kv, accepted_path, n_accepted, prefix_len, n_nodes, batch,
                                                 rounded, new_len, fspad_stream(stream)));

@@ -28,3 +28,12 @@ def test_kept_values_of_a_write(lib, k, v, kr, vr, refused):  # noqa: F811
     """K and V go at the same time: what is kept of one must not lie where the other is read or written, and in its own rows' place only row by row."""
     rc, log = run(lib, "kv_write_packed", k=k, v=v, k_rounded=kr, v_rounded=vr)
     assert (rc, len(log)) == ((ERR["RANGE"], 0) if refused else (0, 1))
+
+
+KEPT = LAYERS * 2 * 2 * HKV * NODES * 256  # bytes of tree_kv for two sequences
+
+
+@pytest.mark.parametrize("rounded,refused", [(A, False), (B, False), (A + KEPT, False), (A + 16, True), (A - 16, True), (A + KEPT - 16, True)])
+def test_kept_values_of_an_append(lib, rounded, refused):  # noqa: F811
+    rc, log = run(lib, "kv_append_packed", tree_kv=A, rounded=rounded)
+    assert (rc, len(log)) == ((ERR["RANGE"], 0) if refused else (0, 1))
