@@ -17,6 +17,17 @@ int check_device(const fspad_ctx *ctx)
     if (cudaGetDevice(&d) != cudaSuccess) return FSPAD_ERR_CUDA;
     return d == ctx->device ? FSPAD_OK : FSPAD_ERR_DEVICE;
 }
+// Frequencies of the rotary pairs in turns a position.  Each host thread keeps those of its last theta (64 powers take 3 us): kept in the context, calls of two
+// threads with a theta each got a mixture.
+void rope_turns(double theta, double (&to)[FSPAD_HEAD_DIM / 2])
+{
+    thread_local double last = 0.0, turns[FSPAD_HEAD_DIM / 2];       // (no theta is 0)
+    if (last != theta) {
+        for (int i = 0; i < FSPAD_HEAD_DIM / 2; ++i) turns[i] = std::pow(theta, -2.0 * i / FSPAD_HEAD_DIM) / (2.0 * 3.14159265358979323846);
+        last = theta;
+    }
+    std::memcpy(to, turns, sizeof turns);
+}
 // Whether two arrays of so many bytes share any.
 bool overlap(const void *a, size_t na, const void *b, size_t nb)
 {
@@ -68,11 +79,7 @@ int fspad_rope_qkv(fspad_ctx *ctx, const fspad_bf16 *qkv, int64_t row_stride, co
     if (batch == 0) return FSPAD_OK;
     if (q == qkv || k == qkv || v == qkv || q == k || q == v || k == v) return FSPAD_ERR_RANGE;
     FspadRopeTable t;
-    if (ctx->rope_theta != theta) {
-        for (int i = 0; i < half; ++i) ctx->rope_turns[i] = std::pow(theta, -2.0 * i / FSPAD_HEAD_DIM) / (2.0 * 3.14159265358979323846);
-        ctx->rope_theta = theta;
-    }
-    std::memcpy(t.turns, ctx->rope_turns, sizeof t.turns);
+    rope_turns(theta, t.turns);
     t.split0 = sec_t;
     t.split1 = sec_t + sec_h;
     return result(fspad_launch_rope_qkv(ctx, qkv, row_stride, positions, start, parent, n_nodes, batch, t, adjacent != 0, q, k, v,

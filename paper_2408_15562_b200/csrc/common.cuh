@@ -58,7 +58,6 @@ struct fspad_ctx {
     int lm_attr_done;
     int fs_attr_done;         // dynamic shared-memory limit raised for the Feature Sampler's product kernel
     int packed_attr_done;     // ... for the kernels of the attention over the 4-bit cache, a bit each
-    double rope_theta, rope_turns[FSPAD_HEAD_DIM / 2];       // the rotary frequencies of the last theta (64 powers: 3 us)
 
     void *dx_part;            // draft step: per-piece top-k lists [max_batch * 16 rows][pieces][16], 64-bit sort keys (0: none)
     int *dx_done;             // draft step: finished pieces of each sequence [max_batch]; zero between calls
