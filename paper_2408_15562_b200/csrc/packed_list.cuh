@@ -11,9 +11,15 @@
 namespace packed {
 
 constexpr int D = FSPAD_HEAD_DIM;
-constexpr float kLazyLog2 = 8.f;         // a row's reference maximum may lag its true maximum by this much (log2)
-// Weights are 2^(score - reference + 7), at most 2^15 with the lag: as fp16 operands they keep their 11 bits down to 2^-21 of the reference's own.
+// (With a lag of 4 the accumulators are rescaled so often that one tree of 60 nodes and 64 heads over 8, 32700 keys, takes 90.5 us, not 87.5; a longer one leaves kDown no exact form.)
+constexpr float kLazyLog2 = 7.f;         // a row's reference maximum may lag its true maximum by this much (log2)
+// Weights are 2^(score - reference + 7), at most 2^14 with the lag: as fp16 operands they keep their 11 bits down to 2^-21 of the reference's own.
 constexpr float kBiasLog2 = 7.f;
+// What is added up is a row of V times 2^-14 of its weight, so at most the row itself: V of the tree may be of any size, and 2^14 times it beyond 32 bits.  The
+// cache's V goes into its products times 2^-14, which is exact (it is a multiple of 2^-10, and fp16's least value is 2^-24); of the tree's keys the weights do.
+constexpr float kDown = 0x1p-14f, kUp = 0x1p14f;
+constexpr uint32_t kDown2 = 0x04000400u, kOne2 = 0x3c003c00u;        // 2^-14 and 1, a pair in fp16
+static_assert(kLazyLog2 + kBiasLog2 == 14.f && kDown * kUp == 1.f, "of the tree's keys the weights are 2^(score - reference - kLazyLog2)");
 constexpr float kLog2e = 1.4426950408889634f;
 
 // Division by a number that the host knows: x / d = (x * mul) >> 32 >> shift for 0 <= x < 2^31 (d of s bits: mul = 2^(31 + s) / d rounded up, which is off
@@ -327,7 +333,7 @@ tree_attn_packed_merge_kernel(const Args a, int rows, int parts)
             }
         }
         if (warp < rows && there) {
-            const float inv = 1.f / l;
+            const float inv = kUp / l;
             const int node = a.by_G.of(gr);
             *reinterpret_cast<uint2 *>(a.out + (((size_t)run.x * a.N + node) * a.Hq + run.y * a.G + (gr - node * a.G)) * D + 4 * lane) =
                 make_uint2(umma::pack_bf16(acc.x * inv, acc.y * inv), umma::pack_bf16(acc.z * inv, acc.w * inv));

@@ -189,9 +189,11 @@ tree_attn_packed_kernel(const Args a)
 #pragma unroll
         for (int x = 0; x < NT; ++x) m_run[x][0] = m_run[x][1] = -INFINITY, l_run[x][0] = l_run[x][1] = 0.f;
 
-        // scores (masked; `to_log2` of each row's makes log2 units of them) of 16 T keys -> weights; the row's reference follows its maximum where that is far ahead of it
-        auto softmax = [&](auto &s, const float (&to_log2)[NT][2], auto tiles) {
+        // scores (masked; `to_log2` of each row's makes log2 units of them) of 16 T keys -> weights, of the tree's times kDown; the row's reference follows its maximum
+        // where that is far ahead of it
+        auto softmax = [&](auto &s, const float (&to_log2)[NT][2], auto tiles, auto tree) {
             constexpr int T = decltype(tiles)::value;
+            constexpr bool of_tree = decltype(tree)::value;
 #pragma unroll
             for (int x = 0; x < NT; ++x) {
                 float mx[2] = {-INFINITY, -INFINITY};
@@ -224,14 +226,14 @@ tree_attn_packed_kernel(const Args a)
                 }
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
-                    const float ref = m_run[x][y] == -INFINITY ? 0.f : kBiasLog2 - m_run[x][y];
+                    const float bias = of_tree ? -kLazyLog2 : kBiasLog2, ref = m_run[x][y] == -INFINITY ? 0.f : bias - m_run[x][y];
 #pragma unroll
                     for (int t = 0; t < T; ++t)
 #pragma unroll
                         for (int z = 0; z < 4; z += 2) {
                             const float p = ex2f(fmaf(s[t][x][y + z], to_log2[x][y], ref));
                             s[t][x][y + z] = p;
-                            l_run[x][y] += p;
+                            l_run[x][y] = of_tree ? fmaf(p, kUp, l_run[x][y]) : l_run[x][y] + p;
                         }
                 }
             }
@@ -311,7 +313,7 @@ tree_attn_packed_kernel(const Args a)
             float plain[NT][2];
 #pragma unroll
             for (int x = 0; x < NT; ++x) plain[x][0] = plain[x][1] = a.scale_log2;
-            softmax(s, plain, std::integral_constant<int, 1>());
+            softmax(s, plain, std::integral_constant<int, 1>(), std::true_type());
             // A row of V with an infinity or a NaN in it must not reach the queries that do not see it (0 times it is a NaN): it is taken
             // out of the product, and the queries that do see it get NaN.
             uint32_t keys = 0;
@@ -415,7 +417,7 @@ tree_attn_packed_kernel(const Args a)
 #pragma unroll
                             for (int x = 0; x < NT; ++x) s[t][x][y] = -INFINITY;
             }
-            softmax(s, cs, std::integral_constant<int, 2>());
+            softmax(s, cs, std::integral_constant<int, 2>(), std::false_type());
             each<2>([&](auto t_) {
                 constexpr int t = decltype(t_)::value;
                 uint32_t p[NT][2];
@@ -433,7 +435,7 @@ tree_attn_packed_kernel(const Args a)
                         if (16 * t + 8 * y + key_of(2 * c) >= left) sa[y] = 0u;
                         if (16 * t + 8 * y + key_of(2 * c + 1) >= left) sb[y] = 0u;
                     }
-                    sc[y] = fspad_e4m3_to_f16(sb[y] * 256u + sa[y]);
+                    sc[y] = fspad_hmul2(fspad_e4m3_to_f16(sb[y] * 256u + sa[y]), kDown2);
                 }
 #pragma unroll
                 for (int i2 = 0; i2 < 2; ++i2) {     // elements 16 g + 8 i2 ..
@@ -480,7 +482,7 @@ tree_attn_packed_kernel(const Args a)
                 if (gr >= a.M) continue;
                 if (whole) {
                     const int node = a.by_G.of(gr);
-                    const float inv = 1.f / l;
+                    const float inv = kUp / l;
                     uint4 *dst = reinterpret_cast<uint4 *>(a.out + ((size_t)(b * a.N + node) * a.Hq + h * a.G + (gr - node * a.G)) * D + 16 * g);
 #pragma unroll
                     for (int j = 0; j < 8; j += 4)

@@ -112,7 +112,8 @@ __device__ __forceinline__ void softmax_chunk(bool tree, uint32_t tS, uint32_t t
         }
     }
     m_run = m_new;
-    const uint64_t scale2 = f32x2(cs, cs), neg = f32x2(kBiasLog2 - m_safe, kBiasLog2 - m_safe);
+    const float shift = (tree ? -kLazyLog2 : kBiasLog2) - m_safe;        // (of the tree's keys times kDown)
+    const uint64_t scale2 = f32x2(cs, cs), neg = f32x2(shift, shift);
     uint64_t acc[4] = {0ull, 0ull, 0ull, 0ull};
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
@@ -130,7 +131,7 @@ __device__ __forceinline__ void softmax_chunk(bool tree, uint32_t tS, uint32_t t
     }
     float lo, hi;
     f32x2_split(f32x2_add(f32x2_add(acc[0], acc[1]), f32x2_add(acc[2], acc[3])), lo, hi);
-    l_run += lo + hi;
+    l_run += (lo + hi) * (tree ? kUp : 1.f);
 }
 
 __global__ void __launch_bounds__(NT, 1)
@@ -357,7 +358,7 @@ tree_attn_packed_umma_kernel(const Args a)
             }
             __syncwarp();
             if (whole) {
-                const float inv = 1.f / l_fin;
+                const float inv = kUp / l_fin;
                 f0 *= inv;
                 f1 *= inv;
             }
@@ -600,7 +601,7 @@ tree_attn_packed_umma_kernel(const Args a)
                         const uint32_t st = n % STAGES;
                         if (cc >= 2 && !mbar_wait(bar((plane ? V_FREE : K_FREE) + slot), ((cc >> 1) - 1u) & 1u)) { failed = true; break; }
                         if (!mbar_wait(bar(ST_FULL + st), (n / STAGES) & 1u)) { failed = true; break; }
-                        const uint32_t from = sStage + st * STAGE, to = (plane ? sV : sK) + slot * TILE;
+                        const uint32_t from = sStage + st * STAGE, to = (plane ? sV : sK) + slot * TILE, down = plane ? kDown2 : kOne2;
                         // a lane takes a block of 16: blocks 4 x + (lane & 3) of eight rows at a time, so that the stores do not collide
                         uint32_t w0[8], w1[8], sc[8];        // (all of them under way before the first is used)
 #pragma unroll
@@ -613,7 +614,7 @@ tree_attn_packed_umma_kernel(const Args a)
                         for (int k = 0; k < 8; ++k) {
                             const int r = w4 * 32 + (k >> 1) * 8 + (lane >> 2), blk = 4 * (k & 1) + (lane & 3);
                             if (r >= left) sc[k] = 0u;       // what lies behind the end may be anything: zeros
-                            const uint32_t s2 = fspad_e4m3_to_f16(sc[k] * 0x101u);
+                            const uint32_t s2 = fspad_hmul2(fspad_e4m3_to_f16(sc[k] * 0x101u), down);
                             uint32_t f0[4], f1[4];
                             fspad_e2m1_to_f16(w0[k], f0);
                             fspad_e2m1_to_f16(w1[k], f1);
