@@ -519,9 +519,15 @@ int fspad_kv_append_packed(fspad_ctx *ctx, uint8_t *codes, uint8_t *scales, cons
  *   layer  of the cache;  parent [batch][n_nodes], prefix_len [batch] int32, 0 <= L_b <= 128 * blocks_per_seq
  *   workspace  of at least fspad_tree_attn_packed_workspace_bytes(ctx, n_nodes, batch) bytes, scratch: no other call may use it
  *              until this one is done
- * Single-precision accumulation and softmax: scores q.k beyond its range are infinities, sum_j exp(s_j - max s) |v_j| must lie in it, and results below about
- * 2^-110 lose bits.  A tree row of V with an infinity or a NaN makes the outputs of the nodes that see it NaN, and of
- * no others; so does such a row of K.  Errors: FSPAD_ERR_RANGE for a workspace that is too small, and, in the status word, for a
+ * Single-precision scores, softmax and sums: scores q.k beyond its range are infinities, sum_j exp(s_j - max s) |v_j| must lie
+ * in it, and results below about 2^-110 lose bits.  For the product with V the weights are rounded, of the cache's keys to fp16,
+ * of the tree's to bf16; against the cache the queries are fp16 scaled by a power of two, exact for elements of at least 2^-31 of
+ * the row's largest.
+ * A tree row of V with an infinity or a NaN makes the outputs of the nodes that see it NaN, and of no others.  In K such an
+ * element acts through the score, for the same nodes: NaN and +infinity make the output NaN, with -infinity the row has no
+ * weight (where no row has any, the output is NaN).  A block of the cache that reads as NaN is seen by all queries of its
+ * sequence and kv head: in K it makes their outputs NaN, in V the block's 16 elements of them.
+ * Errors: FSPAD_ERR_RANGE for a workspace that is too small, and, in the status word, for a
  * prefix length or a table entry out of range; FSPAD_ERR_TOO_LARGE where batch * Hkv * ceil(n_nodes * Hq / Hkv / 16) * (4 blocks_per_seq + ceil(n_nodes / 32)) is not below
  * 2^31 - 10^6; otherwise as fspad_tree_attn_paged.
  */
