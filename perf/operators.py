@@ -167,6 +167,13 @@ def _gen(seed):
 
 
 def prepare(case, seed):
+    s = _inputs(case, seed)
+    if own:
+        s["ctx"] = _context(case)
+    return s
+
+
+def _inputs(case, seed):
     g, rng, kind = _gen(seed), np.random.RandomState(seed % (1 << 31)), case["kind"]
     i32 = lambda a: torch.from_numpy(np.ascontiguousarray(a, np.int32)).cuda()  # noqa: E731
     s = dict(case=case)
@@ -238,19 +245,16 @@ def run(s):
     return {"rope": _rope, "plan": _plan, "write": _write, "append": _append, "attn": _attn}[kind](s)
 
 
-def _context(s, **more):
+def _context(c):
     """The handle that a program makes once and keeps."""
-    if "ctx" not in s:
-        from paper_2408_15562_b200 import binding
-        c = s["case"]
-        hkv = c.get("hkv", 1)
-        s["ctx"] = binding.Context(c.get("hq", hkv), hkv, 16, 256, max_nodes=min(256, c.get("nodes", 1)), max_batch=c.get("batch", 1),
-                                   n_layers=c.get("layers", 1))
-    return s["ctx"]
+    from paper_2408_15562_b200 import binding
+    hkv = c.get("hkv", 1)
+    return binding.Context(c.get("hq", hkv), hkv, 16, 256, max_nodes=min(256, c.get("nodes", 1)), max_batch=c.get("batch", 1),
+                           n_layers=c.get("layers", 1))
 
 
 def _own(s, kind):
-    ctx = _context(s)
+    ctx = s["ctx"]
     if kind == "rope":
         q, k, v = ctx.rope_qkv(s["qkv"], s["theta"], s["sections"], parent=s["parent"], start=s["start"], positions=s["positions"],
                                adjacent=bool(s["case"]["adjacent"]))
@@ -409,7 +413,7 @@ def _attn(s):
 
 
 def exact(case, seed):
-    s, kind = prepare(case, seed), case["kind"]
+    s, kind = _inputs(case, seed), case["kind"]
     if kind == "plan":
         return None
     if kind == "rope":
