@@ -417,6 +417,22 @@ tree_attn_packed_kernel(const Args a)
 #pragma unroll
                             for (int x = 0; x < NT; ++x) s[t][x][y] = -INFINITY;
             }
+            uint32_t scv[2][2];                      // scales of V, times kDown, of columns 2c.. and 2c + 8.. of the two sixteens of keys
+            auto scales_v = [&](auto t_) {
+                constexpr int t = decltype(t_)::value;
+                uint32_t sa[2] = {ld1<t * 128>(at_sa), ld1<t * 128 + 64>(at_sa)}, sb[2] = {ld1<t * 128>(at_sb), ld1<t * 128 + 64>(at_sb)};
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    // what lies behind the sequence's end may be anything, and 0 times a NaN is one: its scale is zero
+                    if (left < UNIT) {
+                        if (16 * t + 8 * y + key_of(2 * c) >= left) sa[y] = 0u;
+                        if (16 * t + 8 * y + key_of(2 * c + 1) >= left) sb[y] = 0u;
+                    }
+                    scv[t][y] = fspad_hmul2(fspad_e4m3_to_f16(sb[y] * 256u + sa[y]), kDown2);
+                }
+            };
+            // (of two eights of rows ahead of the exponentials: 24 rows, 32 sequences of 12000 keys 8 kv heads 271 -> 266 us; of one eight there they cost 1.5 %)
+            if constexpr (NT > 1) each<2>(scales_v);
             softmax(s, cs, std::integral_constant<int, 2>(), std::false_type());
             each<2>([&](auto t_) {
                 constexpr int t = decltype(t_)::value;
@@ -427,16 +443,7 @@ tree_attn_packed_kernel(const Args a)
                     p[x][1] = transpose8(pack_f16(s[t][x][2], s[t][x][3]));
                 }
                 const uint2 w[4] = {ld8<t * 1024>(at_va), ld8<t * 1024>(at_vb), ld8<t * 1024 + 512>(at_va), ld8<t * 1024 + 512>(at_vb)};
-                uint32_t sa[2] = {ld1<t * 128>(at_sa), ld1<t * 128 + 64>(at_sa)}, sb[2] = {ld1<t * 128>(at_sb), ld1<t * 128 + 64>(at_sb)}, sc[2];
-#pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    // what lies behind the sequence's end may be anything, and 0 times a NaN is one: its scale is zero
-                    if (left < UNIT) {
-                        if (16 * t + 8 * y + key_of(2 * c) >= left) sa[y] = 0u;
-                        if (16 * t + 8 * y + key_of(2 * c + 1) >= left) sb[y] = 0u;
-                    }
-                    sc[y] = fspad_hmul2(fspad_e4m3_to_f16(sb[y] * 256u + sa[y]), kDown2);
-                }
+                if constexpr (NT == 1) scales_v(t_);
 #pragma unroll
                 for (int i2 = 0; i2 < 2; ++i2) {     // elements 16 g + 8 i2 ..
                     uint32_t f[2][2][4];             // [columns 2c.. / 2c + 8..][even / odd elements][pair of keys of element 2 j (+ 1)]
@@ -447,8 +454,8 @@ tree_attn_packed_kernel(const Args a)
                         fspad_e2m1_to_f16(((wa >> 4) & 0x0f0f0f0fu) | (wb & 0xf0f0f0f0u), f[y][1]);
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            f[y][0][j] = fspad_hmul2(f[y][0][j], sc[y]);
-                            f[y][1][j] = fspad_hmul2(f[y][1][j], sc[y]);
+                            f[y][0][j] = fspad_hmul2(f[y][0][j], scv[t][y]);
+                            f[y][1][j] = fspad_hmul2(f[y][1][j], scv[t][y]);
                         }
                     }
 #pragma unroll
