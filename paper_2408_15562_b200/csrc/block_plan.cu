@@ -4,8 +4,8 @@
 // One cluster does it all, in phases that a cluster barrier separates, so that no host round trip and no second launch is needed: every CTA
 // scans the (at most 1024) sequences for itself, a thread each; blocks of dropped sequences are pushed onto the free stack; blocks are popped
 // into the tables; then the rows' slots are written.  What bounds it is latency: for a step of a batch (16 sequences 4.0 us) the barriers and dependent
-// loads; for prompts the instructions of eight SMs besides (200 requests of up to 600 rows, 61000 in all, 11.0 us, 1 MB written; 16000 rows 5.6 us).  A
-// second launch for the rows alone, on all SMs, would cost a step of a batch more than it gives a prompt.
+// loads; for prompts the instructions of eight SMs besides (200 requests of up to 600 rows, 61000 in all, 11.1 us, 1 MB written; 16000 rows 5.6 us): a
+// second launch for the rows alone, on all SMs, where max_rows is large, is what would shorten those.
 #include "packed.cuh"
 
 namespace {

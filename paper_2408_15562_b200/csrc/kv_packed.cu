@@ -12,7 +12,8 @@
 // Bound by memory in the end, 256 bytes read and 72 written a row (256 more where the caller asks for the values that are kept), and by the issue of
 // instructions nearly as much (some 80 for eight elements; 84 % of the slots taken when they were 130).  Half a warp
 // takes a row, 16 bytes a lane, so that two lanes share a scale; four pairs of rows are in flight (two: 30.7 us against 29.4 on 16K rows of 8 heads, eight:
-// 33.7 against 33.1 when both were slower).  16K rows with the values kept 29.4 us, 5.2 TB/s; 64 paths of 24 nodes in 16 layers 45.3 us, 5.1 TB/s.
+// 33.7 against 33.1 when both were slower).  With the values kept, by the bytes of the rows that are: 16411 rows of 8 heads 29.8 us, 5.15 TB/s (a seventh of
+// them left out 29.2 us, 4.8 TB/s); 64 paths of up to 24 nodes in 16 layers 45.1 us, 5.0 TB/s.  Without, where nothing but the instructions is left: 23.6 us and 33.2 us, 3.7 and 3.8 TB/s.
 #include "packed.cuh"
 
 namespace {

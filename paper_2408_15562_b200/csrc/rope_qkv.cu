@@ -8,8 +8,9 @@
 // Bound by memory: a row is read and written once, Q in place order, K and V into the head-major layout of the tree arrays.  A
 // thread keeps the sines of eight pairs of one row in registers and takes those pairs of one head after the other, 32 bytes each way; how
 // many heads fall to a thread follows from how many rows there are, so that few rows still reach every SM.  What a thread needs of the first four heads
-// is asked for before positions and sines, which take as long as the loads.  8201 rows of 48 heads, three axes: 32.9 us, 6.1 TB/s, 94 % of the floor (with
-// the loads behind the sines 36.0); 60 nodes 3.8 us, a launch and three trips to memory in turn.
+// is asked for before positions and sines, which take as long as the loads.  8201 rows of 48 heads, three axes: 32.9 us, 6.1 TB/s, 95 % of the copy rate (with
+// the loads behind the sines 36.0); 60 nodes 3.9 us, a launch and three trips to memory in turn; 64 trees of 60 nodes 19.6 us, 4.8 TB/s: each CTA takes its
+// tree's depths for itself.
 #include "packed.cuh"
 
 namespace {
@@ -170,7 +171,7 @@ cudaError_t fspad_launch_rope_qkv(fspad_ctx *ctx, const fspad_bf16 *qkv, long lo
     if (groups > 65535) groups = 65535;
     a.heads_per = (int)((heads + groups - 1) / groups);
     // many rows: shorter CTAs, for the last ones leave SMs idle (8201 rows of 48 heads: 39.9 us with 16 heads a thread, 36.0 with 4 and 40.4 with 3, before the
-    // loads went ahead of the sines; trees, whose CTAs all take the depths again, do not gain: 64 of 60 nodes 21.8 us with 10 heads and 23.3 with 5)
+    // loads went ahead of the sines; trees, whose CTAs all take the depths again, did not gain: 64 of 60 nodes 21.8 us with 10 heads and 23.3 with 5)
     if (!tree && a.heads_per > 4) a.heads_per = 4;
     const dim3 grid((unsigned)tiles, (unsigned)((heads + a.heads_per - 1) / a.heads_per), (unsigned)seqs);
     auto kernel = tree ? (adjacent ? rope_qkv_kernel<true, true> : rope_qkv_kernel<true, false>)

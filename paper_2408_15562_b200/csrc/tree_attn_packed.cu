@@ -13,10 +13,10 @@
 // second trip through shared memory): the order of the elements within a product and of the keys within a unit is chosen so
 // that every lane reads 16 bytes of a row of K, and 8 of a row of V, and finds its operands in them.  The tree's rows are taken as bf16.
 //
-// What bounds it.  Long contexts: 32 tokens of 64 heads over 8, 4000 to 32000 keys, 136 us with the merge, 645 MB read at 4.7 TB/s (72 % of the measured copy
-// rate).  The integer pipe is 59 % busy and 65 % of the issue slots are taken: a unit of 32 keys takes some 660 instructions, 140 of them conversions of codes
-// and scales, which each element needs once however few rows there are; 16 warps an SM, with all registers taken, do not hide the rest.  Short ones:
-// one token over 2000 keys 8.4 us, of which the two launches, the list and the first trips to memory in turn are the most.
+// What bounds it.  Long contexts: 32 tokens of 64 heads over 8, 4000 to 32000 keys, 139 us with the merge (139 to 153 from one board to another), 645 MB read at
+// 4.65 TB/s (72 % of the measured copy rate).  The integer pipe is 59 % busy and 65 % of the issue slots are taken: a unit of 32 keys takes some 660 instructions,
+// 140 of them conversions of codes and scales, which each element needs once however few rows there are; 16 warps an SM, with all registers taken, do not hide the
+// rest.  Short ones: one token over 2000 keys 8.7 us, of which the two launches, the list and the first trips to memory in turn are the most.
 #include <type_traits>
 
 #include "packed_list.cuh"
@@ -525,9 +525,10 @@ template <int NT> cudaError_t launch_few(fspad_ctx *ctx, Args &a, cudaStream_t s
 
 // Which of the two kernels takes a call.  Up to 32 query rows a kv head this one does (above 16 in two tiles, each of which takes the cache's codes apart for itself):
 // the other's fixed costs are for 128 rows, and paid for every (sequence, kv head).  us, this kernel and the other, 20 to 32 rows: one sequence of 8 kv heads, 300 to
-// 4000 keys 11 - 15 and 14 - 17, sixteen of 1500 27 and 36, thirty-two 43 and 59; sixteen of 32 heads and 300 keys 37 and 61; but thirty-two of 12000 keys 204
-// and 191.  A tree of more than 24 nodes without shared heads has so many keys of its own that few runs are better off there: 32 nodes, 8 heads, one
-// sequence of 300 to 4000 keys 17 - 21 and 15 - 17, four 18 - 28 and 15 - 23, but thirty-two 28 - 91 and 35 - 93.  48 rows: 32 heads, sixteen of 1500 keys 120 and 103, of 300 61 and 63.
+// 4000 keys 11 - 15 and 13 - 16, thirty-two of 1500 54 - 56 and 65, twenty nodes of sixteen sequences, 32 heads and 300 keys 42 and 62; but sixteen of 8 heads
+// and 1500 keys 30 - 32 and 29, thirty-two of 4000 to 12000 186 and 182, of 12000 265 - 268 and 245.  A tree of more than 24 nodes without shared heads has keys of
+// its own besides: 32 nodes, 8 heads, one sequence of 300 keys 12.2 and 13.8, of 4000 16.5 and 16.3, four 13.4 and 14.3, 27.1 and 26.2, but thirty-two 26 and 37, 111 and
+// 110: the line by the number of runs gives a long cache's few per cent for a short one's.  48 rows: 32 heads, sixteen of 1500 keys 120 and 103, of 300 61 and 63.
 static bool many_rows(const fspad_ctx *ctx, int N, int B)
 {
     const fspad_config &c = ctx->cfg;

@@ -11,8 +11,8 @@
 // chunks in turn, each with an accumulator of its own, and are merged at the end.  Either way the groups' products alternate: while one
 // group is at its exponentials the tensor cores work for the other.
 //
-// Queries are fp16 too, each row scaled by a power of two (exact); but against the tree's rows, which are bf16 of any size, they are taken as
-// they are: the tree's chunks come first, with bf16 operands (one product's operands have one type), and the query tile is then written
+// Queries are fp16 too, each row scaled by a power of two (exact for elements of at least 2^-31 of the row's largest); but against the tree's rows, which are
+// bf16 of any size, they are taken as they are: the tree's chunks come first, with bf16 operands (one product's operands have one type), and the query tile is then written
 // again.  With one row tile its two forms lie in the two tiles' places.
 //
 // What bounds it: with two row tiles a chunk takes 4450 cycles, in which the products take 2900 (128 x 128 x 16 with both operands in shared memory 108 cycles, with
