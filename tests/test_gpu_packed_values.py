@@ -59,3 +59,16 @@ def test_a_cached_row_of_k_that_is_no_number_is_seen_by_all_of_its_sequence(node
     want = np.zeros(got.shape, bool)
     want[1, :, group:] = True
     np.testing.assert_array_equal(np.isnan(got), want)
+
+
+@pytest.mark.parametrize("nodes,heads", [(1, (4, 2)), (20, (2, 2)), (60, (4, 2)), (130, (4, 2))])
+def test_cached_v_of_the_least_and_the_largest_scales(nodes, heads):
+    """Kept values from 2^-10 (fp16's least one, with the factor that the sums take) to 2688, a kv head of each kind."""
+    case = Case(36, 2, nodes, *heads, [900, 130])
+    real = case.scales != 0x7F
+    case.codes[:, 1] = case.rng.integers(0, 256, case.codes[:, 1].shape, np.uint8)
+    for h, (lo, hi) in enumerate(((1, 9), (118, 127))):
+        s = case.rng.integers(lo, hi, case.scales[:, 1, :, h].shape).astype(np.uint8)
+        case.scales[:, 1, :, h] = np.where(real[:, 1, :, h], s, 0x7F)
+    case.tv[:, 0] = synth.f32_to_bf16_bits((packed.bf16(case.tv[:, 0]) * 2.0 ** -8).astype(np.float32))
+    case.check(_run(case))
