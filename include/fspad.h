@@ -58,7 +58,7 @@ typedef enum {
     FSPAD_ERR_BAD_TREE = -8,       /* parent[0] != -1 or parent[i] outside [0, i)      */
     FSPAD_ERR_NOMEM = -9,          /* device or host allocation failed at create time  */
     FSPAD_ERR_TOO_LARGE = -10,     /* size beyond the fixed capacity of a no-allocation call */
-    FSPAD_ERR_DEVICE = -11         /* the context belongs to another device than the current one (calls around the 4-bit cache) */
+    FSPAD_ERR_DEVICE = -11         /* the context belongs to another device than the current one (calls around the 4-bit and 8-bit caches and on blocks) */
 } fspad_error;
 
 typedef struct {
@@ -539,6 +539,111 @@ int fspad_tree_attn_packed(fspad_ctx *ctx, const fspad_bf16 *q, const uint8_t *c
                            const int32_t *block_table, int blocks_per_seq, int n_blocks, const fspad_bf16 *tree_k,
                            const fspad_bf16 *tree_v, const int32_t *parent, const int32_t *prefix_len, int n_nodes, int batch,
                            fspad_bf16 *out, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * ---- A cache held in 8 bits ----
+ *
+ * A row of 128 elements is kept as 128 e4m3 codes; 32 rows of a head, a group, share a single-precision scale: 129 bytes a row on the average in place of 256.  An element stands for
+ * code * scale; the error of a row's elements is at most 1/16 of each (of those below 2^-14 of the group's largest, 2^-18 of that).  Paged as above:
+ *   codes  [n_layers][2][n_blocks][Hkv][128][128] bytes
+ *   scales [n_layers][2][n_blocks][Hkv][4] float: of rows 0 .. 31, 32 .. 63, 64 .. 95, 96 .. 127 of a block.  In [2^-64, 2^64]; what lies outside is taken
+ *          as the nearer end (no number: as 2^-64).  The writes leave powers of two; a caller's own cache may have others.
+ * cache row r of sequence b is row r % 128 of block block_table[b][r / 128].  What lies behind a sequence's last row may be anything.
+ *
+ * Writing rows: those of one call that fall into a group are written together.  need = the least 2^e, e from -64 to 64, with max |x| <= 448 * 2^e over them; if one of
+ * them is the group's row 0 (they begin it), its scale becomes need, and what the group's other rows held is lost.  Otherwise the rows that it holds stay: its scale s becomes the larger of need and s (of
+ * the next power of two, where s is none; of need, where s is outside the range), and where that is more than s all 32 rows' codes are rounded again, to the nearest code * s / s', ties to the even one: a value changes only where it falls below
+ * the least codes (a caller's own scale may cost a rounding).  Codes are x / scale to the nearest, ties to the even one, beyond 448 to 448; the
+ * sign of an element is kept where its code is zero.  An infinity or a NaN has no part in the maximum and is kept as NaN.
+ *
+ * The calls below run on the context's device, which must be the current one (else FSPAD_ERR_DEVICE).
+ *
+ * Rows of one layer by slots: a prompt's rows, or a step's, of any number of sequences.
+ *   k, v   [Hkv][rows][128] bf16 (what fspad_rope_qkv writes for batch = 1)
+ *   slots  [rows] int64: block * 128 + row of the block (fspad_block_plan); -1: the row is left out.  No slot may occur twice, and the rows of a group
+ *          must stand within 32 entries one behind the other (as in fspad_block_plan's order they do): a group that breaks either rule is left with any codes and scale
+ *   layer  0 .. n_layers - 1;  codes, scales, n_blocks as above
+ *   k_rounded, v_rounded [Hkv][rows][128] bf16 or both NULL: receive the values that are kept (rows left out: unchanged; values so small that bf16 does not have them do not occur);
+ *          may be k and v, in this order; otherwise they must not overlap k, v or one another (FSPAD_ERR_RANGE)
+ * A slot outside the cache sets FSPAD_ERR_RANGE in the status word and its row is left out.  FSPAD_ERR_TOO_LARGE: rows * Hkv of 2^30 or more.
+ */
+int fspad_kv_write_fp8(fspad_ctx *ctx, const fspad_bf16 *k, const fspad_bf16 *v, const int64_t *slots, int rows, int layer,
+                       uint8_t *codes, float *scales, int n_blocks, fspad_bf16 *k_rounded, fspad_bf16 *v_rounded, void *stream);
+
+/*
+ * fspad_kv_append for the 8-bit cache: for every layer, K and V, sequence b and kv head, cache row L_b + j receives
+ * tree_kv[..][accepted_path[b][j]], j = 0 .. n_accepted[b] - 1.  new_len[b] = L_b + n_accepted[b] (may be NULL, but must not
+ * overlap prefix_len, n_accepted, accepted_path or block_table: FSPAD_ERR_RANGE).  Arguments, `rounded` among them, and errors as in fspad_kv_append_packed.
+ * The groups of the written rows must not be shared (whole blocks that fspad_block_fork shares hold none).
+ */
+int fspad_kv_append_fp8(fspad_ctx *ctx, uint8_t *codes, float *scales, const int32_t *block_table, int blocks_per_seq, int n_blocks,
+                        const fspad_bf16 *tree_kv, const int32_t *accepted_path, const int32_t *n_accepted, const int32_t *prefix_len,
+                        int n_nodes, int batch, fspad_bf16 *rounded, int32_t *new_len, void *stream);
+
+/*
+ * fspad_tree_attn_paged over the 8-bit cache: the keys of node i of sequence b are cache rows 0 .. L_b - 1 and, in bf16, the rows of the
+ * node itself and of its ancestors in tree_k / tree_v.  n_nodes = 1 is the single-token step.
+ *
+ *   q, out [batch][n_nodes][Hq][128] bf16;  tree_k, tree_v [batch][Hkv][n_nodes][128] bf16 (required).  out must not overlap an input
+ *              (FSPAD_ERR_RANGE where it begins at the same address)
+ *   layer  of the cache;  parent [batch][n_nodes], prefix_len [batch] int32, 0 <= L_b <= 128 * blocks_per_seq
+ *   workspace  of at least fspad_tree_attn_fp8_workspace_bytes(ctx) bytes (39 MB on a B200, whatever the sizes),
+ *              scratch: no other call may use it until this one is done
+ * Single-precision scores, softmax and sums: scores q.k beyond its range are infinities, sum_j exp(s_j - max s) |v_j| must lie
+ * in it, and results below about 2^-110 lose bits.  Against the cache a query element is exact down to 2^-10 of its row's largest (the
+ * row's, of a node and head) and off by at most 2^-18 of that below; weights are rounded for the product with V, to 2^-9 of their value at the coarsest
+ * (of the tree's keys to bf16).
+ * A tree row of V with an infinity or a NaN makes the outputs of the nodes that see it NaN, and of no others.  In K such an
+ * element acts through the score, for the same nodes: NaN and +infinity make the output NaN, with -infinity the row has no
+ * weight (where no row has any, the output is NaN).  A NaN of the cache is seen by all queries of its sequence and kv head: in K it makes their
+ * outputs NaN, in V the one element of them.  A query with an infinity or a NaN has NaN outputs.
+ * Errors: FSPAD_ERR_RANGE for a workspace that is too small, and, in the status word, for a
+ * prefix length or a table entry out of range; FSPAD_ERR_TOO_LARGE where batch * Hkv * ceil(n_nodes * Hq / Hkv / 8) * (blocks_per_seq + ceil(n_nodes / 128)) is not below
+ * 2^31 - 10^6 or n_blocks * Hkv * 128 is 2^31 or more; otherwise as fspad_tree_attn_paged.
+ */
+size_t fspad_tree_attn_fp8_workspace_bytes(const fspad_ctx *ctx);
+int fspad_tree_attn_fp8(fspad_ctx *ctx, const fspad_bf16 *q, const uint8_t *codes, const float *scales, int layer,
+                        const int32_t *block_table, int blocks_per_seq, int n_blocks, const fspad_bf16 *tree_k,
+                        const fspad_bf16 *tree_v, const int32_t *parent, const int32_t *prefix_len, int n_nodes, int batch,
+                        fspad_bf16 *out, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * ---- Blocks that several sequences hold ----
+ *
+ * The state is fspad_block_plan's and one array more, all in device memory:
+ *   block_table [batch][blocks_per_seq], held [batch] int32: the blocks of a sequence, and how many it holds
+ *   shares [n_blocks] int32: how many sequences hold a block beyond the first; 0 of blocks that one holds, or none
+ *   free_blocks [n_blocks], n_free [1] int32: a stack of the blocks that nobody holds; its top is free_blocks[n_free - 1]
+ * fspad_block_plan gives sequences blocks, and never rows of shared ones (it adds behind a sequence's last row); but its `drop` would give shared blocks back: a sequence that may
+ * hold some is dropped by fspad_block_free before the plan.
+ * What does not fit sets FSPAD_ERR_RANGE in the status word and changes nothing of the state; the pairs are then -1 throughout.  No two of the arrays may
+ * overlap (FSPAD_ERR_RANGE), but for src and dst.  FSPAD_ERR_TOO_LARGE: batch > 1024, more than 2^19 blocks, 2^31 rows or more a sequence.
+ *
+ * Fork: for i = 0, 1, ... n - 1 sequence dst[i] goes on from the rows of sequence src[i] (src may name one several times): the
+ * len / 128 whole blocks of them are shared, and where len is no multiple of 128 a block is popped for the last rows and the pair (the source's block, the
+ * new one) appended to `pairs`, for fspad_block_copy.  held[dst[i]] and len[dst[i]] are set.
+ *   src, dst [n], len [batch] int32 (len is updated);  pairs [n][2] int32, written: -1 behind the last pair
+ * dst[i] must hold nothing, be named once and not be a source; src[i] must hold its len rows.
+ *
+ * Free: every sequence b with drop[b] not 0 gives back its blocks: a block that others hold loses a holder, the others go onto the stack, the highest number first, whatever
+ * their order in the tables.  held[b] becomes 0; drop [batch] int32.  A block held more often than its count says does not fit.
+ *
+ * Compact: the blocks that sequences hold get the lowest numbers among those that are held or free.  With n blocks held: the i-th of those that are not among
+ * the n lowest, in order, moves to the i-th free one that is.  `pairs` [max_pairs][2] int32 receives (from, to), -1 behind the last; tables, shares and the stack are brought up to date (the stack then
+ * has its lowest block on top).  More than max_pairs moves, a block on the stack twice or held and on the stack do not fit; n_blocks / 2 pairs are always enough.
+ *
+ * Copy: in every plane of a pool, block pairs[i][0] to block pairs[i][1], for any cache: [planes][n_blocks][block_bytes], planes = 2 n_layers.
+ * A second array of the same planes and blocks (pool2, block_bytes2; or NULL and 0) goes along, such as the scales.  Block bytes are multiples of 16, pools 16-byte aligned.
+ * The list ends with pairs of -1, if it has any (what stands behind one may be copied or not); no block may be written twice, or read and written.  A number outside the pool sets FSPAD_ERR_RANGE in the status word and its pair is left out.
+ */
+int fspad_block_fork(fspad_ctx *ctx, const int32_t *src, const int32_t *dst, int n, int32_t *len, int batch, int blocks_per_seq, int n_blocks,
+                     int32_t *block_table, int32_t *held, int32_t *shares, int32_t *free_blocks, int32_t *n_free, int32_t *pairs, void *stream);
+int fspad_block_free(fspad_ctx *ctx, const int32_t *drop, int batch, int blocks_per_seq, int n_blocks, int32_t *block_table, int32_t *held,
+                     int32_t *shares, int32_t *free_blocks, int32_t *n_free, void *stream);
+int fspad_block_compact(fspad_ctx *ctx, int batch, int blocks_per_seq, int n_blocks, int32_t *block_table, int32_t *held, int32_t *shares,
+                        int32_t *free_blocks, int32_t *n_free, int32_t *pairs, int max_pairs, void *stream);
+int fspad_block_copy(fspad_ctx *ctx, void *pool, int64_t block_bytes, void *pool2, int64_t block_bytes2, int planes, int n_blocks,
+                     const int32_t *pairs, int n_pairs, void *stream);
 
 /*
  * One whole verify step on DEVICE buffers ("Preliminaries": the target's single

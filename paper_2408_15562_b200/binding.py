@@ -25,7 +25,8 @@ EXPORTS = ["fspad_create", "fspad_destroy", "fspad_status", "fspad_strerror", "f
            "fspad_tree_attn", "fspad_tree_accept", "fspad_accept_stats", "fspad_kv_compact",
            "fspad_tree_attn_paged", "fspad_kv_compact_paged", "fspad_kv_append", "fspad_lm_head_stats", "fspad_lm_head_accept", "fspad_feature_sampler", "fspad_feature_sampler_workspace_bytes", "fspad_verify_step", "fspad_verify_step_host", "fspad_selftest_wait_timeout", "fspad_accept_stats_noalloc", "fspad_tree_build", "fspad_draft_expand",
            "fspad_device", "fspad_rope_qkv", "fspad_block_plan", "fspad_kv_write_packed", "fspad_kv_append_packed", "fspad_tree_attn_packed",
-           "fspad_tree_attn_packed_workspace_bytes"]
+           "fspad_tree_attn_packed_workspace_bytes", "fspad_block_fork", "fspad_block_free", "fspad_block_compact", "fspad_block_copy"]
+EXPORTS_FP8 = ["fspad_kv_write_fp8", "fspad_kv_append_fp8", "fspad_tree_attn_fp8", "fspad_tree_attn_fp8_workspace_bytes"]
 
 
 class FspadConfig(ctypes.Structure):
@@ -84,6 +85,15 @@ def load():
     lib.fspad_tree_attn_packed_workspace_bytes.argtypes = [vp, ci, ci]
     lib.fspad_tree_attn_packed_workspace_bytes.restype = ctypes.c_size_t
     lib.fspad_tree_attn_packed.argtypes = [vp] * 4 + [ci, vp, ci, ci] + [vp] * 4 + [ci, ci, vp, vp, ctypes.c_size_t, vp]
+    lib.fspad_kv_write_fp8.argtypes = [vp] * 4 + [ci, ci, vp, vp, ci, vp, vp, vp]
+    lib.fspad_kv_append_fp8.argtypes = [vp] * 4 + [ci, ci] + [vp] * 4 + [ci, ci, vp, vp, vp]
+    lib.fspad_tree_attn_fp8_workspace_bytes.argtypes = [vp]
+    lib.fspad_tree_attn_fp8_workspace_bytes.restype = ctypes.c_size_t
+    lib.fspad_tree_attn_fp8.argtypes = [vp] * 4 + [ci, vp, ci, ci] + [vp] * 4 + [ci, ci, vp, vp, ctypes.c_size_t, vp]
+    lib.fspad_block_fork.argtypes = [vp] * 3 + [ci, vp, ci, ci, ci] + [vp] * 7
+    lib.fspad_block_free.argtypes = [vp] * 2 + [ci] * 3 + [vp] * 6
+    lib.fspad_block_compact.argtypes = [vp] + [ci] * 3 + [vp] * 6 + [ci, vp]
+    lib.fspad_block_copy.argtypes = [vp, vp, ctypes.c_int64, vp, ctypes.c_int64, ci, ci, vp, ci, vp]
     _lib = lib
     return lib
 
@@ -138,6 +148,7 @@ class Context:
                                max_batch, softmax_scale)
         self._h = ctypes.c_void_p()
         self._workspace = None      # of the attention over the 4-bit cache
+        self._workspace_fp8 = None  # ... over the 8-bit cache
         self._sizes = (n_q_heads, n_kv_heads, n_layers, max_nodes)
         rc = load().fspad_create(ctypes.byref(self.cfg), ctypes.byref(self._h))
         if rc != 0:
@@ -423,6 +434,52 @@ class Context:
 
     def tree_attn_packed_workspace_bytes(self, n_nodes: int, batch: int) -> int:
         return int(load().fspad_tree_attn_packed_workspace_bytes(self._h, n_nodes, batch))
+
+    # -- the cache held in 8 bits: codes [layers][2][n_blocks][Hkv][128][128] (uint8: e4m3), scales [layers][2][n_blocks][Hkv][4] (float32) ---------
+    def new_fp8_cache(self, n_blocks: int, device="cuda"):
+        """(codes, scales) of an empty cache of n_blocks blocks of 128 rows, every layer of the context."""
+        shape = (self.cfg.n_layers, 2, n_blocks, self.cfg.n_kv_heads)
+        return (torch.zeros(shape + (128, 128), dtype=torch.uint8, device=device), torch.ones(shape + (4,), dtype=torch.float32, device=device))
+
+    def kv_write_fp8(self, k, v, slots, codes, scales, layer=0, k_rounded=None, v_rounded=None, stream=None):
+        """Rows k, v [Hkv][rows][128] (bf16, device; a leading axis of one is allowed) into the slots [rows] (int64; -1: left out) of a layer.  The rows
+        of 32 of a block that share a scale stand within 32 entries, as block_plan's do."""
+        self._packed_call("kv_write_fp8", stream, k, v, slots, codes, scales, layer, k_rounded, v_rounded)
+
+    def kv_append_fp8(self, codes, scales, block_table, tree_kv, accepted_path, n_accepted, prefix_len, rounded=None, new_len=None, stream=None):
+        """tree_kv [layers][2][B][Hkv][N][128] (bf16): rows of the accepted path written behind the prefix of the 8-bit cache."""
+        return self._packed_call("kv_append_fp8", stream, codes, scales, block_table, tree_kv, accepted_path, n_accepted, prefix_len, rounded, new_len)
+
+    def tree_attn_fp8(self, q, codes, scales, block_table, tree_k, tree_v, parent, prefix_len, layer=0, out=None, workspace=None, stream=None):
+        """Tree-masked attention of q [B][N][Hq][128] over a layer of the 8-bit cache and the tree's bf16 rows [B][Hkv][N][128].  Without
+        `workspace` (uint8) the context's own is used: no two such calls, captured ones among them, may then run at the same time."""
+        r = self._packed_call("tree_attn_fp8", stream, q, codes, scales, block_table, tree_k, tree_v, parent, prefix_len, layer, out,
+                              self._workspace_fp8 if workspace is None else workspace)
+        if type(r) is tuple:         # (the first call's: it lives as long as the context, so that a captured call's stays where it is)
+            r, self._workspace_fp8 = r
+        return r
+
+    def tree_attn_fp8_workspace_bytes(self) -> int:
+        return int(load().fspad_tree_attn_fp8_workspace_bytes(self._h))
+
+    # -- blocks that several sequences hold (block_plan's state, and shares [n_blocks]: the holders of a block beyond the first) ------------------
+    def block_fork(self, src, dst, length, block_table, held, shares, free_blocks, n_free, pairs=None, stream=None):
+        """Sequences dst [n] go on from the rows of sequences src [n] (int32, device): whole blocks are shared, a last one that is not full is to be copied: the
+        returned pairs [n][2] (from, to; -1 behind the last) are block_copy's.  The state and length [B] are updated."""
+        return self._packed_call("block_fork", stream, src, dst, length, block_table, held, shares, free_blocks, n_free, pairs)
+
+    def block_free(self, drop, block_table, held, shares, free_blocks, n_free, stream=None):
+        """Sequences with drop[b] not 0 give back their blocks; those that nobody else holds go onto the stack."""
+        self._packed_call("block_free", stream, drop, block_table, held, shares, free_blocks, n_free)
+
+    def block_compact(self, block_table, held, shares, free_blocks, n_free, pairs=None, stream=None):
+        """The blocks in use get the lowest numbers; returns the pairs [n_blocks // 2][2] (from, to; -1 behind the last) for block_copy."""
+        return self._packed_call("block_compact", stream, block_table, held, shares, free_blocks, n_free, pairs)
+
+    def block_copy(self, pool, pairs, stream=None):
+        """Block pairs[i][0] to block pairs[i][1] in every plane of a cache [layers][2][n_blocks]..., or of two arrays that belong together (codes, scales)."""
+        first, second = (tuple(pool) + (None,))[:2] if isinstance(pool, (tuple, list)) else (pool, None)
+        self._packed_call("block_copy", stream, first, second, pairs)
 
 
 def accept_stats_noalloc(logits, temperature, rows_per_seq, out, stream=None) -> int:

@@ -1,0 +1,226 @@
+// Rows into the cache held in 8 bits: a prompt's rows, or a step's, by slots, and the accepted path's rows of every layer ("Preliminaries": the accepted
+// tokens continue the sequence, the others and their descendants are discarded).
+//
+// Of a group of 32 rows of a head: s = the least power of two with max |x| <= 448 s, codes e4m3(x / s), to the nearest, ties to the even one.  Rows of one
+// call that fall into a group are taken together by one warp, 16 bytes a lane, half a warp a row, all of them in registers: the group's maximum is known before the first
+// code is made, and no row is read twice.  A group that was begun before (its row 0 is not among them) keeps its scale or, where the new rows need a larger one, is
+// rounded again by it: with powers of two that changes only what falls below the least codes.
+// An element that is not finite has no part in the maximum and is kept as NaN.
+//
+// Bound by memory: 256 bytes read and 128 written a row (256 more where the caller asks for the values that are kept).
+#include "fp8.cuh"
+
+namespace {
+
+constexpr int kWarps = 8;                // of a CTA
+constexpr int kRows = FSPAD_FP8_GROUP;
+constexpr int kPairs = kRows / 2;        // a pair of rows an instruction
+
+// Larger finite magnitude among two pairs of bf16 that may hold infinities and NaN: what is none counts as 0.
+__device__ __forceinline__ uint32_t finite_most(uint32_t w)
+{
+    uint32_t lo = w & 0x7fffu, hi = (w >> 16) & 0x7fffu;
+    lo = lo < 0x7f80u ? lo : 0u;
+    hi = hi < 0x7f80u ? hi : 0u;
+    return max(lo, hi);
+}
+
+// Rows of a group: lane t has row t's place in `src` (rows of 128 elements) and its row of the group; bit t of `there` says whether there is one.
+// codes: row 0 of the group; scale: the group's; begun: its rows before the new ones stay.  `back`, if not NULL, receives the values that are kept, at src's places.
+__device__ __forceinline__ void put_group(const uint4 *src, uint4 *back, uint8_t *codes, float *scale, uint32_t there, long long from, int to, bool begun)
+{
+    const int lane = threadIdx.x & 31, piece = lane & 15, half = lane >> 4;
+    const float old = begun ? *scale : 0.f;          // (asked for before the rows)
+    uint4 x[kPairs];
+    uint32_t most = 0, odd = 0;
+#pragma unroll
+    for (int u = 0; u < kPairs; ++u) {
+        x[u] = make_uint4(0u, 0u, 0u, 0u);
+        const long long at = __shfl_sync(0xffffffffu, from, 2 * u + half);
+        if ((there >> (2 * u + half)) & 1u) x[u] = src[at * 16 + piece];
+    }
+#pragma unroll
+    for (int u = 0; u < kPairs; ++u) {
+        const uint32_t m = fspad_most2(fspad_most2(x[u].x, x[u].y), fspad_most2(x[u].z, x[u].w));
+        uint32_t top = max(m & 0xffffu, m >> 16);
+        if (top >= 0x7f80u) {                        // (rare)
+            odd |= 1u << u;
+            top = max(max(finite_most(x[u].x), finite_most(x[u].y)), max(finite_most(x[u].z), finite_most(x[u].w)));
+        }
+        most = max(most, top);
+    }
+    most = __reduce_max_sync(0xffffffffu, most);
+    int field = fspad_fp8_field(most);
+    bool again = false;
+    float ratio = 1.f;
+    if (begun && old >= kFp8Least && old <= kFp8Most) {          // (a scale outside the range, or none, is of rows that do not count)
+        field = max(field, (int)((__float_as_uint(old) + 0x7fffffu) >> 23));
+        ratio = old * fspad_field_float(254 - field);            // (a reciprocal's field; exact)
+        again = ratio != 1.f;
+    }
+    const float s = fspad_field_float(field), inv = fspad_field_float(254 - field);
+    if (again) {
+        // 32 rows of 128 codes: 16 codes a lane at a time
+#pragma unroll 2
+        for (int i = 0; i < 8; ++i) {
+            uint4 *at = reinterpret_cast<uint4 *>(codes) + i * 32 + lane;
+            uint4 c = *at;
+            uint32_t *w = &c.x;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                uint32_t h[2] = {fspad_e4m3_to_f16(w[j]), fspad_e4m3_to_f16(w[j] >> 16)}, r[2];
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h[y]));
+                    r[y] = fspad_f32_to_e4m3(f.x * ratio, f.y * ratio);
+                }
+                w[j] = r[0] | (r[1] << 16);
+            }
+            *at = c;
+        }
+    }
+    __syncwarp();                                    // (the new rows' codes come after)
+    if (lane == 0 && !(begun && !again && s == old)) *scale = s;
+#pragma unroll
+    for (int u = 0; u < kPairs; ++u) {
+        if (!((there >> (2 * u)) & 3u)) continue;
+        const long long at = __shfl_sync(0xffffffffu, from, 2 * u + half);
+        const int row = __shfl_sync(0xffffffffu, to, 2 * u + half);
+        uint32_t *w = &x[u].x;
+        uint32_t c[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c[j] = fspad_f32_to_e4m3(__uint_as_float(w[j] << 16) * inv, __uint_as_float(w[j] & 0xffff0000u) * inv);
+        if ((odd >> u) & 1u) {                       // (an infinity, which would be cut to 448)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if ((w[j] & 0x7fffu) >= 0x7f80u) c[j] = (c[j] & 0xff00u) | 0x7fu;
+                if (((w[j] >> 16) & 0x7fffu) >= 0x7f80u) c[j] = (c[j] & 0xffu) | 0x7f00u;
+            }
+        }
+        if ((there >> (2 * u + half)) & 1u) {
+            reinterpret_cast<uint2 *>(codes)[row * 16 + piece] = make_uint2(c[0] | (c[1] << 16), c[2] | (c[3] << 16));
+            if (back) {
+                uint4 o;
+                uint32_t *ow = &o.x;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t h = fspad_e4m3_to_f16(c[j]);
+                    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h));
+                    const __nv_bfloat162 v = __floats2bfloat162_rn(f.x * s, f.y * s);
+                    ow[j] = *reinterpret_cast<const uint32_t *>(&v);
+                }
+                back[at * 16 + piece] = o;
+            }
+        }
+    }
+}
+
+// Rows [2][Hkv][rows] to the slots slots[rows] of one layer.  A warp looks at `each` entries (a power of two, at most 32) of a head's K or V and takes the groups that have their first row there;
+// the rows of a group stand within 32 entries.
+__global__ void __launch_bounds__(kWarps * 32)
+kv_write_fp8_kernel(const uint4 *k, const uint4 *v, const long long *__restrict__ slots, int rows, int Hkv, int each, uint8_t *codes, float *scales,
+                    int n_blocks, uint4 *k_rounded, uint4 *v_rounded, int *__restrict__ status)
+{
+    fspad_pdl_trigger();
+    fspad_pdl_wait();
+    const int lane = threadIdx.x & 31;
+    const unsigned jobs = ((unsigned)rows + each - 1) / each, job = blockIdx.x * kWarps + (threadIdx.x >> 5), of_head = job / jobs;
+    if (of_head >= 2u * Hkv) return;
+    const int first = (int)(job - of_head * jobs) * each, plane = of_head >= (unsigned)Hkv ? 1 : 0, head = (int)of_head - plane * Hkv;
+    // entries first - 32 .. first + 63
+    long long s[3];
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        const long long at = (long long)first + 32 * (i - 1) + lane;
+        s[i] = at >= 0 && at < rows ? slots[at] : -1;
+        if (s[i] < 0 || s[i] >= (long long)n_blocks * 128) {
+            bad |= s[i] != -1;
+            s[i] = -1;
+        }
+    }
+    if (bad) fspad_report(status, FSPAD_ERR_RANGE);
+    const long long group0 = s[0] >> 5, group1 = s[1] >> 5, group2 = s[2] >> 5;      // (-1: none)
+    const long long ahead = __shfl_up_sync(0xffffffffu, group1, 1), last = __shfl_sync(0xffffffffu, group0, 31);
+    // an entry whose predecessor is of the same group is not its first; of the others that is looked up
+    uint32_t firsts = __ballot_sync(0xffffffffu, lane < each && group1 >= 0 && group1 != (lane > 0 ? ahead : last));
+    while (firsts) {
+        const int i = __ffs(firsts) - 1;
+        firsts &= firsts - 1;
+        const long long group = __shfl_sync(0xffffffffu, group1, i);
+        const uint32_t before = __ballot_sync(0xffffffffu, group0 == group), now = __ballot_sync(0xffffffffu, group1 == group),
+                       after = __ballot_sync(0xffffffffu, group2 == group);
+        if ((before & (i < 31 ? ~0u << (i + 1) : 0u)) | (now & ((1u << i) - 1u))) continue;
+        const uint32_t there = (now >> i) | (i > 0 ? after << (32 - i) : 0u);
+        const long long sl1 = __shfl_sync(0xffffffffu, s[1], (i + lane) & 31), sl2 = __shfl_sync(0xffffffffu, s[2], (i + lane) & 31);
+        const long long slot = i + lane < 32 ? sl1 : sl2;
+        const bool begun = !__any_sync(0xffffffffu, ((there >> lane) & 1u) && (slot & 31) == 0);
+        const long long block = group >> 2, g = ((long long)plane * n_blocks + block) * Hkv + head;
+        put_group(plane ? v : k, plane ? v_rounded : k_rounded, codes + (g * 128 + (group & 3) * kRows) * 128, scales + g * FSPAD_FP8_GROUPS + (group & 3), there,
+                  (long long)head * rows + first + i + lane, (int)(slot & 31), begun);
+    }
+}
+
+// cache row L_b + j <- tree row path[b][j] of the slice, j < n_acc[b]; a warp per (layer, K/V, sequence, head).
+__global__ void __launch_bounds__(kWarps * 32)
+kv_append_fp8_kernel(uint8_t *codes, float *scales, const int *__restrict__ table, int table_stride, int n_blocks, const uint4 *tree_kv,
+                     const int *__restrict__ path, const int *__restrict__ n_acc, const int *__restrict__ prefix_len, int n_layers, int B, int Hkv, int N,
+                     int path_stride, uint4 *rounded, int *__restrict__ new_len, int *__restrict__ status)
+{
+    fspad_pdl_trigger();
+    fspad_pdl_wait();
+    const int lane = threadIdx.x & 31;
+    const unsigned number = blockIdx.x * kWarps + (threadIdx.x >> 5), of_seq = number / (unsigned)Hkv, lk = of_seq / (unsigned)B;  // lk: layer * 2 + (K or V)
+    if (lk >= 2u * n_layers) return;
+    const int h = (int)(number - of_seq * Hkv), b = (int)(of_seq - lk * B);
+    int L = prefix_len[b], n = n_acc[b];
+    bool bad = false;
+    if (n < 0 || n > path_stride || n > N) { bad = true; n = 0; }
+    if (L < 0 || (long long)L + n > (long long)table_stride * 128) { bad = true; n = 0; }
+    if (new_len && lane == 0 && lk == 0 && h == 0) new_len[b] = L + n;
+    const int *pth = path + (size_t)b * path_stride;
+    const int end = L + n;                           // (at most 128 * table_stride, which is an int)
+    for (int r0 = L & ~(kRows - 1); n > 0 && r0 < end; r0 += kRows) {
+        const int r = r0 + lane;
+        int node = -1;
+        if (r >= L && r < end) {
+            node = pth[r - L];
+            if (node < 0 || node >= N) { bad = true; node = -1; }
+        }
+        const int block = table[(size_t)b * table_stride + (r0 >> 7)];
+        if (block < 0 || block >= n_blocks) { bad = true; continue; }
+        const uint32_t there = __ballot_sync(0xffffffffu, node >= 0);
+        const long long g = ((long long)lk * n_blocks + block) * Hkv + h;
+        if (there)
+            put_group(tree_kv, rounded, codes + (g * 128 + (r0 & 127)) * 128, scales + g * FSPAD_FP8_GROUPS + ((r0 & 127) / kRows), there,
+                      (long long)number * N + node, lane, r0 < L);
+    }
+    if (bad) fspad_report(status, FSPAD_ERR_RANGE);
+}
+
+}  // namespace
+
+cudaError_t fspad_launch_kv_write_fp8(fspad_ctx *ctx, const fspad_bf16 *k, const fspad_bf16 *v, const long long *slots, int rows, int layer,
+                                      uint8_t *codes, float *scales, int n_blocks, fspad_bf16 *k_rounded, fspad_bf16 *v_rounded, cudaStream_t st)
+{
+    const int Hkv = ctx->cfg.n_kv_heads;
+    const size_t plane_blocks = (size_t)layer * 2 * n_blocks * Hkv;
+    int each = 32;
+    while (each > 1 && (long long)((rows + each - 1) / each) * Hkv * 2 < 16ll * ctx->sm_count) each /= 2;
+    const long long jobs = (long long)((rows + each - 1) / each) * Hkv * 2;
+    ctx->launches++;
+    return fspad_launch(kv_write_fp8_kernel, dim3((unsigned)((jobs + kWarps - 1) / kWarps)), dim3(kWarps * 32), 0, st, 0, reinterpret_cast<const uint4 *>(k),
+                        reinterpret_cast<const uint4 *>(v), slots, rows, Hkv, each, codes + plane_blocks * 128 * 128, scales + plane_blocks * FSPAD_FP8_GROUPS,
+                        n_blocks, reinterpret_cast<uint4 *>(k_rounded), reinterpret_cast<uint4 *>(v_rounded), ctx->d_status);
+}
+
+cudaError_t fspad_launch_kv_append_fp8(fspad_ctx *ctx, uint8_t *codes, float *scales, FspadPaged paged, const fspad_bf16 *tree_kv, const int *path,
+                                       const int *n_acc, const int *prefix_len, int N, int B, fspad_bf16 *rounded, int *new_len, cudaStream_t st)
+{
+    const fspad_config &c = ctx->cfg;
+    const long long slices = (long long)c.n_layers * 2 * B * c.n_kv_heads;
+    ctx->launches++;
+    return fspad_launch(kv_append_fp8_kernel, dim3((unsigned)((slices + kWarps - 1) / kWarps)), dim3(kWarps * 32), 0, st, 0, codes, scales, paged.table,
+                        paged.stride, paged.n_blocks, reinterpret_cast<const uint4 *>(tree_kv), path, n_acc, prefix_len, c.n_layers, B, c.n_kv_heads, N,
+                        c.max_nodes, reinterpret_cast<uint4 *>(rounded), new_len, ctx->d_status);
+}

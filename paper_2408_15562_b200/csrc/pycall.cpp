@@ -454,13 +454,227 @@ PyObject *call_tree_attn_packed(PyObject *, PyObject *const *args, Py_ssize_t n)
     });
 }
 
+// ---- the 8-bit cache, and blocks ----
+static int cache_fp8(Call &c, PyObject *codes, PyObject *scales, uint8_t **to_codes, float **to_scales)
+{
+    const at::Tensor *t = c.tensor("codes", codes, at::kByte);
+    if (!t) return 0;
+    const long long nb = t->dim() == 6 ? t->size(2) : 0;
+    *to_codes = static_cast<uint8_t *>(c.data("codes", codes, at::kByte, {c.layers, 2, nb, c.hkv, 128, 128}));
+    *to_scales = static_cast<float *>(c.data("scales", scales, at::kFloat, {c.layers, 2, nb, c.hkv, 4}));
+    if (c.ok && nb > INT_MAX) c.fail(PyExc_OverflowError, "too many blocks");
+    return (int)nb;
+}
+
+PyObject *call_kv_write_fp8(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return packed_call(args, n, 6 + 8, [](Call &c, PyObject *const *a, int &rc) -> PyObject * {
+        const at::Tensor *slots = c.tensor("slots", a[2], at::kLong);
+        uint8_t *codes = nullptr;
+        float *scales = nullptr;
+        const int nb = cache_fp8(c, a[3], a[4], &codes, &scales), layer = c.number(a[5]);
+        if (!c.ok) return nullptr;
+        if (slots->dim() != 1 || slots->numel() > INT_MAX) {
+            c.fail(PyExc_ValueError, "slots: expected one axis");
+            return nullptr;
+        }
+        const long long rows = slots->size(0);
+        auto rows_of = [&](const char *name, PyObject *o, bool optional) -> fspad_bf16 * {       // [Hkv][rows][128], or that with an axis of one before it
+            if (!c.ok || (optional && o == Py_None)) return nullptr;
+            const at::Tensor *t = c.tensor(name, o, kBf);
+            if (!t) return nullptr;
+            if (!(t->dim() == 4 && t->size(0) == 1 && t->size(1) == c.hkv && t->size(2) == rows && t->size(3) == 128)) c.shaped(name, t, {c.hkv, rows, 128});
+            return as<fspad_bf16>(*t);
+        };
+        const auto *k = rows_of("k", a[0], false), *v = rows_of("v", a[1], false);
+        auto *kr = rows_of("k_rounded", a[6], true), *vr = rows_of("v_rounded", a[7], true);
+        if (!c.ok) return nullptr;
+        rc = unlocked([&] { return fspad_kv_write_fp8(c.ctx, k, v, as<int64_t>(*slots), (int)rows, layer, codes, scales, nb, kr, vr, c.stream); });
+        if (rc) return nullptr;
+        Py_RETURN_NONE;
+    });
+}
+
+PyObject *call_kv_append_fp8(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return packed_call(args, n, 6 + 9, [](Call &c, PyObject *const *a, int &rc) -> PyObject * {
+        uint8_t *codes = nullptr;
+        float *scales = nullptr;
+        const int nb = cache_fp8(c, a[0], a[1], &codes, &scales);
+        long long B = 0;
+        int bps = 0;
+        const int32_t *table = block_table(c, a[2], &B, &bps);
+        const at::Tensor *tree = c.tensor("tree_kv", a[3], kBf);
+        if (!c.ok) return nullptr;
+        const long long N = tree->dim() == 6 ? tree->size(4) : 0;
+        const auto *kv = static_cast<const fspad_bf16 *>(c.data("tree_kv", a[3], kBf, {c.layers, 2, B, c.hkv, N, 128}));
+        const auto *path = static_cast<const int32_t *>(c.data("accepted_path", a[4], kI32, {B, c.max_nodes}));
+        const auto *count = static_cast<const int32_t *>(c.data("n_accepted", a[5], kI32, {B})), *len = static_cast<const int32_t *>(c.data("prefix_len", a[6], kI32, {B}));
+        auto *rounded = static_cast<fspad_bf16 *>(c.data("rounded", a[7], kBf, {c.layers, 2, B, c.hkv, N, 128}, true));
+        at::Tensor new_len;
+        c.outputs(&new_len, {{"new_len", a[8], kI32, {B}}});
+        if (!c.ok) return nullptr;
+        rc = unlocked([&] { return fspad_kv_append_fp8(c.ctx, codes, scales, table, bps, nb, kv, path, count, len, (int)N, (int)B, rounded, as<int32_t>(new_len), c.stream); });
+        return rc ? nullptr : THPVariable_Wrap(new_len);
+    });
+}
+
+PyObject *call_tree_attn_fp8(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return packed_call(args, n, 6 + 11, [](Call &c, PyObject *const *a, int &rc) -> PyObject * {
+        const at::Tensor *q = c.tensor("q", a[0], kBf);
+        uint8_t *codes = nullptr;
+        float *scales = nullptr;
+        const int nb = cache_fp8(c, a[1], a[2], &codes, &scales), layer = c.number(a[8]);
+        long long B = 0;
+        int bps = 0;
+        const int32_t *table = block_table(c, a[3], &B, &bps);
+        if (!c.ok) return nullptr;
+        const long long N = q->dim() == 4 ? q->size(1) : 0;
+        c.shaped("q", q, {B, N, c.hq, 128});
+        const auto *tk = static_cast<const fspad_bf16 *>(c.data("tree_k", a[4], kBf, {B, c.hkv, N, 128})), *tv = static_cast<const fspad_bf16 *>(c.data("tree_v", a[5], kBf, {B, c.hkv, N, 128}));
+        const auto *parent = static_cast<const int32_t *>(c.data("parent", a[6], kI32, {B, N})), *len = static_cast<const int32_t *>(c.data("prefix_len", a[7], kI32, {B}));
+        at::Tensor out;
+        c.outputs(&out, {{"out", a[9], kBf, {B, N, c.hq, 128}}});
+        // none given: one is made, once everything else has been looked at, and goes back with the output
+        at::Tensor ws;
+        const bool make = a[10] == Py_None;
+        if (make) {
+            const long long bytes = (long long)fspad_tree_attn_fp8_workspace_bytes(c.ctx);
+            if (bytes > 0) c.outputs(&ws, {{"workspace", Py_None, at::kByte, {bytes}}});
+        } else if (const at::Tensor *t = c.tensor("workspace", a[10], at::kByte)) {
+            ws = *t;
+        }
+        if (!c.ok) return nullptr;
+        rc = unlocked([&] { return fspad_tree_attn_fp8(c.ctx, as<fspad_bf16>(*q), codes, scales, layer, table, bps, nb, tk, tv, parent, len, (int)N, (int)B, as<fspad_bf16>(out),
+                                                        ws.defined() ? address(ws) : nullptr, ws.defined() ? (size_t)ws.numel() : 0, c.stream); });
+        if (rc) return nullptr;
+        return make ? Py_BuildValue("(NN)", THPVariable_Wrap(out), THPVariable_Wrap(ws)) : THPVariable_Wrap(out);
+    });
+}
+
+// The state of a pool: table, held, shares, free_blocks, n_free.
+struct Pool {
+    int B, bps, nb;
+    int32_t *table, *held, *shares, *free_blocks, *n_free;
+};
+static Pool pool_of(Call &c, PyObject *const *a)
+{
+    Pool p{};
+    long long B = 0;
+    p.table = const_cast<int32_t *>(block_table(c, a[0], &B, &p.bps));
+    const at::Tensor *f = c.tensor("free_blocks", a[3], kI32);
+    if (!c.ok) return p;
+    if (f->dim() != 1 || f->numel() > INT_MAX) {
+        c.fail(PyExc_ValueError, "free_blocks: expected [blocks]");
+        return p;
+    }
+    p.B = (int)B;
+    p.nb = (int)f->size(0);
+    p.free_blocks = as<int32_t>(*f);
+    p.held = static_cast<int32_t *>(c.data("held", a[1], kI32, {B}));
+    p.shares = static_cast<int32_t *>(c.data("shares", a[2], kI32, {p.nb}));
+    p.n_free = static_cast<int32_t *>(c.data("n_free", a[4], kI32, {1}));
+    return p;
+}
+
+PyObject *call_block_fork(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return packed_call(args, n, 6 + 9, [](Call &c, PyObject *const *a, int &rc) -> PyObject * {
+        const at::Tensor *src = c.tensor("src", a[0], kI32);
+        const Pool p = pool_of(c, a + 3);
+        if (!c.ok) return nullptr;
+        if (src->dim() != 1 || src->numel() > INT_MAX) {
+            c.fail(PyExc_ValueError, "src: expected one axis");
+            return nullptr;
+        }
+        const long long m = src->size(0);
+        const auto *dst = static_cast<const int32_t *>(c.data("dst", a[1], kI32, {m}));
+        auto *len = static_cast<int32_t *>(c.data("length", a[2], kI32, {p.B}));
+        at::Tensor pairs;
+        c.outputs(&pairs, {{"pairs", a[8], kI32, {m, 2}}});
+        if (!c.ok) return nullptr;
+        const auto *s = as<int32_t>(*src);
+        rc = unlocked([&] { return fspad_block_fork(c.ctx, s, dst, (int)m, len, p.B, p.bps, p.nb, p.table, p.held, p.shares, p.free_blocks, p.n_free, as<int32_t>(pairs), c.stream); });
+        return rc ? nullptr : THPVariable_Wrap(pairs);
+    });
+}
+
+PyObject *call_block_free(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return packed_call(args, n, 6 + 6, [](Call &c, PyObject *const *a, int &rc) -> PyObject * {
+        const Pool p = pool_of(c, a + 1);
+        const auto *drop = static_cast<const int32_t *>(c.data("drop", a[0], kI32, {p.B}));
+        if (!c.ok) return nullptr;
+        rc = unlocked([&] { return fspad_block_free(c.ctx, drop, p.B, p.bps, p.nb, p.table, p.held, p.shares, p.free_blocks, p.n_free, c.stream); });
+        if (rc) return nullptr;
+        Py_RETURN_NONE;
+    });
+}
+
+PyObject *call_block_compact(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return packed_call(args, n, 6 + 6, [](Call &c, PyObject *const *a, int &rc) -> PyObject * {
+        const Pool p = pool_of(c, a);
+        if (!c.ok) return nullptr;
+        long long m = std::max(1, p.nb / 2);
+        if (a[5] != Py_None) {
+            const at::Tensor *t = c.tensor("pairs", a[5], kI32);
+            if (t) m = t->dim() == 2 ? t->size(0) : 0;
+        }
+        at::Tensor pairs;
+        c.outputs(&pairs, {{"pairs", a[5], kI32, {m, 2}}});
+        if (m > INT_MAX) c.fail(PyExc_OverflowError, "too many pairs");
+        if (!c.ok) return nullptr;
+        rc = unlocked([&] { return fspad_block_compact(c.ctx, p.B, p.bps, p.nb, p.table, p.held, p.shares, p.free_blocks, p.n_free, as<int32_t>(pairs), (int)m, c.stream); });
+        return rc ? nullptr : THPVariable_Wrap(pairs);
+    });
+}
+
+PyObject *call_block_copy(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return packed_call(args, n, 6 + 3, [](Call &c, PyObject *const *a, int &rc) -> PyObject * {
+        const at::Tensor *pairs = c.tensor("pairs", a[2], kI32);
+        if (!c.ok) return nullptr;
+        if (pairs->dim() != 2 || pairs->size(1) != 2 || pairs->size(0) > INT_MAX) {
+            c.fail(PyExc_ValueError, "pairs: expected [pairs][2]");
+            return nullptr;
+        }
+        void *at[2] = {nullptr, nullptr};
+        long long bytes[2] = {0, 0}, blocks = 0;
+        for (int i = 0; i < 2; ++i) {                        // [layers][2][blocks] and what a block of any cache has
+            if (a[i] == Py_None && i == 1) continue;
+            if (!THPVariable_Check(a[i])) {
+                c.fail(PyExc_TypeError, "pool: expected tensors");
+                return nullptr;
+            }
+            const at::Tensor &is = THPVariable_Unpack(a[i]);
+            const at::Tensor *t = c.tensor("pool", a[i], is.scalar_type());
+            if (!t) return nullptr;
+            if (t->dim() < 4 || t->size(0) != c.layers || t->size(1) != 2 || (i == 1 && t->size(2) != blocks) || t->size(2) > INT_MAX) {
+                c.fail(PyExc_ValueError, "pool: expected [%lld][2][blocks]..., the same blocks in both", c.layers);
+                return nullptr;
+            }
+            blocks = t->size(2);
+            bytes[i] = (long long)c10::elementSize(t->scalar_type());
+            for (int64_t d = 3; d < t->dim(); ++d) bytes[i] *= t->size(d);
+            at[i] = address(*t);
+        }
+        const auto *p = as<int32_t>(*pairs);
+        rc = unlocked([&] { return fspad_block_copy(c.ctx, at[0], bytes[0], at[1], bytes[1], (int)(2 * c.layers), (int)blocks, p, (int)pairs->size(0), c.stream); });
+        if (rc) return nullptr;
+        Py_RETURN_NONE;
+    });
+}
+
 #define FSPAD_ENTRY(name) {#name, (PyCFunction)(void (*)(void))call_##name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FSPAD_ENTRY(tree_attn), FSPAD_ENTRY(tree_attn_paged), FSPAD_ENTRY(tree_accept), FSPAD_ENTRY(kv_compact),
                          FSPAD_ENTRY(kv_compact_paged), FSPAD_ENTRY(kv_append), FSPAD_ENTRY(lm_head_accept),
                          FSPAD_ENTRY(feature_sampler), FSPAD_ENTRY(tree_build), FSPAD_ENTRY(draft_expand),
                          FSPAD_ENTRY(verify_step), FSPAD_ENTRY(verify_step_host), FSPAD_ENTRY(rope_qkv),
                          FSPAD_ENTRY(block_plan), FSPAD_ENTRY(kv_write_packed), FSPAD_ENTRY(kv_append_packed),
-                         FSPAD_ENTRY(tree_attn_packed), {nullptr, nullptr, 0, nullptr}};
+                         FSPAD_ENTRY(tree_attn_packed), FSPAD_ENTRY(kv_write_fp8), FSPAD_ENTRY(kv_append_fp8), FSPAD_ENTRY(tree_attn_fp8),
+                         FSPAD_ENTRY(block_fork), FSPAD_ENTRY(block_free), FSPAD_ENTRY(block_compact), FSPAD_ENTRY(block_copy), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pycall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

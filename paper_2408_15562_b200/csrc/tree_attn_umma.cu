@@ -861,6 +861,18 @@ bool fspad_make_tmap_bf16_2d(CUtensorMap *map, const fspad_bf16 *base, size_t co
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool fspad_make_tmap_u8_2d(CUtensorMap *map, const uint8_t *base, size_t rows, unsigned box_rows)
+{
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn || rows == 0 || rows > 0x7fffffffull) return false;
+    const cuuint64_t dims[2] = {128u, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {128u};
+    const cuuint32_t box[2] = {128u, (cuuint32_t)box_rows};
+    const cuuint32_t estr[2] = {1u, 1u};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // The query rows [nodes of all sequences][Hq][128] as boxes of 64 columns, the G heads of a kv head and the 128 / G nodes of a
 // row tile, which land as one half tile in the rows' order (G divides 128; nodes past a sequence's last one belong to rows that
 // nobody looks at).

@@ -13,6 +13,9 @@
 bool fspad_make_tmap_bf16_2d(CUtensorMap *map, const fspad_bf16 *base, size_t cols, size_t rows, unsigned box_rows,
                              bool wide_l2_fetch = false);
 
+// The same of rows of 128 bytes: boxes of box_rows rows.
+bool fspad_make_tmap_u8_2d(CUtensorMap *map, const uint8_t *base, size_t rows, unsigned box_rows);
+
 namespace umma {
 
 constexpr uint32_t WAIT_CAP = 200000;   // tries of a bounded mbarrier wait
