@@ -68,13 +68,15 @@ __device__ __forceinline__ int prefix_of(const Args &a, int b, bool report)
 }
 template <int UNIT> __device__ __forceinline__ int tree_units(const Args &a) { return (a.N + UNIT - 1) / UNIT; }
 template <int UNIT> __device__ __forceinline__ int run_units(const Args &a, int L) { return tree_units<UNIT>(a) + (int)(((long long)L + UNIT - 1) / UNIT); }
-template <int UNIT> constexpr int kStretch = UNIT == 128 ? 4 : 2;
+// (ROWS: query rows of a CTA, where its units are not enough to tell kernels apart: few with chunks of 128 keys)
+constexpr int kAnyRows = 0, kFewRows = 1;
+template <int UNIT, int ROWS = kAnyRows> constexpr int kStretch = UNIT == 128 && ROWS == kAnyRows ? 4 : 2;
 
 // How many parts the list may be cut into.  With chunks of 128 keys for 256 rows a part of a cut run leaves 128 KB, which cost about a hundredth of what a chunk
 // takes to write and read again: of few chunks, then, fewer parts than SMs (12 sqrt(total); with 5 sqrt(total) 60 nodes over 2K keys took 25.2 us, not 20.4).
-template <int UNIT> __device__ __forceinline__ int parts_of(int total, int ctas)
+template <int UNIT, int ROWS> __device__ __forceinline__ int parts_of(int total, int ctas)
 {
-    if (UNIT == 128 && total < (ctas * ctas) / 150) ctas = max(1, (int)sqrtf((float)(total * 150)));
+    if (UNIT == 128 && ROWS == kAnyRows && total < (ctas * ctas) / 150) ctas = max(1, (int)sqrtf((float)(total * 150)));
     return min(total, ctas);
 }
 
@@ -96,7 +98,7 @@ struct Part {
 
 // All T threads of the CTA call it, and there is a CTA barrier in it; scratch holds T / 32 + 2 W values.  W: how many parts a CTA takes: one, which all its
 // threads ask for, or one for each of its W = T / 32 warps: part0 + w * gridDim.x, so that few parts are on as many SMs.  slots: how many there may be.
-template <int T, int UNIT, int W>
+template <int T, int UNIT, int W, int ROWS = kAnyRows>
 __device__ __forceinline__ Part cut_list(const Args &a, int part0, int slots, Parts &p, int *scratch, bool report)
 {
     const int part = part0 + (W > 1 ? (int)(threadIdx.x >> 5) * (int)gridDim.x : 0), ctas = slots;
@@ -111,10 +113,10 @@ __device__ __forceinline__ Part cut_list(const Args &a, int part0, int slots, Pa
             if (lane >= off) inc += o;
         }
         const int total = __shfl_sync(0xffffffffu, inc, 31);
-        p.n = parts_of<UNIT>(total, ctas);
+        p.n = parts_of<UNIT, ROWS>(total, ctas);
         p.q = total / p.n;
         p.r = total - p.q * p.n;
-        const int want = part < p.n ? p.start(part) : total, most = p.q + kStretch<UNIT>;
+        const int want = part < p.n ? p.start(part) : total, most = p.q + kStretch<UNIT, ROWS>;
         if (a.B * runs <= p.n) {
             // the smallest piece with which there are no more pieces than parts, from below, within a step or two
             int k = 0, sum = 0, q = max(1, (total + p.n - 1) / p.n), by_run = 0;
@@ -183,7 +185,7 @@ __device__ __forceinline__ Part cut_list(const Args &a, int part0, int slots, Pa
         if (w < warp) inc += scratch[w];
         total += scratch[w];
     }
-    p.n = parts_of<UNIT>(total, ctas);
+    p.n = parts_of<UNIT, ROWS>(total, ctas);
     p.q = total / p.n;
     p.r = total - p.q * p.n;
     int x = inc - mine;
