@@ -68,15 +68,18 @@ __device__ __forceinline__ int prefix_of(const Args &a, int b, bool report)
 }
 template <int UNIT> __device__ __forceinline__ int tree_units(const Args &a) { return (a.N + UNIT - 1) / UNIT; }
 template <int UNIT> __device__ __forceinline__ int run_units(const Args &a, int L) { return tree_units<UNIT>(a) + (int)(((long long)L + UNIT - 1) / UNIT); }
-// (ROWS: query rows of a CTA, where its units are not enough to tell kernels apart: few with chunks of 128 keys)
-constexpr int kAnyRows = 0, kFewRows = 1;
-template <int UNIT, int ROWS = kAnyRows> constexpr int kStretch = UNIT == 128 && ROWS == kAnyRows ? 4 : 2;
+// (ROWS: which kernel, where its units are not enough to tell them apart: of the 8-bit cache's, both with chunks of 128 keys, the one for few rows and the one for many)
+constexpr int kAnyRows = 0, kFewRows = 1, kManyRows = 2;
+template <int UNIT, int ROWS = kAnyRows> constexpr int kStretch = ROWS == kManyRows ? 1 : UNIT == 128 && ROWS == kAnyRows ? 4 : 2;
+// What the beginning of a run counts besides its units where the list is cut into equal parts.  (16 trees of 60 nodes over 512 to 4096 keys: a part with three short runs took 139000
+// cycles, one within a run 97000.)
+template <int ROWS> constexpr int kExtra = ROWS == kManyRows ? 3 : 0;
 
 // How many parts the list may be cut into.  With chunks of 128 keys for 256 rows a part of a cut run leaves 128 KB, which cost about a hundredth of what a chunk
 // takes to write and read again: of few chunks, then, fewer parts than SMs (12 sqrt(total); with 5 sqrt(total) 60 nodes over 2K keys took 25.2 us, not 20.4).
 template <int UNIT, int ROWS> __device__ __forceinline__ int parts_of(int total, int ctas)
 {
-    if (UNIT == 128 && ROWS == kAnyRows && total < (ctas * ctas) / 150) ctas = max(1, (int)sqrtf((float)(total * 150)));
+    if (UNIT == 128 && ROWS != kFewRows && total < (ctas * ctas) / 150) ctas = max(1, (int)sqrtf((float)(total * 150)));
     return min(total, ctas);
 }
 
@@ -93,20 +96,26 @@ struct Parts {
 struct Part {
     int b, run, u, left;
     int i0, i1;                          // pieces of the run that the part begins in: the parts that hold the first and the last of them
+    int v;                               // where the run begins in the list, in units and what the beginnings count
     bool by_run;                         // cut in the first way: i0 and i1 hold
 };
 
-// All T threads of the CTA call it, and there is a CTA barrier in it; scratch holds T / 32 + 2 W values.  W: how many parts a CTA takes: one, which all its
+// Units before place y of the list's run number k, which begins at x - y (the beginnings of runs count, but have no units).
+template <int E> __device__ __forceinline__ int units_before(int x, int k, int y) { return x - E * k - min(y, E); }
+
+// All T threads of the CTA call it, and there is a CTA barrier in it; scratch holds T / 32 + max(2 W, 4) values.  W: how many parts a CTA takes: one, which all its
 // threads ask for, or one for each of its W = T / 32 warps: part0 + w * gridDim.x, so that few parts are on as many SMs.  slots: how many there may be.
 template <int T, int UNIT, int W, int ROWS = kAnyRows>
 __device__ __forceinline__ Part cut_list(const Args &a, int part0, int slots, Parts &p, int *scratch, bool report)
 {
     const int part = part0 + (W > 1 ? (int)(threadIdx.x >> 5) * (int)gridDim.x : 0), ctas = slots;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, runs = a.Hkv * a.mtiles;
-    Part s = {0, 0, 0, 0, 0, 0, false};
+    constexpr int E = kExtra<ROWS>;
+    Part s = {0, 0, 0, 0, 0, 0, 0, false};
     if (a.B <= 32) {                     // every warp for itself
         const int n = lane < a.B ? run_units<UNIT>(a, prefix_of(a, lane, report)) : 0;
-        int inc = runs * n;
+        const int nv = lane < a.B ? n + E : 0;       // with what its beginning counts
+        int inc = runs * nv;
 #pragma unroll
         for (int off = 1; off < 32; off <<= 1) {
             const int o = __shfl_up_sync(0xffffffffu, inc, off);
@@ -149,7 +158,7 @@ __device__ __forceinline__ Part cut_list(const Args &a, int part0, int slots, Pa
                 __syncthreads();
                 return s;
             }
-            inc = runs * n;
+            inc = runs * nv;
 #pragma unroll
             for (int off = 1; off < 32; off <<= 1) {
                 const int o = __shfl_up_sync(0xffffffffu, inc, off);
@@ -158,10 +167,18 @@ __device__ __forceinline__ Part cut_list(const Args &a, int part0, int slots, Pa
         }
         if (part < p.n) {
             s.b = __popc(__ballot_sync(0xffffffffu, inc <= want));
-            const int nb = __shfl_sync(0xffffffffu, n, s.b), x = want - (s.b > 0 ? __shfl_sync(0xffffffffu, inc, s.b - 1) : 0);
+            const int nb = __shfl_sync(0xffffffffu, nv, s.b), x = want - (s.b > 0 ? __shfl_sync(0xffffffffu, inc, s.b - 1) : 0);
             s.run = x / nb;
-            s.u = x - s.run * nb;
-            s.left = p.start(part + 1) - want;
+            const int y = x - s.run * nb, end = p.start(part + 1);
+            s.u = max(0, y - E);
+            s.v = want - y;
+            s.left = end - want;
+            if constexpr (E > 0) {
+                const int b1 = __popc(__ballot_sync(0xffffffffu, inc <= end));       // (behind the last sequence: a.B)
+                const int n1 = __shfl_sync(0xffffffffu, nv, min(b1, a.B - 1)), before = b1 > 0 ? __shfl_sync(0xffffffffu, inc, b1 - 1) : 0;
+                const int r1 = b1 < a.B ? (end - before) / n1 : 0, y1 = b1 < a.B ? end - before - r1 * n1 : 0;
+                s.left = units_before<E>(end, min(b1, a.B) * runs + r1, y1) - units_before<E>(want, s.b * runs + s.run, y);
+            }
         }
         __syncthreads();
         return s;
@@ -170,7 +187,7 @@ __device__ __forceinline__ Part cut_list(const Args &a, int part0, int slots, Pa
     const int b0 = min(a.B, tid * per), b1 = min(a.B, b0 + per);
     int mine = 0;
 #pragma unroll 1
-    for (int b = b0; b < b1; ++b) mine += runs * run_units<UNIT>(a, prefix_of(a, b, report));
+    for (int b = b0; b < b1; ++b) mine += runs * (E + run_units<UNIT>(a, prefix_of(a, b, report)));
     int inc = mine;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
@@ -189,14 +206,15 @@ __device__ __forceinline__ Part cut_list(const Args &a, int part0, int slots, Pa
     p.q = total / p.n;
     p.r = total - p.q * p.n;
     int x = inc - mine;
+    static_assert(E == 0 || W == 1, "a part a CTA");
 #pragma unroll 1
-    for (int w = 0; w < W; ++w) {
-        const int its = part0 + w * (int)gridDim.x, want = its < p.n ? p.start(its) : total;
+    for (int w = 0; w < (E > 0 ? 2 : W); ++w) {              // (of a part both ends, where its units have to be counted)
+        const int its = E > 0 ? part0 + w : part0 + w * (int)gridDim.x, want = its < p.n ? p.start(its) : total;
         if (x <= want && want < inc) {
             int b = b0, y = x;
 #pragma unroll 1
             for (; b < b1; ++b) {
-                const int n = runs * run_units<UNIT>(a, prefix_of(a, b, false));
+                const int n = runs * (E + run_units<UNIT>(a, prefix_of(a, b, false)));
                 if (want < y + n) break;
                 y += n;
             }
@@ -208,10 +226,21 @@ __device__ __forceinline__ Part cut_list(const Args &a, int part0, int slots, Pa
     if (part < p.n) {
         const int at = T / 32 + (W > 1 ? 2 * warp : 0);
         s.b = scratch[at];
-        const int nb = run_units<UNIT>(a, prefix_of(a, s.b, false));
+        const int nb = E + run_units<UNIT>(a, prefix_of(a, s.b, false));
         s.run = scratch[at + 1] / nb;
-        s.u = scratch[at + 1] - s.run * nb;
-        s.left = p.start(part + 1) - p.start(part);
+        const int y = scratch[at + 1] - s.run * nb, want = p.start(part), end = p.start(part + 1);
+        s.u = max(0, y - E);
+        s.v = want - y;
+        s.left = end - want;
+        if constexpr (E > 0) {
+            int k1 = a.B * runs, y1 = 0;
+            if (end < total) {
+                const int n1 = E + run_units<UNIT>(a, prefix_of(a, scratch[at + 2], false)), r1 = scratch[at + 3] / n1;
+                k1 = scratch[at + 2] * runs + r1;
+                y1 = scratch[at + 3] - r1 * n1;
+            }
+            s.left = units_before<E>(end, k1, y1) - units_before<E>(want, s.b * runs + s.run, y);
+        }
     }
     return s;
 }
@@ -247,22 +276,22 @@ __device__ __forceinline__ void tell(const Args &a, int n, int b, int run, int i
     a.cuts[8 * n + 4] = i1;
 }
 // One thread for every part, before anything of it is taken.
-template <int UNIT> __device__ __forceinline__ void tell_part(const Args &a, const Parts &p, const Part &s, int part)
+template <int UNIT, int ROWS = kAnyRows> __device__ __forceinline__ void tell_part(const Args &a, const Parts &p, const Part &s, int part)
 {
     if (a.entry_runs) return;
     int i0 = 0, i1 = 0;
     if (s.left > 0 && s.u > 0) {
-        const int start = p.start(part) - s.u;
+        const int start = s.v + kExtra<ROWS>;        // (of the run's first unit)
         i0 = p.owner(start);
         i1 = i0 == part - 1 ? p.owner(start + run_units<UNIT>(a, prefix_of(a, s.b, false)) - 1) : i0;
     }
     tell(a, part, s.b, s.run, i0, i1);
 }
-// One thread, when the part comes to the beginning of a run (s.u = 0): `done` units of the part lie before it.
-__device__ __forceinline__ void tell_run(const Args &a, const Parts &p, const Part &s, int part, int done, int n_run)
+// One thread, when the part comes to the beginning of a run (s.u = 0): `done` units of the part lie before it (where the beginnings of runs count, s.v says where it is).
+template <int ROWS = kAnyRows> __device__ __forceinline__ void tell_run(const Args &a, const Parts &p, const Part &s, int part, int done, int n_run)
 {
     if (!a.entry_runs) return;
-    tell(a, (s.b * a.Hkv * a.mtiles) + s.run, s.b, s.run, part, s.by_run ? s.i1 : p.owner(p.start(part) + done + n_run - 1));
+    tell(a, (s.b * a.Hkv * a.mtiles) + s.run, s.b, s.run, part, s.by_run ? s.i1 : p.owner((kExtra<ROWS> > 0 ? s.v + kExtra<ROWS> : p.start(part) + done) + n_run - 1));
 }
 
 // The pieces of the runs that were cut, merged.  A CTA takes `rows` rows (a power of two, at most WARPS) of a run at a time, each by WARPS / rows warps that take its

@@ -616,13 +616,12 @@ cudaError_t fspad_launch_attn_fp8_umma(fspad_ctx *ctx, packed::Args a, const CUt
 // (of either kernel, so that a workspace made for one call serves every other: the one with 256 rows a CTA needs the most)
 size_t fspad_attn_fp8_workspace(const fspad_ctx *ctx) { return fspad_attn_fp8_umma_workspace(ctx); }
 
-// Whether a call's list can be counted in 32 bits, and the rows of a plane of codes in a TMA coordinate.
+// Whether a call's list (what the beginnings of runs count among it) can be counted in 32 bits, and the rows of a plane of codes in a TMA coordinate.
 bool fspad_attn_fp8_fits(const fspad_ctx *ctx, int N, int B, int bps, int n_blocks)
 {
     const fspad_config &c = ctx->cfg;
-    packed::Args a;
-    a.N = N; a.B = B; a.Hkv = c.n_kv_heads; a.M = N * (c.n_q_heads / c.n_kv_heads); a.mtiles = (a.M + 7) / 8; a.table_stride = bps;
-    return packed::units_fit<128>(a) && (long long)n_blocks * c.n_kv_heads * 128 <= 0x7fffffffll;
+    const long long tiles = ((long long)N * (c.n_q_heads / c.n_kv_heads) + 7) / 8, run = (N + 127) / 128 + (long long)bps + kExtra<kManyRows>;
+    return (double)run * B * c.n_kv_heads * tiles < 2147483647.0 - 1e6 && (long long)n_blocks * c.n_kv_heads * 128 <= 0x7fffffffll;
 }
 
 cudaError_t fspad_launch_tree_attn_fp8(fspad_ctx *ctx, const fspad_bf16 *q, const uint8_t *k_codes, const float *k_scales, const uint8_t *v_codes,

@@ -21,6 +21,8 @@
 #include "fp8.cuh"
 #include "packed_list.cuh"
 
+#include <type_traits>
+
 namespace {
 
 using namespace packed;
@@ -34,21 +36,30 @@ constexpr int TILE = 2 * HALF;
 constexpr int BUFS = 3;                  // K codes | V codes of a chunk; of the tree's chunks the K tile
 constexpr int SMEM = (4 + BUFS) * TILE;  // Q[2] | buffers | V[2]
 constexpr uint32_t TMEM_COLS = 512;      // S, then P, of group g: columns 128 g ..; O of group g: 256 + 128 g ..
-constexpr uint32_t IDESC = (1u << 4) | ((128u >> 3) << 17) | ((128u >> 4) << 24);      // 128 x 128, fp32 accumulator, fp16 operands
-constexpr uint32_t IDESC_F8 = IDESC;     // kind::f8f6f4, e4m3 operands: the same fields
+constexpr uint32_t IDESC = (1u << 4) | ((128u >> 3) << 17) | ((128u >> 4) << 24);      // 128 x 128, fp32 accumulator, fp16 operands (kind::f8f6f4: e4m3 ones)
 constexpr uint32_t IDESC_BF = (1u << 7) | (1u << 10), IDESC_MN = 1u << 16;             // bf16 operands; B (= V) MN-major
 
 // byte offset of 16-byte piece c (0..15) of row r of a tile
 __device__ __forceinline__ uint32_t tile_off(int r, int c) { return (uint32_t)((c >> 3) * HALF + r * 128 + (((c & 7) ^ (r & 7)) << 4)); }
 __device__ __forceinline__ void st_shared(uint32_t at, uint4 v) { st_shared16(at, v.x, v.y, v.z, v.w); }
 
+// Products issued by the one lane whose `e` is not 0, while the whole warp goes through the loop, so that descriptors and addresses are values that are the same in
+// every lane: in a branch of one lane a product took 100 cycles to issue, which bounded the kernel.
 // D[tmem] (+)= A[smem] * B[smem], e4m3 operands, 32 elements deep
-__device__ __forceinline__ void mma_f8_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate)
+__device__ __forceinline__ void mma_f8_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate, uint32_t e)
 {
-    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %5, 0;\n\t"
+    asm volatile("{\n\t.reg .pred p, q;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %5, 0;\n\tsetp.ne.b32 q, %6, 0;\n\t"
                  "mov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], da, db, %4, p;\n\t}\n"
-                 :: "r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate) : "memory");
+                 "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], da, db, %4, p;\n\t}\n"
+                 :: "r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate), "r"(e) : "memory");
+}
+// the same with A from tensor memory, 16-bit operands
+__device__ __forceinline__ void mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate, uint32_t e)
+{
+    asm volatile("{\n\t.reg .pred p, q;\n\t.reg .b64 db;\n\tsetp.ne.b32 p, %5, 0;\n\tsetp.ne.b32 q, %6, 0;\n\t"
+                 "mov.b64 db, {%2, %3};\n\t"
+                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n\t}\n"
+                 :: "r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate), "r"(e) : "memory");
 }
 
 // A stretch of a run that a CTA takes.
@@ -81,11 +92,22 @@ __device__ __forceinline__ float factor(float cs, float scale)
     return fmaxf(cs * scale, 0x1p-126f);
 }
 
+__device__ __forceinline__ void tmem_st32u(uint32_t addr, const uint32_t (&v)[32])
+{
+    __syncwarp();
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+                 "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};\n"
+                 :: "r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]),
+                    "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]),
+                    "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]) : "memory");
+}
+
 // One group's turn at a chunk: scores -> weights.  All 128 scores of a row are in registers after one trip to tensor memory (every further
 // wait for it costs 250 cycles: by quarters, read twice, a turn took 2650); the weights, packed in pairs, go to columns 64 .. 127, over scores.
-// `of_keys`: of each 32 keys the scale of K, log2 of V's scale, and its reciprocal (four of each); of the tree's 1, 0 and 1.
-__device__ __forceinline__ void softmax_chunk(bool tree, uint32_t tS, uint32_t tO, const uint32_t (&see)[4], bool masked, float cs, const float *of_keys, bool row_ok, bool first,
-                                              float &m_run, float &l_run)
+// `enter`, `leave`: around the exponentials, which the groups take in turn.  `of_keys`: of each 32 keys the scale of K, log2 of V's scale, and its reciprocal (four of each); of the tree's 1, 0 and 1.
+template <bool plain, typename E, typename L, typename T>
+__device__ __forceinline__ void softmax_chunk(bool tree, uint32_t tS, uint32_t tO, const uint32_t (&see)[4], float cs, const float *of_keys, bool row_ok, bool first,
+                                              float &m_run, float &l_run, E enter, L leave, T told)
 {
     uint32_t r[4][32];
     __syncwarp();
@@ -95,7 +117,7 @@ __device__ __forceinline__ void softmax_chunk(bool tree, uint32_t tS, uint32_t t
     tmem_ld_pin(r[1]);
     tmem_ld_pin(r[2]);
     tmem_ld_pin(r[3]);
-    if (masked) {
+    if (!plain) {
 #pragma unroll
         for (int x = 0; x < 4; ++x)
 #pragma unroll
@@ -125,40 +147,51 @@ __device__ __forceinline__ void softmax_chunk(bool tree, uint32_t tS, uint32_t t
         }
     }
     m_run = m_new;
-    const float shift = (tree ? -kLazyLog2 : kBiasLog2) - m_safe;        // (of the tree's keys times kDown)
+    const float shift = (!plain && tree ? -kLazyLog2 : kBiasLog2) - m_safe;        // (of the tree's keys times kDown)
+    enter();
     float sum = 0.f;
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
-        const float mul = factor(cs, of_keys[x]), add = shift + of_keys[4 + x];
-        const uint64_t scale2 = f32x2(mul, mul), neg = f32x2(add, add);
-        uint64_t acc[2] = {0ull, 0ull};
-        uint32_t w[16];
+    for (int y = 0; y < 2; ++y) {                    // 64 keys at a time: their product with V can begin
+        uint32_t w[32];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            float x0, x1;
-            f32x2_split(f32x2_fma(f32x2(__uint_as_float(r[x][2 * e]), __uint_as_float(r[x][2 * e + 1])), scale2, neg), x0, x1);
-            const float p0 = ex2f(x0), p1 = ex2f(x1);
-            acc[e & 1] = f32x2_add(acc[e & 1], f32x2(p0, p1));
-            if (tree) w[e] = pack_bf16(p0, p1);
-            else w[e] = pack_f16(p0, p1);
+        for (int z = 0; z < 2; ++z) {
+            const int x = 2 * y + z;
+            const float mul = factor(cs, of_keys[x]), add = shift + of_keys[4 + x];
+            const uint64_t scale2 = f32x2(mul, mul), neg = f32x2(add, add);
+            uint64_t acc[2] = {0ull, 0ull};
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                float x0, x1;
+                f32x2_split(f32x2_fma(f32x2(__uint_as_float(r[x][2 * e]), __uint_as_float(r[x][2 * e + 1])), scale2, neg), x0, x1);
+                const float p0 = ex2f(x0), p1 = ex2f(x1);
+                acc[e & 1] = f32x2_add(acc[e & 1], f32x2(p0, p1));
+                if (!plain && tree) w[16 * z + e] = pack_bf16(p0, p1);
+                else w[16 * z + e] = pack_f16(p0, p1);
+            }
+            float lo, hi;
+            f32x2_split(f32x2_add(acc[0], acc[1]), lo, hi);
+            sum = fmaf(lo + hi, of_keys[8 + x], sum);
         }
-        tmem_st16(tS + 64u + 16u * x, w);
-        float lo, hi;
-        f32x2_split(f32x2_add(acc[0], acc[1]), lo, hi);
-        sum = fmaf(lo + hi, of_keys[8 + x], sum);
+        if (y == 1) leave();
+        tmem_st32u(tS + 64u + 32u * y, w);
+        asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory");
+        told(y);
     }
-    l_run += sum * (tree ? kUp : 1.f);
+    l_run += sum * (!plain && tree ? kUp : 1.f);
 }
 
+constexpr int SCALES = 6;                // (a chunk's are written once the one 6 before it has been through the products)
 struct Small {
-    static constexpr int BARS = 32;
+    static constexpr int BARS = 36;
     unsigned long long bar[BARS];
-    float2 ml[2][128];
+    union {
+        float2 ml[2][128];
+        int scan[NT / 32 + 4];           // (before anything else)
+    };
     float raw[BUFS][8];                  // scales of K and V as they come
-    float scale[5][12];                  // of a chunk, by its number: of each 32 keys K's scale, log2 of V's, 1 / V's; at last of the tree's
+    float scale[SCALES + 1][12];         // of a chunk, by its number: of each 32 keys K's scale, log2 of V's, 1 / V's; at last of the tree's
     unsigned char par[FSPAD_MAX_NODES_WIDE];         // parents plus one
     uint32_t odd[2][4];                  // which V rows of a tree's chunk have an infinity or a NaN in them
-    int scan[NT / 32 + 2];
     uint32_t tmem;
     int fail, soft_fail;                 // (the second: written and read by the softmax warps alone, around their barriers)
 };
@@ -168,8 +201,8 @@ __global__ void __launch_bounds__(NT, 1)
 tree_attn_fp8_umma_kernel(const Args a, const __grid_constant__ CUtensorMap k_map, int k_row0)
 {
     extern __shared__ __align__(1024) unsigned char smem_raw[];      // (nothing else is in shared memory, so it starts on such a boundary: looked at below)
-    enum { B_FULL = 0, B_FREE = BUFS, K_FULL = 2 * BUFS, V_FULL = 3 * BUFS, V_FREE = V_FULL + 2, S_FULL = V_FREE + 2,
-           P_FULL = S_FULL + 2, O_DONE = P_FULL + 2, Q_FULL = O_DONE + 4, DRAIN = Q_FULL + 2, N_BAR };
+    enum { B_FULL = 0, B_FREE = BUFS, K_FULL = 2 * BUFS, T_FULL = 3 * BUFS, V_FULL = 4 * BUFS, V_FREE = V_FULL + 2, S_FULL = V_FREE + 2,
+           P_FULL = S_FULL + 2, O_DONE = P_FULL + 4, Q_FULL = O_DONE + 2, E_FULL = Q_FULL + 2, DRAIN = E_FULL + 2, N_BAR = DRAIN + 2 };
     Small &sm = *reinterpret_cast<Small *>(smem_raw + SMEM);
     static_assert(N_BAR <= Small::BARS, "barriers");
     auto &s_bar = sm.bar;
@@ -193,13 +226,14 @@ tree_attn_fp8_umma_kernel(const Args a, const __grid_constant__ CUtensorMap k_ma
     if (tid == 0) {
         for (int i = 0; i < N_BAR; ++i) {
             int count = 1;
-            if ((i >= K_FULL && i < V_FREE) || (i >= P_FULL && i < O_DONE) || (i >= Q_FULL && i < DRAIN))
+            if (i >= V_FREE && i < S_FULL) count = 2;        // both groups' products
+            if ((i >= T_FULL && i < V_FREE) || (i >= P_FULL && i < O_DONE) || (i >= Q_FULL && i < DRAIN))
                 count = 4;                           // the four warps of a group, or of those that make values
-            if (i >= B_FREE && i < K_FULL) count = 5;        // those, and the tensor cores
+            if (i >= B_FREE && i < K_FULL) count = 7;        // those, the one for the scales, and both groups' products
             mbar_init(bar(i), count);
         }
         s_fail = s_soft_fail = 0;
-        for (int i = 0; i < 12; ++i) s_scale[4][i] = i >= 4 && i < 8 ? 0.f : 1.f;
+        for (int i = 0; i < 12; ++i) s_scale[SCALES][i] = i >= 4 && i < 8 ? 0.f : 1.f;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     }
     if (warp == 9) {
@@ -212,12 +246,13 @@ tree_attn_fp8_umma_kernel(const Args a, const __grid_constant__ CUtensorMap k_ma
     tc_fence_before();
     const int cta = blockIdx.x;
     Parts parts;
-    Part part = cut_list<NT, UNIT, 1>(a, cta, gridDim.x, parts, s_scan, cta == 0);      // (with a barrier in it)
+    Part part = cut_list<NT, UNIT, 1, kManyRows>(a, cta, gridDim.x, parts, s_scan, cta == 0);      // (with a barrier in it)
+    __syncthreads();                                 // (what it has used serves for something else)
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
     const int nt = tree_units<UNIT>(a), runs = a.Hkv * a.mtiles;
 
-    if (warp == 11 && lane == 0) tell_part<UNIT>(a, parts, part, cta);       // (a warp without another job)
+    if (warp == 10 && lane == 0) tell_part<UNIT, kManyRows>(a, parts, part, cta);
 
     const uint32_t base = smem_u32(smem_raw);
     const uint32_t sQ = base, sK = base + 2 * TILE, sV = base + (2 + BUFS) * TILE;
@@ -237,6 +272,7 @@ tree_attn_fp8_umma_kernel(const Args a, const __grid_constant__ CUtensorMap k_ma
         s.two = s.rows > 128;
         part.left -= s.n_ch;
         part.u = 0;
+        part.v += s.n_run + kExtra<kManyRows>;
         if (++part.run == runs) { part.run = 0; ++part.b; }
         return true;
     };
@@ -249,7 +285,17 @@ tree_attn_fp8_umma_kernel(const Args a, const __grid_constant__ CUtensorMap k_ma
         const int grp = warp >> 2, row = tid & 127;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t tS = tmem + lanes + 128u * grp, tO = tmem + lanes + 256u + 128u * grp;
-        uint32_t ph_s = 0, n_done = 0, tree_chunks = 0, chunks = 0;      // phase of S_FULL; products of the group so far; the tree's chunks and all of the CTA so far
+        uint32_t n_done = 0, ph_o = 0, tree_chunks = 0, chunks = 0;    // products of the group so far; the tree's chunks and all of the CTA so far
+        // The groups take turns at their exponentials: while one is there, the products of the other go on.  (In step both waited for the special functions, and then both for
+        // the tensor cores.)  A barrier a group: its 128 threads wait on it, the other's 128 arrive.
+        auto enter = [&] { asm volatile("bar.sync %0, 256;\n" :: "r"(2 + grp) : "memory"); };
+        auto leave = [&] { asm volatile("bar.arrive %0, 256;\n" :: "r"(3 - grp) : "memory"); };
+        if (grp == 1) leave();
+        auto told = [&](int y) {                             // half y of the weights is there
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_light(bar(P_FULL + 2 * grp + y));
+        };
         while (next(s)) {
             const int gr = s.row0 + (s.two ? grp * 128 : 0) + row;           // row of the kv head
             const bool row_ok = gr < a.M;
@@ -321,16 +367,21 @@ tree_attn_fp8_umma_kernel(const Args a, const __grid_constant__ CUtensorMap k_ma
                         }
                 }
             };
-            auto tell_q = [&](int t) {
+            // two row tiles: the group's own warp of the tensor cores is told; one: both are, of either form
+            auto tell_q = [&] {
                 fence_async_smem();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar(Q_FULL + t));
+                if (lane == 0) {
+                    const int b = s.two || grp == 0 ? Q_FULL : E_FULL;
+                    if (!s.two || grp == 0) mbar_arrive(bar(b));
+                    if (!s.two || grp == 1) mbar_arrive(bar(b + 1));
+                }
             };
             // one row tile: group 0's as it is, for the tree, group 1's as e4m3; two: e4m3, or first as they are for the tree
             fetch_q(grp);
             const bool raw = s.two ? s.n_tree > 0 : grp == 0;
             if (!raw) scale_q(grp, true);
-            tell_q(grp);
+            tell_q();
             // (group 0's own chunks of the cache, if there are any, need the factors all the same)
             if (raw && !s.two && s.n_ch > s.n_tree + (s.n_tree & 1)) scale_q(grp, false);
             if (s.n_tree > 0) {
@@ -342,17 +393,41 @@ tree_attn_fp8_umma_kernel(const Args a, const __grid_constant__ CUtensorMap k_ma
                 asm volatile("bar.sync 1, 256;\n" ::: "memory");
             }
             float m_run = -INFINITY, l_run = 0.f;
-            const int n_items = s.two ? 2 * s.n_ch : s.n_ch;
             bool first = true;
-            for (int i = grp; i < n_items; i += 2) {
-                const int c = s.two ? i >> 1 : i, u = s.u0 + c;
+            // Chunks of the cache that exist as a whole have a loop of their own, so that its code is short: jumps over the rest of it cost 600 cycles a turn.
+            const int step = s.two ? 1 : 2, whole_end = s.n_ch - (s.L % UNIT != 0 && s.u0 + s.n_ch == s.n_run ? 1 : 0);
+            int c = s.two ? 0 : grp;
+            auto turn = [&](auto plain_, bool tree, const uint32_t (&see)[4]) {
+                constexpr bool plain = decltype(plain_)::value;
+                if (!failed && !mbar_wait(bar(S_FULL + grp), n_done & 1u)) failed = true;
+                tc_fence_after();
+                if (live) {
+                    const float *of_keys = s_scale[!plain && tree ? SCALES : (chunks + (uint32_t)c) % SCALES];
+                    softmax_chunk<plain>(tree, tS, tO, see, !plain && tree ? a.scale_log2 : cs, of_keys, row_ok, first, m_run, l_run, enter, leave, told);
+                } else {
+                    enter();
+                    leave();
+                    told(0);
+                    told(1);
+                }
+                first = false;
+                ++n_done;
+            };
+#pragma unroll 1
+            while (c < s.n_ch) {
+                if (c >= s.n_tree && c < whole_end) {
+                    const uint32_t all[4] = {~0u, ~0u, ~0u, ~0u};
+#pragma unroll 1
+                    for (; c < whole_end; c += step) turn(std::true_type(), false, all);
+                    continue;
+                }
+                const int u = s.u0 + c;
                 const bool tree = c < s.n_tree;
-                const int key0 = tree ? u * UNIT : (u - nt) * UNIT;
-                const bool masked = tree || key0 + UNIT > s.L;
-                uint32_t see[4] = {~0u, ~0u, ~0u, ~0u};
+                uint32_t see[4];
                 if (tree) {
                     // from the node up, word by word, for an ancestor comes before its descendants (with two words of 64 bits a step took three times as long:
                     // 22 chains of 156 nodes, 32 heads, 186 us against 117; trees of ten nodes' depth 54 and 51)
+                    const int key0 = u * UNIT;
                     int at = node;
                     while (at >= key0 + 128) at = (int)s_par[at] - 1;
 #pragma unroll
@@ -363,37 +438,33 @@ tree_attn_fp8_umma_kernel(const Args a, const __grid_constant__ CUtensorMap k_ma
                             at = (int)s_par[at] - 1;
                         }
                     }
-                } else if (masked) {
-                    const int left = s.L - key0;             // 1 .. 127
+                } else {
+                    const int left = s.L - (u - nt) * UNIT;  // 1 .. 127
 #pragma unroll
                     for (int x = 0; x < 4; ++x) see[x] = left >= 32 * x + 32 ? ~0u : left > 32 * x ? (1u << (left - 32 * x)) - 1u : 0u;
                 }
-                if (!failed && !mbar_wait(bar(S_FULL + grp), ph_s)) failed = true;
-                ph_s ^= 1u;
-                tc_fence_after();
-                if (live) {
-                    softmax_chunk(tree, tS, tO, see, masked, tree ? a.scale_log2 : cs,
-                                  tree ? s_scale[4] : s_scale[(chunks + (uint32_t)c) & 3u], row_ok, first, m_run, l_run);
-                    if (tree) {
-                        const uint32_t *odd = s_odd[(tree_chunks + c) & 1];
-                        if ((see[0] & odd[0]) | (see[1] & odd[1]) | (see[2] & odd[2]) | (see[3] & odd[3])) l_run = NAN;
+                turn(std::false_type(), tree, see);
+                if (tree) {
+                    const uint32_t *odd = s_odd[(tree_chunks + c) & 1];
+                    if ((see[0] & odd[0]) | (see[1] & odd[1]) | (see[2] & odd[2]) | (see[3] & odd[3])) l_run = NAN;
+                    if (s.two && c == s.n_tree - 1 && s.n_ch > s.n_tree) {   // (the tile's last reader's scores are here)
+                        scale_q(grp, true);
+                        tell_q();
                     }
-                    asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory");
                 }
-                first = false;
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive_light(bar(P_FULL + grp));
-                ++n_done;
-                if (s.two && c == s.n_tree - 1 && s.n_ch > s.n_tree) {       // (the tile's last reader's scores are here)
-                    scale_q(grp, true);
-                    tell_q(grp);
-                }
+                c += step;
+            }
+            if (!s.two && grp == 1 && (s.n_ch & 1)) {        // (group 1 takes as many turns as group 0)
+                enter();
+                leave();
             }
             tree_chunks += s.n_tree;
             chunks += (uint32_t)s.n_ch;
             // ---- the group's last product, then the rows ----
-            if (!first && !failed && !mbar_wait(bar(O_DONE + 2 * grp + (int)((n_done - 1) & 1u)), ((n_done - 1) >> 1) & 1u)) failed = true;
+            if (!first) {
+                if (!failed && !mbar_wait(bar(O_DONE + grp), ph_o)) failed = true;
+                ph_o ^= 1u;
+            }
             tc_fence_after();
             const bool whole = s.n_ch == s.n_run;
             const int slot = cta * 2 + (s.u0 == 0 ? 1 : 0);
@@ -485,6 +556,7 @@ tree_attn_fp8_umma_kernel(const Args a, const __grid_constant__ CUtensorMap k_ma
                 tc_fence_after();
             }
         }
+        if (grp == 0) enter();                               // (what the other has left behind)
         if (lane == 0) bulk_store_wait();                    // (the copies' memory is this CTA's)
     } else if (warp < 12) {
       asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
@@ -494,7 +566,7 @@ tree_attn_fp8_umma_kernel(const Args a, const __grid_constant__ CUtensorMap k_ma
         for (;; done += s.n_ch) {
             const Part at = part;
             if (failed || !next(s)) break;
-            if (s.u0 == 0 && lane == 0) tell_run(a, parts, at, cta, done, s.n_run);
+            if (s.u0 == 0 && lane == 0) tell_run<kManyRows>(a, parts, at, cta, done, s.n_run);
             const int *blocks = a.table + (size_t)s.b * a.table_stride;
             const int kv0 = s.u0 + s.n_tree - nt, n_kv = s.n_ch - s.n_tree;  // chunks of the cache
             int mine = 0;
@@ -528,88 +600,123 @@ tree_attn_fp8_umma_kernel(const Args a, const __grid_constant__ CUtensorMap k_ma
         // a CTA that gives up: what has been asked for gets a bounded time to land
         if (failed)
             for (int x = n > BUFS ? n - BUFS : 0; x < n; ++x) (void)mbar_wait(bar(B_FULL + x % BUFS), (uint32_t)(x / BUFS) & 1u);
-      } else if (warp == 9) {
+      } else if (warp != 10) {
         // ================= tensor cores =================
-        // (A warp for each group kept the groups in step, both at their exponentials or both waiting for products: 5600 cycles a chunk against 4300.)
-        const bool issuer = elect_one();
+        // A warp for each group.  (One for both took 3000 cycles for what the tensor cores do in 1300: a wait for a phase that is long over costs 170 cycles, a product 50, and
+        // nothing in a warp overlaps them.)
+        const int g = warp == 9 ? 0 : 1;
+        const uint32_t issuer = elect_one() ? 1u : 0u;
         const uint32_t hi = (uint32_t)(make_desc(0, 16) >> 32);
         const uint32_t q_lo = (uint32_t)make_desc(sQ, 16), k_lo = (uint32_t)make_desc(sK, 16), v_lo = (uint32_t)make_desc(sV, HALF);
+        const uint32_t tS = tmem + 128u * g, tO = tmem + 256u + 128u * g;
         uint32_t cc = 0;                                     // chunks of the stretches before (slot: modulo 2)
-        uint32_t ph_q[2] = {0u, 0u}, n_p[2] = {0u, 0u};      // phases of Q_FULL; products of each group so far
+        uint32_t ph_q = 0u, ph_e = 0u, ph_t = 0u, n_p = 0u;  // phases of Q_FULL, E_FULL and (by buffers) T_FULL; products of the group so far
         while (!failed && next(s)) {
             // (through a shuffle they are values that the compiler knows to be the same in every lane, as an instruction's operands have to be)
             s.n_ch = __shfl_sync(0xffffffffu, s.n_ch, 0);
             s.n_tree = __shfl_sync(0xffffffffu, s.n_tree, 0);
             s.two = __shfl_sync(0xffffffffu, (int)s.two, 0) != 0;
-            const int n_items = s.two ? 2 * s.n_ch : s.n_ch;
-            auto wait_q = [&](int t) {
-                if (!failed && !mbar_wait(bar(Q_FULL + t), ph_q[t])) failed = true;
-                ph_q[t] ^= 1u;
+            const int turns = s.two ? s.n_ch : (s.n_ch - g + 1) >> 1;
+            auto wait_q = [&] {
+                if (!failed && !mbar_wait(bar(Q_FULL + g), ph_q)) failed = true;
+                ph_q ^= 1u;
             };
-            bool have_q[2] = {false, false};                 // of one row tile: its two forms
-            // item i: group i & 1, chunk i / 2 or, of one row tile, i
-            auto issue_s = [&](int i) {
-                const int g = i & 1, c = s.two ? i >> 1 : i;
-                const bool tree = c < s.n_tree;
-                if (s.two && c == s.n_tree && c > 0) wait_q(g);              // the tile again, as e4m3
+            wait_q();
+            if (!s.two) {                                    // both forms, whichever the group's chunks need: no phase may be missed
+                if (!failed && !mbar_wait(bar(E_FULL + g), ph_e)) failed = true;
+                ph_e ^= 1u;
+            }
+            // the j-th chunk or, of one row tile, the j-th of every other one
+            auto wait_k = [&](int j) {
+                const int c = s.two ? j : 2 * j + g;
                 const uint32_t at = cc + (uint32_t)c, buf = at % BUFS;
-                const int t = s.two ? g : tree ? 0 : 1;
-                if (!s.two && !have_q[t]) {
-                    wait_q(t);
-                    have_q[t] = true;
-                }
-                if ((!s.two || g == 0) && !failed && !mbar_wait(bar(K_FULL + buf), (at / BUFS) & 1u)) failed = true;
-                if (!failed && issuer) {
-                    tc_fence_after();
-                    const uint32_t kb = k_lo + buf * (TILE >> 4), qb = q_lo + (uint32_t)t * (TILE >> 4), d = tmem + 128u * g;
+                if (!failed && !mbar_wait(bar(K_FULL + buf), (at / BUFS) & 1u)) failed = true;
+                if (c < s.n_tree && !failed && !mbar_wait(bar(T_FULL + buf), (ph_t >> buf) & 1u)) failed = true;
+            };
+            auto issue_s = [&](int j) {
+                const int c = s.two ? j : 2 * j + g;
+                const bool tree = c < s.n_tree;
+                const uint32_t buf = (cc + (uint32_t)c) % BUFS;
+                if (s.two && c == s.n_tree && c > 0) wait_q();               // the tile again, as e4m3
+                if (failed) return;
+                tc_fence_after();
+                const uint32_t kb = k_lo + buf * (TILE >> 4), qb = q_lo + (s.two ? (uint32_t)g : tree ? 0u : 1u) * (TILE >> 4);
+                if (tree) {
 #pragma unroll
                     for (int ks = 0; ks < 8; ++ks) {
-                        const uint32_t half = ((ks >> 2) * HALF) >> 4, off = ((ks & 3) * 32) >> 4;
-                        if (tree) mma_f16_ss(d, qb + half + off, kb + half + off, hi, IDESC | IDESC_BF, ks > 0);
-                        else mma_f8_ss(d, qb + half + off, kb + off, hi, IDESC_F8, ks > 0);          // (the queries' second halves against the same codes)
+                        const uint32_t off = ((ks >> 2) * HALF + (ks & 3) * 32) >> 4;
+                        mma_f16_lo(tS, qb + off, hi, kb + off, hi, IDESC | IDESC_BF, ks > 0, issuer);
                     }
-                    mma_commit(bar(S_FULL + g));
-                    if (!s.two || g == 1) mma_commit(bar(B_FREE + buf));
-                }
-                __syncwarp();
-            };
-            if (s.two) wait_q(0);
-#pragma unroll 1
-            for (int i = -2; i < n_items; ++i) {
-                if (i >= 0) {
-                    const int g = i & 1, c = s.two ? i >> 1 : i;
-                    const bool tree = c < s.n_tree;
-                    const uint32_t at = cc + (uint32_t)c, slot = at & 1u;
-                    // (a form that no chunk needs is written all the same; its phase is over before the stretch can be)
-                    if (!s.two && i == n_items - 1) {
-                        if (!have_q[0]) wait_q(0);
-                        if (!have_q[1]) wait_q(1);
-                    }
-                    if ((!s.two || g == 0) && !failed && !mbar_wait(bar(V_FULL + slot), (at >> 1) & 1u)) failed = true;
-                    if (!failed && !mbar_wait(bar(P_FULL + g), n_p[g] & 1u)) failed = true;
-                    if (!failed && issuer) {
-                        tc_fence_after();
-                        const uint32_t vb = v_lo + slot * (TILE >> 4), idesc = IDESC | IDESC_MN | (tree ? IDESC_BF : 0u);
+                } else {
 #pragma unroll
-                        for (int ks = 0; ks < 8; ++ks)       // 16 keys an instruction: 8 columns of packed pairs
-                            mma_f16_ts(tmem + 256u + 128u * g, tmem + 128u * g + 64u + (uint32_t)ks * 8u, vb + (uint32_t)(ks * 16 * 128 >> 4), hi,
-                                       idesc, i > 1 || ks > 0);
-                        mma_commit(bar(O_DONE + 2 * g + (int)(n_p[g] & 1u)));
-                        if (!s.two || g == 1) mma_commit(bar(V_FREE + slot));
-                    }
-                    __syncwarp();
-                    ++n_p[g];
+                    for (int ks = 0; ks < 8; ++ks)           // (the queries' second halves against the same codes)
+                        mma_f8_ss(tS, qb + (uint32_t)(((ks >> 2) * HALF + (ks & 3) * 32) >> 4), kb + (uint32_t)((ks & 3) * 32 >> 4), hi, IDESC, ks > 0, issuer);
                 }
-                if (i == -1 && s.two) wait_q(1);
-                if (i + 2 < n_items) issue_s(i + 2);         // (products complete in order: the scores may replace P)
+                mma_commit_if(bar(S_FULL + g), issuer);
+                mma_commit_if(bar(B_FREE + buf), issuer);                    // (two groups' products with two tiles, one group's twice with one)
+                if (!s.two) mma_commit_if(bar(B_FREE + buf), issuer);
+            };
+            if (turns > 0) {
+                wait_k(0);
+                issue_s(0);
             }
+#pragma unroll 1
+            for (int j = 0; j < turns; ++j) {
+                const int c = s.two ? j : 2 * j + g;
+                const bool tree = c < s.n_tree;
+                const uint32_t at = cc + (uint32_t)c, slot = at & 1u;
+                const uint32_t vb = v_lo + slot * (TILE >> 4), idesc = IDESC | IDESC_MN | (tree ? IDESC_BF : 0u);
+                // (what the next scores and this product need besides the weights is waited for ahead of them: a wait for a phase that is long over costs 170 cycles)
+                if (j + 1 < turns) wait_k(j + 1);
+                if (!failed && !mbar_wait(bar(V_FULL + slot), (at >> 1) & 1u)) failed = true;
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    if (!failed && !mbar_wait(bar(P_FULL + 2 * g + y), n_p & 1u)) failed = true;
+                    if (failed) continue;
+                    tc_fence_after();
+#pragma unroll
+                    for (int ks = 4 * y; ks < 4 * y + 4; ++ks)       // 16 keys an instruction: 8 columns of packed pairs
+                        mma_f16_ts(tO, tS + 64u + (uint32_t)ks * 8u, vb + (uint32_t)(ks * 16 * 128 >> 4), hi, idesc, j > 0 || ks > 0, issuer);
+                }
+                if (!failed && j + 1 >= turns) mma_commit_if(bar(O_DONE + g), issuer);
+                if (!failed && j + 1 < turns) issue_s(j + 1);        // (a thread's products complete in order: the scores may replace the weights)
+                if (!failed) {
+                    mma_commit_if(bar(V_FREE + slot), issuer);
+                    if (!s.two) mma_commit_if(bar(V_FREE + slot), issuer);
+                }
+                ++n_p;
+            }
+            for (int c = 0; c < s.n_tree; ++c) ph_t ^= 1u << ((cc + (uint32_t)c) % BUFS);
             cc += (uint32_t)s.n_ch;
         }
         if (failed) {
             s_fail = 1;
-            if (lane == 0) mma_commit(bar(DRAIN));
-            (void)mbar_wait(bar(DRAIN), 0u);
+            if (lane == 0) mma_commit(bar(DRAIN + g));
+            (void)mbar_wait(bar(DRAIN + g), 0u);
         }
+      } else {
+        // ================= scales =================
+        uint32_t cc = 0;
+        while (!failed && next(s)) {
+            for (int c = 0; c < s.n_ch && !failed; ++c, ++cc) {
+                const uint32_t buf = cc % BUFS;
+                if (!mbar_wait(bar(B_FULL + buf), (cc / BUFS) & 1u)) { failed = true; break; }
+                // K's, log2 of V's, its reciprocal, kept in the range that the cache's may have (behind the end there may be anything)
+                if (c >= s.n_tree && lane < 4) {
+                    const float v = fminf(fmaxf(s_raw[buf][4 + lane], kFp8Least), kFp8Most);
+                    float *to = s_scale[cc % SCALES];
+                    to[lane] = fminf(fmaxf(s_raw[buf][lane], kFp8Least), kFp8Most);
+                    to[4 + lane] = __log2f(v);
+                    to[8 + lane] = __frcp_rn(v);
+                }
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(bar(K_FULL + buf));
+                    mbar_arrive(bar(B_FREE + buf));
+                }
+            }
+        }
+        if (failed) s_fail = 1;
       }
     } else {
         // ================= values =================
@@ -656,21 +763,11 @@ tree_attn_fp8_umma_kernel(const Args a, const __grid_constant__ CUtensorMap k_ma
                     __syncwarp();
                     if (lane == 0) {
                         mbar_arrive(bar(V_FULL + slot));
-                        mbar_arrive(bar(K_FULL + buf));
+                        mbar_arrive(bar(T_FULL + buf));
                         mbar_arrive(bar(B_FREE + buf));
                     }
                 } else {
                     const int left = s.L - (u - nt) * UNIT;  // keys of the chunk that exist
-                    // the scales: K's, log2 of V's, its reciprocal, kept in the range that the cache's may have (behind the end there may be anything)
-                    if (w4 == 0 && lane < 4) {
-                        const float v = fminf(fmaxf(s_raw[buf][4 + lane], kFp8Least), kFp8Most);
-                        float *to = s_scale[cc & 3u];
-                        to[lane] = fminf(fmaxf(s_raw[buf][lane], kFp8Least), kFp8Most);
-                        to[4 + lane] = __log2f(v);
-                        to[8 + lane] = __frcp_rn(v);
-                    }
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(bar(K_FULL + buf));
                     if (cc >= 2 && !mbar_wait(bar(V_FREE + slot), ((cc >> 1) - 1u) & 1u)) { failed = true; break; }
                     const uint32_t from = sKb + HALF, to = sV + slot * TILE;
                     // a lane takes 16 codes of a row, four rows an instruction; of the 16-byte pieces that they become, lanes of a row's second half store the later
