@@ -478,7 +478,7 @@ class Context:
 
     def block_copy(self, pool, pairs, stream=None):
         """Block pairs[i][0] to block pairs[i][1] in every plane of a cache [layers][2][n_blocks]..., or of two arrays that belong together (codes, scales)."""
-        first, second = pool if isinstance(pool, (tuple, list)) and len(pool) == 2 else (pool, None)
+        first, second = (*pool, None)[:2] if isinstance(pool, (tuple, list)) and 1 <= len(pool) <= 2 else (pool, None)
         self._packed_call("block_copy", stream, first, second, pairs)
 
 

@@ -2,19 +2,21 @@
 // tokens continue the sequence, the others and their descendants are discarded).
 //
 // Of a group of 32 rows of a head: s = the least power of two with max |x| <= 448 s, codes e4m3(x / s), to the nearest, ties to the even one.  Rows of one
-// call that fall into a group are taken together by one warp, 16 bytes a lane, half a warp a row, all of them in registers: the group's maximum is known before the first
-// code is made, and no row is read twice.  A group that was begun before (its row 0 is not among them) keeps its scale or, where the new rows need a larger one, is
+// call that fall into a group are taken together by one warp: asynchronous copies bring them into 8 KB of shared memory, where every lane looks at what it has asked for, 16 bytes of a row, once for the group's maximum and again for the
+// codes.  (Kept in registers, all 32 of them, an SM had 16 warps, not 28: 64 paths of up to 24 nodes in 16 layers 62 us.)
+// A group that was begun before (its row 0 is not among them) keeps its scale or, where the new rows need a larger one, is
 // rounded again by it: with powers of two that changes only what falls below the least codes.
 // An element that is not finite has no part in the maximum and is kept as NaN.
 //
 // Bound by memory: 256 bytes read and 128 written a row (256 more where the caller asks for the values that are kept).
 #include "fp8.cuh"
+#include "umma_common.cuh"
 
 namespace {
 
-constexpr int kWarps = 8;                // of a CTA
+constexpr int kWarps = 4;                // of a CTA
 constexpr int kRows = FSPAD_FP8_GROUP;
-constexpr int kPairs = kRows / 2;        // a pair of rows an instruction
+constexpr int kStage = kRows * FSPAD_HEAD_DIM * 2;   // bytes of a warp's rows
 
 // Larger finite magnitude among two pairs of bf16 that may hold infinities and NaN: what is none counts as 0.
 __device__ __forceinline__ uint32_t finite_most(uint32_t w)
@@ -25,29 +27,37 @@ __device__ __forceinline__ uint32_t finite_most(uint32_t w)
     return max(lo, hi);
 }
 
-// Rows of a group: lane t has row t's place in `src` (rows of 128 elements) and its row of the group; bit t of `there` says whether there is one.
-// codes: row 0 of the group; scale: the group's; begun: its rows before the new ones stay.  `back`, if not NULL, receives the values that are kept, at src's places.
-__device__ __forceinline__ void put_group(const uint4 *src, uint4 *back, uint8_t *codes, float *scale, uint32_t there, long long from, int to, bool begun)
+// All lanes: row `from` of lane t of src into the warp's row t, where bit t of `there` says so.
+__device__ __forceinline__ void fetch(uint32_t rows, const uint4 *src, uint32_t there, long long from)
 {
     const int lane = threadIdx.x & 31, piece = lane & 15, half = lane >> 4;
-    const float old = begun ? *scale : 0.f;          // (asked for before the rows)
-    uint4 x[kPairs];
-    uint32_t most = 0, odd = 0;
-#pragma unroll
-    for (int u = 0; u < kPairs; ++u) {
-        x[u] = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll 8
+    for (int u = 0; u < kRows / 2; ++u) {
         const long long at = __shfl_sync(0xffffffffu, from, 2 * u + half);
-        if ((there >> (2 * u + half)) & 1u) x[u] = src[at * 16 + piece];
+        if ((there >> (2 * u + half)) & 1u) umma::cp_async16(rows + (uint32_t)((2 * u + half) * 256 + piece * 16), src + at * 16 + piece, true);
     }
-#pragma unroll
-    for (int u = 0; u < kPairs; ++u) {
-        const uint32_t m = fspad_most2(fspad_most2(x[u].x, x[u].y), fspad_most2(x[u].z, x[u].w));
-        uint32_t top = max(m & 0xffffu, m >> 16);
-        if (top >= 0x7f80u) {                        // (rare)
-            odd |= 1u << u;
-            top = max(max(finite_most(x[u].x), finite_most(x[u].y)), max(finite_most(x[u].z), finite_most(x[u].w)));
+    umma::cp_async_commit();
+}
+
+// Rows of a group that have been asked for: lane t has row t's place in src and its row of the group; bit t of `there` says whether there is one (there != 0).
+// codes: row 0 of the group; scale: the group's; begun: its rows before the new ones stay.  `back`, if not NULL, receives the values that are kept, at src's places.
+__device__ __forceinline__ void put_group(uint32_t rows, uint4 *back, uint8_t *codes, float *scale, uint32_t there, long long from, int to, bool begun)
+{
+    const int lane = threadIdx.x & 31, piece = lane & 15, half = lane >> 4;
+    const float old = begun ? *scale : 0.f;          // (asked for while the rows are on their way)
+    umma::cp_async_wait<0>();
+    const uint32_t at0 = rows + (uint32_t)(half * 256 + piece * 16);
+    uint32_t most = 0;
+#pragma unroll 4
+    for (int u = 0; u < kRows / 2; ++u) {
+        if (!((there >> (2 * u)) & 3u)) continue;
+        if ((there >> (2 * u + half)) & 1u) {
+            const uint4 x = umma::ld_shared16(at0 + 512u * u);
+            const uint32_t m = fspad_most2(fspad_most2(x.x, x.y), fspad_most2(x.z, x.w));
+            uint32_t top = max(m & 0xffffu, m >> 16);
+            if (top >= 0x7f80u) top = max(max(finite_most(x.x), finite_most(x.y)), max(finite_most(x.z), finite_most(x.w)));     // (rare)
+            most = max(most, top);
         }
-        most = max(most, top);
     }
     most = __reduce_max_sync(0xffffffffu, most);
     int field = fspad_fp8_field(most);
@@ -61,7 +71,7 @@ __device__ __forceinline__ void put_group(const uint4 *src, uint4 *back, uint8_t
     const float s = fspad_field_float(field), inv = fspad_field_float(254 - field);
     if (again) {
         // 32 rows of 128 codes: 16 codes a lane at a time
-#pragma unroll 2
+#pragma unroll 4
         for (int i = 0; i < 8; ++i) {
             uint4 *at = reinterpret_cast<uint4 *>(codes) + i * 32 + lane;
             uint4 c = *at;
@@ -81,46 +91,47 @@ __device__ __forceinline__ void put_group(const uint4 *src, uint4 *back, uint8_t
     }
     __syncwarp();                                    // (the new rows' codes come after)
     if (lane == 0 && !(begun && !again && s == old)) *scale = s;
-#pragma unroll
-    for (int u = 0; u < kPairs; ++u) {
+#pragma unroll 2
+    for (int u = 0; u < kRows / 2; ++u) {
         if (!((there >> (2 * u)) & 3u)) continue;
         const long long at = __shfl_sync(0xffffffffu, from, 2 * u + half);
         const int row = __shfl_sync(0xffffffffu, to, 2 * u + half);
-        uint32_t *w = &x[u].x;
-        uint32_t c[4];
+        if (!((there >> (2 * u + half)) & 1u)) continue;
+        const uint4 x = umma::ld_shared16(at0 + 512u * u);
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        uint32_t c[4], m = fspad_most2(fspad_most2(x.x, x.y), fspad_most2(x.z, x.w));
 #pragma unroll
         for (int j = 0; j < 4; ++j) c[j] = fspad_f32_to_e4m3(__uint_as_float(w[j] << 16) * inv, __uint_as_float(w[j] & 0xffff0000u) * inv);
-        if ((odd >> u) & 1u) {                       // (an infinity, which would be cut to 448)
+        if (max(m & 0xffffu, m >> 16) >= 0x7f80u) {  // (an infinity, which would be cut to 448)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 if ((w[j] & 0x7fffu) >= 0x7f80u) c[j] = (c[j] & 0xff00u) | 0x7fu;
                 if (((w[j] >> 16) & 0x7fffu) >= 0x7f80u) c[j] = (c[j] & 0xffu) | 0x7f00u;
             }
         }
-        if ((there >> (2 * u + half)) & 1u) {
-            reinterpret_cast<uint2 *>(codes)[row * 16 + piece] = make_uint2(c[0] | (c[1] << 16), c[2] | (c[3] << 16));
-            if (back) {
-                uint4 o;
-                uint32_t *ow = &o.x;
+        reinterpret_cast<uint2 *>(codes)[row * 16 + piece] = make_uint2(c[0] | (c[1] << 16), c[2] | (c[3] << 16));
+        if (back) {
+            uint32_t o[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t h = fspad_e4m3_to_f16(c[j]);
-                    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h));
-                    const __nv_bfloat162 v = __floats2bfloat162_rn(f.x * s, f.y * s);
-                    ow[j] = *reinterpret_cast<const uint32_t *>(&v);
-                }
-                back[at * 16 + piece] = o;
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t h = fspad_e4m3_to_f16(c[j]);
+                const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h));
+                const __nv_bfloat162 v = __floats2bfloat162_rn(f.x * s, f.y * s);
+                o[j] = *reinterpret_cast<const uint32_t *>(&v);
             }
+            back[at * 16 + piece] = make_uint4(o[0], o[1], o[2], o[3]);
         }
     }
 }
 
 // Rows [2][Hkv][rows] to the slots slots[rows] of one layer.  A warp looks at `each` entries (a power of two, at most 32) of a head's K or V and takes the groups that have their first row there;
 // the rows of a group stand within 32 entries.
-__global__ void __launch_bounds__(kWarps * 32)
+__global__ void __launch_bounds__(kWarps * 32, 7)
 kv_write_fp8_kernel(const uint4 *k, const uint4 *v, const long long *__restrict__ slots, int rows, int Hkv, int each, uint8_t *codes, float *scales,
                     int n_blocks, uint4 *k_rounded, uint4 *v_rounded, int *__restrict__ status)
 {
+    __shared__ __align__(128) unsigned char s_rows[kWarps * kStage];
+    const uint32_t st = umma::smem_u32(s_rows) + (threadIdx.x >> 5) * kStage;
     fspad_pdl_trigger();
     fspad_pdl_wait();
     const int lane = threadIdx.x & 31;
@@ -154,46 +165,63 @@ kv_write_fp8_kernel(const uint4 *k, const uint4 *v, const long long *__restrict_
         const uint32_t there = (now >> i) | (i > 0 ? after << (32 - i) : 0u);
         const long long sl1 = __shfl_sync(0xffffffffu, s[1], (i + lane) & 31), sl2 = __shfl_sync(0xffffffffu, s[2], (i + lane) & 31);
         const long long slot = i + lane < 32 ? sl1 : sl2;
+        const long long from = (long long)head * rows + first + i + lane;
+        fetch(st, plane ? v : k, there, from);
         const bool begun = !__any_sync(0xffffffffu, ((there >> lane) & 1u) && (slot & 31) == 0);
         const long long block = group >> 2, g = ((long long)plane * n_blocks + block) * Hkv + head;
-        put_group(plane ? v : k, plane ? v_rounded : k_rounded, codes + (g * 128 + (group & 3) * kRows) * 128, scales + g * FSPAD_FP8_GROUPS + (group & 3), there,
-                  (long long)head * rows + first + i + lane, (int)(slot & 31), begun);
+        put_group(st, plane ? v_rounded : k_rounded, codes + (g * 128 + (group & 3) * kRows) * 128, scales + g * FSPAD_FP8_GROUPS + (group & 3), there, from,
+                       (int)(slot & 31), begun);
     }
 }
 
-// cache row L_b + j <- tree row path[b][j] of the slice, j < n_acc[b]; a warp per (layer, K/V, sequence, head).
-__global__ void __launch_bounds__(kWarps * 32)
+// cache row L_b + j <- tree row path[b][j] of the slice, j < n_acc[b]; a warp per (layer, K/V, sequence, head) and group of 32 rows (as many as a path of all nodes can touch).
+__global__ void __launch_bounds__(kWarps * 32, 7)
 kv_append_fp8_kernel(uint8_t *codes, float *scales, const int *__restrict__ table, int table_stride, int n_blocks, const uint4 *tree_kv,
                      const int *__restrict__ path, const int *__restrict__ n_acc, const int *__restrict__ prefix_len, int n_layers, int B, int Hkv, int N,
-                     int path_stride, uint4 *rounded, int *__restrict__ new_len, int *__restrict__ status)
+                     int path_stride, int groups, uint4 *rounded, int *__restrict__ new_len, int *__restrict__ status)
 {
+    __shared__ __align__(128) unsigned char s_rows[kWarps * kStage];
+    const uint32_t st = umma::smem_u32(s_rows) + (threadIdx.x >> 5) * kStage;
     fspad_pdl_trigger();
     fspad_pdl_wait();
     const int lane = threadIdx.x & 31;
-    const unsigned number = blockIdx.x * kWarps + (threadIdx.x >> 5), of_seq = number / (unsigned)Hkv, lk = of_seq / (unsigned)B;  // lk: layer * 2 + (K or V)
-    if (lk >= 2u * n_layers) return;
+    const long long job = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
+    // (a slice has 256 bytes of tree_kv at least: 32 bits are enough for its number)
+    const long long slices = (long long)n_layers * 2 * B * Hkv;
+    const int group = (int)(job / slices);           // (the last ones, which few paths reach, at the end)
+    const unsigned number = (unsigned)(job - group * slices), of_seq = number / (unsigned)Hkv, lk = of_seq / (unsigned)B;        // lk: layer * 2 + (K or V)
+    if (group >= groups) return;
     const int h = (int)(number - of_seq * Hkv), b = (int)(of_seq - lk * B);
+    const int *pth = path + (size_t)b * path_stride;
+    // entries 32 (group - 1) .. of the path, before it is known which the group's are
+    const int e0 = 32 * (group - 1) + lane, e1 = e0 + 32;
+    const int p0 = e0 >= 0 && e0 < path_stride ? pth[e0] : -1, p1 = e1 < path_stride ? pth[e1] : -1;
     int L = prefix_len[b], n = n_acc[b];
     bool bad = false;
     if (n < 0 || n > path_stride || n > N) { bad = true; n = 0; }
     if (L < 0 || (long long)L + n > (long long)table_stride * 128) { bad = true; n = 0; }
-    if (new_len && lane == 0 && lk == 0 && h == 0) new_len[b] = L + n;
-    const int *pth = path + (size_t)b * path_stride;
-    const int end = L + n;                           // (at most 128 * table_stride, which is an int)
-    for (int r0 = L & ~(kRows - 1); n > 0 && r0 < end; r0 += kRows) {
-        const int r = r0 + lane;
-        int node = -1;
-        if (r >= L && r < end) {
-            node = pth[r - L];
-            if (node < 0 || node >= N) { bad = true; node = -1; }
-        }
+    if (new_len && lane == 0 && lk == 0 && h == 0 && group == 0) new_len[b] = L + n;
+    const int end = L + n, r0 = (L & ~(kRows - 1)) + group * kRows;
+    if (n > 0 && r0 < end) {
+        // row r0 + lane is entry 32 group + lane - (L % 32)
+        const int back = L & (kRows - 1), from_lane = (lane - back) & 31, q0 = __shfl_sync(0xffffffffu, p0, from_lane), q1 = __shfl_sync(0xffffffffu, p1, from_lane), r = r0 + lane;
+        int node = lane >= back ? q1 : q0;
         const int block = table[(size_t)b * table_stride + (r0 >> 7)];
-        if (block < 0 || block >= n_blocks) { bad = true; continue; }
-        const uint32_t there = __ballot_sync(0xffffffffu, node >= 0);
-        const long long g = ((long long)lk * n_blocks + block) * Hkv + h;
-        if (there)
-            put_group(tree_kv, rounded, codes + (g * 128 + (r0 & 127)) * 128, scales + g * FSPAD_FP8_GROUPS + ((r0 & 127) / kRows), there,
-                      (long long)number * N + node, lane, r0 < L);
+        if (r < L || r >= end) {
+            node = -1;
+        } else if (node < 0 || node >= N) {
+            bad = true;
+            node = -1;
+        }
+        uint32_t there = __ballot_sync(0xffffffffu, node >= 0);
+        const long long from = (long long)number * N + node;
+        if (there) fetch(st, tree_kv, there, from);
+        const bool inside = block >= 0 && block < n_blocks;
+        if (!inside) bad = true;
+        if (there && inside) {
+            const long long g = ((long long)lk * n_blocks + block) * Hkv + h;
+            put_group(st, rounded, codes + (g * 128 + (r0 & 127)) * 128, scales + g * FSPAD_FP8_GROUPS + ((r0 & 127) / kRows), there, from, lane, r0 < L);
+        }
     }
     if (bad) fspad_report(status, FSPAD_ERR_RANGE);
 }
@@ -218,9 +246,11 @@ cudaError_t fspad_launch_kv_append_fp8(fspad_ctx *ctx, uint8_t *codes, float *sc
                                        const int *n_acc, const int *prefix_len, int N, int B, fspad_bf16 *rounded, int *new_len, cudaStream_t st)
 {
     const fspad_config &c = ctx->cfg;
-    const long long slices = (long long)c.n_layers * 2 * B * c.n_kv_heads;
+    const int groups = (N + 2 * kRows - 2) / kRows;              // (that N rows, from anywhere in a group on, touch)
+    const long long jobs = (long long)c.n_layers * 2 * B * c.n_kv_heads * groups;
+    if (jobs > 0x7fffffffll * kWarps) return cudaErrorInvalidConfiguration;
     ctx->launches++;
-    return fspad_launch(kv_append_fp8_kernel, dim3((unsigned)((slices + kWarps - 1) / kWarps)), dim3(kWarps * 32), 0, st, 0, codes, scales, paged.table,
+    return fspad_launch(kv_append_fp8_kernel, dim3((unsigned)((jobs + kWarps - 1) / kWarps)), dim3(kWarps * 32), 0, st, 0, codes, scales, paged.table,
                         paged.stride, paged.n_blocks, reinterpret_cast<const uint4 *>(tree_kv), path, n_acc, prefix_len, c.n_layers, B, c.n_kv_heads, N,
-                        c.max_nodes, reinterpret_cast<uint4 *>(rounded), new_len, ctx->d_status);
+                        c.max_nodes, groups, reinterpret_cast<uint4 *>(rounded), new_len, ctx->d_status);
 }
