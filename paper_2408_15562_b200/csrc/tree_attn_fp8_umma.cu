@@ -1,14 +1,15 @@
 // Attention over the cache held in 8 bits for many query rows a kv head (a tree's verification), on the 5th-generation tensor cores.  (What is computed, and
 // the kernel for few rows: tree_attn_fp8.cu; the list of work and its cutting: packed_list.cuh.)
 //
-// A CTA takes 256 query rows of a kv head and chunks of 128 keys.  Its sixteen warps have four jobs and meet only on mbarriers:
+// A CTA takes 256 query rows of a kv head and chunks of 128 keys.  Its sixteen warps have five jobs and meet only on mbarriers:
 //   warps 0-7   softmax, in two groups of 128 threads, a query row a thread
 //   warp 8      copies: K and V codes of a chunk into one of three buffers, K's by TMA as the tensor cores read them, V's as they lie
-//   warp 9      tensor cores: one lane issues every product; the warp owns the tensor memory
+//   warps 9, 11 tensor cores: a warp for each group, one lane of which issues its products; warp 9 owns the tensor memory
+//   warp 10     scales of a chunk, as the softmax takes them
 //   warps 12-15 V codes -> fp16 values, into V tiles as the tensor cores read them (two of them); the tree's bf16 rows too
-// Per chunk and group: S = Q K^T (128 x 128 x 128) into tensor memory, weights in registers, P back over the scores, O += P V with P read from tensor
-// memory.  With more than 128 rows group g has rows 128 g .. and every chunk; with fewer both have the same rows and take the
-// chunks in turn, each with an accumulator of its own, and are merged at the end.
+// Per chunk and group, 64 keys at a time: S = Q K^T (128 x 64 x 128) into tensor memory, weights in registers, P back over the scores, O += P V with P read from tensor
+// memory; while one half of a chunk is at its exponentials, the products around the other go on.  With more than 128 rows group g has rows 128 g .. and every chunk; with fewer both have the
+// same rows and take the chunks in turn, each with an accumulator of its own, and are merged at the end.
 //
 // K is never touched outside the tensor cores: its e4m3 codes are an operand as they are, and a query is the sum of two e4m3 numbers, the nearest one and what is
 // left, which is exact for elements of at least 2^-10 of the row's largest (a bf16 number has 8 significant bits, the two have 4 each); smaller ones are
@@ -37,6 +38,7 @@ constexpr int BUFS = 3;                  // K codes | V codes of a chunk; of the
 constexpr int SMEM = (4 + BUFS) * TILE;  // Q[2] | buffers | V[2]
 constexpr uint32_t TMEM_COLS = 512;      // S, then P, of group g: columns 128 g ..; O of group g: 256 + 128 g ..
 constexpr uint32_t IDESC = (1u << 4) | ((128u >> 3) << 17) | ((128u >> 4) << 24);      // 128 x 128, fp32 accumulator, fp16 operands (kind::f8f6f4: e4m3 ones)
+constexpr uint32_t IDESC64 = (1u << 4) | ((64u >> 3) << 17) | ((128u >> 4) << 24);       // 128 x 64
 constexpr uint32_t IDESC_BF = (1u << 7) | (1u << 10), IDESC_MN = 1u << 16;             // bf16 operands; B (= V) MN-major
 
 // byte offset of 16-byte piece c (0..15) of row r of a tile
@@ -92,46 +94,39 @@ __device__ __forceinline__ float factor(float cs, float scale)
     return fmaxf(cs * scale, 0x1p-126f);
 }
 
-__device__ __forceinline__ void tmem_st32u(uint32_t addr, const uint32_t (&v)[32])
+// One group's turn at half a chunk: 64 scores of a row -> weights, over the scores' first 32 columns, packed in pairs.
+// `of_keys`: of each 32 keys of the chunk the scale of K, log2 of V's scale, and its reciprocal (four of each); of the tree's 1, 0 and 1.  `wait_o`: until the group's product before the last
+// one (which the scores are known to come behind) is complete too.
+template <bool plain, typename F>
+__device__ __forceinline__ void softmax_half(bool tree, uint32_t tS, uint32_t tO, const uint32_t (&see)[2], float cs, const float *of_keys, bool row_ok, bool first,
+                                             float &m_run, float &l_run, F wait_o)
 {
-    __syncwarp();
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-                 "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};\n"
-                 :: "r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]),
-                    "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]),
-                    "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]) : "memory");
-}
-
-// One group's turn at a chunk: scores -> weights.  All 128 scores of a row are in registers after one trip to tensor memory (every further
-// wait for it costs 250 cycles: by quarters, read twice, a turn took 2650); the weights, packed in pairs, go to columns 64 .. 127, over scores.
-// `enter`, `leave`: around the exponentials, which the groups take in turn.  `of_keys`: of each 32 keys the scale of K, log2 of V's scale, and its reciprocal (four of each); of the tree's 1, 0 and 1.
-template <bool plain, typename E, typename L, typename T>
-__device__ __forceinline__ void softmax_chunk(bool tree, uint32_t tS, uint32_t tO, const uint32_t (&see)[4], float cs, const float *of_keys, bool row_ok, bool first,
-                                              float &m_run, float &l_run, E enter, L leave, T told)
-{
-    uint32_t r[4][32];
+    uint32_t r[2][32];
     __syncwarp();
 #pragma unroll
-    for (int x = 0; x < 4; ++x) tmem_ld32_issue(tS + 32u * x, r[x]);
+    for (int x = 0; x < 2; ++x) tmem_ld32_issue(tS + 32u * x, r[x]);
     tmem_ld_wait(r[0]);
     tmem_ld_pin(r[1]);
-    tmem_ld_pin(r[2]);
-    tmem_ld_pin(r[3]);
     if (!plain) {
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
+        for (int x = 0; x < 2; ++x)
 #pragma unroll
             for (int j = 0; j < 32; ++j)
                 if (!((see[x] >> j) & 1u)) r[x][j] = 0xff800000u;
     }
-    float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    float mx4[2][2] = {{-INFINITY, -INFINITY}, {-INFINITY, -INFINITY}};
 #pragma unroll
-    for (int j = 0; j < 32; j += 2)
+    for (int j = 0; j < 32; j += 4)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) mx4[x] = fmaxf(fmaxf(mx4[x], __uint_as_float(r[x][j])), __uint_as_float(r[x][j + 1]));
-    float mx = -INFINITY;
+        for (int x = 0; x < 2; ++x)
 #pragma unroll
-    for (int x = 0; x < 4; ++x) mx = fmaxf(mx, fmaf(mx4[x], factor(cs, of_keys[x]), of_keys[4 + x]));
+            for (int y = 0; y < 2; ++y) mx4[x][y] = fmaxf(fmaxf(mx4[x][y], __uint_as_float(r[x][j + 2 * y])), __uint_as_float(r[x][j + 2 * y + 1]));
+    float mul[2], mx = -INFINITY;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        mul[x] = factor(cs, of_keys[x]);
+        mx = fmaxf(mx, fmaf(fmaxf(mx4[x][0], mx4[x][1]), mul[x], of_keys[4 + x]));
+    }
     // the reference follows the row's maximum when some row of the warp would see a weight too large otherwise (a warp moves as one:
     // its accesses to tensor memory are collective); a row that does not exist has no say
     const float m_cand = fmaxf(m_run, mx);
@@ -141,41 +136,34 @@ __device__ __forceinline__ void softmax_chunk(bool tree, uint32_t tS, uint32_t t
     if (move) {
         const float alpha = ex2f(m_run - m_safe);
         l_run *= alpha;
-        if (!first) {                    // the group's products so far are complete: the scores that were waited for come behind them
+        if (!first) {
+            wait_o();
 #pragma unroll 1
             for (int blk = 0; blk < 8; ++blk) tmem_scale16(tO + (uint32_t)blk * 16u, alpha);
         }
     }
     m_run = m_new;
     const float shift = (!plain && tree ? -kLazyLog2 : kBiasLog2) - m_safe;        // (of the tree's keys times kDown)
-    enter();
     float sum = 0.f;
 #pragma unroll
-    for (int y = 0; y < 2; ++y) {                    // 64 keys at a time: their product with V can begin
-        uint32_t w[32];
+    for (int x = 0; x < 2; ++x) {
+        const float add = shift + of_keys[4 + x];
+        const uint64_t scale2 = f32x2(mul[x], mul[x]), neg = f32x2(add, add);
+        uint64_t acc[2] = {0ull, 0ull};
+        uint32_t w[16];
 #pragma unroll
-        for (int z = 0; z < 2; ++z) {
-            const int x = 2 * y + z;
-            const float mul = factor(cs, of_keys[x]), add = shift + of_keys[4 + x];
-            const uint64_t scale2 = f32x2(mul, mul), neg = f32x2(add, add);
-            uint64_t acc[2] = {0ull, 0ull};
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                float x0, x1;
-                f32x2_split(f32x2_fma(f32x2(__uint_as_float(r[x][2 * e]), __uint_as_float(r[x][2 * e + 1])), scale2, neg), x0, x1);
-                const float p0 = ex2f(x0), p1 = ex2f(x1);
-                acc[e & 1] = f32x2_add(acc[e & 1], f32x2(p0, p1));
-                if (!plain && tree) w[16 * z + e] = pack_bf16(p0, p1);
-                else w[16 * z + e] = pack_f16(p0, p1);
-            }
-            float lo, hi;
-            f32x2_split(f32x2_add(acc[0], acc[1]), lo, hi);
-            sum = fmaf(lo + hi, of_keys[8 + x], sum);
+        for (int e = 0; e < 16; ++e) {
+            float x0, x1;
+            f32x2_split(f32x2_fma(f32x2(__uint_as_float(r[x][2 * e]), __uint_as_float(r[x][2 * e + 1])), scale2, neg), x0, x1);
+            const float p0 = ex2f(x0), p1 = ex2f(x1);
+            acc[e & 1] = f32x2_add(acc[e & 1], f32x2(p0, p1));
+            if (!plain && tree) w[e] = pack_bf16(p0, p1);
+            else w[e] = pack_f16(p0, p1);
         }
-        if (y == 1) leave();
-        tmem_st32u(tS + 64u + 32u * y, w);
-        asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory");
-        told(y);
+        tmem_st16(tS + 16u * x, w);
+        float lo, hi;
+        f32x2_split(f32x2_add(acc[0], acc[1]), lo, hi);
+        sum = fmaf(lo + hi, of_keys[8 + x], sum);
     }
     l_run += sum * (!plain && tree ? kUp : 1.f);
 }
@@ -202,7 +190,7 @@ tree_attn_fp8_umma_kernel(const Args a, const __grid_constant__ CUtensorMap k_ma
 {
     extern __shared__ __align__(1024) unsigned char smem_raw[];      // (nothing else is in shared memory, so it starts on such a boundary: looked at below)
     enum { B_FULL = 0, B_FREE = BUFS, K_FULL = 2 * BUFS, T_FULL = 3 * BUFS, V_FULL = 4 * BUFS, V_FREE = V_FULL + 2, S_FULL = V_FREE + 2,
-           P_FULL = S_FULL + 2, O_DONE = P_FULL + 4, Q_FULL = O_DONE + 2, E_FULL = Q_FULL + 2, DRAIN = E_FULL + 2, N_BAR = DRAIN + 2 };
+           P_FULL = S_FULL + 4, O_DONE = P_FULL + 4, Q_FULL = O_DONE + 4, E_FULL = Q_FULL + 2, DRAIN = E_FULL + 2, N_BAR = DRAIN + 2 };
     Small &sm = *reinterpret_cast<Small *>(smem_raw + SMEM);
     static_assert(N_BAR <= Small::BARS, "barriers");
     auto &s_bar = sm.bar;
@@ -285,12 +273,7 @@ tree_attn_fp8_umma_kernel(const Args a, const __grid_constant__ CUtensorMap k_ma
         const int grp = warp >> 2, row = tid & 127;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t tS = tmem + lanes + 128u * grp, tO = tmem + lanes + 256u + 128u * grp;
-        uint32_t n_done = 0, ph_o = 0, tree_chunks = 0, chunks = 0;    // products of the group so far; the tree's chunks and all of the CTA so far
-        // The groups take turns at their exponentials: while one is there, the products of the other go on.  (In step both waited for the special functions, and then both for
-        // the tensor cores.)  A barrier a group: its 128 threads wait on it, the other's 128 arrive.
-        auto enter = [&] { asm volatile("bar.sync %0, 256;\n" :: "r"(2 + grp) : "memory"); };
-        auto leave = [&] { asm volatile("bar.arrive %0, 256;\n" :: "r"(3 - grp) : "memory"); };
-        if (grp == 1) leave();
+        uint32_t n_done = 0, tree_chunks = 0, chunks = 0;    // products of the group so far; the tree's chunks and all of the CTA so far
         auto told = [&](int y) {                             // half y of the weights is there
             tc_fence_before();
             __syncwarp();
@@ -399,18 +382,23 @@ tree_attn_fp8_umma_kernel(const Args a, const __grid_constant__ CUtensorMap k_ma
             int c = s.two ? 0 : grp;
             auto turn = [&](auto plain_, bool tree, const uint32_t (&see)[4]) {
                 constexpr bool plain = decltype(plain_)::value;
-                if (!failed && !mbar_wait(bar(S_FULL + grp), n_done & 1u)) failed = true;
-                tc_fence_after();
-                if (live) {
-                    const float *of_keys = s_scale[!plain && tree ? SCALES : (chunks + (uint32_t)c) % SCALES];
-                    softmax_chunk<plain>(tree, tS, tO, see, !plain && tree ? a.scale_log2 : cs, of_keys, row_ok, first, m_run, l_run, enter, leave, told);
-                } else {
-                    enter();
-                    leave();
-                    told(0);
-                    told(1);
+                const float *of_keys = s_scale[!plain && tree ? SCALES : (chunks + (uint32_t)c) % SCALES];
+#pragma unroll 1
+                for (int y = 0; y < 2; ++y) {                // 64 keys at a time
+                    if (!failed && !mbar_wait(bar(S_FULL + 2 * grp + y), n_done & 1u)) failed = true;
+                    tc_fence_after();
+                    if (live) {
+                        const uint32_t see2[2] = {y ? see[2] : see[0], y ? see[3] : see[1]};
+                        softmax_half<plain>(tree, tS + 64u * y, tO, see2, !plain && tree ? a.scale_log2 : cs, of_keys + 2 * y, row_ok, first, m_run, l_run, [&] {
+                            // the other half's product before this one
+                            if (!failed && !mbar_wait(bar(O_DONE + 2 * grp + (y ^ 1)), (n_done + (uint32_t)y - 1u) & 1u)) failed = true;
+                            tc_fence_after();
+                        });
+                        asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory");
+                    }
+                    told(y);
+                    first = false;
                 }
-                first = false;
                 ++n_done;
             };
 #pragma unroll 1
@@ -454,16 +442,11 @@ tree_attn_fp8_umma_kernel(const Args a, const __grid_constant__ CUtensorMap k_ma
                 }
                 c += step;
             }
-            if (!s.two && grp == 1 && (s.n_ch & 1)) {        // (group 1 takes as many turns as group 0)
-                enter();
-                leave();
-            }
             tree_chunks += s.n_tree;
             chunks += (uint32_t)s.n_ch;
             // ---- the group's last product, then the rows ----
             if (!first) {
-                if (!failed && !mbar_wait(bar(O_DONE + grp), ph_o)) failed = true;
-                ph_o ^= 1u;
+                if (!failed && !mbar_wait(bar(O_DONE + 2 * grp + 1), (n_done - 1u) & 1u)) failed = true;
             }
             tc_fence_after();
             const bool whole = s.n_ch == s.n_run;
@@ -556,7 +539,6 @@ tree_attn_fp8_umma_kernel(const Args a, const __grid_constant__ CUtensorMap k_ma
                 tc_fence_after();
             }
         }
-        if (grp == 0) enter();                               // (what the other has left behind)
         if (lane == 0) bulk_store_wait();                    // (the copies' memory is this CTA's)
     } else if (warp < 12) {
       asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
@@ -633,56 +615,59 @@ tree_attn_fp8_umma_kernel(const Args a, const __grid_constant__ CUtensorMap k_ma
                 if (!failed && !mbar_wait(bar(K_FULL + buf), (at / BUFS) & 1u)) failed = true;
                 if (c < s.n_tree && !failed && !mbar_wait(bar(T_FULL + buf), (ph_t >> buf) & 1u)) failed = true;
             };
-            auto issue_s = [&](int j) {
+            auto issue_s = [&](int j, int y) {               // half y of its keys
                 const int c = s.two ? j : 2 * j + g;
                 const bool tree = c < s.n_tree;
                 const uint32_t buf = (cc + (uint32_t)c) % BUFS;
-                if (s.two && c == s.n_tree && c > 0) wait_q();               // the tile again, as e4m3
+                if (y == 0 && s.two && c == s.n_tree && c > 0) wait_q();     // the tile again, as e4m3
                 if (failed) return;
                 tc_fence_after();
-                const uint32_t kb = k_lo + buf * (TILE >> 4), qb = q_lo + (s.two ? (uint32_t)g : tree ? 0u : 1u) * (TILE >> 4);
+                const uint32_t kb = k_lo + buf * (TILE >> 4) + (uint32_t)y * (8192u >> 4), qb = q_lo + (s.two ? (uint32_t)g : tree ? 0u : 1u) * (TILE >> 4), d = tS + 64u * y;
                 if (tree) {
 #pragma unroll
                     for (int ks = 0; ks < 8; ++ks) {
                         const uint32_t off = ((ks >> 2) * HALF + (ks & 3) * 32) >> 4;
-                        mma_f16_lo(tS, qb + off, hi, kb + off, hi, IDESC | IDESC_BF, ks > 0, issuer);
+                        mma_f16_lo(d, qb + off, hi, kb + off, hi, IDESC64 | IDESC_BF, ks > 0, issuer);
                     }
                 } else {
 #pragma unroll
                     for (int ks = 0; ks < 8; ++ks)           // (the queries' second halves against the same codes)
-                        mma_f8_ss(tS, qb + (uint32_t)(((ks >> 2) * HALF + (ks & 3) * 32) >> 4), kb + (uint32_t)((ks & 3) * 32 >> 4), hi, IDESC, ks > 0, issuer);
+                        mma_f8_ss(d, qb + (uint32_t)(((ks >> 2) * HALF + (ks & 3) * 32) >> 4), kb + (uint32_t)((ks & 3) * 32 >> 4), hi, IDESC64, ks > 0, issuer);
                 }
-                mma_commit_if(bar(S_FULL + g), issuer);
-                mma_commit_if(bar(B_FREE + buf), issuer);                    // (two groups' products with two tiles, one group's twice with one)
-                if (!s.two) mma_commit_if(bar(B_FREE + buf), issuer);
+                mma_commit_if(bar(S_FULL + 2 * g + y), issuer);
+                if (y == 1) {                                // (two groups' products with two tiles, one group's twice with one)
+                    mma_commit_if(bar(B_FREE + buf), issuer);
+                    if (!s.two) mma_commit_if(bar(B_FREE + buf), issuer);
+                }
             };
             if (turns > 0) {
                 wait_k(0);
-                issue_s(0);
+                issue_s(0, 0);
+                issue_s(0, 1);
             }
 #pragma unroll 1
             for (int j = 0; j < turns; ++j) {
                 const int c = s.two ? j : 2 * j + g;
                 const bool tree = c < s.n_tree;
                 const uint32_t at = cc + (uint32_t)c, slot = at & 1u;
-                const uint32_t vb = v_lo + slot * (TILE >> 4), idesc = IDESC | IDESC_MN | (tree ? IDESC_BF : 0u);
                 // (what the next scores and this product need besides the weights is waited for ahead of them: a wait for a phase that is long over costs 170 cycles)
                 if (j + 1 < turns) wait_k(j + 1);
                 if (!failed && !mbar_wait(bar(V_FULL + slot), (at >> 1) & 1u)) failed = true;
-#pragma unroll
+#pragma unroll 1
                 for (int y = 0; y < 2; ++y) {
+                    const uint32_t vb = v_lo + slot * (TILE >> 4) + (uint32_t)y * (8192u >> 4), idesc = IDESC | IDESC_MN | (tree ? IDESC_BF : 0u);
                     if (!failed && !mbar_wait(bar(P_FULL + 2 * g + y), n_p & 1u)) failed = true;
                     if (failed) continue;
                     tc_fence_after();
 #pragma unroll
-                    for (int ks = 4 * y; ks < 4 * y + 4; ++ks)       // 16 keys an instruction: 8 columns of packed pairs
-                        mma_f16_ts(tO, tS + 64u + (uint32_t)ks * 8u, vb + (uint32_t)(ks * 16 * 128 >> 4), hi, idesc, j > 0 || ks > 0, issuer);
-                }
-                if (!failed && j + 1 >= turns) mma_commit_if(bar(O_DONE + g), issuer);
-                if (!failed && j + 1 < turns) issue_s(j + 1);        // (a thread's products complete in order: the scores may replace the weights)
-                if (!failed) {
-                    mma_commit_if(bar(V_FREE + slot), issuer);
-                    if (!s.two) mma_commit_if(bar(V_FREE + slot), issuer);
+                    for (int ks = 0; ks < 4; ++ks)           // 16 keys an instruction: 8 columns of packed pairs
+                        mma_f16_ts(tO, tS + 64u * y + (uint32_t)ks * 8u, vb + (uint32_t)(ks * 16 * 128 >> 4), hi, idesc, j + y + ks > 0, issuer);
+                    mma_commit_if(bar(O_DONE + 2 * g + y), issuer);
+                    if (j + 1 < turns) issue_s(j + 1, y);    // (a thread's products complete in order: the scores may replace the weights)
+                    if (y == 1) {
+                        mma_commit_if(bar(V_FREE + slot), issuer);
+                        if (!s.two) mma_commit_if(bar(V_FREE + slot), issuer);
+                    }
                 }
                 ++n_p;
             }

@@ -115,6 +115,15 @@ def test_many_sequences(nodes):
     case.check(_run(case))
 
 
+@pytest.mark.parametrize("nodes,heads,batch", [(40, (8, 2), 40), (60, (8, 2), 20), (70, (6, 2), 33), (100, (2, 2), 70), (33, (8, 1), 90), (256, (2, 1), 9), (1, (16, 4), 70), (6, (8, 2), 50)])
+def test_lists_that_are_cut_wherever_it_falls(nodes, heads, batch):
+    """Ragged runs, many shorter than a part and what a beginning counts, with one row tile, two, and one and two of them in turn."""
+    rng = np.random.default_rng(nodes)
+    lens = np.where(rng.random(batch) < 0.3, rng.integers(0, 3, batch), rng.integers(0, 700, batch))
+    case = Case(nodes, batch, nodes, *heads, lens)
+    case.check(_run(case))
+
+
 @pytest.mark.parametrize("nodes,heads", [(1, (4, 1)), (8, (4, 1)), (60, (4, 1)), (256, (1, 1))])
 def test_one_long_sequence_over_all_sms(nodes, heads):
     case = Case(9, 1, nodes, *heads, [30000])
