@@ -13,7 +13,7 @@
 //   a weight = hi + mid + lo, e5m2, each the nearest number to what is left: 3 significant bits each, off by at most 2^-9 of the weight and 2^-17 (2^11 stands for the largest)
 // V's scale goes into the weights, as an addend of the exponent: the reference that weights are relative to follows the maximum of score + log2(scale).
 //
-// A CTA's warps: 0 copies, 1 the tensor cores' products, 4-7 and 8-11 two groups that take the chunks of 128 keys in turn, a key a thread, each with a
+// A CTA's warps: 0 copies, 1 and 2 the tensor cores' products of the two groups, 4-7 and 8-11 the groups that take the chunks of 128 keys in turn, a key a thread, each with a
 // reference, sums and an accumulator of its own.  The tree's keys (32 at most) are dealt with in single precision, by the second group ahead of the chunks.
 #include "fp8.cuh"
 #include "packed_list.cuh"
@@ -29,13 +29,13 @@ constexpr int SLOT = 128 * 128;          // codes of a chunk's K or V
 constexpr float kLag = 4.f, kBias = 11.f;            // weights are 2^(score - reference + 11), the largest at most 2^15
 constexpr float kOwnDown = 0x1p-11f;                 // ... of which the accumulators and sums are rid at the end
 
-__host__ __device__ constexpr int slots_of(int R) { return R == 32 ? 11 : 12; }
+__host__ __device__ constexpr int slots_of(int R) { return R == 32 ? 10 : 12; }
 __host__ __device__ constexpr int columns_of(int R) { return R == 8 ? 32 : 3 * R; }          // of weights: a multiple of 16
-__host__ __device__ constexpr int tmem_of(int R) { return R == 8 ? 128 : R == 16 ? 256 : 512; }
+__host__ __device__ constexpr int tmem_of(int R) { return R == 32 ? 512 : 256; }
 
 template <int R> struct Small {
-    unsigned long long full[slots_of(R)], free[slots_of(R)], s_full[2], p_full[2], o_done[2], q_full, drain;
-    float raw[8][8];                     // scales of a chunk's K and V, by its number
+    unsigned long long full[slots_of(R)], free[slots_of(R)], s_full[2][2], p_full[2][2], o_done[2][2], q_full, drain[2];
+    alignas(16) float raw[8][8];         // (bulk copies' destination) scales of a chunk's K and V, by its number
     float cs[R];                         // a query's scores -> log2 units
     float ref[2][R], lim[2][R], m[2][R], alpha[2][R];        // of each group's rows: kBias - reference; what a score may reach; the reference; the accumulator's factor
     float top[2][4][R], sum[2][4][R];    // by warps
@@ -45,16 +45,17 @@ template <int R> struct Small {
     uint32_t tmem;
     int fail;
 };
-template <int R> constexpr int bytes_of() { return slots_of(R) * SLOT + 2 * R * 128 + 2 * columns_of(R) * 128 + (int)sizeof(Small<R>); }
+template <int R> constexpr int bytes_of() { return slots_of(R) * SLOT + 2 * R * 128 + 4 * columns_of(R) * 128 + (int)sizeof(Small<R>); }
 
 struct Maps { CUtensorMap k, v; };
 
-__device__ __forceinline__ void mma_f8(uint32_t d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate)
+// (Issued by the one lane whose e is not 0.)
+__device__ __forceinline__ void mma_f8(uint32_t d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate, uint32_t e)
 {
-    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+    asm volatile("{\n\t.reg .pred p, q;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %6, 0;\n\tsetp.ne.b32 q, %7, 0;\n\t"
                  "mov.b64 da, {%1, %2};\n\tmov.b64 db, {%3, %4};\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], da, db, %5, p;\n\t}\n"
-                 :: "r"(d), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate) : "memory");
+                 "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], da, db, %5, p;\n\t}\n"
+                 :: "r"(d), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate), "r"(e) : "memory");
 }
 // N columns of a lane, from tensor memory; all that were asked for are there behind ld_wait.
 __device__ __forceinline__ void ld_issue(uint32_t at, uint32_t (&r)[4])
@@ -85,6 +86,13 @@ __device__ __forceinline__ void st8(uint32_t at, const uint32_t (&r)[8])
 {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};\n"
                  :: "r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
+// The largest of a warp's values (NaN have no part in it).
+__device__ __forceinline__ float warp_max(float x)
+{
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;\n" : "=f"(r) : "f"(x));     // (volatile: of the whole warp, whoever uses it)
+    return r;
 }
 __device__ __forceinline__ void group_sync(int g) { asm volatile("bar.sync %0, 128;\n" :: "r"(1 + g) : "memory"); }
 __device__ __forceinline__ bool group_any(int g, bool x)
@@ -120,7 +128,8 @@ __global__ void __launch_bounds__(NT, 1)
 tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
 {
     constexpr int SLOTS = slots_of(R), NP = columns_of(R), H = R / 2;
-    constexpr uint32_t TMEM = tmem_of(R), O_AT = 4 * R, TREE_AT = O_AT + 2 * NP;     // S of group g: 2 R g ..; O: O_AT + NP g ..
+    static_assert(alignof(Small<R>) == 16 && offsetof(Small<R>, raw) % 16 == 0, "bulk copies' destination");
+    constexpr uint32_t TMEM = tmem_of(R), O_AT = 8 * R, TREE_AT = O_AT + 2 * NP;     // S of group g, one of two in turn: 4 R g + 2 R (0, 1) ..; O: O_AT + NP g ..
     static_assert(TREE_AT + R <= TMEM, "tensor memory");
     constexpr uint32_t IDESC = (1u << 4) | ((128u >> 4) << 24);
     constexpr uint32_t IDESC_S = IDESC | ((2u * R >> 3) << 17);                      // e4m3 x e4m3
@@ -130,16 +139,18 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
         if (threadIdx.x == 0) fspad_report(a.status, FSPAD_ERR_ALIGN);
         return;
     }
-    constexpr int Q_OFF = SLOTS * SLOT, P_OFF = Q_OFF + 2 * R * 128, END = P_OFF + 2 * NP * 128;
+    constexpr int Q_OFF = SLOTS * SLOT, P_OFF = Q_OFF + 2 * R * 128, END = P_OFF + 4 * NP * 128;      // (weights of group g: P_OFF + 2 NP 128 g, one of two in turn)
     Small<R> &sm = *reinterpret_cast<Small<R> *>(smem_raw + END);
     const uint32_t ring = smem_u32(smem_raw), sQ = ring + Q_OFF, sP = ring + P_OFF;
     const int tid = threadIdx.x, lane = tid & 31, warp = uniform_warp();
     auto bar = [&](const unsigned long long &b) { return smem_u32(&b); };
     if (tid == 0) {
         for (int i = 0; i < SLOTS; ++i) { mbar_init(bar(sm.full[i]), 1); mbar_init(bar(sm.free[i]), 1); }
-        for (int g = 0; g < 2; ++g) { mbar_init(bar(sm.s_full[g]), 1); mbar_init(bar(sm.p_full[g]), 4); mbar_init(bar(sm.o_done[g]), 1); }
+        for (int g = 0; g < 2; ++g) {
+            for (int y = 0; y < 2; ++y) { mbar_init(bar(sm.s_full[g][y]), 1); mbar_init(bar(sm.p_full[g][y]), 4); mbar_init(bar(sm.o_done[g][y]), 1); }
+            mbar_init(bar(sm.drain[g]), 1);
+        }
         mbar_init(bar(sm.q_full), 4);
-        mbar_init(bar(sm.drain), 1);
         sm.fail = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     }
@@ -157,7 +168,7 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, sm.tmem, 0);
     const int runs = a.Hkv * a.mtiles;               // (the tree is one unit: it has 32 nodes at most)
-    if (warp == 2 && lane == 0) tell_part<UNIT>(a, parts, part, cta);
+    if (warp == 3 && lane == 0) tell_part<UNIT>(a, parts, part, cta);
 
     // Every warp goes through the CTA's stretches by itself: of run (b, h, tile) the tree, if it is among the units, and n_kv chunks of the cache from kv0 on.
     struct Stretch { int b, h, row0, L, n_run, units, kv0, n_kv; bool tree, whole; };
@@ -216,64 +227,71 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
             sm.fail = 1;
             for (uint32_t x = n > SLOTS ? n - SLOTS : 0u; x < n; ++x) (void)mbar_wait(bar(sm.full[x % SLOTS]), (x / SLOTS) & 1u);
         }
-    } else if (warp == 1) {
+    } else if (warp < 3) {
         // ================= tensor cores =================
-        const bool issuer = elect_one();
+        // A warp for each group: a wait for a phase that is long over costs 200 cycles, a product 50 to 100, and nothing in a warp overlaps them (one warp for both bounded the kernel
+        // with 32 rows, 1650 cycles a chunk).  The scores of a group's next turn are made ahead.
+        const int g = warp - 1;
+        const uint32_t issuer = elect_one() ? 1u : 0u;
         const uint32_t hi = (uint32_t)(make_desc(0, 16) >> 32);                      // 128-byte swizzle, 8 rows 1024 bytes apart
         const uint32_t q_lo = (uint32_t)make_desc(sQ, 16), r_lo = (uint32_t)make_desc(ring, 16);
         // weights: 16 columns of a key side by side, keys one behind the other, eight of them 128 bytes, the next 16 columns 2048 bytes further
-        const uint32_t p_hi = (1u << 14) | (2048u >> 4), p_lo = ((sP >> 4) & 0x3fffu) | ((128u >> 4) << 16);
-        uint32_t n = 0, n_q = 0, n_p[2] = {0u, 0u};  // chunks of the stretches before, stretches with chunks, products of each group
+        const uint32_t p_hi = (1u << 14) | (2048u >> 4), p_lo = (((sP + (uint32_t)(2 * NP * 128 * g)) >> 4) & 0x3fffu) | ((128u >> 4) << 16);
+        const uint32_t tS = tmem + 4u * R * g, tO = tmem + O_AT + (uint32_t)(NP * g);
+        uint32_t n = 0, n_q = 0, n_p = 0;            // chunks of the stretches before, stretches with chunks, turns of the group
         while (!failed && next(s)) {
             s.n_kv = __shfl_sync(0xffffffffu, s.n_kv, 0);
             if (s.n_kv == 0) continue;
             if (!mbar_wait(bar(sm.q_full), n_q & 1u)) failed = true;
             ++n_q;
-            auto scores = [&](int i) {
-                const uint32_t at = 2u * (n + (uint32_t)i), slot = at % SLOTS;
-                if (!failed && !mbar_wait(bar(sm.full[slot]), (at / SLOTS) & 1u)) failed = true;
-                if (!failed && issuer) {
-                    tc_fence_after();
-#pragma unroll
-                    for (int ks = 0; ks < 4; ++ks) mma_f8(tmem + 2u * R * (i & 1), r_lo + slot * (SLOT >> 4) + ks * 2u, hi, q_lo + ks * 2u, hi, IDESC_S, ks > 0);
-                    mma_commit(bar(sm.s_full[i & 1]));
-                    mma_commit(bar(sm.free[slot]));
-                }
-                __syncwarp();
+            const int turns = (s.n_kv - g + 1) >> 1;
+            auto wait_k = [&](int t) {
+                const uint32_t at = 2u * (n + (uint32_t)(2 * t + g));
+                if (!failed && !mbar_wait(bar(sm.full[at % SLOTS]), (at / SLOTS) & 1u)) failed = true;
             };
-            scores(0);
-            if (s.n_kv > 1) scores(1);
+            auto scores = [&](int t) {
+                const uint32_t slot = 2u * (n + (uint32_t)(2 * t + g)) % SLOTS, y = (n_p + (uint32_t)t) & 1u;
+                if (failed) return;
+                tc_fence_after();
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks) mma_f8(tS + 2u * R * y, r_lo + slot * (SLOT >> 4) + ks * 2u, hi, q_lo + ks * 2u, hi, IDESC_S, ks > 0, issuer);
+                mma_commit_if(bar(sm.s_full[g][y]), issuer);
+                mma_commit_if(bar(sm.free[slot]), issuer);
+            };
 #pragma unroll 1
-            for (int i = 0; i < s.n_kv; ++i) {
-                const int g = i & 1;
-                const uint32_t at = 2u * (n + (uint32_t)i) + 1u, slot = at % SLOTS;
+            for (int t = 0; t < 2 && t < turns; ++t) {
+                wait_k(t);
+                scores(t);
+            }
+#pragma unroll 1
+            for (int t = 0; t < turns; ++t) {
+                const uint32_t at = 2u * (n + (uint32_t)(2 * t + g)) + 1u, slot = at % SLOTS, k = n_p + (uint32_t)t, y = k & 1u;
+                if (t + 2 < turns) wait_k(t + 2);
                 if (!failed && !mbar_wait(bar(sm.full[slot]), (at / SLOTS) & 1u)) failed = true;
-                if (!failed && !mbar_wait(bar(sm.p_full[g]), n_p[g] & 1u)) failed = true;
-                if (!failed && issuer) {
+                if (!failed && !mbar_wait(bar(sm.p_full[g][y]), (k >> 1) & 1u)) failed = true;
+                if (!failed) {
                     tc_fence_after();
 #pragma unroll
                     for (int ks = 0; ks < 4; ++ks)   // 32 keys an instruction
-                        mma_f8(tmem + O_AT + (uint32_t)(NP * g), r_lo + slot * (SLOT >> 4) + ks * 256u, hi, p_lo + (uint32_t)((NP * 128 >> 4) * g) + ks * 32u, p_hi, IDESC_O,
-                               i > 1 || ks > 0);
-                    mma_commit(bar(sm.o_done[g]));
-                    mma_commit(bar(sm.free[slot]));
+                        mma_f8(tO, r_lo + slot * (SLOT >> 4) + ks * 256u, hi, p_lo + y * (uint32_t)(NP * 128 >> 4) + ks * 32u, p_hi, IDESC_O, t + ks > 0, issuer);
+                    mma_commit_if(bar(sm.o_done[g][y]), issuer);
+                    mma_commit_if(bar(sm.free[slot]), issuer);
                 }
-                __syncwarp();
-                ++n_p[g];
-                if (i + 2 < s.n_kv) scores(i + 2);   // (the group has read the ones before)
+                if (t + 2 < turns) scores(t + 2);    // (the group has read the ones in their place)
             }
+            n_p += (uint32_t)turns;
             n += (uint32_t)s.n_kv;
         }
         if (failed) {
             sm.fail = 1;
-            if (lane == 0) mma_commit(bar(sm.drain));
-            (void)mbar_wait(bar(sm.drain), 0u);
+            if (lane == 0) mma_commit(bar(sm.drain[g]));
+            (void)mbar_wait(bar(sm.drain[g]), 0u);
         }
     } else if (warp >= 4) {
         // ================= queries, weights, rows =================
         const int g = (warp - 4) >> 2, w4 = warp & 3, t = (tid - 128) & 127;         // t: key of a chunk, and element of a row
-        const uint32_t lanes = (uint32_t)(w4 * 32) << 16, tS = tmem + lanes + 2u * R * g, tO = tmem + lanes + O_AT, tT = tmem + lanes + TREE_AT;
-        unsigned char *p_at = smem_raw + P_OFF + NP * 128 * g;
+        const uint32_t lanes = (uint32_t)(w4 * 32) << 16, tS = tmem + lanes + 4u * R * g, tO = tmem + lanes + O_AT, tT = tmem + lanes + TREE_AT;
+        unsigned char *const p_at = smem_raw + P_OFF + 2 * NP * 128 * g;
         uint32_t chunks = 0, n_s = 0, n_o[2] = {0u, 0u};     // chunks of the stretches before; scores of the group, products of both so far
         while (next(s)) {
             if (g == 0 && s.n_kv > 0) {
@@ -413,15 +431,15 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
             bool first = true;
 #pragma unroll 1
             for (int i = g; i < s.n_kv; i += 2) {
-                if (!failed && !mbar_wait(bar(sm.s_full[g]), n_s & 1u)) failed = true;
-                ++n_s;
+                const uint32_t k = n_s++, buf = k & 1u;      // (the group's turns so far)
+                if (!failed && !mbar_wait(bar(sm.s_full[g][buf]), (k >> 1) & 1u)) failed = true;
                 tc_fence_after();
                 float x[R];
                 {
                     uint32_t u[R], v[R];
                     __syncwarp();
-                    ld_issue(tS, u);
-                    ld_issue(tS + R, v);
+                    ld_issue(tS + 2u * R * buf, u);
+                    ld_issue(tS + 2u * R * buf + R, v);
                     ld_wait();
                     pin(u);
                     pin(v);
@@ -445,9 +463,7 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
                     // ---- the references move to the rows' maxima ----
 #pragma unroll
                     for (int r = 0; r < R; ++r) {
-                        float m = x[r];
-#pragma unroll
-                        for (int off = 16; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+                        const float m = warp_max(x[r]);
                         if (lane == r) sm.top[g][w4][r] = m;
                     }
                     group_sync(g);
@@ -461,17 +477,23 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
                     group_sync(g);
 #pragma unroll
                     for (int r = 0; r < R; ++r) l[r] *= sm.alpha[g][r];
-                    if (!first) {                    // (the group's products so far are complete: the scores that were waited for come behind them)
+                    if (!first) {                    // the product of the turn before (those before that are known to be complete: the scores came behind them)
+                        if (!failed && !mbar_wait(bar(sm.o_done[g][buf ^ 1u]), ((k - 1u) >> 1) & 1u)) failed = true;
+                        tc_fence_after();
 #pragma unroll 1
-                        for (int c = 0; c < 3 * R; c += 8) {
-                            uint32_t u[8];
+                        for (int z = 0; z < 3; ++z) {
+                            uint32_t u[R];
                             __syncwarp();
-                            ld_issue(tO + (uint32_t)(NP * g + c), u);
+                            ld_issue(tO + (uint32_t)(NP * g + z * R), u);
                             ld_wait();
                             pin(u);
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) u[j] = __float_as_uint(__uint_as_float(u[j]) * sm.alpha[g][(c + j) % R]);
-                            st8(tO + (uint32_t)(NP * g + c), u);
+                            for (int j = 0; j < R; ++j) u[j] = __float_as_uint(__uint_as_float(u[j]) * sm.alpha[g][j]);
+#pragma unroll
+                            for (int j = 0; j < R; j += 8) {
+                                const uint32_t v[8] = {u[j], u[j + 1], u[j + 2], u[j + 3], u[j + 4], u[j + 5], u[j + 6], u[j + 7]};
+                                st8(tO + (uint32_t)(NP * g + z * R + j), v);
+                            }
                         }
                         asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory");
                     }
@@ -494,7 +516,7 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
                 auto word = [&](int i4) { return i4 < 3 * R / 4 ? words[i4 / (R / 4)][i4 % (R / 4)] : 0u; };
 #pragma unroll
                 for (int c = 0; c < NP / 16; ++c)
-                    *reinterpret_cast<uint4 *>(p_at + c * 2048 + t * 16) = make_uint4(word(4 * c), word(4 * c + 1), word(4 * c + 2), word(4 * c + 3));
+                    *reinterpret_cast<uint4 *>(p_at + buf * (NP * 128) + c * 2048 + t * 16) = make_uint4(word(4 * c), word(4 * c + 1), word(4 * c + 2), word(4 * c + 3));
                 if (left < UNIT) {
                     // what lies behind the end may be anything, and 0 times a NaN is one: rows of zeros
                     if (!there)
@@ -504,7 +526,7 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
                 fence_async_smem();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar(sm.p_full[g]));
+                if (lane == 0) mbar_arrive(bar(sm.p_full[g][buf]));
             }
             chunks += (uint32_t)s.n_kv;
             // ---- sums over the keys, then the rows: each group the half of them ----
@@ -516,17 +538,14 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
                 if (lane == r) sm.sum[g][w4][r] = v;
             }
             const int mine[2] = {(s.n_kv + 1) / 2, s.n_kv / 2};      // chunks of each group
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-                n_o[y] += (uint32_t)mine[y];
-                // (each product but the last is known to be complete, of the other group only when both are here)
-            }
+            n_o[0] += (uint32_t)mine[0];
+            n_o[1] += (uint32_t)mine[1];
             tc_fence_before();
             both_sync();
             tc_fence_after();
 #pragma unroll
             for (int y = 0; y < 2; ++y)
-                if (mine[y] > 0 && !failed && !mbar_wait(bar(sm.o_done[y]), (n_o[y] - 1u) & 1u)) failed = true;
+                if (mine[y] > 0 && !failed && !mbar_wait(bar(sm.o_done[y][(n_o[y] - 1u) & 1u]), ((n_o[y] - 1u) >> 1) & 1u)) failed = true;
             tc_fence_after();
             if (failed) sm.fail = 1;
             const int r0 = H * g;

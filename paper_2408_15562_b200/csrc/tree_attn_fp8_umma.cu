@@ -176,7 +176,7 @@ struct Small {
         float2 ml[2][128];
         int scan[NT / 32 + 4];           // (before anything else)
     };
-    float raw[BUFS][8];                  // scales of K and V as they come
+    alignas(16) float raw[BUFS][8];      // scales of K and V as they come (bulk copies' destination)
     float scale[SCALES + 1][12];         // of a chunk, by its number: of each 32 keys K's scale, log2 of V's, 1 / V's; at last of the tree's
     unsigned char par[FSPAD_MAX_NODES_WIDE];         // parents plus one
     uint32_t odd[2][4];                  // which V rows of a tree's chunk have an infinity or a NaN in them
@@ -184,6 +184,7 @@ struct Small {
     int fail, soft_fail;                 // (the second: written and read by the softmax warps alone, around their barriers)
 };
 static_assert(SMEM + sizeof(Small) <= 232448, "shared memory of an SM");
+static_assert(SMEM % 16 == 0 && alignof(Small) >= 16 && offsetof(Small, raw) % 16 == 0, "bulk copies' destination");
 
 __global__ void __launch_bounds__(NT, 1)
 tree_attn_fp8_umma_kernel(const Args a, const __grid_constant__ CUtensorMap k_map, int k_row0)
