@@ -5,7 +5,7 @@
 //   s_j = c q_i . k_j,   out_i = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m)
 // over the L_b cached keys, whose rows are code * scale, and over the node itself and its ancestors among the bf16 tree rows.
 //
-// Few query rows a kv head (up to 32, in tiles of 8, 16 or 32; more: tree_attn_fp8_umma.cu).  Nothing but the tensor cores reads a code: K and V come by TMA and are
+// Few query rows a kv head (up to 16, in tiles of 8 or 16; more: tree_attn_fp8_umma.cu).  Nothing but the tensor cores reads a code: K and V come by TMA and are
 // operands as they are.  The products stand on their heads, so that the cache is the operand with 128 rows: S^T [128 keys][rows] = K Q^T, then
 // O^T [128 elements][rows] += V^T P^T, with V's tile taken as its own transpose.  What the other operand holds is 16 bits wide by nature, and is written as a sum of 8-bit numbers, in
 // columns of their own that are added up afterwards:
@@ -14,7 +14,11 @@
 // V's scale goes into the weights, as an addend of the exponent: the reference that weights are relative to follows the maximum of score + log2(scale).
 //
 // A CTA's warps: 0 copies, 1 and 2 the tensor cores' products of the two groups, 4-7 and 8-11 the groups that take the chunks of 128 keys in turn, a key a thread, each with a
-// reference, sums and an accumulator of its own.  The tree's keys (32 at most) are dealt with in single precision, by the second group ahead of the chunks.
+// reference, sums and an accumulator of its own.  The tree's keys (16 at most) are dealt with in single precision, by the second group ahead of the chunks.
+//
+// Bound by reading the cache where sequences are long: 32 single tokens (4 heads a kv head) over 7 to 32 thousand keys take 190 us, 92 percent of what the codes and scales take at
+// the measured copy bandwidth (one warp for both groups' products 199; with 16 rows, 4 to 12 thousand keys, 104, where it was 120).  A short call is its latencies: one token over
+// 2000 keys takes 9.2 us (launch, list, the queries' and the tree's reads, six chunks, the merge), of which the copies are 0.6.
 #include "fp8.cuh"
 #include "packed_list.cuh"
 
@@ -26,15 +30,15 @@ using namespace umma;
 constexpr int UNIT = 128;                // keys of a chunk
 constexpr int NT = 384;
 constexpr int SLOT = 128 * 128;          // codes of a chunk's K or V
+constexpr int SLOTS = 12;
+constexpr uint32_t TMEM = 256;           // columns
 constexpr float kLag = 4.f, kBias = 11.f;            // weights are 2^(score - reference + 11), the largest at most 2^15
 constexpr float kOwnDown = 0x1p-11f;                 // ... of which the accumulators and sums are rid at the end
 
-__host__ __device__ constexpr int slots_of(int R) { return R == 32 ? 10 : 12; }
 __host__ __device__ constexpr int columns_of(int R) { return R == 8 ? 32 : 3 * R; }          // of weights: a multiple of 16
-__host__ __device__ constexpr int tmem_of(int R) { return R == 32 ? 512 : 256; }
 
 template <int R> struct Small {
-    unsigned long long full[slots_of(R)], free[slots_of(R)], s_full[2][2], p_full[2][2], o_done[2][2], q_full, drain[2];
+    unsigned long long full[SLOTS], free[SLOTS], s_full[2][2], p_full[2][2], o_done[2][2], q_full, drain[2];
     alignas(16) float raw[8][8];         // (bulk copies' destination) scales of a chunk's K and V, by its number
     float cs[R];                         // a query's scores -> log2 units
     float ref[2][R], lim[2][R], m[2][R], alpha[2][R];        // of each group's rows: kBias - reference; what a score may reach; the reference; the accumulator's factor
@@ -45,7 +49,7 @@ template <int R> struct Small {
     uint32_t tmem;
     int fail;
 };
-template <int R> constexpr int bytes_of() { return slots_of(R) * SLOT + 2 * R * 128 + 4 * columns_of(R) * 128 + (int)sizeof(Small<R>); }
+template <int R> constexpr int bytes_of() { return SLOTS * SLOT + 2 * R * 128 + 4 * columns_of(R) * 128 + (int)sizeof(Small<R>); }
 
 struct Maps { CUtensorMap k, v; };
 
@@ -74,7 +78,6 @@ __device__ __forceinline__ void ld_issue(uint32_t at, uint32_t (&r)[16])
                    "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
                  : "r"(at) : "memory");
 }
-__device__ __forceinline__ void ld_issue(uint32_t at, uint32_t (&r)[32]) { tmem_ld32_issue(at, r); }
 __device__ __forceinline__ void ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory"); }
 // (no use of them can be scheduled ahead of the wait)
 template <int N> __device__ __forceinline__ void pin(uint32_t (&r)[N])
@@ -127,9 +130,9 @@ template <int R>
 __global__ void __launch_bounds__(NT, 1)
 tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
 {
-    constexpr int SLOTS = slots_of(R), NP = columns_of(R), H = R / 2;
+    constexpr int NP = columns_of(R), H = R / 2;
     static_assert(alignof(Small<R>) == 16 && offsetof(Small<R>, raw) % 16 == 0, "bulk copies' destination");
-    constexpr uint32_t TMEM = tmem_of(R), O_AT = 8 * R, TREE_AT = O_AT + 2 * NP;     // S of group g, one of two in turn: 4 R g + 2 R (0, 1) ..; O: O_AT + NP g ..
+    constexpr uint32_t O_AT = 8 * R, TREE_AT = O_AT + 2 * NP;     // S of group g, one of two in turn: 4 R g + 2 R (0, 1) ..; O: O_AT + NP g ..
     static_assert(TREE_AT + R <= TMEM, "tensor memory");
     constexpr uint32_t IDESC = (1u << 4) | ((128u >> 4) << 24);
     constexpr uint32_t IDESC_S = IDESC | ((2u * R >> 3) << 17);                      // e4m3 x e4m3
@@ -167,7 +170,7 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
     Part part = cut_list<NT, UNIT, 1, kFewRows>(a, cta, gridDim.x, parts, sm.scan, cta == 0);        // (with a barrier in it)
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, sm.tmem, 0);
-    const int runs = a.Hkv * a.mtiles;               // (the tree is one unit: it has 32 nodes at most)
+    const int runs = a.Hkv * a.mtiles;               // (the tree is one unit: it has 16 nodes at most)
     if (warp == 3 && lane == 0) tell_part<UNIT>(a, parts, part, cta);
 
     // Every warp goes through the CTA's stretches by itself: of run (b, h, tile) the tree, if it is among the units, and n_kv chunks of the cache from kv0 on.
@@ -229,8 +232,8 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
         }
     } else if (warp < 3) {
         // ================= tensor cores =================
-        // A warp for each group: a wait for a phase that is long over costs 200 cycles, a product 50 to 100, and nothing in a warp overlaps them (one warp for both bounded the kernel
-        // with 32 rows, 1650 cycles a chunk).  The scores of a group's next turn are made ahead.
+        // A warp for each group: a wait for a phase that is long over costs 200 cycles, a product 50 to 100, and nothing in a warp overlaps them (one warp for both took
+        // up to 1650 cycles a chunk).  The scores of a group's next turn are made ahead.
         const int g = warp - 1;
         const uint32_t issuer = elect_one() ? 1u : 0u;
         const uint32_t hi = (uint32_t)(make_desc(0, 16) >> 32);                      // 128-byte swizzle, 8 rows 1024 bytes apart
@@ -619,7 +622,7 @@ template <int R> cudaError_t launch_few(fspad_ctx *ctx, Args &a, const Maps &map
     a.mtiles = (a.M + R - 1) / R;
     a.by_tiles.set((unsigned)a.mtiles);
     scratch_in<R>(a, ctas, workspace);
-    cudaError_t e = raise_shared(ctx, R == 8 ? 4 : R == 16 ? 5 : 6, reinterpret_cast<const void *>(&tree_attn_fp8_kernel<R>), bytes_of<R>());
+    cudaError_t e = raise_shared(ctx, R == 8 ? 4 : 5, reinterpret_cast<const void *>(&tree_attn_fp8_kernel<R>), bytes_of<R>());
     if (e != cudaSuccess) return e;
     const int entries = merge_entries(a, ctas);
     ctx->launches++;
@@ -660,7 +663,9 @@ cudaError_t fspad_launch_tree_attn_fp8(fspad_ctx *ctx, const fspad_bf16 *q, cons
     Maps maps;
     const size_t rows = (size_t)paged.n_blocks * c.n_kv_heads * 128;
     if (!fspad_make_tmap_u8_2d(&maps.k, k_codes, rows, 128u)) return cudaErrorInvalidValue;
-    if (a.M > 32) return fspad_launch_attn_fp8_umma(ctx, a, maps.k, 0, workspace, st);
+    // Measured on both sides, 8 kv heads, us: up to 16 rows here and there, 32 sequences of 4 to 12 thousand keys 104 and 160, 16 of 512 to 4096 34 and 46, 64 of 100 to 600 47 and 74, one of
+    // 2000 11.3 and 16.0.  From 17 rows on a tile of 32 rows here (192 columns of weights a chunk) took 157 against 163, 60 against 47, 90 against 74 and 15.8 against 17.1: not kept.
+    if (a.M > 16) return fspad_launch_attn_fp8_umma(ctx, a, maps.k, 0, workspace, st);
     if (!fspad_make_tmap_u8_2d(&maps.v, v_codes, rows, 128u)) return cudaErrorInvalidValue;
-    return a.M <= 8 ? launch_few<8>(ctx, a, maps, workspace, st) : a.M <= 16 ? launch_few<16>(ctx, a, maps, workspace, st) : launch_few<32>(ctx, a, maps, workspace, st);
+    return a.M <= 8 ? launch_few<8>(ctx, a, maps, workspace, st) : launch_few<16>(ctx, a, maps, workspace, st);
 }
