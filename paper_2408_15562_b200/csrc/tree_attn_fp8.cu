@@ -14,7 +14,7 @@
 // V's scale goes into the weights, as an addend of the exponent: the reference that weights are relative to follows the maximum of score + log2(scale).
 //
 // A CTA's warps: 0 copies, 1 and 2 the tensor cores' products of the two groups, 4-7 and 8-11 the groups that take the chunks of 128 keys in turn, a key a thread, each with a
-// reference, sums and an accumulator of its own.  The tree's keys (16 at most) are dealt with in single precision, by the second group ahead of the chunks.
+// reference, sums and an accumulator of its own; 12-15 make the queries' two forms and deal with the tree's keys (16 at most) in single precision, up to two stretches ahead.
 //
 // Bound by reading the cache where sequences are long: 32 single tokens (4 heads a kv head) over 7 to 32 thousand keys take 190 us, 92 percent of what the codes and scales take at
 // the measured copy bandwidth (one warp for both groups' products 199; with 16 rows, 4 to 12 thousand keys, 104, where it was 120).  A short call is its latencies: one token over
@@ -28,28 +28,29 @@ using namespace packed;
 using namespace umma;
 
 constexpr int UNIT = 128;                // keys of a chunk
-constexpr int NT = 384;
+constexpr int NT = 512;
 constexpr int SLOT = 128 * 128;          // codes of a chunk's K or V
-constexpr int SLOTS = 12;
 constexpr uint32_t TMEM = 256;           // columns
 constexpr float kLag = 4.f, kBias = 11.f;            // weights are 2^(score - reference + 11), the largest at most 2^15
 constexpr float kOwnDown = 0x1p-11f;                 // ... of which the accumulators and sums are rid at the end
 
+__host__ __device__ constexpr int slots_of(int R) { return R == 8 ? 12 : 11; }                // (what shared memory holds)
 __host__ __device__ constexpr int columns_of(int R) { return R == 8 ? 32 : 3 * R; }          // of weights: a multiple of 16
 
 template <int R> struct Small {
-    unsigned long long full[SLOTS], free[SLOTS], s_full[2][2], p_full[2][2], o_done[2][2], q_full, drain[2];
+    unsigned long long full[slots_of(R)], free[slots_of(R)], s_full[2][2], p_full[2][2], o_done[2][2], ready[2], tree_done[2], over[2], drain[2];
     alignas(16) float raw[8][8];         // (bulk copies' destination) scales of a chunk's K and V, by its number
-    float cs[R];                         // a query's scores -> log2 units
+    alignas(16) float tree_w[R * R];     // [nodes][R]: scores, then weights of the tree's keys
+    float cs[2][R];                      // a query's scores -> log2 units (of two stretches in turn, as whatever the front's warps make)
     float ref[2][R], lim[2][R], m[2][R], alpha[2][R];        // of each group's rows: kBias - reference; what a score may reach; the reference; the accumulator's factor
     float top[2][4][R], sum[2][4][R];    // by warps
-    float tree_m[R], tree_l[R];
+    float tree_m[2][R], tree_l[2][R];
     uint32_t see[R], odd;
     int scan[NT / 32 + 2];
     uint32_t tmem;
     int fail;
 };
-template <int R> constexpr int bytes_of() { return SLOTS * SLOT + 2 * R * 128 + 4 * columns_of(R) * 128 + (int)sizeof(Small<R>); }
+template <int R> constexpr int bytes_of() { return slots_of(R) * SLOT + 4 * R * 128 + 4 * columns_of(R) * 128 + (int)sizeof(Small<R>); }
 
 struct Maps { CUtensorMap k, v; };
 
@@ -104,6 +105,7 @@ __device__ __forceinline__ bool group_any(int g, bool x)
     asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %2, 0;\n\tbarrier.cta.red.or.pred q, %1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}\n" : "=r"(r) : "r"(1 + g), "r"((uint32_t)x) : "memory");
     return r != 0;
 }
+__device__ __forceinline__ void front_sync() { asm volatile("bar.sync 4, 128;\n" ::: "memory"); }
 __device__ __forceinline__ void both_sync() { asm volatile("bar.sync 3, 256;\n" ::: "memory"); }
 
 // Two weights as three pairs of e5m2 numbers (an e5m2 number is a half's upper byte): hi, mid and lo in the low 16 bits of what comes back.
@@ -130,10 +132,10 @@ template <int R>
 __global__ void __launch_bounds__(NT, 1)
 tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
 {
-    constexpr int NP = columns_of(R), H = R / 2;
+    constexpr int SLOTS = slots_of(R), NP = columns_of(R), H = R / 2;
     static_assert(alignof(Small<R>) == 16 && offsetof(Small<R>, raw) % 16 == 0, "bulk copies' destination");
-    constexpr uint32_t O_AT = 8 * R, TREE_AT = O_AT + 2 * NP;     // S of group g, one of two in turn: 4 R g + 2 R (0, 1) ..; O: O_AT + NP g ..
-    static_assert(TREE_AT + R <= TMEM, "tensor memory");
+    constexpr uint32_t O_AT = 8 * R, TREE_AT = O_AT + 2 * NP;     // S of group g, one of two in turn: 4 R g + 2 R (0, 1) ..; O: O_AT + NP g ..; tree: TREE_AT + R (0, 1) ..
+    static_assert(TREE_AT + 2 * R <= TMEM, "tensor memory");
     constexpr uint32_t IDESC = (1u << 4) | ((128u >> 4) << 24);
     constexpr uint32_t IDESC_S = IDESC | ((2u * R >> 3) << 17);                      // e4m3 x e4m3
     constexpr uint32_t IDESC_O = IDESC | ((uint32_t)(NP >> 3) << 17) | (1u << 10) | (1u << 15) | (1u << 16);     // e4m3 x e5m2, both with their rows running fastest
@@ -142,7 +144,7 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
         if (threadIdx.x == 0) fspad_report(a.status, FSPAD_ERR_ALIGN);
         return;
     }
-    constexpr int Q_OFF = SLOTS * SLOT, P_OFF = Q_OFF + 2 * R * 128, END = P_OFF + 4 * NP * 128;      // (weights of group g: P_OFF + 2 NP 128 g, one of two in turn)
+    constexpr int Q_OFF = SLOTS * SLOT, P_OFF = Q_OFF + 4 * R * 128, END = P_OFF + 4 * NP * 128;      // (weights of group g: P_OFF + 2 NP 128 g, one of two in turn)
     Small<R> &sm = *reinterpret_cast<Small<R> *>(smem_raw + END);
     const uint32_t ring = smem_u32(smem_raw), sQ = ring + Q_OFF, sP = ring + P_OFF;
     const int tid = threadIdx.x, lane = tid & 31, warp = uniform_warp();
@@ -152,8 +154,10 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
         for (int g = 0; g < 2; ++g) {
             for (int y = 0; y < 2; ++y) { mbar_init(bar(sm.s_full[g][y]), 1); mbar_init(bar(sm.p_full[g][y]), 4); mbar_init(bar(sm.o_done[g][y]), 1); }
             mbar_init(bar(sm.drain[g]), 1);
+            mbar_init(bar(sm.ready[g]), 4);
+            mbar_init(bar(sm.tree_done[g]), 4);
+            mbar_init(bar(sm.over[g]), 10);
         }
-        mbar_init(bar(sm.q_full), 4);
         sm.fail = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     }
@@ -241,12 +245,12 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
         // weights: 16 columns of a key side by side, keys one behind the other, eight of them 128 bytes, the next 16 columns 2048 bytes further
         const uint32_t p_hi = (1u << 14) | (2048u >> 4), p_lo = (((sP + (uint32_t)(2 * NP * 128 * g)) >> 4) & 0x3fffu) | ((128u >> 4) << 16);
         const uint32_t tS = tmem + 4u * R * g, tO = tmem + O_AT + (uint32_t)(NP * g);
-        uint32_t n = 0, n_q = 0, n_p = 0;            // chunks of the stretches before, stretches with chunks, turns of the group
-        while (!failed && next(s)) {
+        uint32_t n = 0, n_p = 0, number = 0;         // chunks of the stretches before, turns of the group, stretches
+        for (; !failed && next(s); ++number) {
             s.n_kv = __shfl_sync(0xffffffffu, s.n_kv, 0);
-            if (s.n_kv == 0) continue;
-            if (!mbar_wait(bar(sm.q_full), n_q & 1u)) failed = true;
-            ++n_q;
+            // (of every stretch, whether there is something to do in it or not: a parity tells a phase from the next only)
+            if (!mbar_wait(bar(sm.ready[number & 1u]), (number >> 1) & 1u)) failed = true;
+            const uint32_t q_at = q_lo + (number & 1u) * (uint32_t)(2 * R * 128 >> 4);
             const int turns = (s.n_kv - g + 1) >> 1;
             auto wait_k = [&](int t) {
                 const uint32_t at = 2u * (n + (uint32_t)(2 * t + g));
@@ -257,7 +261,7 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
                 if (failed) return;
                 tc_fence_after();
 #pragma unroll
-                for (int ks = 0; ks < 4; ++ks) mma_f8(tS + 2u * R * y, r_lo + slot * (SLOT >> 4) + ks * 2u, hi, q_lo + ks * 2u, hi, IDESC_S, ks > 0, issuer);
+                for (int ks = 0; ks < 4; ++ks) mma_f8(tS + 2u * R * y, r_lo + slot * (SLOT >> 4) + ks * 2u, hi, q_at + ks * 2u, hi, IDESC_S, ks > 0, issuer);
                 mma_commit_if(bar(sm.s_full[g][y]), issuer);
                 mma_commit_if(bar(sm.free[slot]), issuer);
             };
@@ -284,20 +288,23 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
             }
             n_p += (uint32_t)turns;
             n += (uint32_t)s.n_kv;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(sm.over[number & 1u]));
         }
         if (failed) {
             sm.fail = 1;
             if (lane == 0) mma_commit(bar(sm.drain[g]));
             (void)mbar_wait(bar(sm.drain[g]), 0u);
         }
-    } else if (warp >= 4) {
-        // ================= queries, weights, rows =================
-        const int g = (warp - 4) >> 2, w4 = warp & 3, t = (tid - 128) & 127;         // t: key of a chunk, and element of a row
-        const uint32_t lanes = (uint32_t)(w4 * 32) << 16, tS = tmem + lanes + 4u * R * g, tO = tmem + lanes + O_AT, tT = tmem + lanes + TREE_AT;
-        unsigned char *const p_at = smem_raw + P_OFF + 2 * NP * 128 * g;
-        uint32_t chunks = 0, n_s = 0, n_o[2] = {0u, 0u};     // chunks of the stretches before; scores of the group, products of both so far
-        while (next(s)) {
-            if (g == 0 && s.n_kv > 0) {
+    } else if (warp >= 12) {
+        // ================= queries and the tree's keys, a stretch or two ahead of the groups =================
+        const int w4 = warp & 3, t = tid & 127;      // t: element of a row
+        const uint32_t tT = tmem + ((uint32_t)(w4 * 32) << 16) + TREE_AT;
+        for (uint32_t number = 0; next(s); ++number) {
+            const uint32_t y2 = number & 1u;         // (what the stretch before the last used is free again)
+            if (number >= 2 && !failed && !mbar_wait(bar(sm.over[y2]), ((number >> 1) - 1u) & 1u)) failed = true;
+            tc_fence_after();
+            if (s.n_kv > 0) {
                 // ---- queries: half a warp a row ----
 #pragma unroll
                 for (int x = 0; x < R / 8; ++x) {
@@ -310,7 +317,7 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
                     const uint32_t top = max(m & 0xffffu, m >> 16);
                     const int e = top == 0u || top >= 0x7f80u ? 7 : max((int)(top >> 7) - 127, -100);
                     const float up = __uint_as_float((uint32_t)(127 + 7 - e) << 23);
-                    if (piece == 0) sm.cs[r] = a.scale_log2 * __uint_as_float((uint32_t)(127 - 7 + e) << 23);
+                    if (piece == 0) sm.cs[y2][r] = a.scale_log2 * __uint_as_float((uint32_t)(127 - 7 + e) << 23);
                     const uint32_t in[4] = {w.x, w.y, w.z, w.w};
                     uint32_t q_hi[4], q_lo[4];
 #pragma unroll
@@ -325,22 +332,18 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
                         const int row = r + y * R;
-                        const uint32_t at = sQ + (uint32_t)(row * 128 + (((piece >> 1) ^ (row & 7)) << 4) + (piece & 1) * 8);
+                        const uint32_t at = sQ + y2 * (uint32_t)(2 * R * 128) + (uint32_t)(row * 128 + (((piece >> 1) ^ (row & 7)) << 4) + (piece & 1) * 8);
                         const uint32_t *c = y ? q_lo : q_hi;
                         asm volatile("st.shared.v2.b32 [%0], {%1, %2};\n" :: "r"(at), "r"(c[0] | (c[1] << 16)), "r"(c[2] | (c[3] << 16)) : "memory");
                     }
                 }
                 fence_async_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(sm.q_full));
             }
-            if (t < R) {
-                sm.m[g][t] = sm.lim[g][t] = -INFINITY;
-                sm.ref[g][t] = kBias;
-            }
-            if (g == 1 && s.tree) {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(sm.ready[y2]));
+            if (s.tree) {
                 // ---- the tree's keys, in single precision ----
-                float *w_at = reinterpret_cast<float *>(p_at);       // [N][R]
+                float *const w_at = sm.tree_w;
                 const size_t first = ((size_t)s.b * a.Hkv + s.h) * a.N * D;
                 if (w4 == 0) {
                     // each node's ancestors and itself, a node a lane, by doubling: after a round a lane has those up to 2^r above, and the node that far up
@@ -361,7 +364,7 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
                     if (lane < R) sm.see[lane] = gr < a.M ? mine : 0u;
                     if (lane == 0) sm.odd = 0u;
                 }
-                group_sync(g);
+                front_sync();
 #pragma unroll 1
                 for (int x = t; x < R * a.N; x += 128) {     // row x % R, key x / R
                     const int r = x % R, j = x / R, gr = s.row0 + r, node = a.by_G.of(gr);
@@ -383,7 +386,7 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
                     }
                     w_at[x] = d;
                 }
-                group_sync(g);
+                front_sync();
                 if (t < R) {
                     float m = -INFINITY, l = 0.f;
                     for (int j = 0; j < a.N; ++j) m = fmaxf(m, w_at[j * R + t]);
@@ -393,10 +396,10 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
                         w_at[j * R + t] = w;
                         l += w;
                     }
-                    sm.tree_m[t] = m;
-                    sm.tree_l[t] = l;
+                    sm.tree_m[y2][t] = m;
+                    sm.tree_l[y2][t] = l;
                 }
-                group_sync(g);
+                front_sync();
                 float acc[R];
 #pragma unroll
                 for (int r = 0; r < R; ++r) acc[r] = 0.f;
@@ -422,12 +425,31 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) v[j] = __float_as_uint(acc[r + j]);
                     __syncwarp();
-                    st8(tT + r, v);
+                    st8(tT + y2 * (uint32_t)R + (uint32_t)r, v);
                 }
                 asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory");
+                tc_fence_before();
+                front_sync();
+                if (t < R && (sm.see[t] & sm.odd)) sm.tree_l[y2][t] = NAN;
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(sm.tree_done[y2]));
+        }
+        if (failed) sm.fail = 1;
+    } else if (warp >= 4) {
+        // ================= weights, rows =================
+        const int g = (warp - 4) >> 2, w4 = warp & 3, t = (tid - 128) & 127;         // t: key of a chunk, and element of a row
+        const uint32_t lanes = (uint32_t)(w4 * 32) << 16, tS = tmem + lanes + 4u * R * g, tO = tmem + lanes + O_AT, tT = tmem + lanes + TREE_AT;
+        unsigned char *const p_at = smem_raw + P_OFF + 2 * NP * 128 * g;
+        uint32_t chunks = 0, n_s = 0, n_o[2] = {0u, 0u}, stretch = 0;        // chunks of the stretches before; scores of the group, products of both so far; stretches
+        for (; next(s); ++stretch) {
+            const uint32_t at2 = stretch & 1u;
+            if (t < R) {
+                sm.m[g][t] = sm.lim[g][t] = -INFINITY;
+                sm.ref[g][t] = kBias;
             }
             group_sync(g);
-            if (g == 1 && s.tree && t < R && (sm.see[t] & sm.odd)) sm.tree_l[t] = NAN;
+            if (s.n_kv > g && !failed && !mbar_wait(bar(sm.ready[at2]), (stretch >> 1) & 1u)) failed = true;
             float l[R];
 #pragma unroll
             for (int r = 0; r < R; ++r) l[r] = 0.f;
@@ -459,7 +481,7 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
                 bool above = false;
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
-                    x[r] = there ? fmaf(x[r], fmaxf(sm.cs[r] * ks, 0x1p-126f), lv) : -INFINITY;
+                    x[r] = there ? fmaf(x[r], fmaxf(sm.cs[at2][r] * ks, 0x1p-126f), lv) : -INFINITY;
                     above |= x[r] > sm.lim[g][r];
                 }
                 if (group_any(g, above)) {
@@ -549,6 +571,7 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
 #pragma unroll
             for (int y = 0; y < 2; ++y)
                 if (mine[y] > 0 && !failed && !mbar_wait(bar(sm.o_done[y][(n_o[y] - 1u) & 1u]), ((n_o[y] - 1u) >> 1) & 1u)) failed = true;
+            if (s.tree && !failed && !mbar_wait(bar(sm.tree_done[at2]), (stretch >> 1) & 1u)) failed = true;
             tc_fence_after();
             if (failed) sm.fail = 1;
             const int r0 = H * g;
@@ -558,7 +581,7 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
             for (int y = 0; y < 2; ++y)
 #pragma unroll
                 for (int z = 0; z < 3; ++z) ld_issue(tO + (uint32_t)(NP * y + z * R + r0), o[y][z]);
-            ld_issue(tT + (uint32_t)r0, tr);
+            ld_issue(tT + at2 * (uint32_t)R + (uint32_t)r0, tr);
             ld_wait();
 #pragma unroll
             for (int y = 0; y < 2; ++y)
@@ -577,8 +600,8 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
                     lr[y] = mine[y] > 0 ? ((sm.sum[y][0][r] + sm.sum[y][1][r]) + (sm.sum[y][2][r] + sm.sum[y][3][r])) * kOwnDown : 0.f;
                     v[y] = mine[y] > 0 ? ((__uint_as_float(o[y][0][x]) + __uint_as_float(o[y][1][x])) + __uint_as_float(o[y][2][x])) * (kOwnDown * kDown) : 0.f;
                 }
-                m[2] = s.tree ? sm.tree_m[r] : -INFINITY;
-                lr[2] = s.tree ? sm.tree_l[r] : 0.f;
+                m[2] = s.tree ? sm.tree_m[at2][r] : -INFINITY;
+                lr[2] = s.tree ? sm.tree_l[at2][r] : 0.f;
                 v[2] = s.tree ? __uint_as_float(tr[x]) : 0.f;
                 const float top = fmaxf(fmaxf(m[0], m[1]), m[2]);
                 float sum = 0.f, acc = 0.f;
@@ -599,6 +622,7 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
             }
             // nobody goes on to the next stretch (whose scores, weights and sums use the same places) before all have read
             tc_fence_before();
+            if (lane == 0) mbar_arrive(bar(sm.over[at2]));
             both_sync();
             tc_fence_after();
         }
