@@ -72,8 +72,8 @@ template <int UNIT> __device__ __forceinline__ int run_units(const Args &a, int 
 constexpr int kAnyRows = 0, kFewRows = 1, kManyRows = 2;
 template <int UNIT, int ROWS = kAnyRows> constexpr int kStretch = ROWS == kManyRows ? 1 : UNIT == 128 && ROWS == kAnyRows ? 4 : 2;
 // What the beginning of a run counts besides its units where the list is cut into equal parts.  (16 trees of 60 nodes over 512 to 4096 keys: a part with three short runs took 139000
-// cycles, one within a run 97000.)
-template <int ROWS> constexpr int kExtra = ROWS == kManyRows ? 3 : 0;
+// cycles, one within a run 97000.  Few rows, 64 single tokens over 100 to 600 keys: 29.9 us without, 24.6 with 4, 24.4 with 7; 32 over 7 to 32 thousand 182, 183 and 184.)
+template <int ROWS> constexpr int kExtra = ROWS == kManyRows ? 3 : ROWS == kFewRows ? 4 : 0;
 
 // How many parts the list may be cut into.  With chunks of 128 keys for 256 rows a part of a cut run leaves 128 KB, which cost about a hundredth of what a chunk
 // takes to write and read again: of few chunks, then, fewer parts than SMs (12 sqrt(total); with 5 sqrt(total) 60 nodes over 2K keys took 25.2 us, not 20.4).
@@ -103,7 +103,7 @@ struct Part {
 // Units before place y of the list's run number k, which begins at x - y (the beginnings of runs count, but have no units).
 template <int E> __device__ __forceinline__ int units_before(int x, int k, int y) { return x - E * k - min(y, E); }
 
-// All T threads of the CTA call it, and there is a CTA barrier in it; scratch holds T / 32 + max(2 W, 4) values.  W: how many parts a CTA takes: one, which all its
+// All T threads of the CTA call it, and there is a CTA barrier in it; scratch holds T / 32 + 2 W values (4 in place of 2 where kExtra is not 0).  W: how many parts a CTA takes: one, which all its
 // threads ask for, or one for each of its W = T / 32 warps: part0 + w * gridDim.x, so that few parts are on as many SMs.  slots: how many there may be.
 template <int T, int UNIT, int W, int ROWS = kAnyRows>
 __device__ __forceinline__ Part cut_list(const Args &a, int part0, int slots, Parts &p, int *scratch, bool report)
@@ -128,7 +128,8 @@ __device__ __forceinline__ Part cut_list(const Args &a, int part0, int slots, Pa
         const int want = part < p.n ? p.start(part) : total, most = p.q + kStretch<UNIT, ROWS>;
         if (a.B * runs <= p.n) {
             // the smallest piece with which there are no more pieces than parts, from below, within a step or two
-            int k = 0, sum = 0, q = max(1, (total + p.n - 1) / p.n), by_run = 0;
+            const int units = ROWS == kFewRows ? total - E * a.B * runs : total;
+            int k = 0, sum = 0, q = max(1, (units + p.n - 1) / p.n), by_run = 0;
             while (q <= most) {
                 k = lane < a.B ? (n + q - 1) / q : 0;
                 inc = runs * k;

@@ -16,9 +16,11 @@
 // A CTA's warps: 0 copies, 1 and 2 the tensor cores' products of the two groups, 4-7 and 8-11 the groups that take the chunks of 128 keys in turn, a key a thread, each with a
 // reference, sums and an accumulator of its own; 12-15 make the queries' two forms and deal with the tree's keys (16 at most) in single precision, up to two stretches ahead.
 //
-// Bound by reading the cache where sequences are long: 32 single tokens (4 heads a kv head) over 7 to 32 thousand keys take 190 us, 92 percent of what the codes and scales take at
-// the measured copy bandwidth (one warp for both groups' products 199; with 16 rows, 4 to 12 thousand keys, 104, where it was 120).  A short call is its latencies: one token over
-// 2000 keys takes 9.2 us (launch, list, the queries' and the tree's reads, six chunks, the merge), of which the copies are 0.6.
+// Bound by reading the cache where sequences are long: 32 single tokens (8 heads a kv head) over 4 to 32 thousand keys take 184 us, 95 percent of what the codes and scales take at
+// the measured copy bandwidth (199 with one warp for both groups' products, 190 without warps of their own for queries and trees); with 16 rows, 32 sequences of 4 to 12 thousand keys
+// take 97.  Short sequences are bound by a stretch's chain, some 7000 cycles with three chunks: a turn 1700 to 2000 (the first moves the references), the sums 700, the last product 1100, the
+// rows 700; 64 single tokens over 100 to 600 keys take 23.0 us (32.6 with queries and tree in the groups' own way).  A short call is its latencies: one token over 2000 keys
+// takes 9.3 us, the list 2400 cycles of it, the part 7000, and the merge behind it; its copies take 0.6.
 #include "fp8.cuh"
 #include "packed_list.cuh"
 
@@ -45,8 +47,9 @@ template <int R> struct Small {
     float ref[2][R], lim[2][R], m[2][R], alpha[2][R];        // of each group's rows: kBias - reference; what a score may reach; the reference; the accumulator's factor
     float top[2][4][R], sum[2][4][R];    // by warps
     float tree_m[2][R], tree_l[2][R];
-    uint32_t see[R], odd;
-    int scan[NT / 32 + 2];
+    float end[2][4][R];                  // by groups: the factors of a row's three parts, and of what they add up to
+    uint32_t odd;
+    int scan[NT / 32 + 4];
     uint32_t tmem;
     int fail;
 };
@@ -175,14 +178,14 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, sm.tmem, 0);
     const int runs = a.Hkv * a.mtiles;               // (the tree is one unit: it has 16 nodes at most)
-    if (warp == 3 && lane == 0) tell_part<UNIT>(a, parts, part, cta);
+    if (warp == 3 && lane == 0) tell_part<UNIT, kFewRows>(a, parts, part, cta);
 
     // Every warp goes through the CTA's stretches by itself: of run (b, h, tile) the tree, if it is among the units, and n_kv chunks of the cache from kv0 on.
     struct Stretch { int b, h, row0, L, n_run, units, kv0, n_kv; bool tree, whole; };
     auto next = [&](Stretch &s) -> bool {
         if (part.left <= 0) return false;
+        if (s.b != part.b) s.L = prefix_of(a, part.b, false);
         s.b = part.b;
-        s.L = prefix_of(a, part.b, false);
         s.n_run = run_units<UNIT>(a, s.L);
         s.units = min(s.n_run - part.u, part.left);
         s.tree = part.u == 0;
@@ -193,11 +196,13 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
         s.row0 = (part.run - s.h * a.mtiles) * R;
         part.left -= s.units;
         part.u = 0;
+        part.v += s.n_run + kExtra<kFewRows>;
         if (++part.run == runs) { part.run = 0; ++part.b; }
         return true;
     };
     bool failed = false;
     Stretch s;
+    s.b = -1;
 
     if (warp == 0) {
         // ================= copies =================
@@ -205,7 +210,7 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
         for (int done = 0;; done += s.units) {
             const Part at = part;
             if (failed || !next(s)) break;
-            if (s.tree && lane == 0) tell_run(a, parts, at, cta, done, s.n_run);
+            if (s.tree && lane == 0) tell_run<kFewRows>(a, parts, at, cta, done, s.n_run);
             const int *blocks = a.table + (size_t)s.b * a.table_stride;
             int mine = 0;
             for (int i = 0; i < s.n_kv && !failed; ++i, ++chunk) {
@@ -301,16 +306,35 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
         const int w4 = warp & 3, t = tid & 127;      // t: element of a row
         const uint32_t tT = tmem + ((uint32_t)(w4 * 32) << 16) + TREE_AT;
         for (uint32_t number = 0; next(s); ++number) {
-            const uint32_t y2 = number & 1u;         // (what the stretch before the last used is free again)
+            const uint32_t y2 = number & 1u;
+            // what is needed first is asked for at once: the half warp's query rows (8 x + 2 w4 + lane / 16, 16 bytes a lane), parents, the first node's K and V
+            const int half = 2 * w4 + (lane >> 4), piece = lane & 15;
+            const size_t first = ((size_t)s.b * a.Hkv + s.h) * a.N * D;
+            const unsigned short *const v_at = reinterpret_cast<const unsigned short *>(a.tv + first) + t;
+            const uint4 *const k_at = reinterpret_cast<const uint4 *>(a.tk + first) + piece;
+            uint4 qw[R / 8], k0 = make_uint4(0u, 0u, 0u, 0u);
+            uint32_t v0 = 0u;
+            int up = -1;
+#pragma unroll
+            for (int x = 0; x < R / 8; ++x) {
+                const int gr = s.row0 + 8 * x + half, node = a.by_G.of(gr);
+                qw[x] = make_uint4(0u, 0u, 0u, 0u);
+                if (gr < a.M) qw[x] = __ldg(reinterpret_cast<const uint4 *>(a.q + ((size_t)(s.b * a.N + node) * a.Hq + s.h * a.G + (gr - node * a.G)) * D) + piece);
+            }
+            if (s.tree) {
+                k0 = __ldg(k_at);
+                v0 = __ldg(v_at);
+                if (w4 == 0 && lane < a.N) up = __ldg(a.parent + (size_t)s.b * a.N + lane);
+            }
+            // (what the stretch before the last used is free again)
             if (number >= 2 && !failed && !mbar_wait(bar(sm.over[y2]), ((number >> 1) - 1u) & 1u)) failed = true;
             tc_fence_after();
             if (s.n_kv > 0) {
                 // ---- queries: half a warp a row ----
 #pragma unroll
                 for (int x = 0; x < R / 8; ++x) {
-                    const int r = 8 * x + 2 * w4 + (lane >> 4), piece = lane & 15, gr = s.row0 + r, node = a.by_G.of(gr);
-                    uint4 w = make_uint4(0u, 0u, 0u, 0u);
-                    if (gr < a.M) w = __ldg(reinterpret_cast<const uint4 *>(a.q + ((size_t)(s.b * a.N + node) * a.Hq + s.h * a.G + (gr - node * a.G)) * D) + piece);
+                    const int r = 8 * x + half;
+                    const uint4 w = qw[x];
                     uint32_t m = fspad_most2(fspad_most2(w.x, w.y), fspad_most2(w.z, w.w));
 #pragma unroll
                     for (int off = 8; off > 0; off >>= 1) m = fspad_most2(m, __shfl_xor_sync(0xffffffffu, m, off));
@@ -344,15 +368,28 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
             if (s.tree) {
                 // ---- the tree's keys, in single precision ----
                 float *const w_at = sm.tree_w;
-                const size_t first = ((size_t)s.b * a.Hkv + s.h) * a.N * D;
+                // (which of them a row sees is looked at behind the products; a row's 16 lanes have 8 elements each)
+#pragma unroll 2
+                for (int j = 0; j < a.N; ++j) {
+                    const uint4 k = j == 0 ? k0 : __ldg(k_at + (size_t)j * 16);
+#pragma unroll
+                    for (int x = 0; x < R / 8; ++x) {
+                        float d = 0.f;
+                        auto two = [&](uint32_t p, uint32_t q) {
+                            d = fmaf(__uint_as_float(p << 16), __uint_as_float(q << 16), d);
+                            d = fmaf(__uint_as_float(p & 0xffff0000u), __uint_as_float(q & 0xffff0000u), d);
+                        };
+                        two(qw[x].x, k.x); two(qw[x].y, k.y); two(qw[x].z, k.z); two(qw[x].w, k.w);
+#pragma unroll
+                        for (int off = 8; off > 0; off >>= 1) d += __shfl_xor_sync(0xffffffffu, d, off);
+                        if (piece == 0) w_at[j * R + 8 * x + half] = d * a.scale_log2;
+                    }
+                }
+                uint32_t see = 0u;                   // of row `lane`, in the first warp
                 if (w4 == 0) {
                     // each node's ancestors and itself, a node a lane, by doubling: after a round a lane has those up to 2^r above, and the node that far up
                     uint32_t above = 1u << lane;
-                    int up = -1;
-                    if (lane < a.N) {
-                        up = __ldg(a.parent + (size_t)s.b * a.N + lane);
-                        if (lane == 0 ? up != -1 : (up < 0 || up >= lane)) { fspad_report(a.status, FSPAD_ERR_BAD_TREE); up = -1; }
-                    }
+                    if (lane < a.N && (lane == 0 ? up != -1 : (up < 0 || up >= lane))) { fspad_report(a.status, FSPAD_ERR_BAD_TREE); up = -1; }
 #pragma unroll 1
                     for (int reach = 1; reach < a.N; reach <<= 1) {
                         const uint32_t m = __shfl_sync(0xffffffffu, above, up & 31);
@@ -360,39 +397,17 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
                         if (up >= 0) { above |= m; up = nx; }
                     }
                     const int gr = s.row0 + lane;
-                    const uint32_t mine = __shfl_sync(0xffffffffu, above, a.by_G.of(min(gr, a.M - 1)) & 31);
-                    if (lane < R) sm.see[lane] = gr < a.M ? mine : 0u;
+                    see = __shfl_sync(0xffffffffu, above, a.by_G.of(min(gr, a.M - 1)) & 31);
+                    if (gr >= a.M) see = 0u;
                     if (lane == 0) sm.odd = 0u;
-                }
-                front_sync();
-#pragma unroll 1
-                for (int x = t; x < R * a.N; x += 128) {     // row x % R, key x / R
-                    const int r = x % R, j = x / R, gr = s.row0 + r, node = a.by_G.of(gr);
-                    float d = -INFINITY;
-                    if ((sm.see[r] >> j) & 1u) {
-                        const uint4 *qq = reinterpret_cast<const uint4 *>(a.q + ((size_t)(s.b * a.N + node) * a.Hq + s.h * a.G + (gr - node * a.G)) * D);
-                        const uint4 *kk = reinterpret_cast<const uint4 *>(a.tk + first + (size_t)j * D);
-                        float acc[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-                        for (int i = 0; i < 16; ++i) {
-                            const uint4 u = __ldg(qq + i), v = __ldg(kk + i);
-                            auto two = [](float &to, uint32_t p, uint32_t q) {
-                                to = fmaf(__uint_as_float(p << 16), __uint_as_float(q << 16), to);
-                                to = fmaf(__uint_as_float(p & 0xffff0000u), __uint_as_float(q & 0xffff0000u), to);
-                            };
-                            two(acc[0], u.x, v.x); two(acc[1], u.y, v.y); two(acc[2], u.z, v.z); two(acc[3], u.w, v.w);
-                        }
-                        d = ((acc[0] + acc[1]) + (acc[2] + acc[3])) * a.scale_log2;
-                    }
-                    w_at[x] = d;
                 }
                 front_sync();
                 if (t < R) {
                     float m = -INFINITY, l = 0.f;
-                    for (int j = 0; j < a.N; ++j) m = fmaxf(m, w_at[j * R + t]);
+                    for (int j = 0; j < a.N; ++j) m = fmaxf(m, (see >> j) & 1u ? w_at[j * R + t] : -INFINITY);
                     const float safe = m == -INFINITY ? 0.f : m;
                     for (int j = 0; j < a.N; ++j) {
-                        const float w = ex2f(w_at[j * R + t] - safe);
+                        const float w = (see >> j) & 1u ? ex2f(w_at[j * R + t] - safe) : 0.f;
                         w_at[j * R + t] = w;
                         l += w;
                     }
@@ -406,7 +421,7 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
                 uint32_t odd = 0u;
 #pragma unroll 2
                 for (int j = 0; j < a.N; ++j) {
-                    const uint32_t v16 = __ldg(reinterpret_cast<const unsigned short *>(a.tv + first + (size_t)j * D) + t);
+                    const uint32_t v16 = j == 0 ? v0 : __ldg(v_at + (size_t)j * D);
                     // (an infinity or a NaN must not reach the rows that do not see it: it is taken out, and those that do get NaN)
                     const bool is_odd = (v16 & 0x7f80u) == 0x7f80u;
                     if (is_odd) odd |= 1u << j;
@@ -430,7 +445,7 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
                 asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory");
                 tc_fence_before();
                 front_sync();
-                if (t < R && (sm.see[t] & sm.odd)) sm.tree_l[y2][t] = NAN;
+                if (t < R && (see & sm.odd)) sm.tree_l[y2][t] = NAN;
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(sm.tree_done[y2]));
@@ -567,14 +582,34 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
             n_o[1] += (uint32_t)mine[1];
             tc_fence_before();
             both_sync();
-            tc_fence_after();
+            if (s.tree && !failed && !mbar_wait(bar(sm.tree_done[at2]), (stretch >> 1) & 1u)) failed = true;
+            const int rows = min(R, a.M - s.row0), r0 = g * ((rows + 1) >> 1), r1 = g ? rows : (rows + 1) >> 1, slot = cta * 2 + (s.tree ? 1 : 0);
+            if (t >= r0 && t < r1) {                 // (while the last products are under way)
+                float m[3], lr[3];
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    m[y] = mine[y] > 0 ? sm.m[y][t] : -INFINITY;
+                    lr[y] = mine[y] > 0 ? ((sm.sum[y][0][t] + sm.sum[y][1][t]) + (sm.sum[y][2][t] + sm.sum[y][3][t])) * kOwnDown : 0.f;
+                }
+                m[2] = s.tree ? sm.tree_m[at2][t] : -INFINITY;
+                lr[2] = s.tree ? sm.tree_l[at2][t] : 0.f;
+                const float top = fmaxf(fmaxf(m[0], m[1]), m[2]);
+                float sum = 0.f;
+#pragma unroll
+                for (int y = 0; y < 3; ++y) {
+                    const float f = m[y] == -INFINITY ? 1.f : ex2f(m[y] - top);      // (without a maximum a part is zero, or NaN)
+                    sm.end[g][y][t] = f;
+                    sum = fmaf(f, lr[y], sum);
+                }
+                sm.end[g][3][t] = kUp / sum;
+                if (!s.whole) a.part_ml[(size_t)slot * R + t] = make_float2(top, sum);
+            }
+            group_sync(g);
 #pragma unroll
             for (int y = 0; y < 2; ++y)
                 if (mine[y] > 0 && !failed && !mbar_wait(bar(sm.o_done[y][(n_o[y] - 1u) & 1u]), ((n_o[y] - 1u) >> 1) & 1u)) failed = true;
-            if (s.tree && !failed && !mbar_wait(bar(sm.tree_done[at2]), (stretch >> 1) & 1u)) failed = true;
             tc_fence_after();
             if (failed) sm.fail = 1;
-            const int r0 = H * g;
             uint32_t o[2][3][H], tr[H];
             __syncwarp();
 #pragma unroll
@@ -588,36 +623,23 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
 #pragma unroll
                 for (int z = 0; z < 3; ++z) pin(o[y][z]);
             pin(tr);
-            const int slot = cta * 2 + (s.tree ? 1 : 0);
 #pragma unroll
             for (int x = 0; x < H; ++x) {
                 const int r = r0 + x, gr = s.row0 + r;
-                if (gr >= a.M) break;
-                float m[3], lr[3], v[3];
+                if (r >= r1) break;
+                float v[3], acc = 0.f;
 #pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    m[y] = mine[y] > 0 ? sm.m[y][r] : -INFINITY;
-                    lr[y] = mine[y] > 0 ? ((sm.sum[y][0][r] + sm.sum[y][1][r]) + (sm.sum[y][2][r] + sm.sum[y][3][r])) * kOwnDown : 0.f;
+                for (int y = 0; y < 2; ++y)
                     v[y] = mine[y] > 0 ? ((__uint_as_float(o[y][0][x]) + __uint_as_float(o[y][1][x])) + __uint_as_float(o[y][2][x])) * (kOwnDown * kDown) : 0.f;
-                }
-                m[2] = s.tree ? sm.tree_m[at2][r] : -INFINITY;
-                lr[2] = s.tree ? sm.tree_l[at2][r] : 0.f;
                 v[2] = s.tree ? __uint_as_float(tr[x]) : 0.f;
-                const float top = fmaxf(fmaxf(m[0], m[1]), m[2]);
-                float sum = 0.f, acc = 0.f;
 #pragma unroll
-                for (int y = 0; y < 3; ++y) {
-                    const float f = m[y] == -INFINITY ? 1.f : ex2f(m[y] - top);      // (without a maximum a part is zero, or NaN)
-                    sum = fmaf(f, lr[y], sum);
-                    acc = fmaf(f, v[y], acc);
-                }
+                for (int y = 0; y < 3; ++y) acc = fmaf(sm.end[g][y][r], v[y], acc);
                 if (s.whole) {
                     const int node = a.by_G.of(gr);
-                    const __nv_bfloat16 b = __float2bfloat16_rn(acc * (kUp / sum));
+                    const __nv_bfloat16 b = __float2bfloat16_rn(acc * sm.end[g][3][r]);
                     reinterpret_cast<__nv_bfloat16 *>(a.out)[((size_t)(s.b * a.N + node) * a.Hq + s.h * a.G + (gr - node * a.G)) * D + t] = b;
                 } else {
                     a.part_o[((size_t)slot * R + r) * D + t] = acc;
-                    if (t == 0) a.part_ml[(size_t)slot * R + r] = make_float2(top, sum);
                 }
             }
             // nobody goes on to the next stretch (whose scores, weights and sums use the same places) before all have read
@@ -666,7 +688,7 @@ size_t fspad_attn_fp8_workspace(const fspad_ctx *ctx) { return fspad_attn_fp8_um
 bool fspad_attn_fp8_fits(const fspad_ctx *ctx, int N, int B, int bps, int n_blocks)
 {
     const fspad_config &c = ctx->cfg;
-    const long long tiles = ((long long)N * (c.n_q_heads / c.n_kv_heads) + 7) / 8, run = (N + 127) / 128 + (long long)bps + kExtra<kManyRows>;
+    const long long tiles = ((long long)N * (c.n_q_heads / c.n_kv_heads) + 7) / 8, run = (N + 127) / 128 + (long long)bps + max(kExtra<kManyRows>, kExtra<kFewRows>);
     return (double)run * B * c.n_kv_heads * tiles < 2147483647.0 - 1e6 && (long long)n_blocks * c.n_kv_heads * 128 <= 0x7fffffffll;
 }
 
@@ -687,8 +709,8 @@ cudaError_t fspad_launch_tree_attn_fp8(fspad_ctx *ctx, const fspad_bf16 *q, cons
     Maps maps;
     const size_t rows = (size_t)paged.n_blocks * c.n_kv_heads * 128;
     if (!fspad_make_tmap_u8_2d(&maps.k, k_codes, rows, 128u)) return cudaErrorInvalidValue;
-    // Measured on both sides, 8 kv heads, us: up to 16 rows here and there, 32 sequences of 4 to 12 thousand keys 104 and 160, 16 of 512 to 4096 34 and 46, 64 of 100 to 600 47 and 74, one of
-    // 2000 11.3 and 16.0.  From 17 rows on a tile of 32 rows here (192 columns of weights a chunk) took 157 against 163, 60 against 47, 90 against 74 and 15.8 against 17.1: not kept.
+    // Measured on both sides, 8 kv heads, us: 16 rows here and there, 32 sequences of 4 to 12 thousand keys 97 and 160, 16 of 512 to 4096 24 and 46, 64 of 100 to 600 32 and 74.
+    // A tile of 32 rows here (192 columns of weights a chunk) took from 17 rows on 157 against 163, but 60 against 47 and 90 against 74: not kept.
     if (a.M > 16) return fspad_launch_attn_fp8_umma(ctx, a, maps.k, 0, workspace, st);
     if (!fspad_make_tmap_u8_2d(&maps.v, v_codes, rows, 128u)) return cudaErrorInvalidValue;
     return a.M <= 8 ? launch_few<8>(ctx, a, maps, workspace, st) : launch_few<16>(ctx, a, maps, workspace, st);
