@@ -8,7 +8,9 @@
 // rounded again by it: with powers of two that changes only what falls below the least codes.
 // An element that is not finite has no part in the maximum and is kept as NaN.
 //
-// Bound by memory: 256 bytes read and 128 written a row (256 more where the caller asks for the values that are kept).
+// Bound by memory: 256 bytes read and 128 written a row (256 more where the caller asks for the values that are kept).  Prompts of four requests, 16400 rows of 8 heads with the kept values, take
+// 32 us (161 MB: 5.0 TB/s), those paths 55 us (252 MB with the kept values: 4.6 TB/s, reads and writes mixed and begun groups read again).  One row of each of 256 sequences takes 6.0 us, of one sequence in
+// 32 layers 4.0: a launch, and loads that depend on one another (slot, row and scale, group).
 #include "fp8.cuh"
 #include "umma_common.cuh"
 
