@@ -598,7 +598,7 @@ int fspad_kv_append_fp8(fspad_ctx *ctx, uint8_t *codes, float *scales, const int
  * weight (where no row has any, the output is NaN).  A NaN of the cache is seen by all queries of its sequence and kv head: in K it makes their
  * outputs NaN, in V the one element of them.  A query with an infinity or a NaN has NaN outputs.
  * Errors: FSPAD_ERR_RANGE for a workspace that is too small, and, in the status word, for a
- * prefix length or a table entry out of range; FSPAD_ERR_TOO_LARGE where batch * Hkv * ceil(n_nodes * Hq / Hkv / 8) * (blocks_per_seq + ceil(n_nodes / 128) + 3) is not below
+ * prefix length or a table entry out of range; FSPAD_ERR_TOO_LARGE where batch * Hkv * ceil(n_nodes * Hq / Hkv / 8) * (blocks_per_seq + ceil(n_nodes / 128) + 4) is not below
  * 2^31 - 10^6 or n_blocks * Hkv * 128 is 2^31 or more; otherwise as fspad_tree_attn_paged.
  */
 size_t fspad_tree_attn_fp8_workspace_bytes(const fspad_ctx *ctx);
