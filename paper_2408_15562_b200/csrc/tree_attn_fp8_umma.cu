@@ -174,8 +174,12 @@ __device__ __forceinline__ void softmax_half(bool tree, uint32_t tS, uint32_t tO
 }
 
 constexpr int SCALES = 6;                // (a chunk's are written once the one 6 before it has been through the products)
+// Places for the flags of a tree's chunk.  The softmax reads them after its last word on the chunk, which lets the product go that frees the chunk's V tile: the tree's chunk
+// after the next may have its flags written while a warp has yet to read.  The one after that may not: it waits for the product of a later chunk, which that warp either has a hand in itself
+// or meets behind the barrier at a stretch's end.  (With two places, and the flags read ahead of that word, 16 trees of 60 nodes over 512 to 4096 keys took 0.7 us longer.)
+constexpr uint32_t ODDS = 3;
 struct Small {
-    static constexpr int BARS = 36;
+    static constexpr int BARS = 34;
     unsigned long long bar[BARS];
     union {
         float2 ml[2][128];
@@ -184,7 +188,7 @@ struct Small {
     alignas(16) float raw[BUFS][8];      // scales of K and V as they come (bulk copies' destination)
     float scale[SCALES + 1][12];         // of a chunk, by its number: of each 32 keys K's scale, log2 of V's, 1 / V's; at last of the tree's
     unsigned char par[FSPAD_MAX_NODES_WIDE];         // parents plus one
-    uint32_t odd[2][4];                  // which V rows of a tree's chunk have an infinity or a NaN in them
+    uint32_t odd[ODDS][4];               // which V rows of a tree's chunk have an infinity or a NaN in them
     uint32_t tmem;
     int fail, soft_fail;                 // (the second: written and read by the softmax warps alone, around their barriers)
 };
@@ -280,10 +284,10 @@ tree_attn_fp8_umma_kernel(const Args a, const __grid_constant__ CUtensorMap k_ma
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t tS = tmem + lanes + 128u * grp, tO = tmem + lanes + 256u + 128u * grp;
         uint32_t n_done = 0, tree_chunks = 0, chunks = 0;    // products of the group so far; the tree's chunks and all of the CTA so far
-        auto told = [&](int y) {                             // half y of the weights is there
+        auto told = [&](int y) {                             // half y of the weights is there, and what was read of shared memory before may be written again
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive_light(bar(P_FULL + 2 * grp + y));
+            if (lane == 0) mbar_arrive(bar(P_FULL + 2 * grp + y));
         };
         while (next(s)) {
             const int gr = s.row0 + (s.two ? grp * 128 : 0) + row;           // row of the kv head
@@ -439,7 +443,7 @@ tree_attn_fp8_umma_kernel(const Args a, const __grid_constant__ CUtensorMap k_ma
                 }
                 turn(std::false_type(), tree, see);
                 if (tree) {
-                    const uint32_t *odd = s_odd[(tree_chunks + c) & 1];
+                    const uint32_t *odd = s_odd[(tree_chunks + (uint32_t)c) % ODDS];
                     if ((see[0] & odd[0]) | (see[1] & odd[1]) | (see[2] & odd[2]) | (see[3] & odd[3])) l_run = NAN;
                     if (s.two && c == s.n_tree - 1 && s.n_ch > s.n_tree) {   // (the tile's last reader's scores are here)
                         scale_q(grp, true);
@@ -722,7 +726,7 @@ tree_attn_fp8_umma_kernel(const Args a, const __grid_constant__ CUtensorMap k_ma
                 if (c < s.n_tree) {
                     // a chunk of the tree: V before K, so that whoever sees its scores sees which of its V rows are odd
                     const int key0 = u * UNIT;
-                    uint32_t *odd = s_odd[tree_chunks & 1];
+                    uint32_t *odd = s_odd[tree_chunks % ODDS];
                     ++tree_chunks;
                     const int piece = lane & 15, rows = min(a.N - key0, UNIT);
                     const size_t first = (((size_t)s.b * a.Hkv + s.h) * a.N + key0) * D + piece * 8;

@@ -224,6 +224,29 @@ def test_values_that_are_no_numbers_reach_only_those_who_see_them(what, nodes, g
     assert np.abs(got - want)[good].max() <= 3e-2
 
 
+@pytest.mark.parametrize("nodes,heads,batch", [(40, (8, 2), 700), (17, (1, 1), 1500), (128, (2, 2), 500), (150, (2, 1), 400), (200, (2, 2), 400), (40, (56, 28), 30)])
+def test_trees_without_a_cache_one_behind_the_other(nodes, heads, batch):
+    """Nothing but trees, many to a part, with infinities and NaN in V of every third: the flags of V's rows are in one of two places in turn, and each
+    tree's nodes have those of their own tree, in every one of several calls."""
+    case = Case(31, batch, nodes, *heads, np.zeros(batch, np.int32), bps=1)
+    rng = case.rng
+    odd = np.zeros((batch, nodes), bool)
+    for b in range(0, batch, 3):
+        for i in rng.integers(0, nodes, 2):
+            case.tv[b, :, i, rng.integers(0, 128)] = rng.choice([0x7F80, 0xFF80, 0x7FC0])
+            odd[b, i] = True
+    sees = odd.copy()                                # a node that is odd, or has an ancestor that is (parents come first)
+    for i in range(1, nodes):
+        sees[:, i] |= sees[np.arange(batch), case.parent[:, i]]
+    assert sees.any() and not sees.all()
+    ctx, args = case.context(), case.arguments()
+    want = np.broadcast_to(sees[:, :, None, None], (batch, nodes, case.hq, 128))
+    for _ in range(5):
+        out = ctx.tree_attn_fp8(*args)
+        ctx.check()
+        np.testing.assert_array_equal(torch.isnan(out).cpu().numpy(), want)
+
+
 @pytest.mark.parametrize("nodes", [1, 4, 60])
 def test_tree_rows_of_the_largest_values(nodes):
     case = Case(23, 2, nodes, 8, 2, [150, 0])
