@@ -203,8 +203,9 @@ kv_append_fp8_kernel(uint8_t *codes, float *scales, const int *__restrict__ tabl
     if (n < 0 || n > path_stride || n > N) { bad = true; n = 0; }
     if (L < 0 || (long long)L + n > (long long)table_stride * 128) { bad = true; n = 0; }
     if (new_len && lane == 0 && lk == 0 && h == 0 && group == 0) new_len[b] = L + n;
-    const int end = L + n, r0 = (L & ~(kRows - 1)) + group * kRows;
-    if (n > 0 && r0 < end) {
+    const int end = L + n, begin = L & ~(kRows - 1);
+    if (n > 0 && group * kRows < end - begin) {      // (looked at before it is added: a row's number may be as large as 32 bits hold)
+        const int r0 = begin + group * kRows;
         // row r0 + lane is entry 32 group + lane - (L % 32)
         const int back = L & (kRows - 1), from_lane = (lane - back) & 31, q0 = __shfl_sync(0xffffffffu, p0, from_lane), q1 = __shfl_sync(0xffffffffu, p1, from_lane), r = r0 + lane;
         int node = lane >= back ? q1 : q0;

@@ -202,6 +202,28 @@ def test_appends_out_of_range_are_reported_and_leave_out_their_rows(what):
     np.testing.assert_array_equal(d_scales.cpu().numpy(), scales)
 
 
+@pytest.mark.parametrize("behind,n", [(0, 20), (0, 1), (3, 200), (128, 256)])
+def test_append_at_the_end_of_the_longest_table(behind, n):
+    """Row numbers next to 2^31: the longest table that is accepted, whose last blocks are the sequence's."""
+    rng = np.random.default_rng(9)
+    N, hkv, bps, nb = 256, 1, (2 ** 31 - 1) // 128, 4
+    L = np.array([bps * 128 - n - behind], np.int32)
+    table = np.full((1, bps), -7, np.int32)
+    table[0, -nb:] = rng.permutation(nb)
+    codes, scales = _garbage(rng, 1, nb, hkv)
+    tree = _rows(rng, (1, 2, 1, hkv, N, 128))
+    path, n_acc = np.full((1, N), -1, np.int32), np.array([n], np.int32)
+    path[0, :n] = np.sort(rng.permutation(N)[:n])
+    d_codes, d_scales = dev(codes), dev(scales)
+    ctx = _context(hkv, hkv, max_batch=1, max_nodes=N)
+    new_len = ctx.kv_append_fp8(d_codes, d_scales, dev(table), b16(tree), dev(path), dev(n_acc), dev(L))
+    ctx.check()
+    fp8.append(codes, scales, table, tree, path, n_acc, L)
+    assert new_len.tolist() == [int(L[0]) + n]
+    _same(d_codes, codes)
+    np.testing.assert_array_equal(d_scales.cpu().numpy(), scales)
+
+
 # ---- blocks ------------------------------------------------------------------------------------------------------------------------------
 
 
