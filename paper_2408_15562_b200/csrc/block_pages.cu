@@ -357,7 +357,9 @@ block_copy_kernel(unsigned char *pool0, long long bytes0, unsigned char *pool1, 
     }
 }
 
-cudaError_t raise(const void *kernel, int bytes) { return bytes <= 48 * 1024 ? cudaSuccess : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); }
+// Dynamic shared memory of the calls that keep sets of blocks.
+constexpr int free_bytes(int n_blocks) { return (n_blocks + 31) / 32 * 4; }
+constexpr int compact_bytes(int n_blocks) { return (n_blocks + 31) / 32 * 12; }
 
 }  // namespace
 
@@ -369,8 +371,8 @@ cudaError_t fspad_launch_block_fork(fspad_ctx *ctx, const FspadPool &pool, const
 
 cudaError_t fspad_launch_block_free(fspad_ctx *ctx, const FspadPool &pool, const int *drop, cudaStream_t st)
 {
-    const int smem = (pool.n_blocks + 31) / 32 * 4;
-    const cudaError_t e = raise(reinterpret_cast<const void *>(&block_free_kernel), smem);
+    const int smem = free_bytes(pool.n_blocks);
+    const cudaError_t e = packed::raise_shared(ctx, 6, reinterpret_cast<const void *>(&block_free_kernel), free_bytes(FSPAD_PAGES_MAX_BLOCKS));
     if (e != cudaSuccess) return e;
     ctx->launches++;
     return fspad_launch(block_free_kernel, dim3(1), dim3(kThreads), smem, st, 0, pool, drop, ctx->d_status);
@@ -378,8 +380,8 @@ cudaError_t fspad_launch_block_free(fspad_ctx *ctx, const FspadPool &pool, const
 
 cudaError_t fspad_launch_block_compact(fspad_ctx *ctx, const FspadPool &pool, int *pairs, int max_pairs, cudaStream_t st)
 {
-    const int smem = (pool.n_blocks + 31) / 32 * 12;
-    const cudaError_t e = raise(reinterpret_cast<const void *>(&block_compact_kernel), smem);
+    const int smem = compact_bytes(pool.n_blocks);
+    const cudaError_t e = packed::raise_shared(ctx, 7, reinterpret_cast<const void *>(&block_compact_kernel), compact_bytes(FSPAD_PAGES_MAX_BLOCKS));
     if (e != cudaSuccess) return e;
     ctx->launches++;
     return fspad_launch(block_compact_kernel, dim3(1), dim3(kThreads), smem, st, 0, pool, pairs, max_pairs, ctx->d_status);
@@ -389,7 +391,7 @@ cudaError_t fspad_launch_block_copy(fspad_ctx *ctx, void *pool0, long long bytes
                                     const int *pairs, int n_pairs, cudaStream_t st)
 {
     const int smem = kSlots * kPiece;
-    const cudaError_t e = raise(reinterpret_cast<const void *>(&block_copy_kernel), smem);
+    const cudaError_t e = packed::raise_shared(ctx, 8, reinterpret_cast<const void *>(&block_copy_kernel), smem);
     if (e != cudaSuccess) return e;
     const long long pieces = (bytes0 + kPiece - 1) / kPiece + (bytes1 + kPiece - 1) / kPiece, all = pieces * planes * n_pairs;
     ctx->launches++;

@@ -57,7 +57,7 @@ struct fspad_ctx {
     struct FspadStatsPart *lm_parts;
     int lm_attr_done;
     int fs_attr_done;         // dynamic shared-memory limit raised for the Feature Sampler's product kernel
-    int packed_attr_done;     // ... for the kernels of the attention over the 4-bit cache, a bit each
+    int packed_attr_done;     // ... for the kernels of the attention over the 4-bit and 8-bit caches and of the calls on blocks, a bit each
 
     void *dx_part;            // draft step: per-piece top-k lists [max_batch * 16 rows][pieces][16], 64-bit sort keys (0: none)
     int *dx_done;             // draft step: finished pieces of each sequence [max_batch]; zero between calls

@@ -40,6 +40,18 @@ cudaError_t fspad_launch_tree_attn_packed(fspad_ctx *ctx, const fspad_bf16 *q, c
                                           const fspad_bf16 *tv, const int *parent, const int *prefix_len, int N, int B,
                                           fspad_bf16 *out, void *workspace, cudaStream_t st);
 
+namespace packed {
+// A kernel's dynamic shared memory, once a context: to the most that any call needs, for the limit is the kernel's, whoever launches it.  (Its static memory counts against the
+// 48 KB that need no such call.)
+static inline cudaError_t raise_shared(fspad_ctx *ctx, int bit, const void *kernel, int bytes)
+{
+    if ((ctx->packed_attr_done >> bit) & 1) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) ctx->packed_attr_done |= 1 << bit;
+    return e;
+}
+}  // namespace packed
+
 #ifdef __CUDACC__
 // Eight codes (a 32-bit word) as four pairs of fp16 values, the pair of byte i in r[i].
 __device__ __forceinline__ void fspad_e2m1_to_f16(uint32_t w, uint32_t (&r)[4])

@@ -385,15 +385,6 @@ template <int BM> static inline void scratch_in(Args &a, int parts, void *worksp
     a.cuts = reinterpret_cast<int *>(a.part_ml + (size_t)parts * 2 * BM);
 }
 
-// A kernel's dynamic shared memory, once a context.
-static inline cudaError_t raise_shared(fspad_ctx *ctx, int bit, const void *kernel, int bytes)
-{
-    if ((ctx->packed_attr_done >> bit) & 1) return cudaSuccess;
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e == cudaSuccess) ctx->packed_attr_done |= 1 << bit;
-    return e;
-}
-
 // Parts there can be -> how the runs that were cut are told of; and the merge's launch: entries x groups of so many rows, so that they are all there at once (three CTAs an SM).
 static inline int merge_entries(Args &a, int parts)
 {

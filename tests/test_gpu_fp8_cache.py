@@ -1,4 +1,6 @@
 """Writes into the 8-bit cache, and forks, drops, compactions and copies of blocks, on the GPU against the definitions: bit for bit."""
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -386,6 +388,65 @@ def test_blocks_beside_the_stack_and_the_tables_stay_where_they_are():
     p.put()
     pairs = p.compact().cpu().numpy()
     assert pairs[:3].tolist() == [[66, 3], [68, 10], [-1, -1]]
+
+
+def _spread(p, n):
+    """n blocks of the whole range, the first and the last among them, held by the sequences one behind the other (the first block by the last sequence too), the others
+    free in any order."""
+    t, h, s, f, _ = p.state
+    blocks = np.concatenate([[0, p.nb - 1], 1 + p.rng.choice(p.nb - 2, n - 2, replace=False)]).astype(np.int32)
+    for b in range(p.B):
+        mine = blocks[b::p.B]
+        h[b] = len(mine)
+        t[b, :h[b]] = mine
+    t[-1, h[-1]], s[blocks[0]] = blocks[0], 1
+    h[-1] += 1
+    rest = np.setdiff1d(np.arange(p.nb, dtype=np.int32), blocks)
+    f[:len(rest)] = p.rng.permutation(rest)
+    p.state = (t, h, s, f, len(rest))
+    p.put()
+
+
+@pytest.mark.parametrize("nb", [32768, 32769, 130400, 131072, 391200, 393216, 400000, 2 ** 19])
+def test_pools_of_any_size_up_to_the_largest(nb):
+    """More words of bits than threads, and shared memory around what a kernel has without asking and far beyond."""
+    p = Pool(np.random.default_rng(nb), 9, 60, nb)
+    _spread(p, 400)
+    assert p.fork([8], [8]) is None                  # (a target that is a source changes nothing)
+    assert p.compact() is not None
+    assert p.drop([0, 1, 0, 1, 1, 0, 0, 1, 1])
+    assert p.compact() is not None
+    assert p.drop([1] * 9) and p.state[4] == nb
+
+
+def test_pools_of_two_sizes_from_two_threads():
+    """Calls of two host threads, a context each: neither takes from the other what its pool needs of shared memory."""
+    pools, wrong = [Pool(np.random.default_rng(i), 9, 60, nb) for i, nb in enumerate((2 ** 19, 140000))], []
+    for p in pools:
+        _spread(p, 300)
+    torch.cuda.synchronize()
+
+    def work(p, i):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                pairs = torch.zeros((p.nb // 2, 2), dtype=torch.int32, device="cuda")
+                for _ in range(300):
+                    p.ctx.block_compact(*p.d, pairs=pairs)
+                    p.ctx.block_free(dev(np.zeros(9, np.int32)), *p.d)
+                torch.cuda.current_stream().synchronize()
+            p.ctx.check()
+        except Exception as e:                       # noqa: BLE001
+            wrong.append((i, e))
+
+    threads = [threading.Thread(target=work, args=(p, i)) for i, p in enumerate(pools)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong, wrong
+    for p in pools:
+        _, p.state = fp8.compact(*p.state)
+        p.same()
 
 
 @pytest.mark.parametrize("dtype,tail", [(torch.uint8, (2, 128, 128)), (torch.bfloat16, (2, 128, 128)), (torch.float32, (1, 4)), (torch.uint8, (3, 128, 8)), (torch.int32, (5000,))])
