@@ -552,7 +552,7 @@ int fspad_tree_attn_packed(fspad_ctx *ctx, const fspad_bf16 *q, const uint8_t *c
  *
  * Writing rows: those of one call that fall into a group are written together.  need = the least 2^e, e from -64 to 64, with max |x| <= 448 * 2^e over them; if one of
  * them is the group's row 0 (they begin it), its scale becomes need, and what the group's other rows held is lost.  Otherwise the rows that it holds stay: its scale s becomes the larger of need and s (of
- * the next power of two, where s is none; of need, where s is outside the range), and where that is more than s all 32 rows' codes are rounded again, to the nearest code * s / s', ties to the even one: a value changes only where it falls below
+ * the next power of two, where s is none; s outside the range is the nearer end, as above), and where that is more than s all 32 rows' codes are rounded again, to the nearest code * s / s', ties to the even one: a value changes only where it falls below
  * the least codes (a caller's own scale may cost a rounding).  Codes are x / scale to the nearest, ties to the even one, beyond 448 to 448; the
  * sign of an element is kept where its code is zero.  An infinity or a NaN has no part in the maximum and is kept as NaN.
  *

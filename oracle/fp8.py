@@ -45,7 +45,8 @@ def put(codes, scales, blk, off, x):
             finite = np.where(np.isfinite(y), np.abs(y), 0.0)
             s = least_scale(finite.max())
             old = float(scales[b, h, g])
-            if not (at % GROUP == 0).any() and 2.0 ** -64 <= old <= 2.0 ** 64:
+            if not (at % GROUP == 0).any():
+                old = min(max(old, 2.0 ** -64), 2.0 ** 64) if old == old else 2.0 ** -64
                 s = max(s, 2.0 ** np.ceil(np.log2(old)))
                 if s != old:
                     lines = np.s_[b, h, g * GROUP:(g + 1) * GROUP]

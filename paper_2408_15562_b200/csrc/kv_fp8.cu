@@ -65,9 +65,10 @@ __device__ __forceinline__ void put_group(uint32_t rows, uint4 *back, uint8_t *c
     int field = fspad_fp8_field(most);
     bool again = false;
     float ratio = 1.f;
-    if (begun && old >= kFp8Least && old <= kFp8Most) {          // (a scale outside the range, or none, is of rows that do not count)
-        field = max(field, (int)((__float_as_uint(old) + 0x7fffffu) >> 23));
-        ratio = old * fspad_field_float(254 - field);            // (a reciprocal's field; exact)
+    if (begun) {
+        const float is = fminf(fmaxf(old, kFp8Least), kFp8Most);         // (what the attention takes it for)
+        field = max(field, (int)((__float_as_uint(is) + 0x7fffffu) >> 23));
+        ratio = is * fspad_field_float(254 - field);             // (a reciprocal's field; exact)
         again = ratio != 1.f;
     }
     const float s = fspad_field_float(field), inv = fspad_field_float(254 - field);

@@ -183,6 +183,23 @@ def test_scales_far_apart_and_a_callers_own(nodes, what):
     case.check(_run(case))
 
 
+@pytest.mark.parametrize("own", [0.0, -1.0, 1e-30, float("nan"), 1e30, float("inf")])
+@pytest.mark.parametrize("nodes", [1, 20])
+def test_a_write_leaves_what_a_scale_outside_the_range_stands_for(nodes, own):
+    """A begun group with a scale of no use: the attention takes the nearer end, and so does a write of further rows (here of tiny ones)."""
+    case = Case(24, 1, nodes, 4, 2, [37])
+    blk = int(case.table[0, 0])
+    case.scales[0, 1, blk, :, 1] = own
+    args, ctx = case.arguments(), case.context()
+    first = ctx.tree_attn_fp8(*args)
+    x = b16(synth.f32_to_bf16_bits((case.rng.standard_normal((2, 2, 3, 128)) * 2.0 ** -70).astype(np.float32)))
+    ctx.kv_write_fp8(x[0], x[1], dev(blk * 128 + 37 + np.arange(3)), args[1], args[2])
+    again = ctx.tree_attn_fp8(*args)
+    ctx.check()
+    assert torch.equal(again, first)
+    assert (args[2][0, 1, blk, :, 1] == 2.0 ** (64 if own > 1 else -64)).all()
+
+
 @pytest.mark.parametrize("nodes", [1, 60])
 def test_one_heavy_key_and_many_light_ones(nodes):
     """One key with half of the weight, 20000 others with the rest: weights of 2^-15 of the largest, all alike, whose roundings add up."""

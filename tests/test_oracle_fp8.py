@@ -50,6 +50,18 @@ def test_a_group_begins_and_goes_on():
     assert scales[1, 0, 1] == 2.0 ** -10
 
 
+@pytest.mark.parametrize("own,end", [(0.0, -64), (-1.0, -64), (1e-30, -64), (float("nan"), -64), (1e30, 64), (float("inf"), 64)])
+def test_a_scale_outside_the_range_is_the_nearer_end(own, end):
+    codes, scales = np.zeros((1, 1, 128, 128), np.uint8), np.full((1, 1, 4), own, np.float32)
+    codes[0, 0, 0, :3] = 0x38, 0x7E, 0xB8              # 1, 448 and -1
+    before = codes[0, 0, 0].copy()
+    x = np.zeros((1, 1, 128))
+    x[0, 0, 0] = 2.0 ** -60
+    v = fp8.put(codes, scales, [0], [1], bits(x))
+    assert scales[0, 0, 0] == 2.0 ** end and v[0, 0, 0] == (2.0 ** -60 if end < 0 else 0)
+    np.testing.assert_array_equal(codes[0, 0, 0], before)
+
+
 def test_rows_one_by_one_end_where_rows_together_do():
     """Normal values: a scale that rises step by step leaves the codes that the last one gives at once (double rounding only below the least normal code)."""
     rng = np.random.default_rng(1)
