@@ -3,7 +3,7 @@
 //
 // Of a group of 32 rows of a head: s = the least power of two with max |x| <= 448 s, codes e4m3(x / s), to the nearest, ties to the even one.  Rows of one
 // call that fall into a group are taken together by one warp: asynchronous copies bring them into 8 KB of shared memory, where every lane looks at what it has asked for, 16 bytes of a row, once for the group's maximum and again for the
-// codes.  (Kept in registers, all 32 of them, an SM had 16 warps, not 28: 64 paths of up to 24 nodes in 16 layers 62 us.)
+// codes.  (Kept in registers, all 32 of them, an SM had 16 warps, not 24: 64 paths of up to 24 nodes in 16 layers 62 us.)
 // A group that was begun before (its row 0 is not among them) keeps its scale or, where the new rows need a larger one, is
 // rounded again by it: with powers of two that changes only what falls below the least codes.
 // An element that is not finite has no part in the maximum and is kept as NaN.
@@ -18,6 +18,7 @@ namespace {
 
 constexpr int kWarps = 4;                // of a CTA
 constexpr int kRows = FSPAD_FP8_GROUP;
+constexpr int kCtas = 6;                 // of an SM: 32 KB each, and 1 KB of the system's
 constexpr int kStage = kRows * FSPAD_HEAD_DIM * 2;   // bytes of a warp's rows
 
 // Larger finite magnitude among two pairs of bf16 that may hold infinities and NaN: what is none counts as 0.
@@ -129,7 +130,7 @@ __device__ __forceinline__ void put_group(uint32_t rows, uint4 *back, uint8_t *c
 
 // Rows [2][Hkv][rows] to the slots slots[rows] of one layer.  A warp looks at `each` entries (a power of two, at most 32) of a head's K or V and takes the groups that have their first row there;
 // the rows of a group stand within 32 entries.
-__global__ void __launch_bounds__(kWarps * 32, 7)
+__global__ void __launch_bounds__(kWarps * 32, kCtas)
 kv_write_fp8_kernel(const uint4 *k, const uint4 *v, const long long *__restrict__ slots, int rows, int Hkv, int each, uint8_t *codes, float *scales,
                     int n_blocks, uint4 *k_rounded, uint4 *v_rounded, int *__restrict__ status)
 {
@@ -178,7 +179,7 @@ kv_write_fp8_kernel(const uint4 *k, const uint4 *v, const long long *__restrict_
 }
 
 // cache row L_b + j <- tree row path[b][j] of the slice, j < n_acc[b]; a warp per (layer, K/V, sequence, head) and group of 32 rows (as many as a path of all nodes can touch).
-__global__ void __launch_bounds__(kWarps * 32, 7)
+__global__ void __launch_bounds__(kWarps * 32, kCtas)
 kv_append_fp8_kernel(uint8_t *codes, float *scales, const int *__restrict__ table, int table_stride, int n_blocks, const uint4 *tree_kv,
                      const int *__restrict__ path, const int *__restrict__ n_acc, const int *__restrict__ prefix_len, int n_layers, int B, int Hkv, int N,
                      int path_stride, int groups, uint4 *rounded, int *__restrict__ new_len, int *__restrict__ status)
