@@ -573,7 +573,9 @@ int fspad_kv_write_fp8(fspad_ctx *ctx, const fspad_bf16 *k, const fspad_bf16 *v,
 /*
  * fspad_kv_append for the 8-bit cache: for every layer, K and V, sequence b and kv head, cache row L_b + j receives
  * tree_kv[..][accepted_path[b][j]], j = 0 .. n_accepted[b] - 1.  new_len[b] = L_b + n_accepted[b] (may be NULL, but must not
- * overlap prefix_len, n_accepted, accepted_path or block_table: FSPAD_ERR_RANGE).  Arguments, `rounded` among them, and errors as in fspad_kv_append_packed.
+ * overlap prefix_len, n_accepted, accepted_path or block_table: FSPAD_ERR_RANGE).  Arguments, `rounded` among them, and errors as in fspad_kv_append_packed;
+ * new_len[b] is then L_b where the count or the length is out of range, so that nothing of the sequence is written, and otherwise L_b + n_accepted[b], whichever rows
+ * were left out for their node or their block.
  * The groups of the written rows must not be shared (whole blocks that fspad_block_fork shares hold none).
  */
 int fspad_kv_append_fp8(fspad_ctx *ctx, uint8_t *codes, float *scales, const int32_t *block_table, int blocks_per_seq, int n_blocks,

@@ -204,6 +204,44 @@ def test_appends_out_of_range_are_reported_and_leave_out_their_rows(what):
     np.testing.assert_array_equal(d_scales.cpu().numpy(), scales)
 
 
+@pytest.mark.parametrize("what", ["node", "low node", "count", "negative count", "length", "negative length", "block", "low block"])
+def test_what_an_append_out_of_range_returns(what):
+    """Lengths, and kept values: those of rows that are left out are as they were."""
+    rng = np.random.default_rng(10)
+    B, N, hkv = 2, 8, 2
+    table, L = rng.permutation(4).reshape(2, 2).astype(np.int32), np.array([126, 20], np.int32)
+    codes, scales = _garbage(rng, 1, 4, hkv)
+    tree = _rows(rng, (1, 2, B, hkv, N, 128))
+    path, n_acc = np.tile(np.arange(N, dtype=np.int32), (B, 1)), np.array([5, 4], np.int32)
+    kept = np.arange(5)                              # of sequence 0: rows 126 .. 130, from the third on in the second block
+    length = 131
+    if what == "node": path[0, 3], kept = N, np.array([0, 1, 2, 4])
+    if what == "low node": path[0, 1], kept = -1, np.array([0, 2, 3, 4])
+    if what == "count": n_acc[0], kept, length = N + 1, kept[:0], 126
+    if what == "negative count": n_acc[0], kept, length = -1, kept[:0], 126
+    if what == "length": L[0], kept, length = 252, kept[:0], 252
+    if what == "negative length": L[0], kept, length = -3, kept[:0], -3
+    if what == "block": table[0, 1], kept = 4, kept[:2]
+    if what == "low block": table[0, 0], kept = -1, kept[2:]
+    d_codes, d_scales = dev(codes), dev(scales)
+    ctx = _context(hkv, hkv, max_batch=B, max_nodes=N)
+    back = torch.full((1, 2, B, hkv, N, 128), float("nan"), dtype=torch.bfloat16, device="cuda")
+    for keep in (None, back):                        # (once more changes nothing: the scales have risen, the rows are the same)
+        new_len = ctx.kv_append_fp8(d_codes, d_scales, dev(table), b16(tree), dev(path), dev(n_acc), dev(L), rounded=keep)
+        assert ctx.status() == -5
+        assert new_len.tolist() == [length, 24]
+    want = np.full(back.shape, np.nan)
+    for plane in (0, 1):
+        for b, at in ((0, kept), (1, np.arange(4))):
+            pos = L[b] + at
+            if len(at):
+                v = fp8.put(codes[0, plane], scales[0, plane], table[b, pos // 128], pos % 128, np.swapaxes(tree[0, plane, b][:, path[b, at]], 0, 1))
+                want[0, plane, b][:, path[b, at]] = np.swapaxes(v, 0, 1)
+    np.testing.assert_array_equal(back.float().cpu().numpy(), want)
+    _same(d_codes, codes)
+    np.testing.assert_array_equal(d_scales.cpu().numpy(), scales)
+
+
 @pytest.mark.parametrize("behind,n", [(0, 20), (0, 1), (3, 200), (128, 256)])
 def test_append_at_the_end_of_the_longest_table(behind, n):
     """Row numbers next to 2^31: the longest table that is accepted, whose last blocks are the sequence's."""
