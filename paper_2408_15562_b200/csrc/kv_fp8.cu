@@ -226,6 +226,8 @@ kv_append_fp8_kernel(uint8_t *codes, float *scales, const int *__restrict__ tabl
         if (there && inside) {
             const long long g = ((long long)lk * n_blocks + block) * Hkv + h;
             put_group(st, rounded, codes + (g * 128 + (r0 & 127)) * 128, scales + g * FSPAD_FP8_GROUPS + ((r0 & 127) / kRows), there, from, lane, r0 < L);
+        } else {
+            umma::cp_async_wait<0>();                // (rows that nobody takes: they land before the CTA's memory goes)
         }
     }
     if (bad) fspad_report(status, FSPAD_ERR_RANGE);
