@@ -543,8 +543,9 @@ int fspad_tree_attn_packed(fspad_ctx *ctx, const fspad_bf16 *q, const uint8_t *c
 /*
  * ---- A cache held in 8 bits ----
  *
- * A row of 128 elements is kept as 128 e4m3 codes; 32 rows of a head, a group, share a single-precision scale: 129 bytes a row on the average in place of 256.  An element stands for
- * code * scale; the error of a row's elements is at most 1/16 of each (of those below 2^-14 of the group's largest, 2^-18 of that).  Paged as above:
+ * A row of 128 elements is kept as 128 e4m3 codes; 32 rows of a head, a group, share a single-precision scale: 128.125 bytes a row on the average in place of 256.  An element stands for
+ * code * scale; its error is at most 1/16 of it or, where that is more, 2^-10 scales, which is below 2^-17 of the group's largest (twice that where the group has been rounded
+ * again).  Paged as above:
  *   codes  [n_layers][2][n_blocks][Hkv][128][128] bytes
  *   scales [n_layers][2][n_blocks][Hkv][4] float: of rows 0 .. 31, 32 .. 63, 64 .. 95, 96 .. 127 of a block.  In [2^-64, 2^64]; what lies outside is taken
  *          as the nearer end (no number: as 2^-64).  The writes leave powers of two; a caller's own cache may have others.
@@ -592,9 +593,9 @@ int fspad_kv_append_fp8(fspad_ctx *ctx, uint8_t *codes, float *scales, const int
  *   workspace  of at least fspad_tree_attn_fp8_workspace_bytes(ctx) bytes (39 MB on a B200, whatever the sizes),
  *              scratch: no other call may use it until this one is done
  * Single-precision scores, softmax and sums: scores q.k beyond its range are infinities, sum_j exp(s_j - max s) |v_j| must lie
- * in it, and results below about 2^-110 lose bits.  Against the cache a query element is exact down to 2^-10 of its row's largest (the
- * row's, of a node and head) and off by at most 2^-18 of that below; weights are rounded for the product with V, to 2^-9 of their value at the coarsest
- * (of the tree's keys to bf16).
+ * in it, and results below about 2^-110 lose bits.  Against the cache a query element is exact down to 2^-9 of its row's largest (the
+ * row's, of a node and head; or 2^-100, if that is more) and off by at most 2^-17 of that below, with up to 16 rows a kv head 2^-13 and 2^-21; weights are rounded for the product with V, at the
+ * coarsest to 2^-9 of their value or, of small ones, 2^-28 of the largest (each times its row's scale), of the tree's keys to bf16.
  * A tree row of V with an infinity or a NaN makes the outputs of the nodes that see it NaN, and of no others.  In K such an
  * element acts through the score, for the same nodes: NaN and +infinity make the output NaN, with -infinity the row has no
  * weight (where no row has any, the output is NaN).  A NaN of the cache is seen by all queries of its sequence and kv head: in K it makes their

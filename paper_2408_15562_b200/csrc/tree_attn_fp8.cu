@@ -9,7 +9,7 @@
 // operands as they are.  The products stand on their heads, so that the cache is the operand with 128 rows: S^T [128 keys][rows] = K Q^T, then
 // O^T [128 elements][rows] += V^T P^T, with V's tile taken as its own transpose.  What the other operand holds is 16 bits wide by nature, and is written as a sum of 8-bit numbers, in
 // columns of their own that are added up afterwards:
-//   a query  = hi + lo / 16, e4m3, the row scaled by a power of two to a largest magnitude in [2^7, 2^8): exact for elements of at least 2^-14 of that
+//   a query  = hi + lo / 16, e4m3, the row scaled by a power of two to a largest magnitude in [2^7, 2^8): exact from 2^-6 on, at most 2^-13 of the largest, and off by at most 2^-14 below, 2^-21 of it
 //   a weight = hi + mid + lo, e5m2, each the nearest number to what is left: 3 significant bits each, off by at most 2^-9 of the weight and 2^-17 (2^11 stands for the largest)
 // V's scale goes into the weights, as an addend of the exponent: the reference that weights are relative to follows the maximum of score + log2(scale).
 //

@@ -12,8 +12,8 @@
 // same rows and take the chunks in turn, each with an accumulator of its own, and are merged at the end.
 //
 // K is never touched outside the tensor cores: its e4m3 codes are an operand as they are, and a query is the sum of two e4m3 numbers, the nearest one and what is
-// left, which is exact for elements of at least 2^-10 of the row's largest (a bf16 number has 8 significant bits, the two have 4 each); smaller ones are
-// off by at most 2^-18 of the largest.  32 keys' scale is a factor of 32 columns of the scores.  V's scale goes into the weights, as an addend of the
+// left, which is exact for elements of at least 2^-9 of the row's largest (a bf16 number has 8 significant bits, the two have 4 each, whole multiples of 2^-9 where the largest lies in
+// [2^7, 2^8)); smaller ones are off by at most 2^-17 of the largest.  32 keys' scale is a factor of 32 columns of the scores.  V's scale goes into the weights, as an addend of the
 // exponent: the reference that a row's weights are relative to follows the maximum of score + log2(scale), and the sum of the weights takes each
 // group's part times 1 / scale.  Against the tree's rows, which are bf16 of any size, the queries are taken as they are: its chunks come first, and the query
 // tile is then written again.  With one row tile its two forms lie in the two tiles' places.

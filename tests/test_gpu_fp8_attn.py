@@ -162,6 +162,36 @@ def test_scores_that_rise_along_the_cache(nodes):
     case.check(_run(case))
 
 
+@pytest.mark.parametrize("nodes,last", [(1, 13), (4, 13), (5, 9), (60, 9)])
+def test_how_exact_small_elements_of_a_query_are(nodes, last):
+    """Of each row one element next to 2^-e beside the largest, 1, against a key whose two elements cancel but for the small one's last bit (2^-7 of it, or -2^-8): the scores are 2 and
+    -1 from sums of 2 * 2^8, the other cached key's is 0, the values 1 and -1, the result tanh(score / 2).  An element is exact from 2^-9 of the largest on, up to 16 rows a kv head 2^-13 (`last`); a smaller one (at e = last
+    the ones below a power of two are) may be off by 2^-17, or 2^-21, of the largest: by 2^-(last + 8), the score by that times 256 * 2^(e + 4) / 2^4, 2^(e - last), and the result by
+    half of that.  Otherwise: the score's sum to 2^-15 of the magnitudes, 2^-6, half of that in the result; the weights to 2^-9 and the result to 2^-9."""
+    for e in range(4, last + 2):
+        case = Case(e, 1, nodes, 8, 2, [2])
+        rng, blk = case.rng, int(case.table[0, 0])
+        kv = np.zeros((2, 2, 128))
+        kv[0, 0] = 256.0
+        kv[0, 0, 0] = -2.0 ** (8 - e)
+        kv[1] = [[1.0], [-1.0]]
+        case.codes[0, :, blk, :, :2] = fp8.encode(kv)[:, None]
+        case.scales[0, 0, blk, :, 0], case.scales[0, 1, blk, :, 0] = 2.0 ** (e + 4), 1.0
+        below = rng.random((1, nodes, 8)) < 0.5
+        x = np.zeros(case.q.shape)
+        np.put_along_axis(x, rng.integers(1, 128, below.shape)[..., None], np.where(below, 1 - 2.0 ** -8, 1 + 2.0 ** -7)[..., None] * 2.0 ** -e, -1)
+        x[..., 0] = 1.0
+        case.q = synth.f32_to_bf16_bits(x.astype(np.float32))
+        np.testing.assert_array_equal(packed.bf16(case.q), x)
+        t = np.zeros(case.tk.shape, np.float32)
+        t[..., 0] = -2.0 ** 12                         # (the tree's keys have no weight)
+        case.tk = synth.f32_to_bf16_bits(t)
+        want = np.tanh(np.where(below, -0.5, 1.0))[..., None]
+        err = np.abs(_run(case, softmax_scale=2.0 ** -4).float().cpu().numpy() - want).max(-1)
+        small = np.where(below, 1 - 2.0 ** -8, 1.0) * 2.0 ** -e < 2.0 ** -last
+        assert (err <= 2.0 ** -7 + 2.0 ** -8 + np.where(small, 2.0 ** (e - last) / 2, 0.0)).all(), (e, err.max())
+
+
 @pytest.mark.parametrize("nodes", [1, 60])
 @pytest.mark.parametrize("what", ["k", "v", "own", "v falls"])
 def test_scales_far_apart_and_a_callers_own(nodes, what):

@@ -90,6 +90,23 @@ def test_the_kept_values_are_within_a_sixteenth():
     np.testing.assert_array_equal(got, v[:, 1])
 
 
+def test_how_far_small_elements_are_off():
+    """At most 2^-10 scales, which is below 2^-17 of the group's largest but may be above 2^-18 of it; each time the group is rounded again at most as much of the new scale: all in all twice the last."""
+    codes, scales = np.zeros((1, 1, 128, 128), np.uint8), np.ones((1, 1, 4), np.float32)
+    x = np.zeros((1, 1, 128))
+    x[0, 0, :2] = 225, 2.0 ** -10
+    v = fp8.put(codes, scales, [0], [0], bits(x))
+    assert scales[0, 0, 0] == 1 and v[0, 0, 1] == 0 and 2.0 ** -18 < 2.0 ** -10 / 225 < 2.0 ** -17
+    rng = np.random.default_rng(5)
+    f = rng.standard_normal((32, 1, 128)) * 2.0 ** np.arange(-16, 16)[:, None, None]
+    y = packed.bf16(bits(f))
+    for i in range(32):
+        fp8.put(codes, scales, [0], [i], bits(f[i:i + 1]))
+    got, s = fp8.rows_of(codes[None, None], scales[None, None], 0, 0, np.array([0]), 0, 32)
+    assert (s < np.abs(y).max() / 224).all()
+    assert (np.abs(got - y[:, 0]) <= np.maximum(np.abs(y[:, 0]) / 16, s[:, None] * 2.0 ** -10) + s[:, None] * 2.0 ** -10).all()
+
+
 def test_attention_is_the_plain_one_on_the_decoded_rows():
     rng = np.random.default_rng(3)
     B, N, hq, hkv, L = 2, 5, 4, 2, np.array([70, 0])
