@@ -26,6 +26,7 @@ EXPORTS = ["fspad_create", "fspad_destroy", "fspad_status", "fspad_strerror", "f
            "fspad_tree_attn_paged", "fspad_kv_compact_paged", "fspad_kv_append", "fspad_lm_head_stats", "fspad_lm_head_accept", "fspad_feature_sampler", "fspad_feature_sampler_workspace_bytes", "fspad_verify_step", "fspad_verify_step_host", "fspad_selftest_wait_timeout", "fspad_accept_stats_noalloc", "fspad_tree_build", "fspad_draft_expand",
            "fspad_device", "fspad_rope_qkv", "fspad_block_plan", "fspad_kv_write_packed", "fspad_kv_append_packed", "fspad_tree_attn_packed",
            "fspad_tree_attn_packed_workspace_bytes", "fspad_block_fork", "fspad_block_free", "fspad_block_compact", "fspad_block_copy"]
+# (those whose names have a digit)
 EXPORTS_FP8 = ["fspad_kv_write_fp8", "fspad_kv_append_fp8", "fspad_tree_attn_fp8", "fspad_tree_attn_fp8_workspace_bytes"]
 
 

@@ -1,5 +1,5 @@
-// What the two kernels of the attention over the 4-bit cache share: their arguments, the list of work that its CTAs cut into equal parts, and the merge of
-// the runs that were cut.
+// What the kernels of the attention over the 4-bit cache and over the 8-bit one share, two of each: their arguments, the list of work that their CTAs cut into equal parts, and the
+// merge of the runs that were cut.
 //
 // For every sequence, kv head and tile of BM query rows the list holds a run of units of UNIT keys: the tree's first, then the cache's.  Every CTA (or warp) takes an
 // equal part of the list wherever the cuts fall, so that ragged lengths and any number of sequences fill the SMs alike, and nothing about the lengths has to be

@@ -679,7 +679,7 @@ template <int R> cudaError_t launch_few(fspad_ctx *ctx, Args &a, const Maps &map
 }  // namespace
 
 size_t fspad_attn_fp8_umma_workspace(const fspad_ctx *ctx);
-cudaError_t fspad_launch_attn_fp8_umma(fspad_ctx *ctx, packed::Args a, const CUtensorMap &k_map, int k_row0, void *workspace, cudaStream_t st);
+cudaError_t fspad_launch_attn_fp8_umma(fspad_ctx *ctx, packed::Args a, const CUtensorMap &k_map, void *workspace, cudaStream_t st);
 
 // (of either kernel, so that a workspace made for one call serves every other: the one with 256 rows a CTA needs the most)
 size_t fspad_attn_fp8_workspace(const fspad_ctx *ctx) { return fspad_attn_fp8_umma_workspace(ctx); }
@@ -711,7 +711,7 @@ cudaError_t fspad_launch_tree_attn_fp8(fspad_ctx *ctx, const fspad_bf16 *q, cons
     if (!fspad_make_tmap_u8_2d(&maps.k, k_codes, rows, 128u)) return cudaErrorInvalidValue;
     // Measured on both sides, 8 kv heads, us: 16 rows here and there, 32 sequences of 4 to 12 thousand keys 97 and 160, 16 of 512 to 4096 24 and 46, 64 of 100 to 600 32 and 74.
     // A tile of 32 rows here (192 columns of weights a chunk) took from 17 rows on 157 against 163, but 60 against 47 and 90 against 74: not kept.
-    if (a.M > 16) return fspad_launch_attn_fp8_umma(ctx, a, maps.k, 0, workspace, st);
+    if (a.M > 16) return fspad_launch_attn_fp8_umma(ctx, a, maps.k, workspace, st);
     if (!fspad_make_tmap_u8_2d(&maps.v, v_codes, rows, 128u)) return cudaErrorInvalidValue;
     return a.M <= 8 ? launch_few<8>(ctx, a, maps, workspace, st) : launch_few<16>(ctx, a, maps, workspace, st);
 }

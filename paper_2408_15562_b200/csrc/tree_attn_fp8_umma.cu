@@ -196,7 +196,7 @@ static_assert(SMEM + sizeof(Small) <= 232448, "shared memory of an SM");
 static_assert(SMEM % 16 == 0 && alignof(Small) >= 16 && offsetof(Small, raw) % 16 == 0, "bulk copies' destination");
 
 __global__ void __launch_bounds__(NT, 1)
-tree_attn_fp8_umma_kernel(const Args a, const __grid_constant__ CUtensorMap k_map, int k_row0)
+tree_attn_fp8_umma_kernel(const Args a, const __grid_constant__ CUtensorMap k_map)
 {
     extern __shared__ __align__(1024) unsigned char smem_raw[];      // (nothing else is in shared memory, so it starts on such a boundary: looked at below)
     enum { B_FULL = 0, B_FREE = BUFS, K_FULL = 2 * BUFS, T_FULL = 3 * BUFS, V_FULL = 4 * BUFS, V_FREE = V_FULL + 2, S_FULL = V_FREE + 2,
@@ -579,7 +579,7 @@ tree_attn_fp8_umma_kernel(const Args a, const __grid_constant__ CUtensorMap k_ma
                         mbar_arrive(full);                   // (the tree's rows are for others to fetch)
                     } else {
                         mbar_expect_tx(full, 2 * HALF + 32);
-                        tma_load_2d(to, &k_map, 0, k_row0 + (int)(at_head * 128), full);
+                        tma_load_2d(to, &k_map, 0, (int)(at_head * 128), full);
                         bulk_load(to + HALF, a.vc + at_head * HALF, HALF, full);
                         bulk_load(smem_u32(&s_raw[buf][0]), a.ks + at_head * 16, 16, full);
                         bulk_load(smem_u32(&s_raw[buf][4]), a.vs + at_head * 16, 16, full);
@@ -817,8 +817,8 @@ size_t fspad_attn_fp8_umma_workspace(const fspad_ctx *ctx)
     return scratch_bytes<BM>(ctx->sm_count);
 }
 
-// k_map: rows of the K codes as boxes of 128 rows, the plane's first row k_row0.
-cudaError_t fspad_launch_attn_fp8_umma(fspad_ctx *ctx, packed::Args a, const CUtensorMap &k_map, int k_row0, void *workspace, cudaStream_t st)
+// k_map: rows of the plane's K codes as boxes of 128 rows.
+cudaError_t fspad_launch_attn_fp8_umma(fspad_ctx *ctx, packed::Args a, const CUtensorMap &k_map, void *workspace, cudaStream_t st)
 {
     const int ctas = ctx->sm_count, smem = SMEM + (int)sizeof(Small);
     a.mtiles = (a.M + BM - 1) / BM;
@@ -828,6 +828,6 @@ cudaError_t fspad_launch_attn_fp8_umma(fspad_ctx *ctx, packed::Args a, const CUt
     if (e != cudaSuccess) return e;
     const int entries = merge_entries(a, ctas);
     ctx->launches++;
-    e = fspad_launch(tree_attn_fp8_umma_kernel, dim3((unsigned)ctas), dim3(NT), smem, st, 0, a, k_map, k_row0);
+    e = fspad_launch(tree_attn_fp8_umma_kernel, dim3((unsigned)ctas), dim3(NT), smem, st, 0, a, k_map);
     return e == cudaSuccess ? launch_merge<BM>(ctx, a, entries, ctas, st) : e;
 }
