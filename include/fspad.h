@@ -595,7 +595,8 @@ int fspad_kv_append_fp8(fspad_ctx *ctx, uint8_t *codes, float *scales, const int
  * Single-precision scores, softmax and sums: scores q.k beyond its range are infinities, sum_j exp(s_j - max s) |v_j| must lie
  * in it, and results below about 2^-110 lose bits.  Against the cache a query element is exact down to 2^-9 of its row's largest (the
  * row's, of a node and head; or 2^-100, if that is more) and off by at most 2^-17 of that below, with up to 16 rows a kv head 2^-13 and 2^-21; weights are rounded for the product with V, at the
- * coarsest to 2^-9 of their value or, of small ones, 2^-28 of the largest (each times its row's scale), of the tree's keys to bf16.
+ * coarsest to 2^-9 of their value or, of small ones, 2^-28 of the largest (each times its row's scale), of the tree's keys to bf16.  A key
+ * whose weight times its row's scale of V is below 2^-133 of the largest such product may have no part in the sum of the weights.
  * A tree row of V with an infinity or a NaN makes the outputs of the nodes that see it NaN, and of no others.  In K such an
  * element acts through the score, for the same nodes: NaN and +infinity make the output NaN, with -infinity the row has no
  * weight (where no row has any, the output is NaN).  A NaN of the cache is seen by all queries of its sequence and kv head: in K it makes their

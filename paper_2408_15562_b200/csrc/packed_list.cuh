@@ -296,8 +296,8 @@ template <int ROWS = kAnyRows> __device__ __forceinline__ void tell_run(const Ar
 }
 
 // The pieces of the runs that were cut, merged.  A CTA takes `rows` rows (a power of two, at most WARPS) of a run at a time, each by WARPS / rows warps that take its
-// pieces in turn, four elements a lane.
-template <int BM, int WARPS, int U>           // U: pieces of a row under way
+// pieces in turn, four elements a lane.  WIDE: the pieces' references may lie 2^128 apart and more, with sums that weigh alike (of the 8-bit cache they hold V's scales).
+template <int BM, int WARPS, int U, bool WIDE>           // U: pieces of a row under way
 __global__ void __launch_bounds__(WARPS * 32, WARPS > 8 ? 1 : U > 2 ? 3 : 6)
 tree_attn_packed_merge_kernel(const Args a, int rows, int parts)
 {
@@ -316,13 +316,14 @@ tree_attn_packed_merge_kernel(const Args a, int rows, int parts)
         const bool there = gr < a.M;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
         float l = 0.f, m = -INFINITY;
+        auto ex2 = [](float x) { return WIDE ? umma::ex2f_wide(x) : umma::ex2f(x); };
         auto add = [&](float2 ml, float4 v, float m_new) {   // (without a maximum a piece's sum and row are zero, or NaN)
-            const float w = ml.x == -INFINITY ? 1.f : umma::ex2f(ml.x - m_new);
+            const float w = ml.x == -INFINITY ? 1.f : ex2(ml.x - m_new);
             l += w * ml.y;
             acc.x += w * v.x; acc.y += w * v.y; acc.z += w * v.z; acc.w += w * v.w;
         };
         auto move = [&](float m_new) {
-            const float w = m == -INFINITY ? 1.f : umma::ex2f(m - m_new);
+            const float w = m == -INFINITY ? 1.f : ex2(m - m_new);
             l *= w;
             acc.x *= w; acc.y *= w; acc.z *= w; acc.w *= w;
             m = m_new;
@@ -392,20 +393,20 @@ static inline int merge_entries(Args &a, int parts)
     a.entry_runs = runs <= parts ? 1 : 0;
     return a.entry_runs ? (int)runs : parts;
 }
-template <int BM> static inline cudaError_t launch_merge(fspad_ctx *ctx, const Args &a, int entries, int parts, cudaStream_t st)
+template <int BM, bool WIDE = false> static inline cudaError_t launch_merge(fspad_ctx *ctx, const Args &a, int entries, int parts, cudaStream_t st)
 {
     const int m = a.M < BM ? a.M : BM;
     ctx->launches++;
     // a row a CTA, with twice the warps, where that is no more than a CTA an SM (long runs in many pieces: 21.6 us against 24.9 on one token over 32K keys)
     if ((long long)entries * m <= ctx->sm_count)
-        return fspad_launch(tree_attn_packed_merge_kernel<BM, 16, 8>, dim3((unsigned)entries, (unsigned)m), dim3(512), 0, st, 0, a, 1, parts);
+        return fspad_launch(tree_attn_packed_merge_kernel<BM, 16, 8, WIDE>, dim3((unsigned)entries, (unsigned)m), dim3(512), 0, st, 0, a, 1, parts);
     int rows = 1;
     while (rows < 8 && rows < m && (long long)entries * ((m + rows - 1) / rows) > 3 * ctx->sm_count) rows *= 2;
     const dim3 grid((unsigned)entries, (unsigned)((m + rows - 1) / rows));
     // runs in two pieces or three: fewer loads a row and twice the rows on an SM (16 trees of 60 nodes, 32 heads over 8, 512 to 4096 keys 95.6 -> 87.7 us, but
     // one tree over 2K keys, in 19 pieces a run, 19.6 -> 23.9)
-    if ((long long)a.B * a.Hkv * a.mtiles * 2 >= parts) return fspad_launch(tree_attn_packed_merge_kernel<BM, 8, 2>, grid, dim3(256), 0, st, 0, a, rows, parts);
-    return fspad_launch(tree_attn_packed_merge_kernel<BM, 8, 8>, grid, dim3(256), 0, st, 0, a, rows, parts);
+    if ((long long)a.B * a.Hkv * a.mtiles * 2 >= parts) return fspad_launch(tree_attn_packed_merge_kernel<BM, 8, 2, WIDE>, grid, dim3(256), 0, st, 0, a, rows, parts);
+    return fspad_launch(tree_attn_packed_merge_kernel<BM, 8, 8, WIDE>, grid, dim3(256), 0, st, 0, a, rows, parts);
 }
 
 // Whether the units of a call, at most, can be counted in 32 bits (and 25 times as many as are cut into fewer parts than there are CTAs).

@@ -509,7 +509,7 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
                     group_sync(g);
                     if (t < R) {
                         const float was = sm.m[g][t], m = fmaxf(fmaxf(fmaxf(sm.top[g][0][t], sm.top[g][1][t]), fmaxf(sm.top[g][2][t], sm.top[g][3][t])), was);
-                        sm.alpha[g][t] = m == -INFINITY ? 1.f : ex2f(was - m);
+                        sm.alpha[g][t] = m == -INFINITY ? 1.f : ex2f_wide(was - m);
                         sm.m[g][t] = m;
                         sm.lim[g][t] = m + kLag;
                         sm.ref[g][t] = m == -INFINITY ? kBias : kBias - m;
@@ -597,7 +597,7 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
                 float sum = 0.f;
 #pragma unroll
                 for (int y = 0; y < 3; ++y) {
-                    const float f = m[y] == -INFINITY ? 1.f : ex2f(m[y] - top);      // (without a maximum a part is zero, or NaN)
+                    const float f = m[y] == -INFINITY ? 1.f : ex2f_wide(m[y] - top);      // (without a maximum a part is zero, or NaN)
                     sm.end[g][y][t] = f;
                     sum = fmaf(f, lr[y], sum);
                 }
@@ -673,7 +673,7 @@ template <int R> cudaError_t launch_few(fspad_ctx *ctx, Args &a, const Maps &map
     const int entries = merge_entries(a, ctas);
     ctx->launches++;
     e = fspad_launch(tree_attn_fp8_kernel<R>, dim3((unsigned)ctas), dim3(NT), bytes_of<R>(), st, 0, a, maps);
-    return e == cudaSuccess ? launch_merge<R>(ctx, a, entries, ctas, st) : e;
+    return e == cudaSuccess ? launch_merge<R, true>(ctx, a, entries, ctas, st) : e;
 }
 
 }  // namespace

@@ -139,7 +139,7 @@ __device__ __forceinline__ void softmax_half(bool tree, uint32_t tS, uint32_t tO
     const float m_new = move ? m_cand : m_run;
     const float m_safe = m_new == -INFINITY ? 0.f : m_new;
     if (move) {
-        const float alpha = ex2f(m_run - m_safe);
+        const float alpha = ex2f_wide(m_run - m_safe);
         l_run *= alpha;
         if (!first) {
             wait_o();
@@ -474,7 +474,7 @@ tree_attn_fp8_umma_kernel(const Args a, const __grid_constant__ CUtensorMap k_ma
                 const float2 o = s_ml[grp ^ 1][row];
                 m_fin = fmaxf(m_run, o.x);
                 const float ref = m_fin == -INFINITY ? 0.f : m_fin;
-                const float own = ex2f(m_run - ref), other = ex2f(o.x - ref);
+                const float own = ex2f_wide(m_run - ref), other = ex2f_wide(o.x - ref);
                 l_fin = (m_run == -INFINITY ? l_run : l_run * own) + (o.x == -INFINITY ? o.y : o.y * other);     // (without a maximum: zero, or a NaN)
                 f0 = grp == 0 ? own : other;
                 f1 = grp == 0 ? other : own;
@@ -829,5 +829,5 @@ cudaError_t fspad_launch_attn_fp8_umma(fspad_ctx *ctx, packed::Args a, const CUt
     const int entries = merge_entries(a, ctas);
     ctx->launches++;
     e = fspad_launch(tree_attn_fp8_umma_kernel, dim3((unsigned)ctas), dim3(NT), smem, st, 0, a, k_map);
-    return e == cudaSuccess ? launch_merge<BM>(ctx, a, entries, ctas, st) : e;
+    return e == cudaSuccess ? launch_merge<BM, true>(ctx, a, entries, ctas, st) : e;
 }

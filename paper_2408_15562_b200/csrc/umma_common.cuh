@@ -261,6 +261,13 @@ __device__ __forceinline__ float ex2f(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// The same down to 2^-149, as a square, off by twice as much (2^-21): a factor that brings sums of different references together may be that small where one of them stands for far larger values
+// than the other.  (The instruction that does not flush took 0.6 us more on one token over 2000 keys, in the factors of a merge, and 1.2 on a tree over 32700; this 0.1 and nothing.)
+__device__ __forceinline__ float ex2f_wide(float x)
+{
+    const float half = ex2f(0.5f * x);
+    return half * half;
+}
 
 // two single-precision operations in one instruction
 __device__ __forceinline__ uint64_t f32x2(float lo, float hi)

@@ -213,6 +213,29 @@ def test_scales_far_apart_and_a_callers_own(nodes, what):
     case.check(_run(case))
 
 
+@pytest.mark.parametrize("nodes,heads", [(1, (4, 1)), (5, (8, 2)), (20, (4, 1)), (60, (8, 2)), (1, (16, 16))])
+@pytest.mark.parametrize("L", [64, 256, 700, 5000])
+@pytest.mark.parametrize("what", ["up", "down", "mixed", "in turn"])
+def test_values_scales_at_both_ends_of_the_range(nodes, heads, L, what):
+    """V's scales of 2^-64 and 2^64, where all keys weigh alike: those with tiny values have their share of the sum of the weights, whichever come first and whichever part takes them."""
+    case = Case(25, 2, nodes, *heads, [L, 0])
+    groups = (L + 31) // 32
+    exp = dict(up=np.where(np.arange(groups) < groups // 2, -64, 64), down=np.where(np.arange(groups) < groups // 2, 64, -64),
+               mixed=case.rng.choice([-64, 64], groups), **{"in turn": np.where(np.arange(groups) // 4 % 2, 64, -64)})[what]
+    for g in range(groups):
+        case.scales[0, 1, case.table[0, g // 4], :, g % 4] = 2.0 ** float(exp[g])
+    case.codes[:, 0, case.table[0, :(L + 127) // 128]] = 0
+    case.tk[:] = 0
+    case.check(_run(case))
+    # the tiny values' keys weigh e^-2 of the others: times their scale 2^-131 of the largest
+    case.q[:] = 0
+    case.q[..., 0] = 0x3F80
+    for g in np.flatnonzero(exp < 0):
+        case.codes[0, 0, case.table[0, g // 4], :, 32 * (g % 4):32 * (g % 4) + 32, 0] = fp8.encode(np.array(-2.0))
+        case.scales[0, 0, case.table[0, g // 4], :, g % 4] = 1.0
+    case.check(_run(case, softmax_scale=1.0), scale=1.0)
+
+
 @pytest.mark.parametrize("own", [0.0, -1.0, 1e-30, float("nan"), 1e30, float("inf")])
 @pytest.mark.parametrize("nodes", [1, 20])
 def test_a_write_leaves_what_a_scale_outside_the_range_stands_for(nodes, own):
