@@ -39,6 +39,7 @@ cudaError_t fspad_launch_block_copy(fspad_ctx *ctx, void *pool0, long long bytes
 // Exponent fields of the least and the largest scale that the writes leave.
 constexpr int kFp8LeastField = 127 - 64, kFp8MostField = 127 + 64;
 constexpr float kFp8Least = 0x1p-64f, kFp8Most = 0x1p64f;
+constexpr float kMost = 0x1.fffffep127f;                         // (single precision's)
 
 // Exponent field of the least power of two 2^e with which a finite bf16 magnitude (its bits) is at most 448 * 2^e = 1.75 * 2^(e + 8).
 __device__ __forceinline__ int fspad_fp8_field(uint32_t magnitude)

@@ -496,7 +496,7 @@ tree_attn_fp8_kernel(const Args a, const __grid_constant__ Maps maps)
                 bool above = false;
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
-                    x[r] = there ? fmaf(x[r], fmaxf(sm.cs[at2][r] * ks, 0x1p-126f), lv) : -INFINITY;
+                    x[r] = there ? fmaf(x[r], fminf(fmaxf(sm.cs[at2][r] * ks, 0x1p-126f), kMost), lv) : -INFINITY;       // (scores of 0 stay that)
                     above |= x[r] > sm.lim[g][r];
                 }
                 if (group_any(g, above)) {

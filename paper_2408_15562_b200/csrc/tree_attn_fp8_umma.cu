@@ -93,10 +93,10 @@ __device__ __forceinline__ void tmem_scale16(uint32_t at, float alpha)
     tmem_st16(at, r);
 }
 
-// A query's factor times 32 keys' scale; not less than the least normal number (masked scores are -infinity, and must stay it).
+// A query's factor times 32 keys' scale; not less than the least normal number (masked scores are -infinity, and must stay it), and no infinity (scores of 0 must stay that).
 __device__ __forceinline__ float factor(float cs, float scale)
 {
-    return fmaxf(cs * scale, 0x1p-126f);
+    return fminf(fmaxf(cs * scale, 0x1p-126f), kMost);
 }
 
 // One group's turn at half a chunk: 64 scores of a row -> weights, over the scores' first 32 columns, packed in pairs.

@@ -213,6 +213,26 @@ def test_scales_far_apart_and_a_callers_own(nodes, what):
     case.check(_run(case))
 
 
+@pytest.mark.parametrize("nodes", [1, 5, 20, 60])
+def test_scores_of_nothing_beside_scores_beyond_the_range(nodes):
+    """Keys of zeros score 0 whatever the queries' and scales' sizes; the others' scores are -infinity here."""
+    case = Case(26, 1, nodes, 4, 1, [300])
+    rng, x = case.rng, np.zeros(case.q.shape, np.float32)
+    x[..., 0], x[..., 5] = 2.0 ** 100, -2.0 ** 90
+    case.q = synth.f32_to_bf16_bits(x)
+    zero = rng.permutation(300)[:7]
+    k = np.zeros((300, 128))
+    k[:, 0] = -1.0 - rng.random(300)
+    k[zero] = 0
+    pos = np.arange(300)
+    case.codes[0, 0, case.table[0, pos // 128], 0, pos % 128] = fp8.encode(k)
+    case.scales[0, 0] = np.where(np.isnan(case.scales[0, 0]), np.nan, np.float32(2.0 ** 60))
+    case.tk[:] = 0
+    want = fp8.tree_attn(case.q, case.codes, case.scales, 0, case.table, case.tk, case.tv, case.parent, case.L)[0]
+    got = _run(case).float().cpu().numpy()
+    assert np.isfinite(want).all() and np.abs(got - want).max() <= 2.0 ** -7 * np.abs(want).max()
+
+
 @pytest.mark.parametrize("nodes,heads", [(1, (4, 1)), (5, (8, 2)), (20, (4, 1)), (60, (8, 2)), (1, (16, 16))])
 @pytest.mark.parametrize("L", [64, 256, 700, 5000])
 @pytest.mark.parametrize("what", ["up", "down", "mixed", "in turn"])
