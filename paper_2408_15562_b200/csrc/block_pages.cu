@@ -6,9 +6,10 @@
 // memory, so that lists come out in the order of the blocks' numbers whatever the order of the threads.  What bounds these is latency: dependent loads, barriers.
 // The contents move in one kernel for any cache: bulk copies through shared memory, six on the way in and up to six on the way out of an SM, 16 KB each.
 //
-// Measured, captured: 64 answers to four prompts of 5001 rows in 32 layers, the fork and the copy of 60 and more blocks a plane, 120 us (537 MB written, which alone take 91 us; a source that several
-// pairs name comes from L2, and keeping its piece in shared memory for the next pair did not help: 119.8 against 116.6); 88 moves of 400 blocks in bf16 74 us (5.0 TB/s).  Two
-// answers to 300 rows take 11.0 us, and a pool of 48 blocks with 7 moves 9.7: two or three launches and their dependent loads.
+// Measured, captured in a graph (in brackets called one after another): 64 answers to four prompts of 5001 rows in 32 layers, the fork and the copy of 60 and more blocks a plane, 114 to 120 us, by the
+// board (117; 537 MB written, which alone take 91 us; a source that several pairs name comes from L2, and keeping its piece in shared memory for the next pair did not help: 119.8 against 116.6);
+// 88 moves of 400 blocks in bf16 74 us (76; 5.0 TB/s).  Two answers to 300 rows take 8.7 to 11.0 us (17.6), and a pool of 48 blocks with 7 moves 9.1 to 9.8 (14.2): two or three launches and their
+// dependent loads.
 #include "fp8.cuh"
 #include "umma_common.cuh"
 

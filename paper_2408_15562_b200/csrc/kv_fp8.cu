@@ -8,9 +8,11 @@
 // rounded again by it: with powers of two that changes only what falls below the least codes.
 // An element that is not finite has no part in the maximum and is kept as NaN.
 //
-// Bound by memory: 256 bytes read and 128 written a row (256 more where the caller asks for the values that are kept).  Prompts of four requests, 16400 rows of 8 heads with the kept values, take
-// 32 us (161 MB: 5.0 TB/s), those paths 55 us (252 MB with the kept values: 4.6 TB/s, reads and writes mixed and begun groups read again).  One row of each of 256 sequences takes 6.0 us, of one sequence in
-// 32 layers 4.0: a launch, and loads that depend on one another (slot, row and scale, group).
+// Bound by memory: 256 bytes read and 128 written a row (256 more where the caller asks for the values that are kept), and 4 KB read and written of a group that is rounded again.  Captured in a
+// graph and repeated, so that no scale rises any more, prompts of four requests, 16400 rows of 8 heads with the kept values, take 32 us (161 MB: 5.0 TB/s; 33 called one after another) and those paths 55
+// (252 MB with the kept values: 4.6 TB/s; by the counters 99 MB are read, so no group is, and 93 written, the rest of it later).  One row of each of 256 sequences takes 6.0 us, of one sequence in 32 layers
+// 4.0 (5.3 called one after another): a launch, and loads that depend on one another (slot, row and scale, group).  Where the scales of the begun groups rise, nearly all of them, the paths read 163 MB and
+// write 126: one call alone with nothing in L2 takes 76 us against 61, the prompts 39 against 37, the rows of 256 sequences 16.4 against 12.3, of one sequence 8 to 9 either way.
 #include "fp8.cuh"
 #include "umma_common.cuh"
 

@@ -16,11 +16,11 @@
 // A CTA's warps: 0 copies, 1 and 2 the tensor cores' products of the two groups, 4-7 and 8-11 the groups that take the chunks of 128 keys in turn, a key a thread, each with a
 // reference, sums and an accumulator of its own; 12-15 make the queries' two forms and deal with the tree's keys (16 at most) in single precision, up to two stretches ahead.
 //
-// Bound by reading the cache where sequences are long: 32 single tokens (8 heads a kv head) over 4 to 32 thousand keys take 184 us, 95 percent of what the codes and scales take at
-// the measured copy bandwidth (199 with one warp for both groups' products, 190 without warps of their own for queries and trees); with 16 rows, 32 sequences of 4 to 12 thousand keys
+// Bound by reading the cache where sequences are long: 32 single tokens (8 heads a kv head) over 4 to 32 thousand keys take 184 us captured in a graph (196 called one after another), 95 percent of what the codes and scales take at
+// the measured copy bandwidth (captured, as all that follows: 199 with one warp for both groups' products, 190 without warps of their own for queries and trees); with 16 rows, 32 sequences of 4 to 12 thousand keys
 // take 97.  Short sequences are bound by a stretch's chain, some 7000 cycles with three chunks: a turn 1700 to 2000 (the first moves the references), the sums 700, the last product 1100, the
-// rows 700; 64 single tokens over 100 to 600 keys take 23.0 us (32.6 with queries and tree in the groups' own way).  A short call is its latencies: one token over 2000 keys
-// takes 9.3 us, the list 2400 cycles of it, the part 7000, and the merge behind it; its copies take 0.6.
+// rows 700; 64 single tokens over 100 to 600 keys take 23.1 us (32.6 with queries and tree in the groups' own way).  A short call is its latencies: one token over 2000 keys
+// takes 9.3 us (9.8 called one after another), the list 2400 cycles of it, the part 7000, and the merge behind it; its copies take 0.6.
 #include "fp8.cuh"
 #include "packed_list.cuh"
 
