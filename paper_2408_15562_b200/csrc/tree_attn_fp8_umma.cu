@@ -101,7 +101,7 @@ __device__ __forceinline__ float factor(float cs, float scale)
 }
 
 // One group's turn at half a chunk: 64 scores of a row -> weights, over the scores' first 32 columns, packed in pairs.
-// `of_keys`: of each 32 keys of the chunk the scale of K, log2 of V's scale, and its reciprocal (four of each); of the tree's 1, 0 and 1.  `wait_o`: until the group's product before the last
+// `of_keys`: of each 32 keys of the chunk the scale of K, log2 of V's scale, and its reciprocal (four of each); the tree's have none.  `wait_o`: until the group's product before the last
 // one (which the scores are known to come behind) is complete too.
 template <bool plain, typename F>
 __device__ __forceinline__ void softmax_half(bool tree, uint32_t tS, uint32_t tO, const uint32_t (&see)[2], float cs, const float *of_keys, bool row_ok, bool first,
@@ -127,11 +127,12 @@ __device__ __forceinline__ void softmax_half(bool tree, uint32_t tS, uint32_t tO
         for (int x = 0; x < 2; ++x)
 #pragma unroll
             for (int y = 0; y < 2; ++y) mx4[x][y] = fmaxf(fmaxf(mx4[x][y], __uint_as_float(r[x][j + 2 * y])), __uint_as_float(r[x][j + 2 * y + 1]));
-    float mul[2], mx = -INFINITY;
+    float mul[2], log_v[2], mx = -INFINITY;
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-        mul[x] = factor(cs, of_keys[x]);
-        mx = fmaxf(mx, fmaf(fmaxf(mx4[x][0], mx4[x][1]), mul[x], of_keys[4 + x]));
+        mul[x] = factor(cs, !plain && tree ? 1.f : of_keys[x]);
+        log_v[x] = !plain && tree ? 0.f : of_keys[4 + x];
+        mx = fmaxf(mx, fmaf(fmaxf(mx4[x][0], mx4[x][1]), mul[x], log_v[x]));
     }
     // the reference follows the row's maximum when some row of the warp would see a weight too large otherwise (a warp moves as one:
     // its accesses to tensor memory are collective); a row that does not exist has no say
@@ -153,7 +154,7 @@ __device__ __forceinline__ void softmax_half(bool tree, uint32_t tS, uint32_t tO
     float sum = 0.f;
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-        const float add = shift + of_keys[4 + x];
+        const float add = shift + log_v[x];
         const uint64_t scale2 = f32x2(mul[x], mul[x]), neg = f32x2(add, add);
         uint64_t acc[2] = {0ull, 0ull};
         uint32_t w[16];
@@ -169,16 +170,17 @@ __device__ __forceinline__ void softmax_half(bool tree, uint32_t tS, uint32_t tO
         tmem_st16(tS + 16u * x, w);
         float lo, hi;
         f32x2_split(f32x2_add(acc[0], acc[1]), lo, hi);
-        sum = fmaf(lo + hi, of_keys[8 + x], sum);
+        sum = fmaf(lo + hi, !plain && tree ? 1.f : of_keys[8 + x], sum);
     }
     l_run += sum * (!plain && tree ? kUp : 1.f);
 }
 
 constexpr int SCALES = 6;                // (a chunk's are written once the one 6 before it has been through the products)
-// Places for the flags of a tree's chunk.  The softmax reads them after its last word on the chunk, which lets the product go that frees the chunk's V tile: the tree's chunk
-// after the next may have its flags written while a warp has yet to read.  The one after that may not: it waits for the product of a later chunk, which that warp either has a hand in itself
-// or meets behind the barrier at a stretch's end.  (With two places, and the flags read ahead of that word, 16 trees of 60 nodes over 512 to 4096 keys took 0.7 us longer.)
-constexpr uint32_t ODDS = 3;
+// Places for the flags of a tree's chunk.  The softmax reads them after its last word on chunk c, which lets the product go that frees the chunk's V tile, so that flags of chunks c + 2 and c + 3
+// may be written while a warp has yet to read c's (of one row tile, c + 1 is the other group's; a tree of more than 128 nodes has two chunks in a stretch, its last row tile may be the
+// only one).  Those of chunk c + 4 and later wait for the product of c + 2: in the same stretch that warp has a hand in it, with one row tile or two, and a later stretch lies behind the barrier
+// at this one's end.  (With two places, and the flags read ahead of that word, 16 trees of 60 nodes over 512 to 4096 keys took 0.7 us longer.)
+constexpr uint32_t ODDS = 4;
 struct Small {
     static constexpr int BARS = 34;
     unsigned long long bar[BARS];
@@ -187,7 +189,7 @@ struct Small {
         int scan[NT / 32 + 4];           // (before anything else)
     };
     alignas(16) float raw[BUFS][8];      // scales of K and V as they come (bulk copies' destination)
-    float scale[SCALES + 1][12];         // of a chunk, by its number: of each 32 keys K's scale, log2 of V's, 1 / V's; at last of the tree's
+    float scale[SCALES][12];             // of a chunk of the cache, by its number: of each 32 keys K's scale, log2 of V's, 1 / V's
     unsigned char par[FSPAD_MAX_NODES_WIDE];         // parents plus one
     uint32_t odd[ODDS][4];               // which V rows of a tree's chunk have an infinity or a NaN in them
     uint32_t tmem;
@@ -232,7 +234,6 @@ tree_attn_fp8_umma_kernel(const Args a, const __grid_constant__ CUtensorMap k_ma
             mbar_init(bar(i), count);
         }
         s_fail = s_soft_fail = 0;
-        for (int i = 0; i < 12; ++i) s_scale[SCALES][i] = i >= 4 && i < 8 ? 0.f : 1.f;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     }
     if (warp == 9) {
@@ -393,7 +394,7 @@ tree_attn_fp8_umma_kernel(const Args a, const __grid_constant__ CUtensorMap k_ma
             int c = s.two ? 0 : grp;
             auto turn = [&](auto plain_, bool tree, const uint32_t (&see)[4]) {
                 constexpr bool plain = decltype(plain_)::value;
-                const float *of_keys = s_scale[!plain && tree ? SCALES : (chunks + (uint32_t)c) % SCALES];
+                const float *of_keys = s_scale[(chunks + (uint32_t)c) % SCALES];
 #pragma unroll 1
                 for (int y = 0; y < 2; ++y) {                // 64 keys at a time
                     if (!failed && !mbar_wait(bar(S_FULL + 2 * grp + y), n_done & 1u)) failed = true;

@@ -314,7 +314,7 @@ def test_values_that_are_no_numbers_reach_only_those_who_see_them(what, nodes, g
     assert np.abs(got - want)[good].max() <= 3e-2
 
 
-@pytest.mark.parametrize("nodes,heads,batch", [(40, (8, 2), 700), (17, (1, 1), 1500), (128, (2, 2), 500), (150, (2, 1), 400), (200, (2, 2), 400), (40, (56, 28), 30)])
+@pytest.mark.parametrize("nodes,heads,batch", [(40, (8, 2), 700), (17, (1, 1), 1500), (128, (2, 2), 500), (150, (2, 1), 400), (200, (2, 2), 400), (40, (56, 28), 30), (130, (4, 2), 300), (160, (4, 2), 200)])
 def test_trees_without_a_cache_one_behind_the_other(nodes, heads, batch):
     """Nothing but trees, many to a part, with infinities and NaN in V of every third: the flags of V's rows are in one of two places in turn, and each
     tree's nodes have those of their own tree, in every one of several calls."""
