@@ -18,8 +18,8 @@
 // group's part times 1 / scale.  Against the tree's rows, which are bf16 of any size, the queries are taken as they are: its chunks come first, and the query
 // tile is then written again.  With one row tile its two forms lie in the two tiles' places.
 //
-// Measured, captured in a graph: 16 trees of 60 nodes, 32 heads over 8, 512 to 4096 keys 73.4 us (75 called one after another; floor 21.5: 36 GFLOP at the measured bf16 rate); one tree of 60 over 32700
-// keys with 64 heads over 8 86.5 us (92; 38.5).  A chunk of 256 rows costs some 4900 cycles, of which the products take 2560 (scores of 64 keys: 32 instructions of 48 cycles; the others 16 of 64) and the
+// Measured, captured in a graph: 16 trees of 60 nodes, 32 heads over 8, 512 to 4096 keys 73.7 us (75 called one after another; floor 21.5: 36 GFLOP at the measured bf16 rate); one tree of 60 over 32700
+// keys with 64 heads over 8 86.4 us (91; 38.5).  A chunk of 256 rows costs some 4900 cycles, of which the products take 2560 (scores of 64 keys: 32 instructions of 48 cycles; the others 16 of 64) and the
 // exponentials, on their unit, 2100: each is a third busy over a call, and what bounds it is the chain of a half chunk, wait, load, maximum, vote, exponentials, store, with two warps a scheduler.  Not kept,
 // on these two: scores of halves ahead from one issuing warp 110 and 110, whole chunks with a warp a group 97 and 103, those with the groups' exponentials in turn 92 and 92, beginnings of
 // runs not counted in the cut 94.5 and 86.
